@@ -12,7 +12,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtetra_b200.so")
 BINDING = os.path.join(HERE, "_binding.so")
-SOURCES = ["tetra_tables.cpp", "tetra_decode.cu", "tetra_gemv.cu", "tetra_list.cu", "tetra_batched.cu", "tetra_api.cu", "tetra_noalloc.cu", "q4_gemv.cu", "q4_list.cu", "tetra_encode.cu"]
+SOURCES = ["tetra_tables.cpp", "tetra_decode.cu", "tetra_gemv.cu", "tetra_list.cu", "tetra_batched.cu", "tetra_api.cu", "tetra_noalloc.cu", "q4_gemv.cu", "q4_list.cu", "tetra_encode.cu",
+           "kv_append.cu", "kv_attend.cu"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
          "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "--use_fast_math"]
@@ -32,7 +33,8 @@ def _stale() -> bool:
             return True
     t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".o")]  # the objects are the build's own
-    deps += [os.path.join(os.path.dirname(HERE), "include", h) for h in ("tetra.h", "tetra_q4.h")]
+    include = os.path.join(os.path.dirname(HERE), "include")
+    deps += [os.path.join(include, h) for h in os.listdir(include)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

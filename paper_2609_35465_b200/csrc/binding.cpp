@@ -11,14 +11,17 @@
 #include <dlfcn.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdint>
 #include <string>
 
 #include "../../include/tetra.h"
+#include "../../include/tetra_kv.h"
 #include "../../include/tetra_q4.h"
 
 namespace {
@@ -42,6 +45,9 @@ struct Api {
     decltype(&tetra_q4_gemv) q4_gemv;
     decltype(&tetra_q4_rows) q4_rows;
     decltype(&tetra_q4_list_run) q4_list_run;
+    decltype(&tetra_kv_append) kv_append;
+    decltype(&tetra_kv_read) kv_read;
+    decltype(&tetra_kv_attend) kv_attend;
 } api;
 PyObject* tetra_error = nullptr;  // the exception class
 
@@ -350,6 +356,129 @@ FASTCALL(py_q4_list_run) {
     });
 }
 
+// ---- the cache of keys and values ---------------------------------------------------------------------------------------
+// These calls take tensors with shapes, so type, shape, device and strides are all checked.
+const at::Tensor& typed(PyObject* o, at::ScalarType type, const char* what, const char* name) {
+    const at::Tensor& t = tensor(o);
+    if (t.scalar_type() != type) fail(tetra_error, "%s %s: %s, the call takes %s", what, name, c10::toString(t.scalar_type()), c10::toString(type));
+    if (!t.is_cuda()) fail(tetra_error, "%s %s: tensor is not on the device", what, name);
+    if (t.device().index() != c10::cuda::current_device())
+        fail(tetra_error, "%s %s: tensor is on device %d, the current device is %d", what, name, int(t.device().index()), int(c10::cuda::current_device()));
+    return t;
+}
+// ... with these sizes, one after another in memory.
+void* shaped(PyObject* o, at::ScalarType type, at::IntArrayRef sizes, const char* what, const char* name) {
+    const at::Tensor& t = typed(o, type, what, name);
+    if (t.sizes() != sizes) fail(tetra_error, "%s %s: wrong shape", what, name);
+    if (!t.is_contiguous()) fail(tetra_error, "%s %s: tensor is not contiguous", what, name);
+    return t.data_ptr();
+}
+// Rows of heads [rows][heads][D] whose rows may lie apart; a row's heads are contiguous.
+void* rows_of_heads(PyObject* o, at::ScalarType type, int64_t rows, int64_t D, const char* what, const char* name, int64_t& heads, int64_t& stride) {
+    const at::Tensor& t = typed(o, type, what, name);
+    if (t.dim() != 3 || t.size(0) != rows || t.size(2) != D) fail(tetra_error, "%s %s: wrong shape", what, name);
+    heads = t.size(1);
+    if ((t.stride(2) != 1 && D > 1) || (t.stride(1) != D && heads > 1)) fail(tetra_error, "%s %s: the heads of a row are not contiguous", what, name);
+    stride = rows > 1 ? t.stride(0) : heads * D;
+    if (stride < heads * D) fail(tetra_error, "%s %s: rows overlap", what, name);
+    return t.data_ptr();
+}
+int narrow(int64_t v, const char* what, const char* name) {
+    if (v > INT32_MAX) fail(tetra_error, "%s %s: too large", what, name);
+    return int(v);
+}
+// cache [pages, kv_heads, page_tokens / 16, 32 D + 16], page_table [seqs, width], row_start [seqs + 1], lengths [seqs]
+tetra_kv_cache kv_cache_of(PyObject* const* a, const char* what) {
+    const at::Tensor& c = typed(a[0], at::kByte, what, "cache");
+    if (c.dim() != 4 || !c.is_contiguous() || c.size(3) < 16 || (c.size(3) - 16) % 32) fail(tetra_error, "%s cache: wrong shape", what);
+    const at::Tensor& table = typed(a[1], at::kInt, what, "page_table");
+    if (table.dim() != 2 || (table.stride(1) != 1 && table.size(1) > 1)) fail(tetra_error, "%s page_table: wrong shape", what);
+    const int64_t seqs = table.size(0), stride = seqs > 1 ? table.stride(0) : table.size(1);
+    tetra_kv_cache k;
+    k.cache = c.data_ptr();
+    k.page_table = static_cast<const int32_t*>(table.data_ptr());
+    k.row_start = static_cast<const int32_t*>(shaped(a[2], at::kInt, {seqs + 1}, what, "row_start"));
+    k.lengths = static_cast<const int32_t*>(shaped(a[3], at::kInt, {seqs}, what, "lengths"));
+    k.table_stride = stride;
+    k.pages = narrow(c.size(0), what, "cache");
+    k.page_tokens = narrow(c.size(2) * TETRA_KV_BLOCK, what, "cache");
+    k.kv_heads = narrow(c.size(1), what, "cache");
+    k.head_dim = narrow((c.size(3) - 16) / 32, what, "cache");
+    k.seqs = narrow(seqs, what, "page_table");
+    k.width = narrow(table.size(1), what, "page_table");
+    return k;
+}
+double real(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1. && PyErr_Occurred()) throw Failed();
+    return v;
+}
+
+// cache, page_table, row_start, lengths, q, k, v, q_out, inv_freq, q_weight, k_weight, eps, stream
+FASTCALL(py_kv_append) {
+    return guarded(n, 13, [&] {
+        const char* what = "tetra_kv_append";
+        const tetra_kv_cache c = kv_cache_of(a, what);
+        const at::ScalarType type = tensor(a[5]).scalar_type();
+        if (type != at::kFloat && type != at::kHalf) fail(tetra_error, "%s k: %s, the call takes Float or Half", what, c10::toString(type));
+        const int64_t rows = tensor(a[5]).dim() == 3 ? tensor(a[5]).size(0) : 0, D = c.head_dim;
+        tetra_kv_rows r = {};
+        int64_t heads = 0;
+        r.k = rows_of_heads(a[5], type, rows, D, what, "k", heads, r.k_stride);
+        if (heads != c.kv_heads) fail(tetra_error, "%s k: wrong shape", what);
+        r.v = rows_of_heads(a[6], type, rows, D, what, "v", heads, r.v_stride);
+        if (heads != c.kv_heads) fail(tetra_error, "%s v: wrong shape", what);
+        if ((a[4] == Py_None) != (a[7] == Py_None)) fail(tetra_error, "%s: q and q_out are given together", what);
+        if (a[4] != Py_None) {
+            r.q = rows_of_heads(a[4], type, rows, D, what, "q", heads, r.q_stride);
+            r.q_heads = narrow(heads, what, "q");
+            r.q_out = shaped(a[7], at::kHalf, {rows, heads, D}, what, "q_out");
+        }
+        if (a[8] != Py_None) r.inv_freq = static_cast<const double*>(shaped(a[8], at::kDouble, {D / 2}, what, "inv_freq"));
+        if (a[9] != Py_None) r.q_weight = static_cast<const float*>(shaped(a[9], at::kFloat, {D}, what, "q_weight"));
+        if (a[10] != Py_None) r.k_weight = static_cast<const float*>(shaped(a[10], at::kFloat, {D}, what, "k_weight"));
+        r.eps = real(a[11]);
+        r.rows = narrow(rows, what, "k");
+        r.half_type = type == at::kHalf;
+        void* s = stream_of(a[12]);
+        if (rows > 0) check(unlocked([&] { return api.kv_append(&c, &r, s); }), what);
+        return same(a[7]);
+    });
+}
+// cache, page_table, row_start, lengths, k_out, v_out, stream
+FASTCALL(py_kv_read) {
+    return guarded(n, 7, [&] {
+        const char* what = "tetra_kv_read";
+        const tetra_kv_cache c = kv_cache_of(a, what);
+        const int64_t rows = tensor(a[4]).dim() == 3 ? tensor(a[4]).size(0) : 0;
+        void* k = shaped(a[4], at::kHalf, {rows, c.kv_heads, c.head_dim}, what, "k_out");
+        void* v = shaped(a[5], at::kHalf, {rows, c.kv_heads, c.head_dim}, what, "v_out");
+        const int count = narrow(rows, what, "k_out");
+        void* s = stream_of(a[6]);
+        if (rows > 0) check(unlocked([&] { return api.kv_read(&c, k, v, count, s); }), what);
+        return Py_BuildValue("(OO)", a[4], a[5]);
+    });
+}
+// cache, page_table, row_start, lengths, q, out, scale, workspace, stream
+FASTCALL(py_kv_attend) {
+    return guarded(n, 9, [&] {
+        const char* what = "tetra_kv_attend";
+        const tetra_kv_cache c = kv_cache_of(a, what);
+        const int64_t rows = tensor(a[4]).dim() == 3 ? tensor(a[4]).size(0) : 0;
+        int64_t heads = 0, stride = 0;
+        void* q = rows_of_heads(a[4], at::kHalf, rows, c.head_dim, what, "q", heads, stride);
+        void* out = shaped(a[5], at::kHalf, {rows, heads, c.head_dim}, what, "out");
+        const int q_heads = narrow(heads, what, "q"), count = narrow(rows, what, "q");
+        const float scale = a[6] == Py_None ? float(1. / std::sqrt(double(c.head_dim))) : float(real(a[6]));
+        const at::Tensor& ws = typed(a[7], at::kByte, what, "workspace");
+        if (!ws.is_contiguous()) fail(tetra_error, "%s workspace: tensor is not contiguous", what);
+        void *wp = ws.data_ptr(), *s = stream_of(a[8]);
+        const size_t wn = size_t(ws.numel());
+        if (rows > 0) check(unlocked([&] { return api.kv_attend(&c, q, stride, out, count, q_heads, scale, wp, wn, s); }), what);
+        return same(a[5]);
+    });
+}
+
 // library path, exception class
 FASTCALL(py_setup) {
     return guarded(n, 2, [&] {
@@ -378,6 +507,9 @@ FASTCALL(py_setup) {
         get(api.q4_gemv, "tetra_q4_gemv");
         get(api.q4_rows, "tetra_q4_rows");
         get(api.q4_list_run, "tetra_q4_list_run");
+        get(api.kv_append, "tetra_kv_append");
+        get(api.kv_read, "tetra_kv_read");
+        get(api.kv_attend, "tetra_kv_attend");
         Py_XDECREF(tetra_error);
         tetra_error = same(a[1]);
         return same(Py_None);
@@ -387,7 +519,8 @@ FASTCALL(py_setup) {
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(setup),        METHOD(gemv),          METHOD(gemv_tail), METHOD(gemv_noalloc), METHOD(gemv_batched),
                          METHOD(gemv_list),    METHOD(grouped_run),   METHOD(pack_codes), METHOD(decode_packed), METHOD(encode_blocks),
-                         METHOD(q4_pack),      METHOD(q4_gemv),       METHOD(q4_rows),   METHOD(q4_list_run),  {nullptr, nullptr, 0, nullptr}};
+                         METHOD(q4_pack),      METHOD(q4_gemv),       METHOD(q4_rows),   METHOD(q4_list_run),  METHOD(kv_append),
+                         METHOD(kv_read),      METHOD(kv_attend),     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of the Tetra C ABI.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -107,6 +107,13 @@ def lib():
         L.tetra_q4_list_workspace_bytes.restype = sz
         L.tetra_q4_list_plan.argtypes = [vp, i32, i32, vp, sz, vp]
         L.tetra_q4_list_run.argtypes = [vp, i32, vp]
+        L.tetra_kv_cache_bytes.argtypes = [i32, i32, i32, i32]
+        L.tetra_kv_cache_bytes.restype = sz
+        L.tetra_kv_workspace_bytes.argtypes = [i32]
+        L.tetra_kv_workspace_bytes.restype = sz
+        L.tetra_kv_append.argtypes = [vp, vp, vp]
+        L.tetra_kv_read.argtypes = [vp, vp, vp, i32, vp]
+        L.tetra_kv_attend.argtypes = [vp, vp, C.c_int64, vp, i32, i32, C.c_float, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -380,3 +387,63 @@ def tetra_q4_list_plan(problems, G: int, stream=None) -> torch.Tensor:
 
 def tetra_q4_list_run(workspace: torch.Tensor, G: int, stream=None):
     (_nat or _native()).q4_list_run(workspace, G, stream)
+
+
+# ---------------------------------------------------------------------------
+# keys and values of a served model (include/tetra_kv.h)
+# ---------------------------------------------------------------------------
+class KvCache(C.Structure):
+    """Mirror of tetra_kv_cache."""
+    _fields_ = [("cache", C.c_void_p), ("page_table", C.c_void_p), ("row_start", C.c_void_p), ("lengths", C.c_void_p),
+                ("table_stride", C.c_int64), ("pages", C.c_int32), ("page_tokens", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("seqs", C.c_int32), ("width", C.c_int32)]
+
+
+class KvRows(C.Structure):
+    """Mirror of tetra_kv_rows."""
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p), ("inv_freq", C.c_void_p),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("eps", C.c_double), ("rows", C.c_int32), ("q_heads", C.c_int32), ("half_type", C.c_int32)]
+
+
+KV_BLOCK = 16
+
+
+def tetra_kv_cache(pages: int, page_tokens: int, kv_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """A cache of keys and values: uint8 [pages, kv_heads, page_tokens / 16, 32 head_dim + 16], not initialised (a
+    block's first token sets it up)."""
+    n = lib().tetra_kv_cache_bytes(pages, page_tokens, kv_heads, head_dim)
+    if n == 0:
+        raise TetraError("tetra_kv_cache_bytes: shape rejected (%d pages of %d tokens, %d heads of %d)"
+                         % (pages, page_tokens, kv_heads, head_dim))
+    return torch.empty((pages, kv_heads, page_tokens // KV_BLOCK, 32 * head_dim + 16), dtype=torch.uint8, device=device)
+
+
+def tetra_kv_workspace(head_dim: int, device="cuda") -> torch.Tensor:
+    """The workspace of tetra_kv_attend, zeroed; calls that share one must not overlap on the GPU."""
+    n = lib().tetra_kv_workspace_bytes(head_dim)
+    if n == 0:
+        raise TetraError("tetra_kv_workspace_bytes: head_dim %d rejected" % head_dim)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def tetra_kv_append(q, k, v, cache, page_table, row_start, lengths, q_out, inv_freq=None, q_weight=None, k_weight=None,
+                    eps: float = 1e-6, stream=None):
+    """Appends rows of keys and values to the cache and makes the attention's queries; returns q_out.
+
+    q [rows, q_heads, D], k and v [rows, kv_heads, D]: float32 or float16, rows may lie apart (slices of one buffer); q and
+    q_out (float16 [rows, q_heads, D]) may be None together.  page_table int32 [seqs, width], row_start int32 [seqs + 1],
+    lengths int32 [seqs]: tokens before this step.  inv_freq float64 [D / 2]; q_weight, k_weight float32 [D]: head norms."""
+    return (_nat or _native()).kv_append(cache, page_table, row_start, lengths, q, k, v, q_out, inv_freq, q_weight, k_weight, eps, stream)
+
+
+def tetra_kv_read(cache, page_table, row_start, lengths, k_out, v_out, stream=None):
+    """What the cache holds for the rows' positions, as float16 [rows, kv_heads, D]; returns (k_out, v_out)."""
+    return (_nat or _native()).kv_read(cache, page_table, row_start, lengths, k_out, v_out, stream)
+
+
+def tetra_kv_attend(q, cache, page_table, row_start, lengths, out, workspace, scale=None, stream=None):
+    """Attention of the step's rows (float16 [rows, q_heads, D]) over the cache, causal among them; returns out.
+
+    Same page_table, row_start and lengths as the tetra_kv_append before it; scale: 1 / sqrt(D) unless given."""
+    return (_nat or _native()).kv_attend(cache, page_table, row_start, lengths, q, out, scale, workspace, stream)
