@@ -23,6 +23,7 @@
 #include "../../include/tetra.h"
 #include "../../include/tetra_kv.h"
 #include "../../include/tetra_q4.h"
+#include "../../include/tetra_sample.h"
 
 namespace {
 
@@ -48,6 +49,7 @@ struct Api {
     decltype(&tetra_kv_append) kv_append;
     decltype(&tetra_kv_read) kv_read;
     decltype(&tetra_kv_attend) kv_attend;
+    decltype(&tetra_sample) sample;
 } api;
 PyObject* tetra_error = nullptr;  // the exception class
 
@@ -479,6 +481,34 @@ FASTCALL(py_kv_attend) {
     });
 }
 
+// logits, u, tokens, prob, temperature, top_k, top_p, min_p, stream
+FASTCALL(py_sample) {
+    return guarded(n, 9, [&] {
+        const char* what = "tetra_sample";
+        const at::ScalarType type = tensor(a[0]).scalar_type();
+        if (type != at::kFloat && type != at::kHalf) fail(tetra_error, "%s logits: %s, the call takes Float or Half", what, c10::toString(type));
+        const at::Tensor& x = typed(a[0], type, what, "logits");
+        if (x.dim() != 2 || (x.stride(1) != 1 && x.size(1) > 1)) fail(tetra_error, "%s logits: wrong shape", what);
+        const int64_t rows = x.size(0);
+        tetra_sample_rows r = {};
+        r.logits = x.data_ptr();
+        r.rows = narrow(rows, what, "logits");
+        r.vocab = narrow(x.size(1), what, "logits");
+        r.row_stride = rows > 1 ? x.stride(0) : x.size(1);
+        r.half_type = type == at::kHalf;
+        r.u = static_cast<const float*>(shaped(a[1], at::kFloat, {rows}, what, "u"));
+        r.tokens = static_cast<int32_t*>(shaped(a[2], at::kInt, {rows}, what, "tokens"));
+        if (a[3] != Py_None) r.prob = static_cast<float*>(shaped(a[3], at::kFloat, {rows}, what, "prob"));
+        if (a[4] != Py_None) r.temperature = static_cast<const float*>(shaped(a[4], at::kFloat, {rows}, what, "temperature"));
+        if (a[5] != Py_None) r.top_k = static_cast<const int32_t*>(shaped(a[5], at::kInt, {rows}, what, "top_k"));
+        if (a[6] != Py_None) r.top_p = static_cast<const float*>(shaped(a[6], at::kFloat, {rows}, what, "top_p"));
+        if (a[7] != Py_None) r.min_p = static_cast<const float*>(shaped(a[7], at::kFloat, {rows}, what, "min_p"));
+        void* s = stream_of(a[8]);
+        if (rows > 0) check(unlocked([&] { return api.sample(&r, s); }), what);
+        return same(a[2]);
+    });
+}
+
 // library path, exception class
 FASTCALL(py_setup) {
     return guarded(n, 2, [&] {
@@ -510,6 +540,7 @@ FASTCALL(py_setup) {
         get(api.kv_append, "tetra_kv_append");
         get(api.kv_read, "tetra_kv_read");
         get(api.kv_attend, "tetra_kv_attend");
+        get(api.sample, "tetra_sample");
         Py_XDECREF(tetra_error);
         tetra_error = same(a[1]);
         return same(Py_None);
@@ -520,7 +551,7 @@ FASTCALL(py_setup) {
 PyMethodDef methods[] = {METHOD(setup),        METHOD(gemv),          METHOD(gemv_tail), METHOD(gemv_noalloc), METHOD(gemv_batched),
                          METHOD(gemv_list),    METHOD(grouped_run),   METHOD(pack_codes), METHOD(decode_packed), METHOD(encode_blocks),
                          METHOD(q4_pack),      METHOD(q4_gemv),       METHOD(q4_rows),   METHOD(q4_list_run),  METHOD(kv_append),
-                         METHOD(kv_read),      METHOD(kv_attend),     {nullptr, nullptr, 0, nullptr}};
+                         METHOD(kv_read),      METHOD(kv_attend),     METHOD(sample),  {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of the Tetra C ABI.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -113,6 +113,7 @@ def lib():
         L.tetra_kv_workspace_bytes.restype = sz
         L.tetra_kv_append.argtypes = [vp, vp, vp]
         L.tetra_kv_read.argtypes = [vp, vp, vp, i32, vp]
+        L.tetra_sample.argtypes = [vp, vp]
         L.tetra_kv_attend.argtypes = [vp, vp, C.c_int64, vp, i32, i32, C.c_float, vp, sz, vp]
         _lib = L
     return _lib
@@ -447,3 +448,21 @@ def tetra_kv_attend(q, cache, page_table, row_start, lengths, out, workspace, sc
 
     Same page_table, row_start and lengths as the tetra_kv_append before it; scale: 1 / sqrt(D) unless given."""
     return (_nat or _native()).kv_attend(cache, page_table, row_start, lengths, q, out, scale, workspace, stream)
+
+
+# ---------------------------------------------------------------------------
+# the next token (include/tetra_sample.h)
+# ---------------------------------------------------------------------------
+class SampleRows(C.Structure):
+    """Mirror of tetra_sample_rows."""
+    _fields_ = [("logits", C.c_void_p), ("u", C.c_void_p), ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p),
+                ("min_p", C.c_void_p), ("tokens", C.c_void_p), ("prob", C.c_void_p), ("row_stride", C.c_int64), ("rows", C.c_int32),
+                ("vocab", C.c_int32), ("half_type", C.c_int32)]
+
+
+def tetra_sample(logits, u, tokens, prob=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """The next token of each row of logits (float32 or float16 [rows, vocab], rows may lie apart); returns tokens (int32 [rows]).
+
+    u float32 [rows]: uniform numbers of [0, 1).  Per row, or None: temperature float32 (1; 0 takes the largest logit), top_k
+    int32, top_p float32, min_p float32 (off).  prob float32 [rows]: the probability with which the token was taken."""
+    return (_nat or _native()).sample(logits, u, tokens, prob, temperature, top_k, top_p, min_p, stream)
