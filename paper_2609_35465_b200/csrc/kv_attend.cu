@@ -29,8 +29,10 @@ namespace tetra {
 namespace {
 
 constexpr int kAttThreads = 256, kAttWarps = kAttThreads / 32;
+constexpr uint32_t kAttLeastUnits = 4;     // of a CTA: what sharing an item costs is worth some work
 constexpr int kAttSegs = 32;              // parts of items that a CTA looks up at a time
 constexpr int kAttMaxCtas = 512;          // of a launch: pieces in the workspace
+constexpr int kAttBatch = 8;               // pieces that are loaded at a time
 constexpr float kNoRef = -1e30f;          // reference of a column that has seen nothing
 constexpr float kLeastLog = -60.f;        // log2 of the least s_V that counts: 127 * 2^-60 is zero in float16
 constexpr float kHigh = 15.f, kBase = 7.f; // a weight reaches 2^kHigh at most, a new reference puts the largest at 2^kBase
@@ -40,13 +42,14 @@ struct AttCfg {
     static constexpr int REC = kv_record_bytes(D);
     static constexpr int CHUNKS = D / 32;                      // 512-byte chunks of the keys, and of the values
     static constexpr int FRAGS = NT * D / 16;                  // accumulators, four floats a lane each
-    static constexpr int STAGES = D == 64 ? 4 : 2;
+    static constexpr int ROUND = FRAGS < kAttWarps ? FRAGS : kAttWarps;  // of them that are merged at a time, one a warp
     static constexpr int CTAS = D == 256 || (D == 128 && NT == 4) ? 1 : 2;  // of an SM
+    static constexpr int STAGES = D == 64 || CTAS == 1 && D == 128 ? 3 : 2;
     static constexpr int RING = kAttWarps * STAGES * REC;
-    static constexpr int MERGE = kAttWarps / 2 * 32 * (FRAGS * 16 + NT * 16);
+    static constexpr int MERGE = kAttWarps * 512 * (ROUND + NT);
     static constexpr int QBYTES = NT > 1 ? NT * CHUNKS * 512 : 0;
-    static constexpr int PIECE = 32 * (FRAGS * 4 + NT * 4);    // floats of a piece in the workspace
-    static constexpr int SMEM = RING + MERGE + QBYTES;          // and 8 bytes a sequence
+    static constexpr int PIECE = 32 * FRAGS * 4 + NT * 16;     // floats of a piece in the workspace: accumulators; references and sums
+    static constexpr int SMEM = RING + MERGE + QBYTES;          // and 4 bytes a sequence
 };
 
 // A CTA's part of an item.
@@ -56,7 +59,7 @@ struct Seg {
     int32_t col0, cols;    // the item's first column, and the sequence's columns
     uint32_t r0, r1;       // blocks, of those that the item's last row sees
     int32_t first, last;   // CTAs that the item begins and ends in
-    int64_t before;        // tokens before the step
+    int32_t before;        // tokens before the step
 };
 
 struct AttParams {
@@ -66,6 +69,7 @@ struct AttParams {
     int64_t q_stride;
     float scale;           // times log2 e
     int32_t group;
+    int32_t unit_shift;    // blocks of a unit: 8 << unit_shift
     float* pieces;         // [CTA][2][PIECE]
     uint32_t* arrived;     // [CTA]: pieces of the item that begins in this CTA and ends beyond it
 };
@@ -107,199 +111,282 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
-// The sequence's columns, chunks of them, and blocks that its last row sees (one at least, so that an item without a
-// token is somebody's work: its rows are zero).
+// a / b, without a division where the quotient is plain (which it mostly is: one row, one chunk, one part).
+__device__ __forceinline__ uint32_t quotient(uint32_t a, uint32_t b) { return a < b ? 0u : b == 1u ? a : a / b; }
+
+// What a sequence asks for: its items, and units an item (one at least, so that an item without a token is somebody's
+// work: its rows are zero).
+struct Work {
+    int32_t row0, rows, before;
+    uint32_t chunks, blocks, units;
+};
 template <int NT>
-__device__ __forceinline__ void sequence_work(const AttParams& p, int s, int& a, int& rows, int64_t& before, uint32_t& chunks, uint32_t& blocks) {
+__device__ __forceinline__ Work sequence_work(const AttParams& p, int s) {
+    Work w;
     int b;
-    p.c.rows_of(s, a, b);
-    rows = b - a;
-    before = __ldg(p.c.lengths + s);
-    chunks = (uint32_t(rows) * p.group + 8 * NT - 1) / (8 * NT);
-    const int64_t most = int64_t(p.c.width) * p.c.blocks_per_page, seen = before + rows;
-    const int64_t n = seen <= 0 ? 0 : (seen + kKvBlock - 1) / kKvBlock;
-    blocks = uint32_t(n < 1 ? 1 : n > most ? most : n);
+    p.c.rows_of(s, w.row0, b);
+    w.rows = b - w.row0;
+    w.before = __ldg(p.c.lengths + s);
+    w.chunks = (uint32_t(w.rows) * p.group + 8 * NT - 1) / (8 * NT);
+    const uint32_t most = uint32_t(p.c.width) * uint32_t(p.c.blocks_per_page);
+    const int64_t seen = int64_t(w.before) + w.rows;
+    const uint32_t n = seen <= 0 ? 0u : uint32_t((seen + kKvBlock - 1) / kKvBlock);
+    w.blocks = min(n, most);
+    w.units = max(1u, (w.blocks + (kAttWarps << p.unit_shift) - 1) / (kAttWarps << p.unit_shift));
+    return w;
+}
+// The part of units [u0, u1) of an item.
+template <int NT>
+__device__ __forceinline__ void set_seg(const AttParams& p, const Work& w, int s, uint32_t item, uint32_t u0, uint32_t u1, int first, int last, Seg& q) {
+    q.seq = s;
+    const uint32_t head = quotient(item, w.chunks);
+    q.head = int(head);
+    q.row0 = w.row0;
+    q.col0 = int(item - head * w.chunks) * 8 * NT;
+    q.cols = w.rows * p.group;
+    q.before = w.before;
+    q.first = first;
+    q.last = last;
+    const uint32_t rows = q.col0 + 8 * NT >= q.cols ? w.rows : (q.col0 + 8 * NT - 1) / uint32_t(p.group) + 1;  // up to the item's last
+    const int64_t seen = int64_t(w.before) + rows;
+    const uint32_t n = seen <= 0 ? 0u : min(w.blocks, uint32_t((seen + kKvBlock - 1) / kKvBlock));
+    q.r0 = u0 * (kAttWarps << p.unit_shift);
+    q.r1 = min(n, u1 * (kAttWarps << p.unit_shift));
 }
 
-// Column (of the sequence) -> row of the step and query head; its last position.
-__device__ __forceinline__ int64_t column_at(const AttParams& p, const Seg& g, int col, int heads_all, int D) {
-    const int row = col / p.group, h = col % p.group;
-    return (int64_t(g.row0 + row) * heads_all + g.head * p.group + h) * D;
+// Parts of an item of so many units when a CTA takes `share` at most, and units of a part.
+__device__ __forceinline__ uint32_t parts_of(uint32_t units, uint32_t share, uint32_t& each) {
+    if (units <= share) {
+        each = units;
+        return 1;
+    }
+    const uint32_t parts = (units + share - 1) / share;
+    each = (units + parts - 1) / parts;
+    return (units + each - 1) / each;
+}
+
+template <int N>
+__device__ __forceinline__ void block_sums(uint32_t (&v)[N], uint32_t (*warp_sums)[kAttWarps]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = __reduce_add_sync(0xFFFFFFFFu, v[i]);
+        if (lane == 0) warp_sums[i][warp] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = 0;
+#pragma unroll
+        for (int w = 0; w < kAttWarps; ++w) v[i] += warp_sums[i][w];
+    }
+    __syncthreads();
 }
 
 template <int D, int NT>
 __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(AttParams p) {
     using C = AttCfg<D, NT>;
-    constexpr int CHUNKS = C::CHUNKS, STAGES = C::STAGES, REC = C::REC, FRAGS = C::FRAGS;
+    constexpr int CHUNKS = C::CHUNKS, STAGES = C::STAGES, REC = C::REC, FRAGS = C::FRAGS, ROUND = C::ROUND;
     extern __shared__ __align__(16) unsigned char smem[];
     unsigned char* ring = smem;
-    float4* merge = reinterpret_cast<float4*>(smem + C::RING);                             // [warps / 2][FRAGS + NT][32]
+    float4* merge = reinterpret_cast<float4*>(smem + C::RING);                             // [warps][ROUND + NT][32]
     unsigned char* qs = smem + C::RING + C::MERGE;                                         // [NT][CHUNKS][32][16 bytes]
-    uint64_t* prefix = reinterpret_cast<uint64_t*>(smem + C::RING + C::MERGE + C::QBYTES); // [seqs + 1]
+    uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + C::RING + C::MERGE + C::QBYTES); // [seqs + 1]
     __shared__ Seg segs[kAttSegs];
     __shared__ int nsegs, cursor_seq;
-    __shared__ uint64_t cursor_unit, range_end, share_units, warp_sums[kAttWarps];
-    __shared__ uint32_t is_last;
+    __shared__ uint32_t cursor_unit, is_last, warp_sums[4][kAttWarps];
 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int heads = p.c.kv_heads, heads_all = heads * p.group;
     pdl_wait();
     pdl_release();
 
-    // Prefix sum of the sequences' units.
-    {
-        const int per = (p.c.seqs + kAttThreads - 1) / kAttThreads, s0 = threadIdx.x * per;
-        uint64_t mine = 0;
-        uint64_t own[TETRA_KV_MAX_SEQS / kAttThreads];
+    // How the work is cut.  Every CTA finds out for itself, in loops that have one turn for up to 256 sequences (kept as loops:
+    // instructions that run once a launch cost their fetch).
+    const int per = (p.c.seqs + kAttThreads - 1) / kAttThreads, s0 = threadIdx.x * per, s1 = min(s0 + per, p.c.seqs);
+    uint32_t total[2] = {0, 0};
+#pragma unroll 1
+    for (int s = s0; s < s1; ++s) {
+        const Work w = sequence_work<NT>(p, s);
+        total[0] += w.chunks * heads;
+        total[1] += w.chunks * heads * w.units;
+    }
+    block_sums(total, warp_sums);
+    const uint32_t G = gridDim.x;
+    // With few items each gets CTAs of its own, as many parts as leave the longest part short: part sizes are tried from
+    // one that may need too many CTAs to one that cannot.  With many, a CTA takes a range of the sequence of all units.
+    const bool few = 2 * total[0] <= G;
+    uint32_t share = max(kAttLeastUnits, (total[1] + G - 1) / G);
+    if (few) {
+        uint32_t tried[3], need[3] = {0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < TETRA_KV_MAX_SEQS / kAttThreads; ++i) {
-            own[i] = 0;
-            if (i < per && s0 + i < p.c.seqs) {
-                int a, rows;
-                int64_t before;
-                uint32_t chunks, blocks;
-                sequence_work<NT>(p, s0 + i, a, rows, before, chunks, blocks);
-                own[i] = uint64_t(chunks) * heads * blocks;
-            }
-            mine += own[i];
+        for (int j = 0; j < 3; ++j) {
+            const uint32_t over = G - (total[0] * (j + 1) >> 2) - (j == 2 ? (total[0] + 3) >> 2 : 0);  // a quarter, half, all of the items' last parts
+            tried[j] = max(kAttLeastUnits, (total[1] + over - 1) / over);
         }
-        uint64_t sum = mine;
+        if (tried[0] > kAttLeastUnits) {
+#pragma unroll 1
+            for (int s = s0; s < s1; ++s) {
+                const Work w = sequence_work<NT>(p, s);
+#pragma unroll
+                for (int j = 0; j < 3; ++j) need[j] += w.chunks * heads * ((w.units + tried[j] - 1) / tried[j]);
+            }
+            block_sums(need, warp_sums);
+        }
+        share = need[0] <= G ? tried[0] : need[1] <= G ? tried[1] : tried[2];
+    }
+    // Prefix sum over the sequences: of CTAs, or of units.
+    {
+        auto wanted = [&](const Work& w) {
+            uint32_t each;
+            return w.chunks * heads * (few ? parts_of(w.units, share, each) : w.units);
+        };
+        uint32_t mine = 0;
+#pragma unroll 1
+        for (int s = s0; s < s1; ++s) {
+            const Work w = sequence_work<NT>(p, s);
+            if (w.chunks) mine += wanted(w);
+        }
+        uint32_t sum = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const uint64_t v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
             if (lane >= o) sum += v;
         }
-        if (lane == 31) warp_sums[warp] = sum;
+        if (lane == 31) warp_sums[0][warp] = sum;
         __syncthreads();
-        uint64_t at = sum - mine;
-        for (int w = 0; w < warp; ++w) at += warp_sums[w];
-#pragma unroll
-        for (int i = 0; i < TETRA_KV_MAX_SEQS / kAttThreads; ++i) {
-            if (i < per && s0 + i < p.c.seqs) prefix[s0 + i] = at;
-            at += own[i];
+        uint32_t at = sum - mine;
+        for (int w = 0; w < warp; ++w) at += warp_sums[0][w];
+        const uint32_t want = few ? blockIdx.x : share * blockIdx.x;
+        if (threadIdx.x == kAttThreads - 1) {
+            prefix[p.c.seqs] = at + mine;
+            if (want >= at + mine) cursor_seq = -1;  // nothing left for this CTA
         }
-        if (threadIdx.x == kAttThreads - 1) prefix[p.c.seqs] = at;
+        if (!few || (at <= want && want < at + mine)) {
+#pragma unroll 1
+            for (int s = s0; s < s1; ++s) {
+                const Work w = sequence_work<NT>(p, s);
+                const uint32_t own = w.chunks ? wanted(w) : 0u;
+                prefix[s] = at;
+                if (at <= want && want < at + own) {
+                    cursor_seq = s;
+                    cursor_unit = want;
+                    if (few) {
+                        uint32_t each;
+                        const uint32_t parts = parts_of(w.units, share, each), local = want - at, item = quotient(local, parts), part = local - item * parts;
+                        set_seg<NT>(p, w, s, item, part * each, (part + 1) * each, int(blockIdx.x - part), int(blockIdx.x - part + parts - 1), segs[0]);
+                        nsegs = 1;
+                    }
+                }
+                at += own;
+            }
+        }
         __syncthreads();
     }
-    const uint64_t units = prefix[p.c.seqs];
-    const uint64_t share = max(uint64_t(2 * kAttWarps), (units + gridDim.x - 1) / gridDim.x);
-    const uint64_t begin = share * blockIdx.x;
-    if (begin >= units) return;
-    for (int s = threadIdx.x; s < p.c.seqs; s += kAttThreads)
-        if (prefix[s] <= begin && begin < prefix[s + 1]) cursor_seq = s;
-    if (threadIdx.x == 0) {
-        cursor_unit = begin;
-        range_end = min(units, begin + share);
-        share_units = share;
-    }
-    __syncthreads();
+    if (cursor_seq < 0) return;
 
     const uint32_t my_ring = smem_u32(ring) + warp * STAGES * REC, lane16 = lane * 16;
     for (;;) {
-        // The next parts of items of this CTA's range.
-        if (threadIdx.x == 0) {
-            int n = 0, s = cursor_seq;
-            uint64_t u = cursor_unit;
-            const uint64_t end = range_end;
-            while (n < kAttSegs && u < end) {
-                while (u >= prefix[s + 1]) ++s;
-                int a, rows;
-                int64_t before;
-                uint32_t chunks, blocks;
-                sequence_work<NT>(p, s, a, rows, before, chunks, blocks);
-                uint64_t item = (u - prefix[s]) / blocks;
-                while (n < kAttSegs && u < end && u < prefix[s + 1]) {
-                    const uint64_t at = prefix[s] + item * blocks;
-                    Seg& q = segs[n++];
-                    q.seq = s;
-                    q.head = int(item / chunks);
-                    q.row0 = a;
-                    q.col0 = int(item % chunks) * 8 * NT;
-                    q.cols = rows * p.group;
-                    q.before = before;
-                    q.first = int(at / share);
-                    q.last = int((at + blocks - 1) / share);
-                    const uint32_t r0 = uint32_t(u - at), r1 = uint32_t(min(uint64_t(blocks), end - at));
-                    const int64_t seen = before + (min(q.col0 + 8 * NT, q.cols) - 1) / p.group + 1;  // of the item's last row
-                    const int64_t nb = seen <= 0 ? 0 : (seen + kKvBlock - 1) / kKvBlock;
-                    q.r0 = r0;
-                    q.r1 = nb < r1 ? uint32_t(nb) : r1;
-                    u = at + r1;
-                    ++item;
+        if (!few) {  // the next parts of items of this CTA's range
+            if (threadIdx.x == 0) {
+                int n = 0, s = cursor_seq;
+                uint32_t u = cursor_unit;
+                const uint32_t end = min(prefix[p.c.seqs], share * (blockIdx.x + 1));
+                while (n < kAttSegs && u < end) {
+                    while (u >= prefix[s + 1]) ++s;
+                    const Work w = sequence_work<NT>(p, s);
+                    uint32_t item = (u - prefix[s]) / w.units;
+                    while (n < kAttSegs && u < end && u < prefix[s + 1]) {
+                        const uint32_t at = prefix[s] + item * w.units, stop = min(at + w.units, end);
+                        set_seg<NT>(p, w, s, item, u - at, stop - at, int(at / share), int((at + w.units - 1) / share), segs[n++]);
+                        u = stop;
+                        ++item;
+                    }
                 }
+                nsegs = n;
+                cursor_seq = s;
+                cursor_unit = u;
             }
-            nsegs = n;
-            cursor_seq = s;
-            cursor_unit = u;
+            __syncthreads();
         }
-        __syncthreads();
         const int count = nsegs;
         if (count == 0) return;
 
-        // The warp's stream of records over these parts: what is copied next (its page number is loaded a record ahead).
-        int ahead_seg = -1;
+        // The warp's stream of records over these parts: lane l looks up the place of the l-th of the next 32.
+        int ahead_seg = -1, ahead_lane = 31;
         uint32_t ahead_rec = 0, ahead_end = 0;
-        const unsigned char* ahead_at = nullptr;
+        const unsigned char* ahead_at = nullptr;  // of the lane's record
         auto advance = [&] {
             ahead_rec += kAttWarps;
+            if (++ahead_lane < 32 && ahead_rec < ahead_end) return;
             while (ahead_rec >= ahead_end) {
-                if (++ahead_seg >= count) {
-                    ahead_seg = count;
-                    ahead_at = nullptr;
-                    return;
-                }
+                if (++ahead_seg >= count) return;
                 ahead_rec = segs[ahead_seg].r0 + warp;
                 ahead_end = segs[ahead_seg].r1;
             }
-            ahead_at = p.c.template record<D>(segs[ahead_seg].seq, ahead_rec, segs[ahead_seg].head);
+            ahead_lane = 0;
+            const uint32_t mine = ahead_rec + lane * kAttWarps;
+            ahead_at = mine < ahead_end ? p.c.template record<D>(segs[ahead_seg].seq, mine, segs[ahead_seg].head) : nullptr;
         };
         uint32_t placed = 0;  // bit per stage: its record has a place
         int stage = 0;
         auto issue = [&](int to) {
             placed &= ~(1u << to);
             if (ahead_seg < count) {
-                if (ahead_at) {
+                const unsigned char* from = reinterpret_cast<const unsigned char*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<uint64_t>(ahead_at), ahead_lane));
+                if (from) {
                     placed |= 1u << to;
                     const uint32_t dst = my_ring + to * REC;
 #pragma unroll
-                    for (int j = 0; j < 2 * CHUNKS; ++j) copy16(dst + j * 512 + lane16, ahead_at + j * 512 + lane16);
-                    if (lane == 0) copy16(dst + 2 * CHUNKS * 512, ahead_at + 2 * CHUNKS * 512);
+                    for (int j = 0; j < 2 * CHUNKS; ++j) copy16(dst + j * 512 + lane16, from + j * 512 + lane16);
+                    if (lane == 0) copy16(dst + 2 * CHUNKS * 512, from + 2 * CHUNKS * 512);
                 }
                 advance();
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         advance();
+        if (NT > 1) {
 #pragma unroll
-        for (int i = 0; i < STAGES; ++i) issue(i);
+            for (int i = 0; i < STAGES; ++i) issue(i);
+        }
 
         for (int i = 0; i < count; ++i) {
             const Seg& sg = segs[i];
             // Queries: lane (g, t) holds column g's dims 32 j + 8 t .. + 7 of every chunk j.
             uint4 qr[NT == 1 ? CHUNKS : 1];
             if (NT == 1) {
-                const int col = sg.col0 + g;
-                const bool live = col < sg.cols;
-                const __half* src = p.q + int64_t(sg.row0 + (live ? col : 0) / p.group) * p.q_stride + (sg.head * p.group + (live ? col : 0) % p.group) * D + 8 * t;
+                const uint32_t col = sg.col0 + g;
+                const bool live = int(col) < sg.cols;
+                const uint32_t row = live ? quotient(col, p.group) : 0, h = live ? col - row * p.group : 0;
+                const __half* src = p.q + int64_t(sg.row0 + row) * p.q_stride + (sg.head * p.group + h) * D + 8 * t;
 #pragma unroll
                 for (int j = 0; j < CHUNKS; ++j) qr[j] = live ? __ldg(reinterpret_cast<const uint4*>(src + 32 * j)) : make_uint4(0, 0, 0, 0);
+                if (i == 0) {  // behind the queries' loads: the first copies wait for a page number
+#pragma unroll
+                    for (int k = 0; k < STAGES; ++k) issue(k);
+                }
             } else {
                 for (int k = threadIdx.x; k < NT * CHUNKS * 32; k += kAttThreads) {
-                    const int l = k & 31, j = k / 32 % CHUNKS, col = sg.col0 + k / (32 * CHUNKS) * 8 + (l >> 2);
+                    const int l = k & 31, j = k / 32 % CHUNKS;
+                    const uint32_t col = sg.col0 + k / (32 * CHUNKS) * 8 + (l >> 2);
                     uint4 v = make_uint4(0, 0, 0, 0);
-                    if (col < sg.cols)
-                        v = __ldg(reinterpret_cast<const uint4*>(p.q + int64_t(sg.row0 + col / p.group) * p.q_stride + (sg.head * p.group + col % p.group) * D + 32 * j + 8 * (l & 3)));
+                    if (int(col) < sg.cols) {
+                        const uint32_t row = quotient(col, p.group), h = col - row * p.group;
+                        v = __ldg(reinterpret_cast<const uint4*>(p.q + int64_t(sg.row0 + row) * p.q_stride + (sg.head * p.group + h) * D + 32 * j + 8 * (l & 3)));
+                    }
                     reinterpret_cast<uint4*>(qs)[k] = v;
                 }
                 __syncthreads();
             }
-            // Last position of the lane's columns (2 t, 2 t + 1 of each eight).
-            int64_t sees[NT][2];
+            // Last position of the lane's columns (2 t, 2 t + 1 of each eight), and of the item's first.
+            int sees[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) sees[nt][k] = sg.before + (sg.col0 + nt * 8 + 2 * t + k) / p.group;
-            const int64_t all_see = sg.before + sg.col0 / p.group;  // the item's first row
+                for (int k = 0; k < 2; ++k)
+                    sees[nt][k] = int(min(int64_t(INT32_MAX), int64_t(sg.before) + quotient(sg.col0 + nt * 8 + 2 * t + k, p.group)));
+            const int all_see = int(min(int64_t(INT32_MAX), int64_t(sg.before) + quotient(sg.col0, p.group)));
 
             float o[FRAGS][4], ref[NT][2], sum[NT][2];
 #pragma unroll
@@ -335,13 +422,13 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                             mma16816(x[nt], c0, c1, c2, c3, b.z, b.w);
                         }
                     }
-                    const int64_t token = int64_t(rec) * kKvBlock + g;  // and 8 on
+                    const int token = int(rec * kKvBlock) + g;  // and 8 on
                     bool over = false;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) x[nt][k] *= by;
-                    if (int64_t(rec) * kKvBlock + kKvBlock - 1 > all_see) {  // the last blocks: some column does not see all of it
+                    if (int(rec * kKvBlock) + kKvBlock - 1 > all_see) {  // the last blocks: some column does not see all of it
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -403,110 +490,118 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                 stage = stage + 1 == STAGES ? 0 : stage + 1;
             }
 
-            // The warps' sums become one, halving the number of warps at a time, in a fixed order.
+            // Two of a fragment's values belong to column 2 t (2 t + 1) and dims d, d + 1.
+            auto store = [&](int f, const float (&v)[4], float s_even, float s_odd) {
+                const int nt = f / (D / 16), m = f % (D / 16), d = m / 2 * 32 + 4 * g + (m & 1) * 2;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t col = sg.col0 + nt * 8 + 2 * t + k, row = quotient(col, p.group), h = col - row * p.group;
+                    const float s = k ? s_odd : s_even, by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
+                    if (int(col) < sg.cols)
+                        *reinterpret_cast<__half2*>(p.out + (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D + d) = __floats2half2_rn(v[k] * by, v[k + 2] * by);
+                }
+            };
+
+            // The warps' sums become one: as many fragments as there are warps at a time, each warp adds one over all of them.
+            const bool whole = sg.first == sg.last;
+            // A piece of an item that several CTAs share: place 1 of the CTA that it begins in, place 0 of the others.
+            float4* piece = reinterpret_cast<float4*>(p.pieces + (size_t(blockIdx.x) * 2 + (int(blockIdx.x) == sg.first)) * C::PIECE);
+            constexpr int SLOT = (ROUND + NT) * 32;
+            float4* mine = merge + warp * SLOT + lane;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int m = 4; m <= 16; m <<= 1) sum[nt][k] += __shfl_xor_sync(0xFFFFFFFFu, sum[nt][k], m);
-#pragma unroll 1
-            for (int half = kAttWarps / 2; half >= 1; half >>= 1) {
-                float4* slot = merge + (warp & (half - 1)) * (FRAGS + NT) * 32 + lane;
-                if (warp >= half && warp < 2 * half) {
+                mine[(ROUND + nt) * 32] = make_float4(ref[nt][0], ref[nt][1], sum[nt][0], sum[nt][1]);
+            }
 #pragma unroll
-                    for (int f = 0; f < FRAGS; ++f) slot[f * 32] = make_float4(o[f][0], o[f][1], o[f][2], o[f][3]);
+            for (int at = 0; at < FRAGS; at += ROUND) {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) slot[(FRAGS + nt) * 32] = make_float4(ref[nt][0], ref[nt][1], sum[nt][0], sum[nt][1]);
-                }
+                for (int f = 0; f < ROUND; ++f) mine[f * 32] = make_float4(o[at + f][0], o[at + f][1], o[at + f][2], o[at + f][3]);
                 __syncthreads();
-                if (warp < half) {
+                if (warp < ROUND) {
+                    const int f = at + warp, nt = f / (D / 16);
+                    const float4* all = merge + lane;
+                    float4 m[kAttWarps];
+                    float r0 = kNoRef, r1 = kNoRef, u0 = 0.f, u1 = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const float4 v = slot[(FRAGS + nt) * 32];
-                        const float r0 = fmaxf(ref[nt][0], v.x), r1 = fmaxf(ref[nt][1], v.y);
-                        const float m0 = ex2(ref[nt][0] - r0), m1 = ex2(ref[nt][1] - r1), n0 = ex2(v.x - r0), n1 = ex2(v.y - r1);
-                        ref[nt][0] = r0;
-                        ref[nt][1] = r1;
-                        sum[nt][0] = sum[nt][0] * m0 + v.z * n0;
-                        sum[nt][1] = sum[nt][1] * m1 + v.w * n1;
+                    for (int w = 0; w < kAttWarps; ++w) {
+                        m[w] = all[w * SLOT + (ROUND + nt) * 32];
+                        r0 = fmaxf(r0, m[w].x);
+                        r1 = fmaxf(r1, m[w].y);
+                    }
 #pragma unroll
-                        for (int m = 0; m < D / 16; ++m) {
-                            const int f = nt * (D / 16) + m;
-                            const float4 u = slot[f * 32];
-                            o[f][0] = o[f][0] * m0 + u.x * n0;
-                            o[f][1] = o[f][1] * m1 + u.y * n1;
-                            o[f][2] = o[f][2] * m0 + u.z * n0;
-                            o[f][3] = o[f][3] * m1 + u.w * n1;
-                        }
+                    for (int w = 0; w < kAttWarps; ++w) {
+                        const float4 x = all[w * SLOT + warp * 32];
+                        const float f0 = ex2(m[w].x - r0), f1 = ex2(m[w].y - r1);
+                        u0 = fmaf(m[w].z, f0, u0);
+                        u1 = fmaf(m[w].w, f1, u1);
+                        v[0] = fmaf(x.x, f0, v[0]);
+                        v[1] = fmaf(x.y, f1, v[1]);
+                        v[2] = fmaf(x.z, f0, v[2]);
+                        v[3] = fmaf(x.w, f1, v[3]);
+                    }
+                    if (whole) {
+                        store(f, v, u0, u1);
+                    } else {
+                        __stcg(piece + f * 32 + lane, make_float4(v[0], v[1], v[2], v[3]));
+                        if (f % (D / 16) == 0 && g == 0) __stcg(piece + FRAGS * 32 + nt * 4 + t, make_float4(r0, r1, u0, u1));
                     }
                 }
                 __syncthreads();
             }
-
-            // Two of a fragment's values belong to column 2 t (2 t + 1) and dims d, d + 1.
-            auto store = [&](int f, const float (&v)[4], float s0, float s1) {
-                const int nt = f / (D / 16), m = f % (D / 16), d = m / 2 * 32 + 4 * g + (m & 1) * 2;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int col = sg.col0 + nt * 8 + 2 * t + k;
-                    const float s = k ? s1 : s0, by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
-                    if (col < sg.cols)
-                        *reinterpret_cast<__half2*>(p.out + column_at(p, sg, col, heads_all, D) + d) = __floats2half2_rn(v[k] * by, v[k + 2] * by);
-                }
-            };
-            if (sg.first == sg.last) {
-                if (warp == 0) {
-#pragma unroll
-                    for (int f = 0; f < FRAGS; ++f) store(f, o[f], sum[f / (D / 16)][0], sum[f / (D / 16)][1]);
-                }
-            } else {
-                // A piece of an item that several CTAs share: place 1 of the CTA that it begins in, place 0 of the others.
-                const int me = blockIdx.x;
-                if (warp == 0) {
-                    float4* piece = reinterpret_cast<float4*>(p.pieces + (size_t(me) * 2 + (me == sg.first)) * C::PIECE) + lane;
-#pragma unroll
-                    for (int f = 0; f < FRAGS; ++f) __stcg(piece + f * 32, make_float4(o[f][0], o[f][1], o[f][2], o[f][3]));
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) __stcg(piece + (FRAGS + nt) * 32, make_float4(ref[nt][0], ref[nt][1], sum[nt][0], sum[nt][1]));
-                    __threadfence();
-                    __syncwarp();
-                    if (lane == 0) {
-                        const uint32_t others = uint32_t(sg.last - sg.first);
-                        const uint32_t had = atomicAdd(p.arrived + sg.first, 1u);
-                        is_last = had == others;
-                        if (had == others) p.arrived[sg.first] = 0u;  // for the next call
-                        __threadfence();
-                    }
+            if (!whole) {
+                if (threadIdx.x == 0) {
+                    uint32_t had;  // behind the barrier: releases the whole CTA's stores, and acquires the others'
+                    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(had) : "l"(p.arrived + sg.first) : "memory");
+                    is_last = had == uint32_t(sg.last - sg.first);
+                    if (is_last) p.arrived[sg.first] = 0u;  // for the next call
                 }
                 __syncthreads();
                 if (is_last) {
-                    const float4* pieces = reinterpret_cast<const float4*>(p.pieces) + lane;
+                    const float4* pieces = reinterpret_cast<const float4*>(p.pieces);
                     constexpr int P4 = C::PIECE / 4;
                     for (int f = warp; f < FRAGS; f += kAttWarps) {
                         const int nt = f / (D / 16);
-                        float r0 = kNoRef, r1 = kNoRef, s0 = 0.f, s1 = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-                        for (int b = sg.first; b <= sg.last; ++b) {
-                            const float4* at = pieces + (size_t(b) * 2 + (b == sg.first)) * P4;
-                            const float4 u = __ldcg(at + f * 32), m = __ldcg(at + (FRAGS + nt) * 32);
-                            const float q0 = fmaxf(r0, m.x), q1 = fmaxf(r1, m.y);
-                            const float f0 = ex2(r0 - q0), f1 = ex2(r1 - q1), n0 = ex2(m.x - q0), n1 = ex2(m.y - q1);
+                        float r0 = kNoRef, r1 = kNoRef, u0 = 0.f, u1 = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                        for (int b = sg.first; b <= sg.last; b += kAttBatch) {
+                            float4 u[kAttBatch], m[kAttBatch];
+#pragma unroll
+                            for (int k = 0; k < kAttBatch; ++k) {
+                                const int c = min(b + k, sg.last);
+                                const float4* at = pieces + (size_t(c) * 2 + (c == sg.first)) * P4;
+                                u[k] = __ldcg(at + f * 32 + lane);
+                                m[k] = __ldcg(at + FRAGS * 32 + nt * 4 + t);
+                                if (b + k > sg.last) m[k] = make_float4(kNoRef, kNoRef, 0.f, 0.f), u[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            }
+                            float q0 = r0, q1 = r1;
+#pragma unroll
+                            for (int k = 0; k < kAttBatch; ++k) q0 = fmaxf(q0, m[k].x), q1 = fmaxf(q1, m[k].y);
+                            const float f0 = ex2(r0 - q0), f1 = ex2(r1 - q1);
+                            u0 *= f0, u1 *= f1, v[0] *= f0, v[1] *= f1, v[2] *= f0, v[3] *= f1;
+#pragma unroll
+                            for (int k = 0; k < kAttBatch; ++k) {
+                                const float n0 = ex2(m[k].x - q0), n1 = ex2(m[k].y - q1);
+                                u0 = fmaf(m[k].z, n0, u0);
+                                u1 = fmaf(m[k].w, n1, u1);
+                                v[0] = fmaf(u[k].x, n0, v[0]);
+                                v[1] = fmaf(u[k].y, n1, v[1]);
+                                v[2] = fmaf(u[k].z, n0, v[2]);
+                                v[3] = fmaf(u[k].w, n1, v[3]);
+                            }
                             r0 = q0;
                             r1 = q1;
-                            s0 = s0 * f0 + m.z * n0;
-                            s1 = s1 * f1 + m.w * n1;
-                            v[0] = v[0] * f0 + u.x * n0;
-                            v[1] = v[1] * f1 + u.y * n1;
-                            v[2] = v[2] * f0 + u.z * n0;
-                            v[3] = v[3] * f1 + u.w * n1;
                         }
-                        store(f, v, s0, s1);
+                        store(f, v, u0, u1);
                     }
                 }
                 __syncthreads();  // is_last
             }
         }
+        if (few) return;
         __syncthreads();  // segs
     }
 }
@@ -518,14 +613,18 @@ template <int D>
 constexpr size_t att_workspace() { return size_t(kAttCounters) + size_t(kAttMaxCtas) * 2 * AttCfg<D, att_most_columns<D>()>::PIECE * 4; }
 
 template <int D, int NT>
-cudaError_t launch_attend(const AttParams& p, int sms, cudaStream_t s) {
+cudaError_t launch_attend(AttParams p, int sms, cudaStream_t s) {
     using C = AttCfg<D, NT>;
-    constexpr int most = C::SMEM + 8 * (TETRA_KV_MAX_SEQS + 1);
+    constexpr int most = C::SMEM + 4 * (TETRA_KV_MAX_SEQS + 1);
     static PerDeviceOnce once;  // per instantiation
     cudaError_t e = once.run([] { return cudaFuncSetAttribute(k_kv_attend<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, most); });
     if (e != cudaSuccess) return e;
     const int grid = C::CTAS * sms < kAttMaxCtas ? C::CTAS * sms : kAttMaxCtas;
-    return launch_pdl(k_kv_attend<D, NT>, grid, kAttThreads, size_t(C::SMEM) + 8 * (p.c.seqs + 1), s, p);
+    // Units are counted in 32 bits, a grid's rounding with them: larger ones where all sequences, as long as the table and with
+    // all of the rows (row_start is not known here), could pass that.
+    const int64_t items = (int64_t(p.c.rows) * p.group / (8 * NT) + 1) * p.c.seqs * p.c.kv_heads, blocks = int64_t(p.c.width) * p.c.blocks_per_page;
+    while (items * (blocks / (kAttWarps << p.unit_shift) + 1) > (1ll << 30) && blocks > (kAttWarps << p.unit_shift)) ++p.unit_shift;
+    return launch_pdl(k_kv_attend<D, NT>, grid, kAttThreads, size_t(C::SMEM) + 4 * (p.c.seqs + 1), s, p);
 }
 
 // Columns of an item by what a sequence has on average: more of them read a block's codes once for more rows, but an
@@ -557,7 +656,7 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const void* q, int64_t q_stride
     const int D = cache->head_dim;
     if (!q || !out || !workspace) return TETRA_ERR_NULL;
     if (q_heads < 1 || q_heads % p.c.kv_heads || q_heads > 4096 || q_stride < int64_t(q_heads) * D) return TETRA_ERR_SHAPE;
-    if (!std::isfinite(scale)) return TETRA_ERR_SHAPE;
+    if (!std::isfinite(scale) || int64_t(cache->seqs) * rows * q_heads > (1ll << 32)) return TETRA_ERR_SHAPE;
     if (!kv_aligned(q, 16) || q_stride % 8 || !kv_aligned(out, 16) || !kv_aligned(workspace, 256)) return TETRA_ERR_ALIGN;
     if (workspace_bytes < tetra_kv_workspace_bytes(D)) return TETRA_ERR_SIZE;
     if (rows == 0) return TETRA_OK;
@@ -568,6 +667,7 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const void* q, int64_t q_stride
     p.q_stride = q_stride;
     p.scale = scale * 1.4426950408889634f;
     p.group = q_heads / p.c.kv_heads;
+    p.unit_shift = 0;
     p.arrived = static_cast<uint32_t*>(workspace);
     p.pieces = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + kAttCounters);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
