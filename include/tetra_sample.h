@@ -40,8 +40,8 @@ typedef struct {
  * u lies in [0, 1) (values outside are taken as the nearest inside, NaN as 0).  T that is not above zero takes the first
  * of the largest logits, with prob 1.  NaN counts as minus infinity, which is never taken; where a logit is plus infinity only
  * those have mass.  A row without a logit above minus infinity gives token -1 and prob 0.
- * The weights are whole multiples of 2^-44 (one below half of that has none), rounded from a float64 exponential, and every sum of them is exact: the
- * result does not depend on any order of summation and is the same from run to run.  One launch, no scratch memory. */
+ * The weights are whole multiples of 2^-44, off by no more than that (the least have none), and every sum of them is exact:
+ * the result does not depend on any order of summation and is the same from run to run.  One launch, no scratch memory. */
 int tetra_sample(const tetra_sample_rows *rows, void *stream);
 
 #ifdef __cplusplus

@@ -1,7 +1,7 @@
 """The choice of the next token on the GPU against the plain form in 64 bits (step_reference.sample).
 
-The kernel's weights are whole multiples of 2^-44 of an exponential that is off by 2^-45 at most, so every partial sum of n of
-them is off by n 2^-44 in units of the largest weight; a draw whose aim is nearer to a border than that may fall on either
+The kernel's weights are whole multiples of 2^-44 that are off by no more than that, so every partial sum of n of them is off
+by n 2^-44 in units of the largest weight; a draw whose aim is nearer to a border than that may fall on either
 side, and none of those tested is (their distance is looked at).  prob is rounded to float32 once."""
 import numpy as np
 import pytest
