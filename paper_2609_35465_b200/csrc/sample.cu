@@ -1,16 +1,16 @@
 // The next token of each row of logits: temperature, top-k, top-p and min-p, from given uniform numbers (tetra_sample).
 //
-// A cluster of eight CTAs takes a row.  Each CTA reads an eighth of it once, as integer keys in the order of the floats, into
-// shared memory; everything after that happens there and in the cluster's distributed shared memory.
+// A cluster of eight CTAs takes a row.  Each CTA reads an eighth of it once into shared memory; everything after that
+// happens there and in the cluster's distributed shared memory.
 //   * Weights are fixed-point numbers (units of 2^-44 of the largest), so sums are exact in whatever order, and what
-//     is found by a histogram here, by a sort there and by a scan at the end agrees to the last bit.
+//     is found by a histogram here, by counting there and by a scan at the end agrees to the last bit.
 //   * The three filters all keep a prefix of the order (logit down, index up), so they come to one cut: the last entry
-//     (key, index) that stays.  Top-k: a histogram of counts over the distance from the largest logit finds the bin of the
-//     k-th; where the bins up to it hold no more than 2048 entries these go to one CTA, which sorts them and does all the
-//     rest.  Otherwise, and for top-p without top-k, a histogram of masses finds the bin that the cut is in, and the one CTA
-//     sorts that bin.  A bin with too many entries (equal logits, outliers) is cut by bisection over the entries instead:
-//     any input is right, the usual ones are fast.
-//   * The draw scans the kept weights in the order of the indexes.
+//     (logit, index) that stays.  A histogram over the distance from the largest logit, of counts for top-k and of masses
+//     for top-p alone, finds the bin that the cut is in.  Where the bins up to it hold no more than 2048 entries, these
+//     go to the first CTA, which does all the rest.  Otherwise the entries of that bin go there, a second histogram among
+//     them finds the cut, and the cluster draws.  A bin with too many entries (equal logits, outliers) is cut by bisection
+//     over the entries instead: any input is right, the usual ones are fast.
+//   * The draw goes through the kept weights in the order of the indexes.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
@@ -24,10 +24,11 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kSmpThreads = 512, kSmpWarps = kSmpThreads / 32, kSmpCtas = 8;
-constexpr int kSmpBins = 1024, kSmpMine = kSmpBins / kSmpCtas;  // bins of the cluster, and those that a CTA adds up
-constexpr int kSmpList = 2048;                                  // entries of a bin that are sorted
+constexpr int kSmpBins = 1024;
+constexpr int kSmpList = 2048;                                  // entries that one CTA takes
+constexpr int kSmpRegion = kSmpList / kSmpCtas;                // ... an equal share of each
+constexpr int kSmpFew = 256;                                    // ... and compares each with each
 constexpr int kSmpBits = 44;                                    // a weight of 1 is 2^44
-constexpr uint32_t kMinusInf = 0x007FFFFFu;                     // its key
 
 static_assert(kSmpCtas * kSmpThreads > 0 && TETRA_SAMPLE_MAX_VOCAB <= 1 << 19, "sums of weights stay below 2^63");
 
@@ -36,38 +37,38 @@ struct Tally {  // so many entries with so much mass
     uint64_t count;
 };
 
-struct SmpShared {
+struct alignas(16) SmpShared {
     uint64_t list[kSmpList];
-    double powers[64];          // 2^(44 + j / 64)
-    uint32_t lo[kSmpBins], hi[kSmpBins];  // counts (lo), or masses
-    Tally mine[kSmpMine];       // inclusive sums over this CTA's bins
-    Tally slots[2][kSmpCtas];   // what the CTAs tell each other
-    Tally warp[kSmpWarps];
-    uint64_t bin[3];            // a crossing: its bin, sum before it, sum in it
-    uint64_t found[2];          // a cut, and the mass up to it
-    uint32_t listed[2];         // by the first gathering, by the second
+    uint64_t weight[kSmpFew];
+    double powers[64];                    // 2^(44 + j / 64)
+    uint32_t count[kSmpBins], lo[kSmpBins], hi[kSmpBins];  // of the bins: entries, mass in two words
+    Tally slots[2][kSmpCtas];             // what the CTAs tell each other
+    Tally warp[kSmpWarps], whole;
+    uint64_t bin, ahead, need, entries;   // a crossing: its bin, the sum before it, what is needed, entries up to its end
+    uint64_t cut;
+    uint32_t listed, sub, few;
 };
 
+// Logits are compared as integers in the order of the floats; NaN is minus infinity, zeros (and what is below 2^-126) are equal.
+__device__ __forceinline__ float clean(float x) { return __fadd_rn(fmaxf(x, -INFINITY), 0.f); }
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t b = __float_as_uint(x);
-    if ((b & 0x7FFFFFFFu) > 0x7F800000u) return kMinusInf;  // NaN
-    if (b == 0x80000000u) return 0x80000000u;               // -0 equals 0
-    return b ^ (b & 0x80000000u ? 0xFFFFFFFFu : 0x80000000u);
+    return b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
-// Weight of a key in units of 2^-44: 2^t, t = (x - max) log2(e) / T = k / 64 + f / 64 with |f| <= 1/2, as 2^(k / 64) from a table
+// Weight of a logit in units of 2^-44: 2^t, t = (x - max) log2(e) / T = k / 64 + f / 64 with |f| <= 1/2, as 2^(k / 64) from a table
 // times the exponential series of f ln 2 / 64 up to the fourth power (the next is 4e-14, 2^-44), rounded once; in float64, whose
 // multiply-adds run at half the rate of float32's here.  Adding 1.5 * 2^52 leaves a whole number in the low bits.
 struct Weigh {
-    uint32_t top;           // largest key
-    double max, by;         // its value; 64 log2(e) / T
+    float top;              // largest logit
+    double by;              // 64 log2(e) / T
     const double* powers;
-    __device__ __forceinline__ uint64_t operator()(uint32_t key) const {
+    __device__ __forceinline__ uint64_t operator()(float x) const {
         constexpr double magic = 6755399441055744.;
-        if (key == top) return 1ull << kSmpBits;
-        const double d = double(value_of(key)) - max, t = d * by;
-        if (!(t > -46. * 64.) || key <= kMinusInf) return 0;  // not where the largest is infinite
+        if (x == top) return 1ull << kSmpBits;
+        const double t = (double(x) - double(top)) * by;
+        if (!(t > -46. * 64.) || x == -INFINITY) return 0;  // not where the largest is infinite
         const double m = t + magic, f = t - (m - magic);
         const int k = __double2loint(m);
         constexpr double c = 0.693147180559945309417 / 64.;
@@ -92,37 +93,49 @@ __device__ __forceinline__ Tally warp_scan(Tally v, int lane) {
     }
     return v;
 }
-// ... over the CTA's threads up to this one; `total` is the CTA's.
+// ... over the CTA's threads up to this one; `total` is the CTA's.  The warps' sums are added by one warp: each thread adding them
+// for itself takes more cycles than all the rest.
 __device__ __forceinline__ Tally block_scan(SmpShared& sm, Tally v, Tally& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     v = warp_scan(v, lane);
-    __syncthreads();
     if (lane == 31) sm.warp[warp] = v;
     __syncthreads();
-    total = {0, 0};
-    Tally before{0, 0};
-#pragma unroll
-    for (int w = 0; w < kSmpWarps; ++w) {
-        if (w == warp) before = total;
-        total = total + sm.warp[w];
+    if (warp == 0) {
+        const Tally own = lane < kSmpWarps ? sm.warp[lane] : Tally{0, 0}, upto = warp_scan(own, lane);
+        if (lane < kSmpWarps) sm.warp[lane] = {upto.mass - own.mass, upto.count - own.count};
+        if (lane == 31) sm.whole = upto;
     }
+    __syncthreads();
+    total = sm.whole;
+    const Tally before = sm.warp[warp];
+    __syncthreads();
     return before + v;
 }
 
-// Sorts list[0 .. size), a power of two, the largest first.  Up to 64 entries are the first warp's own work.
+// Largest mass and least count of N lanes next to each other.
+template <int N>
+__device__ __forceinline__ Tally extremes(Tally v) {
+#pragma unroll
+    for (int o = N / 2; o >= 1; o >>= 1) {
+        v.mass = max(v.mass, __shfl_xor_sync(0xFFFFFFFFu, v.mass, o));
+        v.count = min(v.count, __shfl_xor_sync(0xFFFFFFFFu, v.count, o));
+    }
+    return v;
+}
+
+// Sorts list[0 .. size), a power of two, the largest first.
 __device__ __forceinline__ void sort_list(uint64_t* list, uint32_t size) {
-    const bool small = size <= 64;
+#pragma unroll 1
     for (uint32_t k = 2; k <= size; k <<= 1)
+#pragma unroll 1
         for (uint32_t j = k >> 1; j > 0; j >>= 1) {
-            if (small) __syncwarp();
-            else __syncthreads();
             for (uint32_t i = threadIdx.x; i < size / 2; i += kSmpThreads) {
                 const uint32_t a = (i & ~(j - 1)) << 1 | (i & (j - 1)), b = a | j;
                 const uint64_t u = list[a], v = list[b];
                 if ((u < v) == !(a & k)) list[a] = v, list[b] = u;
             }
+            __syncthreads();
         }
-    __syncthreads();
 }
 __device__ __forceinline__ uint32_t power_of_two(uint32_t n) {
     uint32_t size = 2;
@@ -130,15 +143,31 @@ __device__ __forceinline__ uint32_t power_of_two(uint32_t n) {
     return size;
 }
 
+// Distance bins: logit -> bin, the largest in bin 0; kSmpBins for one without mass (e^-31.25 is less than half a unit).
+struct Bins {
+    float top, range, by;
+    __device__ __forceinline__ Bins(float top_, float least, float T) : top(top_), range(fminf(fminf(top_ - least, 31.25f * T), 3.0e38f)) {
+        by = range > 1e-30f ? float(kSmpBins) / range : 0.f;
+    }
+    __device__ __forceinline__ float at(float x) const {
+        const float d = top - x;
+        return x == top ? 0.f : d <= range ? d * by : float(2 * kSmpBins);  // not where the largest is infinite
+    }
+    __device__ __forceinline__ uint32_t operator()(float x) const {
+        const float b = at(x);
+        return b < float(2 * kSmpBins) ? min(uint32_t(b), uint32_t(kSmpBins - 1)) : uint32_t(kSmpBins);
+    }
+};
+
 struct Row {
     SmpShared& sm;
-    const uint32_t* keys;
-    int count;      // of this CTA's part
-    uint32_t index; // of its first token
+    const float* x;   // this CTA's part, minus infinity up to a multiple of four
+    int count;
+    uint32_t index;   // of its first token
     cg::cluster_group cluster;
     int rank, turn;
 
-    // Every CTA's value for every CTA, in the order of their ranks.
+    // Every CTA's value for every CTA, in the order of their ranks.  The first warp's lanes bring the CTA's.
     __device__ __forceinline__ const Tally* tell(Tally mine) {
         Tally* slots = sm.slots[turn & 1];
         ++turn;
@@ -146,123 +175,249 @@ struct Row {
         cluster.sync();
         return slots;
     }
-    __device__ __forceinline__ uint64_t entry(int i) const { return uint64_t(keys[i]) << 32 | uint32_t(~(index + uint32_t(i))); }
-};
-
-// Distance bins: key -> bin, the largest logit in bin 0; kSmpBins for a key without mass.
-struct Bins {
-    uint32_t top;
-    float max, range, by;
-    __device__ __forceinline__ uint32_t operator()(uint32_t key) const {
-        if (key == top) return 0;
-        const float d = max - value_of(key);
-        if (!(d <= range) || key <= kMinusInf) return kSmpBins;
-        return min(uint32_t(kSmpBins - 1), uint32_t(d * by));
-    }
-};
-
-// The histogram's sums (counts, or masses: as Tally.mass) over the cluster: an eighth of the bins to each CTA, whose inclusive sums
-// are left in sm.mine; what is before them, and the whole.
-__device__ __forceinline__ void add_bins(Row& row, uint64_t& before, uint64_t& whole) {
-    SmpShared& sm = row.sm;
-    row.cluster.sync();
-    uint64_t v = 0;
-    if (threadIdx.x < kSmpMine) {
-        const int b = row.rank * kSmpMine + threadIdx.x;
-#pragma unroll
-        for (int c = 0; c < kSmpCtas; ++c) {
-            const SmpShared* other = row.cluster.map_shared_rank(&sm, c);
-            v += (uint64_t(other->hi[b]) << 32) + other->lo[b];
+    __device__ __forceinline__ uint64_t entry(int i, float v) const { return uint64_t(key_of(v)) << 32 | uint32_t(~(index + uint32_t(i))); }
+    // body(i, x_i) for all of the part's tokens, four of a thread at a time (what is behind the part is minus infinity).
+    template <typename F>
+    __device__ __forceinline__ void each(F&& body) const {
+#pragma unroll 2
+        for (int i = 4 * threadIdx.x; i < count; i += 4 * kSmpThreads) {
+            const float4 v = *reinterpret_cast<const float4*>(x + i);
+            body(i, v.x);
+            body(i + 1, v.y);
+            body(i + 2, v.z);
+            body(i + 3, v.w);
         }
     }
+};
+
+// A mass to a bin's: 64 bits in two words, the carry by hand.
+__device__ __forceinline__ void add_mass(uint32_t* lo, uint32_t* hi, uint64_t w) {
+    const uint32_t low = uint32_t(w), old = atomicAdd(lo, low), high = uint32_t(w >> 32) + (old + low < old);
+    if (high) atomicAdd(hi, high);
+}
+
+__device__ __forceinline__ uint64_t needed(float p, uint64_t mass) {
+    const uint64_t need = uint64_t(ceil(double(p) * double(mass)));
+    return need < 1 ? 1 : need > mass ? mass : need;
+}
+__device__ __forceinline__ uint64_t aimed(float u, uint64_t mass) {
+    const uint64_t aim = uint64_t(fmin(fmax(double(u), 0.), 1.) * double(mass));  // NaN: 0
+    return aim >= mass ? mass - 1 : aim;
+}
+
+// The bin in which this CTA's counts reach k; the last one where they do not.
+__device__ __forceinline__ uint32_t local_bin(SmpShared& sm, uint64_t k) {
+    constexpr int PER = kSmpBins / kSmpThreads;
+    if (threadIdx.x == 0) sm.sub = kSmpBins - 1;
+    __syncthreads();
+    uint64_t sum = 0;
+    uint32_t own[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += own[i] = sm.count[threadIdx.x * PER + i];
     Tally total;
-    const Tally upto = block_scan(sm, {v, 0}, total);
-    if (threadIdx.x < kSmpMine) sm.mine[threadIdx.x] = upto;
-    const Tally* all = row.tell(total);
-    before = whole = 0;
-    for (int c = 0; c < kSmpCtas; ++c) {
-        if (c == row.rank) before = whole;
-        whole += all[c].mass;
+    uint64_t upto = block_scan(sm, {sum, 0}, total).mass - sum;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (upto < k && k <= upto + own[i]) sm.sub = threadIdx.x * PER + i;
+        upto += own[i];
     }
+    __syncthreads();
+    return sm.sub;
 }
 
-// The bin in which the sums reach `need`, 0 < need <= whole: told to all CTAs in sm.bin.
-__device__ __forceinline__ void find_bin(Row& row, uint64_t before, uint64_t need) {
+// The cluster's histogram in the first CTA, which finds the bin in which the sums (entries, or mass) reach k entries, or p of the
+// whole mass, and tells all.  Every CTA's histogram is complete but for a barrier.
+template <bool MASS>
+__device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
     SmpShared& sm = row.sm;
-    if (threadIdx.x < kSmpMine) {
-        const uint64_t upto = before + sm.mine[threadIdx.x].mass, from = threadIdx.x ? before + sm.mine[threadIdx.x - 1].mass : before;
-        if (from < need && need <= upto)
-            for (int r = 0; r < kSmpCtas; ++r) {
-                uint64_t* bin = row.cluster.map_shared_rank(sm.bin, r);
-                bin[0] = uint64_t(row.rank * kSmpMine) + threadIdx.x;
-                bin[1] = from;
-                bin[2] = upto - from;
+    __syncthreads();
+    if (row.rank != 0) {
+        SmpShared* first = row.cluster.map_shared_rank(&sm, 0);
+#pragma unroll
+        for (int i = 0; i < kSmpBins / kSmpThreads; ++i) {
+            const int b = threadIdx.x + i * kSmpThreads;
+            if (sm.count[b]) {
+                atomicAdd(first->count + b, sm.count[b]);
+                if (MASS) add_mass(first->lo + b, first->hi + b, (uint64_t(sm.hi[b]) << 32) + sm.lo[b]);
             }
+        }
     }
     row.cluster.sync();
-}
-
-// Entries of the bins [low, high] that are not below `cut` into the list of the first CTA, whose sm.listed[which] says how
-// many there are (more than kSmpList: the list is not whole).  A row gathers at most twice.
-__device__ __forceinline__ void gather(Row& row, const Bins& bins, uint32_t low, uint32_t high, uint64_t cut, int which) {
-    uint64_t* list = row.cluster.map_shared_rank(row.sm.list, 0);
-    uint32_t* listed = row.cluster.map_shared_rank(row.sm.listed + which, 0);
-    for (int i = threadIdx.x; i < row.count; i += kSmpThreads) {
-        const uint32_t bin = bins(row.keys[i]);
-        if (bin >= low && bin <= high && row.entry(i) >= cut) {
-            const uint32_t at = atomicAdd(listed, 1u);
-            if (at < kSmpList) list[at] = row.entry(i);
+    if (row.rank == 0) {
+        constexpr int PER = kSmpBins / kSmpThreads;
+        Tally own[PER], sum{0, 0}, total;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int b = threadIdx.x * PER + i;
+            own[i] = {MASS ? (uint64_t(sm.hi[b]) << 32) + sm.lo[b] : 0ull, sm.count[b]};
+            sum = sum + own[i];
+        }
+        Tally upto = block_scan(sm, sum, total);
+        upto = {upto.mass - sum.mass, upto.count - sum.count};
+        // With fewer entries than k all stay: the last bin, and no cut.
+        const uint64_t need = MASS ? needed(p, total.mass) : k, whole = total.count;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const Tally from = upto;
+            upto = upto + own[i];
+            const uint64_t a = MASS ? from.mass : from.count, b = MASS ? upto.mass : upto.count;
+            const bool all = !MASS && need >= whole && threadIdx.x == kSmpThreads - 1 && i == PER - 1;
+            if (all || ((MASS || need < whole) && a < need && need <= b))
+                for (int r = 0; r < kSmpCtas; ++r) {
+                    SmpShared* other = row.cluster.map_shared_rank(&sm, r);
+                    other->bin = all ? kSmpBins : uint64_t(threadIdx.x * PER + i);
+                    other->ahead = a;
+                    other->need = need;
+                    other->entries = upto.count;
+                }
         }
     }
     row.cluster.sync();
 }
 
-// The entry in bin sm.bin[0] with which `need` (entries, or mass, counted from the largest logit, of the entries not below
-// `least`) is reached, and the mass in the bin up to it.
-template <bool MASS>
-__device__ __forceinline__ uint64_t find_cut(Row& row, const Bins& bins, const Weigh& weigh, uint64_t need, uint64_t least) {
+// Entries of the bins [low, high] that are not below `cut`: how many there are in the cluster, and all of them in the list of
+// the first CTA where they are kSmpList at most.  Collected at home first: a counter in another CTA takes a thousand cycles.
+__device__ __forceinline__ uint32_t gather(Row& row, const Bins& bins, uint32_t low, uint32_t high, uint64_t cut) {
     SmpShared& sm = row.sm;
-    const uint32_t bin = uint32_t(sm.bin[0]);
-    const uint64_t ahead = sm.bin[1];
-    gather(row, bins, bin, bin, least, MASS);
-    const uint32_t entries = *row.cluster.map_shared_rank(row.sm.listed + MASS, 0);  // that CTA passes another barrier before it ends
-    if (entries <= kSmpList) {
-        if (row.rank == 0) {
-            const uint32_t size = power_of_two(entries);
-            for (uint32_t i = entries + threadIdx.x; i < size; i += kSmpThreads) sm.list[i] = 0;
-            __syncthreads();
-            sort_list(sm.list, size);
-            constexpr int PER = kSmpList / kSmpThreads;
-            uint64_t own[PER], sum = 0;
+    row.each([&](int i, float v) {
+        const uint32_t bin = bins(v);
+        if (bin >= low && bin <= high && row.entry(i, v) >= cut) {
+            const uint32_t at = atomicAdd(&sm.listed, 1u);
+            if (at < kSmpList) sm.list[at] = row.entry(i, v);
+        }
+    });
+    __syncthreads();
+    const uint32_t mine = sm.listed;
+    const Tally* all = row.tell({0, mine});
+    uint32_t before = 0, total = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t at = threadIdx.x * PER + i;
-                own[i] = at < entries ? MASS ? weigh(uint32_t(sm.list[at] >> 32)) : 1ull : 0ull;
-                sum += own[i];
-            }
-            Tally total;
-            uint64_t upto = ahead + block_scan(sm, {sum, 0}, total).mass - sum;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint64_t from = upto;
-                upto += own[i];
-                if (from < need && need <= upto)
-                    for (int r = 0; r < kSmpCtas; ++r) *row.cluster.map_shared_rank(sm.found, r) = sm.list[threadIdx.x * PER + i];
-            }
+    for (int c = 0; c < kSmpCtas; ++c) {
+        if (c == row.rank) before = total;
+        total += uint32_t(all[c].count);
+    }
+    if (threadIdx.x == 0) sm.listed = 0;
+    if (total <= kSmpList) {
+        if (row.rank != 0) {
+            uint64_t* list = row.cluster.map_shared_rank(sm.list, 0) + before;
+            for (uint32_t i = threadIdx.x; i < mine; i += kSmpThreads) list[i] = sm.list[i];
         }
         row.cluster.sync();
-        // sm.bin and sm.found are written again behind a barrier of the cluster that follows these reads.
-        return sm.found[0];
+    }
+    return total;
+}
+
+// Among sm.list[0 .. n), n >= 1, the entry with which `need` is reached from `ahead` on: into *cut.  `scale` (bins.at() - bin) is
+// from 0 to kSmpBins for all of them.  One CTA.
+template <bool MASS>
+__device__ __noinline__ void cut_list(SmpShared& sm, const Bins bins, const Weigh weigh, uint32_t n, float bin, float scale, uint64_t ahead, uint64_t need, uint64_t* cut) {
+    constexpr int PER = kSmpBins / kSmpThreads;
+    auto weight = [&](uint64_t entry) { return MASS ? weigh(value_of(uint32_t(entry >> 32))) : 1ull; };
+    if (n > kSmpFew) {  // a histogram of their own
+        for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = sm.lo[i] = sm.hi[i] = 0;
+        if (threadIdx.x == 0) sm.few = 0;
+        __syncthreads();
+        auto inside = [&](uint64_t entry) {
+            const float f = (bins.at(value_of(uint32_t(entry >> 32))) - bin) * scale;
+            return uint32_t(fminf(fmaxf(f, 0.f), float(kSmpBins - 1)));
+        };
+        for (uint32_t i = threadIdx.x; i < n; i += kSmpThreads) {
+            const uint32_t b = inside(sm.list[i]);
+            atomicAdd(sm.count + b, 1u);
+            if (MASS) add_mass(sm.lo + b, sm.hi + b, weight(sm.list[i]));
+        }
+        __syncthreads();
+        uint64_t own[PER], sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int b = threadIdx.x * PER + i;
+            own[i] = MASS ? (uint64_t(sm.hi[b]) << 32) + sm.lo[b] : sm.count[b];
+            sum += own[i];
+        }
+        Tally total;
+        uint64_t upto = ahead + block_scan(sm, {sum, 0}, total).mass - sum;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (upto < need && need <= upto + own[i]) sm.sub = threadIdx.x * PER + i, sm.need = need - upto;
+            upto += own[i];
+        }
+        __syncthreads();
+        if (sm.count[sm.sub] <= kSmpFew) {  // its entries, to be counted
+            uint64_t keep[kSmpList / kSmpThreads];
+#pragma unroll
+            for (int i = 0; i < kSmpList / kSmpThreads; ++i) {
+                const uint32_t at = threadIdx.x + i * kSmpThreads;
+                keep[i] = at < n && inside(sm.list[at]) == sm.sub ? sm.list[at] : 0;
+            }
+            n = sm.count[sm.sub];
+            need = sm.need;
+            ahead = 0;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kSmpList / kSmpThreads; ++i)
+                if (keep[i]) sm.list[atomicAdd(&sm.few, 1u)] = keep[i];
+            __syncthreads();
+        }
+    }
+    if (n <= kSmpFew) {  // an entry counts what is ahead of it
+        const uint64_t entry = threadIdx.x < n ? sm.list[threadIdx.x] : 0, own = entry ? weight(entry) : 0;
+        if (threadIdx.x < n) sm.weight[threadIdx.x] = own;
+        __syncthreads();
+        if (entry) {
+            uint64_t from = ahead;
+            for (uint32_t j = 0; j < n; ++j) from += sm.list[j] > entry ? sm.weight[j] : 0;
+            if (from < need && need <= from + own) *cut = entry;
+        }
+    } else {  // many equal logits
+        const uint32_t size = power_of_two(n);
+        for (uint32_t i = n + threadIdx.x; i < size; i += kSmpThreads) sm.list[i] = 0;
+        __syncthreads();
+        sort_list(sm.list, size);
+        constexpr int EACH = kSmpList / kSmpThreads;
+        uint64_t own[EACH], sum = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const uint32_t at = threadIdx.x * EACH + i;
+            own[i] = at < n ? weight(sm.list[at]) : 0ull;
+            sum += own[i];
+        }
+        Tally total;
+        uint64_t upto = ahead + block_scan(sm, {sum, 0}, total).mass - sum;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (upto < need && need <= upto + own[i]) *cut = sm.list[threadIdx.x * EACH + i];
+            upto += own[i];
+        }
+    }
+    __syncthreads();
+}
+
+// The entry in bin sm.bin with which sm.need (entries, or mass, counted from the largest logit, of the entries not below `least`)
+// is reached.
+template <bool MASS>
+__device__ __forceinline__ uint64_t find_cut(Row& row, const Bins& bins, const Weigh& weigh, uint64_t least) {
+    SmpShared& sm = row.sm;
+    const uint32_t bin = uint32_t(sm.bin);
+    const uint64_t ahead = sm.ahead, need = sm.need;
+    const uint32_t entries = gather(row, bins, bin, bin, least);
+    if (entries <= kSmpList) {
+        if (row.rank == 0) {
+            cut_list<MASS>(sm, bins, weigh, entries, float(bin), float(kSmpBins), ahead, need, &sm.cut);
+            if (threadIdx.x < kSmpCtas) *row.cluster.map_shared_rank(&sm.cut, threadIdx.x) = sm.cut;
+        }
+        row.cluster.sync();
+        // What is read here is written again behind a barrier of the cluster that follows.
+        return sm.cut;
     }
     // The largest c with enough in the entries >= c: one bit after another.
     uint64_t c = 0;
+#pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
         const uint64_t mid = c | 1ull << bit;
         Tally v{0, 0}, total;
-        for (int i = threadIdx.x; i < row.count; i += kSmpThreads) {
-            const uint64_t entry = row.entry(i);
-            if (entry >= mid && entry >= least && bins(row.keys[i]) == bin) v.mass += MASS ? weigh(row.keys[i]) : 1ull;
-        }
+        row.each([&](int i, float x) {
+            const uint64_t entry = row.entry(i, x);
+            if (entry >= mid && entry >= least && bins(x) == bin) v.mass += MASS ? weigh(x) : 1ull;
+        });
         block_scan(sm, v, total);
         const Tally* all = row.tell(total);
         uint64_t sum = ahead;
@@ -279,209 +434,301 @@ struct Settings {
     float u;
 };
 
-__device__ __forceinline__ uint64_t needed(float p, uint64_t mass) {
-    const uint64_t need = uint64_t(ceil(double(p) * double(mass)));
-    return need < 1 ? 1 : need > mass ? mass : need;
-}
-__device__ __forceinline__ uint64_t aimed(float u, uint64_t mass) {
-    const uint64_t aim = uint64_t(fmin(fmax(double(u), 0.), 1.) * double(mass));  // NaN: 0
-    return aim >= mass ? mass - 1 : aim;
-}
-
-// All of the filters and the draw among sm.list[0 .. n), which holds the first n entries in the order, n >= 1: one CTA.
-__device__ __forceinline__ void finish(SmpShared& sm, const Weigh& weigh, uint32_t n, const Settings& set, int32_t* token, float* prob) {
-    constexpr int PER = kSmpList / kSmpThreads;
-    uint32_t size = power_of_two(n);
-    for (uint32_t i = n + threadIdx.x; i < size; i += kSmpThreads) sm.list[i] = 0;
-    __syncthreads();
-    sort_list(sm.list, size);
-    if (set.k < n) n = uint32_t(set.k);
-    uint64_t entry[PER], own[PER], sum = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const uint32_t at = threadIdx.x * PER + i;
-        entry[i] = at < n ? sm.list[at] : 0;
-        own[i] = at < n ? weigh(uint32_t(entry[i] >> 32)) : 0;
-        sum += own[i];
-    }
+// All of the filters and the draw among sm.list[0 .. n), which holds the first n entries in the order, 1 <= n <= kSmpFew: one CTA.
+// `need`: the mass that top-p wants where that is known, or 0: then the list holds all that top-k leaves.  An entry counts
+// what is ahead of it in the order, then what stays of smaller index.
+__device__ __forceinline__ void finish(SmpShared& sm, const Weigh& weigh, uint32_t n, const Settings& set, uint64_t need, int32_t* token, float* prob) {
     Tally total;
-    uint64_t from = block_scan(sm, {sum, 0}, total).mass - sum;
-    const uint64_t need = set.p < 1.f ? needed(set.p, total.mass) : ~0ull;
-    // What stays, in the order of the indexes: (~index, key) sorted the same way.
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const uint32_t at = threadIdx.x * PER + i;
-        const bool stays = at < n && from < need && own[i] >= set.floor_w;
-        if (at < size) sm.list[at] = stays ? entry[i] << 32 | entry[i] >> 32 : 0;
-        from += own[i];
-    }
-    size = power_of_two(n);
+    const uint64_t entry = threadIdx.x < n ? sm.list[threadIdx.x] : 0;
+    uint64_t own = entry ? weigh(value_of(uint32_t(entry >> 32))) : 0, from = 0;
+    if (threadIdx.x < n) sm.weight[threadIdx.x] = own;
     __syncthreads();
-    sort_list(sm.list, size);
-    sum = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const uint32_t at = threadIdx.x * PER + i;
-        entry[i] = at < n ? sm.list[at] : 0;
-        own[i] = entry[i] ? weigh(uint32_t(entry[i])) : 0;
-        sum += own[i];
+    uint32_t ahead = 0;
+    if (entry) {
+#pragma unroll 4
+        for (uint32_t j = 0; j < n; ++j)
+            if (sm.list[j] > entry) ++ahead, from += sm.weight[j];
     }
-    from = block_scan(sm, {sum, 0}, total).mass - sum;
-    const uint64_t aim = aimed(set.u, total.mass);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (from <= aim && aim < from + own[i]) {
-            *token = int(~uint32_t(entry[i] >> 32));
-            if (prob) *prob = float(double(own[i]) / double(total.mass));
+    const bool in_k = entry && ahead < set.k;
+    block_scan(sm, {in_k ? own : 0, 0}, total);
+    if (need == 0) need = set.p < 1.f ? needed(set.p, total.mass) : ~0ull;
+    if (!(in_k && from < need && own >= set.floor_w)) own = 0;
+    if (threadIdx.x < n) sm.weight[threadIdx.x] = own;
+    __syncthreads();
+    if (own) {
+        uint64_t base = 0, mass = 0;
+#pragma unroll 4
+        for (uint32_t j = 0; j < n; ++j) {
+            const uint64_t w = sm.weight[j];
+            mass += w;
+            base += uint32_t(sm.list[j]) > uint32_t(entry) ? w : 0;
         }
-        from += own[i];
+        const uint64_t aim = aimed(set.u, mass);
+        if (base <= aim && aim < base + own) {
+            *token = int(~uint32_t(entry));
+            if (prob) *prob = float(double(own) / double(mass));
+        }
     }
 }
 
-// Adds a mass to a bin's: 64 bits in two words, the carry by hand.
-__device__ __forceinline__ void add_mass(SmpShared& sm, uint32_t bin, uint64_t w) {
-    const uint32_t lo = uint32_t(w), old = atomicAdd(&sm.lo[bin], lo), hi = uint32_t(w >> 32) + (old + lo < old);
-    if (hi) atomicAdd(&sm.hi[bin], hi);
+// The same from the CTAs' parts: all[c].count entries at sm.list + c * kSmpRegion, all[c].mass the largest of the CTA; top-k is on.
+__device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* all, double by, float T, const Settings& set, int32_t* token, float* prob) {
+    constexpr int PER = kSmpCtas * kSmpRegion / kSmpThreads;
+    uint64_t best = 0, entry[PER];
+    uint32_t n = 0;
+#pragma unroll
+    for (int c = 0; c < kSmpCtas; ++c) best = max(best, all[c].mass), n += uint32_t(all[c].count);
+    const Weigh weigh{value_of(uint32_t(best >> 32)), by, sm.powers};
+    if (weigh.top == -INFINITY) {
+        if (threadIdx.x == 0) {
+            *token = -1;
+            if (prob) *prob = 0.f;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const uint32_t at = threadIdx.x + i * kSmpThreads;
+        entry[i] = at % kSmpRegion < all[at / kSmpRegion].count ? sm.list[at] : 0;
+    }
+    if (threadIdx.x == 0) sm.few = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (entry[i]) sm.list[atomicAdd(&sm.few, 1u)] = entry[i];
+    __syncthreads();
+    if (n > kSmpFew) {
+        cut_list<false>(sm, Bins(weigh.top, -INFINITY, T), weigh, n, 0.f, 1.f, 0, set.k, &sm.cut);
+        const uint64_t cut = sm.cut;
+        if (threadIdx.x == 0) sm.few = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (entry[i] >= cut) sm.list[atomicAdd(&sm.few, 1u)] = entry[i];
+        __syncthreads();
+        n = uint32_t(set.k);
+    }
+    finish(sm, weigh, n, set, 0, token, prob);
 }
 
 template <typename T>
 __cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(kSmpThreads) k_sample(tetra_sample_rows p, int part) {
     extern __shared__ __align__(16) unsigned char smem[];
     SmpShared& sm = *reinterpret_cast<SmpShared*>(smem);
-    uint32_t* keys = reinterpret_cast<uint32_t*>(smem + sizeof(SmpShared));
+    float* held = reinterpret_cast<float*>(smem + sizeof(SmpShared));
+    static_assert(sizeof(SmpShared) % 16 == 0, "the part lies behind it");
     const int r = blockIdx.x / kSmpCtas, rank = blockIdx.x % kSmpCtas, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int begin = min(part * rank, p.vocab), count = min(part, p.vocab - begin);
-    Row row{sm, keys, count, uint32_t(begin), cg::this_cluster(), rank, 0};
-    if (threadIdx.x < 2) sm.listed[threadIdx.x] = 0;
+    Row row{sm, held, count, uint32_t(begin), cg::this_cluster(), rank, 0};
+    if (threadIdx.x == 0) sm.listed = 0;
     if (threadIdx.x < 64) sm.powers[threadIdx.x] = exp2(kSmpBits + threadIdx.x / 64.);
-    for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.lo[i] = sm.hi[i] = 0;
+    for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = sm.lo[i] = sm.hi[i] = 0;
+    if (threadIdx.x < 3 && count + threadIdx.x < ((count + 3) & ~3)) held[count + threadIdx.x] = -INFINITY;
     pdl_wait();
     pdl_release();
-
-    // The part, as keys; its largest entry, its least finite key.
-    const T* x = static_cast<const T*>(p.logits) + r * p.row_stride + begin;
-    uint32_t most = 0, most_at = 0, least = 0xFFFFFFFFu;
-    auto take = [&](int i, float v) {
-        const uint32_t key = key_of(v);
-        keys[i] = key;
-        if (key > most) most = key, most_at = uint32_t(i);  // a thread's tokens come in order: the first of equal ones
-        if (key > kMinusInf) least = min(least, key);
-    };
-    constexpr int VEC = 16 / sizeof(T);
-    if ((reinterpret_cast<uintptr_t>(x) & 15) == 0) {
-#pragma unroll 4
-        for (int i = threadIdx.x; i < count / VEC; i += kSmpThreads) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(x) + i);
-            const T* e = reinterpret_cast<const T*>(&v);
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) take(i * VEC + k, float(e[k]));
-        }
-        for (int i = count / VEC * VEC + threadIdx.x; i < count; i += kSmpThreads) take(i, float(x[i]));
-    } else {
-#pragma unroll 8
-        for (int i = threadIdx.x; i < count; i += kSmpThreads) take(i, float(x[i]));
-    }
-    uint64_t best = most ? uint64_t(most) << 32 | uint32_t(~(uint32_t(begin) + most_at)) : 0;
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) best = max(best, __shfl_xor_sync(0xFFFFFFFFu, best, o));
-    least = __reduce_min_sync(0xFFFFFFFFu, least);
-    if (lane == 0) sm.warp[warp] = {best, least};
-    __syncthreads();
-    for (int w = 0; w < kSmpWarps; ++w) best = max(best, sm.warp[w].mass), least = min(least, uint32_t(sm.warp[w].count));
-    const Tally* all = row.tell({best, least});
-    for (int c = 0; c < kSmpCtas; ++c) best = max(best, all[c].mass), least = min(least, uint32_t(all[c].count));
-    const uint32_t top = uint32_t(best >> 32);
 
     int32_t* token = p.tokens + r;
     float* prob = p.prob ? p.prob + r : nullptr;
     const float T_row = p.temperature ? p.temperature[r] : 1.f, p_row = p.top_p ? p.top_p[r] : 1.f, m_row = p.min_p ? p.min_p[r] : 0.f;
     const int k_row = p.top_k ? p.top_k[r] : 0;
+
+    // The part; its largest entry, its least logit above minus infinity.
+    const T* x = static_cast<const T*>(p.logits) + r * p.row_stride + begin;
+    float most = -INFINITY, least = INFINITY;
+    int most_at = 0;
+    auto take = [&](int i, float v) {
+        if (v > most) most = v, most_at = i;  // a thread's tokens come in order: the first of equal ones
+        if (v > -INFINITY) least = fminf(least, v);
+    };
+    constexpr int VEC = 16 / sizeof(T);
+    if ((reinterpret_cast<uintptr_t>(x) & 15) == 0) {
+        constexpr int AHEAD = 5;
+        const int n = count / VEC;
+        for (int i = threadIdx.x; i < n; i += AHEAD * kSmpThreads) {
+            uint4 v[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (i + k * kSmpThreads < n) v[k] = __ldg(reinterpret_cast<const uint4*>(x) + i + k * kSmpThreads);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int at = (i + k * kSmpThreads) * VEC;
+                if (at < n * VEC) {
+                    const T* e = reinterpret_cast<const T*>(&v[k]);
+                    float f[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        f[j] = clean(float(e[j]));
+                        take(at + j, f[j]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < VEC; j += 4) *reinterpret_cast<float4*>(held + at + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+                }
+            }
+        }
+        for (int i = n * VEC + threadIdx.x; i < count; i += kSmpThreads) {
+            const float v = clean(float(x[i]));
+            held[i] = v;
+            take(i, v);
+        }
+    } else {
+        constexpr int AHEAD = 8;
+        for (int i = threadIdx.x; i < count; i += AHEAD * kSmpThreads) {
+            T v[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (i + k * kSmpThreads < count) v[k] = x[i + k * kSmpThreads];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (i + k * kSmpThreads < count) {
+                    const float f = clean(float(v[k]));
+                    held[i + k * kSmpThreads] = f;
+                    take(i + k * kSmpThreads, f);
+                }
+        }
+    }
+    const uint32_t most_key = __reduce_max_sync(0xFFFFFFFFu, key_of(most));
+    const uint32_t at = __reduce_min_sync(0xFFFFFFFFu, key_of(most) == most_key ? uint32_t(begin + most_at) : 0x7FFFFFFFu);
+    const uint32_t least_key = __reduce_min_sync(0xFFFFFFFFu, key_of(least));
+    if (lane == 0) sm.warp[warp] = {uint64_t(most_key) << 32 | uint32_t(~at), least_key};
+    __syncthreads();
+    Tally first{0, 0xFFFFFFFFu};
+    if (warp == 0) {
+        if (lane < kSmpWarps) first = sm.warp[lane];
+        first = extremes<32>(first);
+    }
+    const Settings set{k_row > 0 ? uint64_t(k_row) : ~0ull, p_row, m_row > 0.f ? uint64_t(ceil(double(m_row) * double(1ull << kSmpBits))) : 0ull, p.u[r]};
+    const double by = 64. * 1.4426950408889634074 / double(T_row);
     const bool one = p_row <= 0.f || m_row > 1.f || k_row == 1;  // the first alone stays
-    if (top <= kMinusInf || !(T_row > 0.f) || one) {
+
+    // Few of many: each CTA sends what may be among its own first k to the first CTA, and that is all they tell each other.  The
+    // bin that holds the k-th of its threads' largest logits is not before that of the k-th of its part, and hardly behind it.
+    if (T_row > 0.f && !one && k_row > 0 && k_row <= kSmpRegion / 2) {
+        if (threadIdx.x == 0) sm.whole = first;
+        __syncthreads();
+        const uint64_t own_best = sm.whole.mass;
+        const float own_top = value_of(uint32_t(own_best >> 32));
+        const Bins bins(own_top, value_of(uint32_t(sm.whole.count)), T_row);
+        if (most > -INFINITY && bins(most) < kSmpBins) atomicAdd(sm.count + bins(most), 1u);
+        const uint32_t last = local_bin(sm, set.k);
+        uint64_t* list = row.cluster.map_shared_rank(sm.list, 0) + rank * kSmpRegion;
+        row.each([&](int i, float v) {
+            if (bins(v) <= last && v > -INFINITY) {
+                const uint32_t at = atomicAdd(&sm.listed, 1u);
+                if (at < kSmpRegion) list[at] = row.entry(i, v);
+            }
+        });
+        __syncthreads();
+        const Tally* all = row.tell({own_best, sm.listed});
+        const bool fits = __all_sync(0xFFFFFFFFu, all[lane % kSmpCtas].count <= kSmpRegion);
+        if (fits) {
+            if (rank == 0) finish_parts(sm, all, by, T_row, set, token, prob);
+            return;
+        }
+        for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = 0;
+        if (threadIdx.x == 0) sm.listed = 0;
+    }
+    const Tally* all = row.tell(first);
+    first = extremes<kSmpCtas>(all[lane % kSmpCtas]);
+    const uint64_t best = first.mass;
+    const uint32_t low = uint32_t(first.count);
+    const float top = value_of(uint32_t(best >> 32));
+
+    const bool none = top == -INFINITY;
+    if (none || !(T_row > 0.f) || one) {
         if (rank == 0 && threadIdx.x == 0) {
-            *token = top <= kMinusInf ? -1 : int(~uint32_t(best));
-            if (prob) *prob = top <= kMinusInf ? 0.f : 1.f;
+            *token = none ? -1 : int(~uint32_t(best));
+            if (prob) *prob = none ? 0.f : 1.f;
         }
         return;
     }
-    const Weigh weigh{top, double(value_of(top)), 64. * 1.4426950408889634074 / double(T_row), sm.powers};
-    const Settings set{k_row > 0 ? uint64_t(k_row) : ~0ull, p_row, m_row > 0.f ? uint64_t(ceil(double(m_row) * double(1ull << kSmpBits))) : 0ull, p.u[r]};
+    const Weigh weigh{top, by, sm.powers};
     const bool nucleus = p_row < 1.f, top_k = k_row > 0 && k_row < p.vocab;
 
     uint64_t cut = 0;
     if (top_k || nucleus) {
-        // e^-31.25 is less than half a unit
-        const float max = value_of(top), range = fminf(fminf(max - value_of(least), 31.25f * T_row), 3.0e38f);
-        const Bins bins{top, max, range, range > 1e-30f ? float(kSmpBins) / range : 0.f};
-        uint64_t before, whole;
+        const Bins bins(top, value_of(low), T_row);
+        auto add = [&](float v) {
+            const uint32_t bin = bins(v);
+            if (bin < kSmpBins) {
+                atomicAdd(sm.count + bin, 1u);
+                add_mass(sm.lo + bin, sm.hi + bin, weigh(v));
+            }
+        };
         if (top_k) {
-            for (int i = threadIdx.x; i < count; i += kSmpThreads) {
-                const uint32_t bin = bins(keys[i]);
-                if (bin < kSmpBins) atomicAdd(&sm.lo[bin], 1u);
-            }
-            add_bins(row, before, whole);
-            uint32_t last = kSmpBins - 1;
-            uint64_t entries = whole;
-            if (set.k < whole) {
-                find_bin(row, before, set.k);
-                last = uint32_t(sm.bin[0]);
-                entries = sm.bin[1] + sm.bin[2];
-            }
-            if (entries <= kSmpList) {
-                gather(row, bins, 0, last, 0, 0);
-                if (rank == 0) finish(sm, weigh, uint32_t(entries), set, token, prob);
-                return;
-            }
-            if (set.k < whole) cut = find_cut<false>(row, bins, weigh, set.k, 0);
-            if (nucleus) {  // the other CTAs have read these counts: add_bins told the sums behind them
-                for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.lo[i] = 0;
-                __syncthreads();
+            row.each([&](int, float v) {
+                const uint32_t bin = bins(v);
+                if (bin < kSmpBins) atomicAdd(sm.count + bin, 1u);
+            });
+            find_bin<false>(row, set.k, 1.f);
+        } else {
+            row.each([&](int, float v) { add(v); });
+            find_bin<true>(row, 0, p_row);
+        }
+        if (sm.entries <= kSmpFew) {
+            const uint32_t n = gather(row, bins, 0, min(uint32_t(sm.bin), uint32_t(kSmpBins - 1)), 0);
+            if (rank == 0) finish(sm, weigh, n, set, top_k ? 0 : sm.need, token, prob);
+            return;
+        }
+        if (top_k) {
+            if (sm.bin < kSmpBins) cut = find_cut<false>(row, bins, weigh, 0);
+            if (nucleus) {  // again, of masses and of what is left
+                for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = sm.lo[i] = sm.hi[i] = 0;
+                row.cluster.sync();
+                row.each([&](int i, float v) {
+                    if (row.entry(i, v) >= cut) add(v);
+                });
+                find_bin<true>(row, 0, p_row);
             }
         }
-        if (nucleus) {
-            for (int i = threadIdx.x; i < count; i += kSmpThreads) {
-                const uint32_t bin = bins(keys[i]);
-                if (bin < kSmpBins && row.entry(i) >= cut) add_mass(sm, bin, weigh(keys[i]));
-            }
-            add_bins(row, before, whole);
-            const uint64_t need = needed(p_row, whole);
-            find_bin(row, before, need);
-            cut = find_cut<true>(row, bins, weigh, need, cut);
-        }
+        if (nucleus) cut = find_cut<true>(row, bins, weigh, cut);
     }
 
-    // The draw: kept weights in the order of the indexes, so many consecutive ones a thread.
-    const int per = (part + kSmpThreads - 1) / kSmpThreads | 1;  // odd: no bank conflicts
-    const int from = min(int(threadIdx.x) * per, count), to = min(from + per, count);
-    auto kept = [&](int i) -> uint64_t {
-        if (row.entry(i) < cut) return 0;
-        const uint64_t w = weigh(keys[i]);
+    // The draw, in the order of the indexes: a warp takes so many consecutive fours.
+    const int fours = (count + 3) / 4, each = (fours + kSmpWarps - 1) / kSmpWarps, from = min(each * warp, fours), to = min(from + each, fours);
+    auto kept = [&](int i, float v) -> uint64_t {
+        if (row.entry(i, v) < cut) return 0;
+        const uint64_t w = weigh(v);
         return w >= set.floor_w ? w : 0;
     };
     uint64_t sum = 0;
-    for (int i = from; i < to; ++i) sum += kept(i);
+#pragma unroll 2
+    for (int i = from + lane; i < to; i += 32) {
+        const float4 v = *reinterpret_cast<const float4*>(held + 4 * i);
+        sum += (kept(4 * i, v.x) + kept(4 * i + 1, v.y)) + (kept(4 * i + 2, v.z) + kept(4 * i + 3, v.w));
+    }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
     Tally total;
-    const uint64_t upto = block_scan(sm, {sum, 0}, total).mass;
+    uint64_t base = block_scan(sm, {lane == 31 ? sum : 0, 0}, total).mass, mass = 0;
+    base = __shfl_sync(0xFFFFFFFFu, base, 31) - sum;  // of the warps before
     all = row.tell(total);
-    uint64_t base = 0, mass = 0;
+#pragma unroll
     for (int c = 0; c < kSmpCtas; ++c) {
-        if (c == rank) base = mass;
+        if (c == rank) base += mass;
         mass += all[c].mass;
     }
     const uint64_t aim = aimed(set.u, mass);
-    const bool mine = base + upto - sum <= aim && aim < base + upto;
-    const uint32_t who = __ballot_sync(0xFFFFFFFFu, mine);
-    if (who) {  // the warp walks through the thread's tokens together
-        const int l = __ffs(who) - 1, a = __shfl_sync(0xFFFFFFFFu, from, l), b = __shfl_sync(0xFFFFFFFFu, to, l);
-        uint64_t at = __shfl_sync(0xFFFFFFFFu, base + upto - sum, l);
-        for (int i = a; i < b; i += 32) {
-            const uint64_t w = i + lane < b ? kept(i + lane) : 0;
-            const uint64_t end = at + warp_scan({w, 0}, lane).mass;
-            if (end - w <= aim && aim < end) {
-                *token = int(row.index) + i + lane;
-                if (prob) *prob = float(double(w) / double(mass));
+    if (base <= aim && aim < base + sum) {  // this warp's
+        for (int i = from; i < to; i += 32) {
+            uint64_t w[4] = {0, 0, 0, 0};
+            const int four = 4 * (i + lane);
+            if (i + lane < to) {
+                const float4 v = *reinterpret_cast<const float4*>(held + four);
+                w[0] = kept(four, v.x), w[1] = kept(four + 1, v.y), w[2] = kept(four + 2, v.z), w[3] = kept(four + 3, v.w);
             }
-            at = __shfl_sync(0xFFFFFFFFu, end, 31);
+            const uint64_t own = w[0] + w[1] + w[2] + w[3];
+            if (!__any_sync(0xFFFFFFFFu, own != 0)) continue;
+            uint64_t end = base + warp_scan({own, 0}, lane).mass, at = end - own;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (at <= aim && aim < at + w[k]) {
+                    *token = int(row.index) + four + k;
+                    if (prob) *prob = float(double(w[k]) / double(mass));
+                }
+                at += w[k];
+            }
+            base = __shfl_sync(0xFFFFFFFFu, end, 31);
+            if (base > aim) break;
         }
     }
 }
