@@ -14,6 +14,8 @@
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
+#include <cfloat>
+
 #include "../../include/tetra.h"
 #include "../../include/tetra_sample.h"
 #include "tetra_gemv_common.cuh"
@@ -23,14 +25,15 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kSmpThreads = 512, kSmpWarps = kSmpThreads / 32, kSmpCtas = 8;
+constexpr int kSmpCtas = 8, kSmpMaxWarps = 32;
 constexpr int kSmpBins = 1024;
+constexpr int kSmpCounted = kSmpBins / 4;                       // bins of masses whose entries are counted too: few are so near
 constexpr int kSmpList = 2048;                                  // entries that one CTA takes
 constexpr int kSmpRegion = kSmpList / kSmpCtas;                // ... an equal share of each
 constexpr int kSmpFew = 256;                                    // ... and compares each with each
 constexpr int kSmpBits = 44;                                    // a weight of 1 is 2^44
 
-static_assert(kSmpCtas * kSmpThreads > 0 && TETRA_SAMPLE_MAX_VOCAB <= 1 << 19, "sums of weights stay below 2^63");
+static_assert(TETRA_SAMPLE_MAX_VOCAB <= 1 << 19, "sums of weights stay below 2^63");
 
 struct Tally {  // so many entries with so much mass
     uint64_t mass;
@@ -40,17 +43,19 @@ struct Tally {  // so many entries with so much mass
 struct alignas(16) SmpShared {
     uint64_t list[kSmpList];
     uint64_t weight[kSmpFew];
+    uint32_t ahead_of[kSmpFew];
     double powers[64];                    // 2^(44 + j / 64)
     uint32_t count[kSmpBins], lo[kSmpBins], hi[kSmpBins];  // of the bins: entries, mass in two words
     Tally slots[2][kSmpCtas];             // what the CTAs tell each other
-    Tally warp[kSmpWarps], whole;
+    Tally warp[kSmpMaxWarps], whole;
     uint64_t bin, ahead, need, entries;   // a crossing: its bin, the sum before it, what is needed, entries up to its end
     uint64_t cut;
-    uint32_t listed, sub, few;
+    uint32_t listed, sub, few, least_key;
 };
 
-// Logits are compared as integers in the order of the floats; NaN is minus infinity, zeros (and what is below 2^-126) are equal.
-__device__ __forceinline__ float clean(float x) { return __fadd_rn(fmaxf(x, -INFINITY), 0.f); }
+// Logits are compared as integers in the order of the floats; NaN is minus infinity, plus infinity the largest float32, zeros
+// (and what is below 2^-126) are equal.
+__device__ __forceinline__ float clean(float x) { return __fadd_rn(fminf(fmaxf(x, -INFINITY), FLT_MAX), 0.f); }
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t b = __float_as_uint(x);
     return b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
@@ -61,15 +66,15 @@ __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float
 // times the exponential series of f ln 2 / 64 up to the fourth power (the next is 4e-14, 2^-44), rounded once; in float64, whose
 // multiply-adds run at half the rate of float32's here.  Adding 1.5 * 2^52 leaves a whole number in the low bits.
 struct Weigh {
-    float top;              // largest logit
-    double by;              // 64 log2(e) / T
+    double top, by;         // largest logit; 64 log2(e) / T
+    float reach;            // distance from the largest to which there is mass: e^-31.25 is less than half a unit
     const double* powers;
+    __device__ __forceinline__ bool has(float x) const { return float(top) - x <= reach; }
+    __device__ __forceinline__ uint64_t any(float x) const { return has(x) ? (*this)(x) : 0; }
+    // ... of one that has mass.
     __device__ __forceinline__ uint64_t operator()(float x) const {
         constexpr double magic = 6755399441055744.;
-        if (x == top) return 1ull << kSmpBits;
-        const double t = (double(x) - double(top)) * by;
-        if (!(t > -46. * 64.) || x == -INFINITY) return 0;  // not where the largest is infinite
-        const double m = t + magic, f = t - (m - magic);
+        const double d = double(x) - top, m = fma(d, by, magic), f = fma(d, by, magic - m);
         const int k = __double2loint(m);
         constexpr double c = 0.693147180559945309417 / 64.;
         double e = fma(c * c * c * c / 24., f, c * c * c / 6.);
@@ -93,9 +98,15 @@ __device__ __forceinline__ Tally warp_scan(Tally v, int lane) {
     }
     return v;
 }
+// What a CTA of so many threads does.
+template <int kSmpThreads>
+struct Sampler {
+
+static constexpr int kSmpWarps = kSmpThreads / 32;
+
 // ... over the CTA's threads up to this one; `total` is the CTA's.  The warps' sums are added by one warp: each thread adding them
 // for itself takes more cycles than all the rest.
-__device__ __forceinline__ Tally block_scan(SmpShared& sm, Tally v, Tally& total) {
+static __device__ __forceinline__ Tally block_scan(SmpShared& sm, Tally v, Tally& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     v = warp_scan(v, lane);
     if (lane == 31) sm.warp[warp] = v;
@@ -114,7 +125,7 @@ __device__ __forceinline__ Tally block_scan(SmpShared& sm, Tally v, Tally& total
 
 // Largest mass and least count of N lanes next to each other.
 template <int N>
-__device__ __forceinline__ Tally extremes(Tally v) {
+static __device__ __forceinline__ Tally extremes(Tally v) {
 #pragma unroll
     for (int o = N / 2; o >= 1; o >>= 1) {
         v.mass = max(v.mass, __shfl_xor_sync(0xFFFFFFFFu, v.mass, o));
@@ -124,7 +135,7 @@ __device__ __forceinline__ Tally extremes(Tally v) {
 }
 
 // Sorts list[0 .. size), a power of two, the largest first.
-__device__ __forceinline__ void sort_list(uint64_t* list, uint32_t size) {
+static __device__ __forceinline__ void sort_list(uint64_t* list, uint32_t size) {
 #pragma unroll 1
     for (uint32_t k = 2; k <= size; k <<= 1)
 #pragma unroll 1
@@ -137,26 +148,24 @@ __device__ __forceinline__ void sort_list(uint64_t* list, uint32_t size) {
             __syncthreads();
         }
 }
-__device__ __forceinline__ uint32_t power_of_two(uint32_t n) {
+static __device__ __forceinline__ uint32_t power_of_two(uint32_t n) {
     uint32_t size = 2;
     while (size < n) size <<= 1;
     return size;
 }
 
-// Distance bins: logit -> bin, the largest in bin 0; kSmpBins for one without mass (e^-31.25 is less than half a unit).
+// How far from the largest logit there is mass.
+static __device__ __forceinline__ float reach_of(float T) { return fminf(31.25f * T, FLT_MAX); }
+
+// Distance bins: logit -> bin, the largest in bin 0; kSmpBins for one without mass.
 struct Bins {
     float top, range, by;
-    __device__ __forceinline__ Bins(float top_, float least, float T) : top(top_), range(fminf(fminf(top_ - least, 31.25f * T), 3.0e38f)) {
+    __device__ __forceinline__ Bins(float top_, float least, float T) : top(top_), range(fminf(top_ - least, reach_of(T))) {
         by = range > 1e-30f ? float(kSmpBins) / range : 0.f;
     }
-    __device__ __forceinline__ float at(float x) const {
-        const float d = top - x;
-        return x == top ? 0.f : d <= range ? d * by : float(2 * kSmpBins);  // not where the largest is infinite
-    }
-    __device__ __forceinline__ uint32_t operator()(float x) const {
-        const float b = at(x);
-        return b < float(2 * kSmpBins) ? min(uint32_t(b), uint32_t(kSmpBins - 1)) : uint32_t(kSmpBins);
-    }
+    __device__ __forceinline__ bool has(float x) const { return top - x <= range; }
+    __device__ __forceinline__ uint32_t operator()(float x) const { return min(uint32_t((top - x) * by), uint32_t(kSmpBins - 1)); }  // of one that has mass
+    __device__ __forceinline__ uint32_t any(float x) const { return has(x) ? (*this)(x) : uint32_t(kSmpBins); }
 };
 
 struct Row {
@@ -191,24 +200,24 @@ struct Row {
 };
 
 // A mass to a bin's: 64 bits in two words, the carry by hand.
-__device__ __forceinline__ void add_mass(uint32_t* lo, uint32_t* hi, uint64_t w) {
+static __device__ __forceinline__ void add_mass(uint32_t* lo, uint32_t* hi, uint64_t w) {
     const uint32_t low = uint32_t(w), old = atomicAdd(lo, low), high = uint32_t(w >> 32) + (old + low < old);
     if (high) atomicAdd(hi, high);
 }
 
-__device__ __forceinline__ uint64_t needed(float p, uint64_t mass) {
+static __device__ __forceinline__ uint64_t needed(float p, uint64_t mass) {
     const uint64_t need = uint64_t(ceil(double(p) * double(mass)));
     return need < 1 ? 1 : need > mass ? mass : need;
 }
-__device__ __forceinline__ uint64_t aimed(float u, uint64_t mass) {
+static __device__ __forceinline__ uint64_t aimed(float u, uint64_t mass) {
     const uint64_t aim = uint64_t(fmin(fmax(double(u), 0.), 1.) * double(mass));  // NaN: 0
     return aim >= mass ? mass - 1 : aim;
 }
 
-// The bin in which this CTA's counts reach k; the last one where they do not.
-__device__ __forceinline__ uint32_t local_bin(SmpShared& sm, uint64_t k) {
+// The bin in which this CTA's counts reach k; kSmpBins where they do not.
+static __device__ __forceinline__ uint32_t local_bin(SmpShared& sm, uint64_t k) {
     constexpr int PER = kSmpBins / kSmpThreads;
-    if (threadIdx.x == 0) sm.sub = kSmpBins - 1;
+    if (threadIdx.x == 0) sm.sub = kSmpBins, sm.least_key = 0xFFFFFFFFu;
     __syncthreads();
     uint64_t sum = 0;
     uint32_t own[PER];
@@ -228,20 +237,8 @@ __device__ __forceinline__ uint32_t local_bin(SmpShared& sm, uint64_t k) {
 // The cluster's histogram in the first CTA, which finds the bin in which the sums (entries, or mass) reach k entries, or p of the
 // whole mass, and tells all.  Every CTA's histogram is complete but for a barrier.
 template <bool MASS>
-__device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
+static __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
     SmpShared& sm = row.sm;
-    __syncthreads();
-    if (row.rank != 0) {
-        SmpShared* first = row.cluster.map_shared_rank(&sm, 0);
-#pragma unroll
-        for (int i = 0; i < kSmpBins / kSmpThreads; ++i) {
-            const int b = threadIdx.x + i * kSmpThreads;
-            if (sm.count[b]) {
-                atomicAdd(first->count + b, sm.count[b]);
-                if (MASS) add_mass(first->lo + b, first->hi + b, (uint64_t(sm.hi[b]) << 32) + sm.lo[b]);
-            }
-        }
-    }
     row.cluster.sync();
     if (row.rank == 0) {
         constexpr int PER = kSmpBins / kSmpThreads;
@@ -249,7 +246,12 @@ __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int b = threadIdx.x * PER + i;
-            own[i] = {MASS ? (uint64_t(sm.hi[b]) << 32) + sm.lo[b] : 0ull, sm.count[b]};
+            own[i] = {0, 0};
+#pragma unroll
+            for (int c = 0; c < kSmpCtas; ++c) {
+                const SmpShared* other = row.cluster.map_shared_rank(&sm, c);
+                own[i] = own[i] + Tally{MASS ? (uint64_t(other->hi[b]) << 32) + other->lo[b] : 0ull, other->count[b]};
+            }
             sum = sum + own[i];
         }
         Tally upto = block_scan(sm, sum, total);
@@ -277,10 +279,10 @@ __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
 
 // Entries of the bins [low, high] that are not below `cut`: how many there are in the cluster, and all of them in the list of
 // the first CTA where they are kSmpList at most.  Collected at home first: a counter in another CTA takes a thousand cycles.
-__device__ __forceinline__ uint32_t gather(Row& row, const Bins& bins, uint32_t low, uint32_t high, uint64_t cut) {
+static __device__ __forceinline__ uint32_t gather(Row& row, const Bins& bins, uint32_t low, uint32_t high, uint64_t cut) {
     SmpShared& sm = row.sm;
     row.each([&](int i, float v) {
-        const uint32_t bin = bins(v);
+        const uint32_t bin = bins.any(v);
         if (bin >= low && bin <= high && row.entry(i, v) >= cut) {
             const uint32_t at = atomicAdd(&sm.listed, 1u);
             if (at < kSmpList) sm.list[at] = row.entry(i, v);
@@ -306,18 +308,18 @@ __device__ __forceinline__ uint32_t gather(Row& row, const Bins& bins, uint32_t 
     return total;
 }
 
-// Among sm.list[0 .. n), n >= 1, the entry with which `need` is reached from `ahead` on: into *cut.  `scale` (bins.at() - bin) is
-// from 0 to kSmpBins for all of them.  One CTA.
+// Among sm.list[0 .. n), n >= 1, the entry with which `need` is reached from `ahead` on: into *cut.  scale (distance * bins.by - bin)
+// is where an entry lies in a histogram of their own.  One CTA.
 template <bool MASS>
-__device__ __noinline__ void cut_list(SmpShared& sm, const Bins bins, const Weigh weigh, uint32_t n, float bin, float scale, uint64_t ahead, uint64_t need, uint64_t* cut) {
+static __device__ __noinline__ void cut_list(SmpShared& sm, const Bins bins, const Weigh weigh, uint32_t n, float bin, float scale, uint64_t ahead, uint64_t need, uint64_t* cut) {
     constexpr int PER = kSmpBins / kSmpThreads;
-    auto weight = [&](uint64_t entry) { return MASS ? weigh(value_of(uint32_t(entry >> 32))) : 1ull; };
+    auto weight = [&](uint64_t entry) { return MASS ? weigh.any(value_of(uint32_t(entry >> 32))) : 1ull; };
     if (n > kSmpFew) {  // a histogram of their own
         for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = sm.lo[i] = sm.hi[i] = 0;
         if (threadIdx.x == 0) sm.few = 0;
         __syncthreads();
         auto inside = [&](uint64_t entry) {
-            const float f = (bins.at(value_of(uint32_t(entry >> 32))) - bin) * scale;
+            const float f = ((bins.top - value_of(uint32_t(entry >> 32))) * bins.by - bin) * scale;
             return uint32_t(fminf(fmaxf(f, 0.f), float(kSmpBins - 1)));
         };
         for (uint32_t i = threadIdx.x; i < n; i += kSmpThreads) {
@@ -394,7 +396,7 @@ __device__ __noinline__ void cut_list(SmpShared& sm, const Bins bins, const Weig
 // The entry in bin sm.bin with which sm.need (entries, or mass, counted from the largest logit, of the entries not below `least`)
 // is reached.
 template <bool MASS>
-__device__ __forceinline__ uint64_t find_cut(Row& row, const Bins& bins, const Weigh& weigh, uint64_t least) {
+static __device__ __forceinline__ uint64_t find_cut(Row& row, const Bins& bins, const Weigh& weigh, uint64_t least) {
     SmpShared& sm = row.sm;
     const uint32_t bin = uint32_t(sm.bin);
     const uint64_t ahead = sm.ahead, need = sm.need;
@@ -416,7 +418,7 @@ __device__ __forceinline__ uint64_t find_cut(Row& row, const Bins& bins, const W
         Tally v{0, 0}, total;
         row.each([&](int i, float x) {
             const uint64_t entry = row.entry(i, x);
-            if (entry >= mid && entry >= least && bins(x) == bin) v.mass += MASS ? weigh(x) : 1ull;
+            if (entry >= mid && entry >= least && bins.any(x) == bin) v.mass += MASS ? weigh(x) : 1ull;
         });
         block_scan(sm, v, total);
         const Tally* all = row.tell(total);
@@ -437,31 +439,38 @@ struct Settings {
 // All of the filters and the draw among sm.list[0 .. n), which holds the first n entries in the order, 1 <= n <= kSmpFew: one CTA.
 // `need`: the mass that top-p wants where that is known, or 0: then the list holds all that top-k leaves.  An entry counts
 // what is ahead of it in the order, then what stays of smaller index.
-__device__ __forceinline__ void finish(SmpShared& sm, const Weigh& weigh, uint32_t n, const Settings& set, uint64_t need, int32_t* token, float* prob) {
-    Tally total;
-    const uint64_t entry = threadIdx.x < n ? sm.list[threadIdx.x] : 0;
-    uint64_t own = entry ? weigh(value_of(uint32_t(entry >> 32))) : 0, from = 0;
-    if (threadIdx.x < n) sm.weight[threadIdx.x] = own;
+static __device__ __forceinline__ void finish(SmpShared& sm, const Weigh& weigh, uint32_t n, const Settings& set, uint64_t need, int32_t* token, float* prob) {
+    constexpr int SIDE = kSmpThreads / kSmpFew;  // threads of an entry
+    const uint32_t i = threadIdx.x % kSmpFew, side = threadIdx.x / kSmpFew;
+    uint64_t entry = i < n ? sm.list[i] : 0;
+    if (threadIdx.x < kSmpFew) sm.ahead_of[threadIdx.x] = 0;
     __syncthreads();
-    uint32_t ahead = 0;
     if (entry) {
+        uint32_t ahead = 0;
 #pragma unroll 4
-        for (uint32_t j = 0; j < n; ++j)
-            if (sm.list[j] > entry) ++ahead, from += sm.weight[j];
+        for (uint32_t j = side; j < n; j += SIDE) ahead += sm.list[j] > entry;
+        if (ahead) atomicAdd(&sm.ahead_of[i], ahead);
     }
-    const bool in_k = entry && ahead < set.k;
-    block_scan(sm, {in_k ? own : 0, 0}, total);
-    if (need == 0) need = set.p < 1.f ? needed(set.p, total.mass) : ~0ull;
-    if (!(in_k && from < need && own >= set.floor_w)) own = 0;
-    if (threadIdx.x < n) sm.weight[threadIdx.x] = own;
     __syncthreads();
-    if (own) {
+    if (side == 0 && entry) sm.list[kSmpFew + sm.ahead_of[i]] = entry;  // in the order
+    if (set.k < n) n = uint32_t(set.k);
+    __syncthreads();
+    const uint64_t* order = sm.list + kSmpFew;
+    entry = threadIdx.x < n ? order[threadIdx.x] : 0;
+    const uint64_t own = entry ? weigh.any(value_of(uint32_t(entry >> 32))) : 0;
+    if (threadIdx.x < n) sm.weight[threadIdx.x] = own;
+    Tally total;
+    const uint64_t from = block_scan(sm, {own, 0}, total).mass - own;
+    if (need == 0) need = set.p < 1.f ? needed(set.p, total.mass) : ~0ull;
+    const bool stays = own && from < need && own >= set.floor_w;
+    n = __syncthreads_count(stays);  // the first so many
+    if (stays) {
         uint64_t base = 0, mass = 0;
 #pragma unroll 4
         for (uint32_t j = 0; j < n; ++j) {
             const uint64_t w = sm.weight[j];
             mass += w;
-            base += uint32_t(sm.list[j]) > uint32_t(entry) ? w : 0;
+            base += uint32_t(order[j]) > uint32_t(entry) ? w : 0;
         }
         const uint64_t aim = aimed(set.u, mass);
         if (base <= aim && aim < base + own) {
@@ -472,14 +481,15 @@ __device__ __forceinline__ void finish(SmpShared& sm, const Weigh& weigh, uint32
 }
 
 // The same from the CTAs' parts: all[c].count entries at sm.list + c * kSmpRegion, all[c].mass the largest of the CTA; top-k is on.
-__device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* all, double by, float T, const Settings& set, int32_t* token, float* prob) {
+static __device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* all, double by, float T, const Settings& set, int32_t* token, float* prob) {
     constexpr int PER = kSmpCtas * kSmpRegion / kSmpThreads;
     uint64_t best = 0, entry[PER];
     uint32_t n = 0;
 #pragma unroll
     for (int c = 0; c < kSmpCtas; ++c) best = max(best, all[c].mass), n += uint32_t(all[c].count);
-    const Weigh weigh{value_of(uint32_t(best >> 32)), by, sm.powers};
-    if (weigh.top == -INFINITY) {
+    const float top = value_of(uint32_t(best >> 32));
+    const Weigh weigh{double(top), by, reach_of(T), sm.powers};
+    if (top == -INFINITY) {
         if (threadIdx.x == 0) {
             *token = -1;
             if (prob) *prob = 0.f;
@@ -491,14 +501,19 @@ __device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* all, do
         const uint32_t at = threadIdx.x + i * kSmpThreads;
         entry[i] = at % kSmpRegion < all[at / kSmpRegion].count ? sm.list[at] : 0;
     }
-    if (threadIdx.x == 0) sm.few = 0;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (entry[i]) sm.list[atomicAdd(&sm.few, 1u)] = entry[i];
+    for (int i = 0; i < PER; ++i) {
+        const uint32_t at = threadIdx.x + i * kSmpThreads;
+        uint32_t place = at % kSmpRegion;
+#pragma unroll
+        for (int c = 0; c < kSmpCtas - 1; ++c)
+            if (c < int(at / kSmpRegion)) place += uint32_t(all[c].count);
+        if (entry[i]) sm.list[place] = entry[i];
+    }
     __syncthreads();
     if (n > kSmpFew) {
-        cut_list<false>(sm, Bins(weigh.top, -INFINITY, T), weigh, n, 0.f, 1.f, 0, set.k, &sm.cut);
+        cut_list<false>(sm, Bins(top, -INFINITY, T), weigh, n, 0.f, 1.f, 0, set.k, &sm.cut);
         const uint64_t cut = sm.cut;
         if (threadIdx.x == 0) sm.few = 0;
         __syncthreads();
@@ -512,7 +527,7 @@ __device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* all, do
 }
 
 template <typename T>
-__cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(kSmpThreads) k_sample(tetra_sample_rows p, int part) {
+static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part) {
     extern __shared__ __align__(16) unsigned char smem[];
     SmpShared& sm = *reinterpret_cast<SmpShared*>(smem);
     float* held = reinterpret_cast<float*>(smem + sizeof(SmpShared));
@@ -608,11 +623,16 @@ __cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(kSmpThreads) 
         const uint64_t own_best = sm.whole.mass;
         const float own_top = value_of(uint32_t(own_best >> 32));
         const Bins bins(own_top, value_of(uint32_t(sm.whole.count)), T_row);
-        if (most > -INFINITY && bins(most) < kSmpBins) atomicAdd(sm.count + bins(most), 1u);
+        const uint32_t bin = most > -INFINITY ? bins.any(most) : uint32_t(kSmpBins);
+        if (bin < kSmpBins) atomicAdd(sm.count + bin, 1u);
         const uint32_t last = local_bin(sm, set.k);
+        if (bin <= last && bin < kSmpBins) atomicMin(&sm.least_key, key_of(most));
+        __syncthreads();
+        // Below k threads' largest there is nothing to find; where there are not so many, all that have mass are sent.
+        const float least_sent = sm.sub < kSmpBins ? value_of(sm.least_key) : fmaxf(own_top - bins.range, -FLT_MAX);
         uint64_t* list = row.cluster.map_shared_rank(sm.list, 0) + rank * kSmpRegion;
         row.each([&](int i, float v) {
-            if (bins(v) <= last && v > -INFINITY) {
+            if (v >= least_sent) {
                 const uint32_t at = atomicAdd(&sm.listed, 1u);
                 if (at < kSmpRegion) list[at] = row.entry(i, v);
             }
@@ -641,30 +661,29 @@ __cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(kSmpThreads) 
         }
         return;
     }
-    const Weigh weigh{top, by, sm.powers};
+    const Weigh weigh{double(top), by, reach_of(T_row), sm.powers};
     const bool nucleus = p_row < 1.f, top_k = k_row > 0 && k_row < p.vocab;
 
     uint64_t cut = 0;
     if (top_k || nucleus) {
         const Bins bins(top, value_of(low), T_row);
         auto add = [&](float v) {
-            const uint32_t bin = bins(v);
-            if (bin < kSmpBins) {
-                atomicAdd(sm.count + bin, 1u);
+            if (bins.has(v)) {
+                const uint32_t bin = bins(v);
+                if (bin < kSmpCounted) atomicAdd(sm.count + bin, 1u);
                 add_mass(sm.lo + bin, sm.hi + bin, weigh(v));
             }
         };
         if (top_k) {
             row.each([&](int, float v) {
-                const uint32_t bin = bins(v);
-                if (bin < kSmpBins) atomicAdd(sm.count + bin, 1u);
+                if (bins.has(v)) atomicAdd(sm.count + bins(v), 1u);
             });
             find_bin<false>(row, set.k, 1.f);
         } else {
             row.each([&](int, float v) { add(v); });
             find_bin<true>(row, 0, p_row);
         }
-        if (sm.entries <= kSmpFew) {
+        if (sm.entries <= kSmpFew && (top_k || sm.bin < kSmpCounted)) {
             const uint32_t n = gather(row, bins, 0, min(uint32_t(sm.bin), uint32_t(kSmpBins - 1)), 0);
             if (rank == 0) finish(sm, weigh, n, set, top_k ? 0 : sm.need, token, prob);
             return;
@@ -685,16 +704,48 @@ __cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(kSmpThreads) 
 
     // The draw, in the order of the indexes: a warp takes so many consecutive fours.
     const int fours = (count + 3) / 4, each = (fours + kSmpWarps - 1) / kSmpWarps, from = min(each * warp, fours), to = min(from + each, fours);
-    auto kept = [&](int i, float v) -> uint64_t {
-        if (row.entry(i, v) < cut) return 0;
-        const uint64_t w = weigh(v);
+    const float cut_at = cut ? value_of(uint32_t(cut >> 32)) : -INFINITY;
+    const uint32_t cut_index = ~uint32_t(cut);  // of the logits that equal the cut's, those up to here stay
+    auto stays = [&](int i, float v) { return v > cut_at || (v == cut_at && row.index + uint32_t(i) <= cut_index); };
+    auto kept = [&](float v) -> uint64_t {
+        const uint64_t w = weigh.any(v);
         return w >= set.floor_w ? w : 0;
     };
     uint64_t sum = 0;
+    if (cut) {  // few stay: they are put next to each other before they are weighed
+        float* queue = reinterpret_cast<float*>(sm.list) + warp * 64;
+        static_assert(kSmpWarps * 64 * sizeof(float) <= sizeof(sm.list), "a queue for each warp");
+        int queued = 0;
+        for (int i = from; i < to; i += 32) {
+            const int four = 4 * (i + lane);
+            const float4 v = i + lane < to ? *reinterpret_cast<const float4*>(held + four) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool in = stays(four + k, f[k]);
+                const uint32_t who = __ballot_sync(0xFFFFFFFFu, in);
+                if (in) queue[queued + __popc(who & ((1u << lane) - 1))] = f[k];
+                queued += __popc(who);
+                if (queued >= 32) {
+                    __syncwarp();
+                    const uint64_t w = weigh(queue[lane]);
+                    sum += w >= set.floor_w ? w : 0;
+                    const float rest = queue[32 + lane];
+                    __syncwarp();
+                    queue[lane] = rest;
+                    queued -= 32;
+                }
+            }
+        }
+        __syncwarp();
+        const uint64_t w = lane < queued ? weigh(queue[lane]) : 0;
+        sum += w >= set.floor_w ? w : 0;
+    } else {
 #pragma unroll 2
-    for (int i = from + lane; i < to; i += 32) {
-        const float4 v = *reinterpret_cast<const float4*>(held + 4 * i);
-        sum += (kept(4 * i, v.x) + kept(4 * i + 1, v.y)) + (kept(4 * i + 2, v.z) + kept(4 * i + 3, v.w));
+        for (int i = from + lane; i < to; i += 32) {
+            const float4 v = *reinterpret_cast<const float4*>(held + 4 * i);
+            sum += (kept(v.x) + kept(v.y)) + (kept(v.z) + kept(v.w));
+        }
     }
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
@@ -714,7 +765,9 @@ __cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(kSmpThreads) 
             const int four = 4 * (i + lane);
             if (i + lane < to) {
                 const float4 v = *reinterpret_cast<const float4*>(held + four);
-                w[0] = kept(four, v.x), w[1] = kept(four + 1, v.y), w[2] = kept(four + 2, v.z), w[3] = kept(four + 3, v.w);
+                const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = stays(four + k, f[k]) ? kept(f[k]) : 0;
             }
             const uint64_t own = w[0] + w[1] + w[2] + w[3];
             if (!__any_sync(0xFFFFFFFFu, own != 0)) continue;
@@ -731,6 +784,13 @@ __cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(kSmpThreads) 
             if (base > aim) break;
         }
     }
+}
+
+};  // Sampler
+
+template <typename T, int THREADS>
+__cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(THREADS) k_sample(tetra_sample_rows p, int part) {
+    Sampler<THREADS>::template run<T>(p, part);
 }
 
 }  // namespace
@@ -755,15 +815,25 @@ int tetra_sample(const tetra_sample_rows* p, void* stream) {
     const size_t smem = sizeof(SmpShared) + 4 * size_t(part);
     constexpr size_t most = sizeof(SmpShared) + 4 * (size_t(TETRA_SAMPLE_MAX_VOCAB) / kSmpCtas);
     static_assert(most <= 232448, "a CTA's shared memory");
+    int sms = 0;
+    if (device_sms(&sms) != cudaSuccess) return TETRA_ERR_CUDA;
     static PerDeviceOnce once;
     const cudaError_t e = once.run([] {
-        const cudaError_t first = cudaFuncSetAttribute(k_sample<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
-        return first != cudaSuccess ? first : cudaFuncSetAttribute(k_sample<__half>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
+        cudaError_t worst = cudaSuccess;
+        for (auto kernel : {k_sample<float, 512>, k_sample<float, 1024>, k_sample<__half, 512>, k_sample<__half, 1024>}) {
+            const cudaError_t got = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
+            if (got != cudaSuccess) worst = got;
+        }
+        return worst;
     });
     if (e != cudaSuccess) return TETRA_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int grid = p->rows * kSmpCtas;
-    return launch_pdl(p->half_type ? k_sample<__half> : k_sample<float>, grid, kSmpThreads, smem, s, *p, part) == cudaSuccess ? TETRA_OK : TETRA_ERR_CUDA;
+    // A CTA on an SM of its own wants more warps to hide its latencies; where there are more clusters than that, two CTAs share an
+    // SM (a seventh of the SMs stay empty: clusters do not cross the boundaries of their groups).
+    const bool alone = grid <= sms - sms / 7;
+    auto kernel = p->half_type ? alone ? k_sample<__half, 1024> : k_sample<__half, 512> : alone ? k_sample<float, 1024> : k_sample<float, 512>;
+    return launch_pdl(kernel, grid, alone ? 1024 : 512, smem, s, *p, part) == cudaSuccess ? TETRA_OK : TETRA_ERR_CUDA;
 }
 
 }  // extern "C"
