@@ -31,7 +31,7 @@ namespace {
 constexpr int kAttThreads = 256, kAttWarps = kAttThreads / 32;
 constexpr uint32_t kAttLeastUnits = 4;     // of a CTA: what sharing an item costs is worth some work
 constexpr int kAttSegs = 32;              // parts of items that a CTA looks up at a time
-constexpr int kAttMaxCtas = 512;          // of a launch: pieces in the workspace
+constexpr int kAttMaxCtas = 384;          // of a launch: pieces in the workspace
 constexpr int kAttBatch = 8;               // pieces that are loaded at a time
 constexpr float kNoRef = -1e30f;          // reference of a column that has seen nothing
 constexpr float kLeastLog = -60.f;        // log2 of the least s_V that counts: 127 * 2^-60 is zero in float16
@@ -70,8 +70,9 @@ struct AttParams {
     float scale;           // times log2 e
     int32_t group;
     int32_t unit_shift;    // blocks of a unit: 8 << unit_shift
-    float* pieces;         // [CTA][2][PIECE]
-    uint32_t* arrived;     // [CTA]: pieces of the item that begins in this CTA and ends beyond it
+    // A CTA may be an item's last and the next one's first: what it keeps for either is apart (second: of the item that begins in it).
+    float* pieces;         // [CTA][4][PIECE]: pieces, then groups' sums, two each
+    uint32_t* arrived;     // [3][CTA]: pieces of the groups that begin in this CTA, two; groups of the item that begins in it
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -165,6 +166,13 @@ __device__ __forceinline__ uint32_t parts_of(uint32_t units, uint32_t share, uin
     return (units + each - 1) / each;
 }
 
+// Units of a part that may do for so many items on G CTAs: a quarter or half of the items' last parts are thought to be short, then
+// all: that one does, since items * 2 <= G.
+__device__ __forceinline__ uint32_t tried_share(uint32_t G, uint32_t items, uint32_t units, int j) {
+    const uint32_t over = G - (j == 0 ? items >> 2 : j == 1 ? items >> 1 : items);
+    return max(kAttLeastUnits, (units + over - 1) / over);
+}
+
 template <int N>
 __device__ __forceinline__ void block_sums(uint32_t (&v)[N], uint32_t (*warp_sums)[kAttWarps]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -194,94 +202,146 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + C::RING + C::MERGE + C::QBYTES); // [seqs + 1]
     __shared__ Seg segs[kAttSegs];
     __shared__ int nsegs, cursor_seq;
-    __shared__ uint32_t cursor_unit, is_last, warp_sums[4][kAttWarps];
+    __shared__ uint32_t cursor_unit, is_last, the_share, are_few, warp_sums[4][kAttWarps];
 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int heads = p.c.kv_heads, heads_all = heads * p.group;
     pdl_wait();
     pdl_release();
 
-    // How the work is cut.  Every CTA finds out for itself, in loops that have one turn for up to 256 sequences (kept as loops:
-    // instructions that run once a launch cost their fetch).
-    const int per = (p.c.seqs + kAttThreads - 1) / kAttThreads, s0 = threadIdx.x * per, s1 = min(s0 + per, p.c.seqs);
-    uint32_t total[2] = {0, 0};
-#pragma unroll 1
-    for (int s = s0; s < s1; ++s) {
-        const Work w = sequence_work<NT>(p, s);
-        total[0] += w.chunks * heads;
-        total[1] += w.chunks * heads * w.units;
-    }
-    block_sums(total, warp_sums);
-    const uint32_t G = gridDim.x;
-    // With few items each gets CTAs of its own, as many parts as leave the longest part short: part sizes are tried from
-    // one that may need too many CTAs to one that cannot.  With many, a CTA takes a range of the sequence of all units.
-    const bool few = 2 * total[0] <= G;
-    uint32_t share = max(kAttLeastUnits, (total[1] + G - 1) / G);
-    if (few) {
-        uint32_t tried[3], need[3] = {0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < 3; ++j) {
-            const uint32_t over = G - (total[0] * (j + 1) >> 2) - (j == 2 ? (total[0] + 3) >> 2 : 0);  // a quarter, half, all of the items' last parts
-            tried[j] = max(kAttLeastUnits, (total[1] + over - 1) / over);
-        }
-        if (tried[0] > kAttLeastUnits) {
-#pragma unroll 1
-            for (int s = s0; s < s1; ++s) {
-                const Work w = sequence_work<NT>(p, s);
-#pragma unroll
-                for (int j = 0; j < 3; ++j) need[j] += w.chunks * heads * ((w.units + tried[j] - 1) / tried[j]);
-            }
-            block_sums(need, warp_sums);
-        }
-        share = need[0] <= G ? tried[0] : need[1] <= G ? tried[1] : tried[2];
-    }
-    // Prefix sum over the sequences: of CTAs, or of units.
+    // The first lines of the page table, which is wanted as soon as it is known whose it is.
     {
-        auto wanted = [&](const Work& w) {
-            uint32_t each;
-            return w.chunks * heads * (few ? parts_of(w.units, share, each) : w.units);
-        };
-        uint32_t mine = 0;
+        const int64_t entries = (p.c.seqs - 1) * p.c.table_stride + p.c.width, at = int64_t(threadIdx.x) * 32;
+        if (at < entries) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.c.table + at));
+    }
+    // How the work is cut.  Every CTA finds out for itself.  With few items each gets CTAs of its own, as many parts as leave the
+    // longest part short: part sizes are tried from one that may need too many CTAs to one that cannot.  With many, a CTA
+    // takes a range of the sequence of all units.  Up to 32 sequences are one warp's work, without a barrier.
+    const uint32_t G = gridDim.x;
+    bool few;
+    uint32_t share;
+    if (p.c.seqs <= 32) {
+        if (warp == 0) {
+            const bool is = lane < p.c.seqs;
+            Work w = is ? sequence_work<NT>(p, lane) : Work{0, 0, 0, 0, 0, 1};
+            const uint32_t items = w.chunks * heads, all_items = __reduce_add_sync(0xFFFFFFFFu, items), all_units = __reduce_add_sync(0xFFFFFFFFu, items * w.units);
+            few = 2 * all_items <= G;
+            share = max(kAttLeastUnits, (all_units + G - 1) / G);
+            if (few) {
+#pragma unroll 1
+                for (int j = 0; j < 3; ++j) {
+                    share = tried_share(G, all_items, all_units, j);
+                    if (__reduce_add_sync(0xFFFFFFFFu, items * ((w.units + share - 1) / share)) <= G) break;
+                }
+            }
+            uint32_t each = 0, parts = 1;
+            if (few) parts = parts_of(w.units, share, each);
+            const uint32_t own = items * (few ? parts : w.units);
+            uint32_t at = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, at, o);
+                if (lane >= o) at += v;
+            }
+            const uint32_t want = few ? blockIdx.x : share * blockIdx.x;
+            if (lane == 31) {
+                prefix[p.c.seqs] = at;
+                if (want >= at) cursor_seq = -1;  // nothing left for this CTA
+                the_share = share;
+                are_few = few;
+            }
+            at -= own;
+            if (is) prefix[lane] = at;
+            if (at <= want && want < at + own) {
+                cursor_seq = lane;
+                cursor_unit = want;
+                if (few) {
+                    const uint32_t local = want - at, item = quotient(local, parts), part = local - item * parts;
+                    set_seg<NT>(p, w, lane, item, part * each, (part + 1) * each, int(blockIdx.x - part), int(blockIdx.x - part + parts - 1), segs[0]);
+                    nsegs = 1;
+                }
+            }
+        }
+        __syncthreads();
+        few = are_few;
+        share = the_share;
+    } else {
+        // ... otherwise all threads', in loops that have one turn for up to 256 sequences (kept as loops: instructions that
+        // run once a launch cost their fetch).
+        const int per = (p.c.seqs + kAttThreads - 1) / kAttThreads, s0 = threadIdx.x * per, s1 = min(s0 + per, p.c.seqs);
+        uint32_t total[2] = {0, 0};
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) {
             const Work w = sequence_work<NT>(p, s);
-            if (w.chunks) mine += wanted(w);
+            total[0] += w.chunks * heads;
+            total[1] += w.chunks * heads * w.units;
         }
-        uint32_t sum = mine;
+        block_sums(total, warp_sums);
+        few = 2 * total[0] <= G;
+        share = max(kAttLeastUnits, (total[1] + G - 1) / G);
+        if (few) {
+            uint32_t tried[3], need[3] = {0, 0, 0};
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-            if (lane >= o) sum += v;
+            for (int j = 0; j < 3; ++j) tried[j] = tried_share(G, total[0], total[1], j);
+            if (tried[0] > kAttLeastUnits) {
+#pragma unroll 1
+                for (int s = s0; s < s1; ++s) {
+                    const Work w = sequence_work<NT>(p, s);
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) need[j] += w.chunks * heads * ((w.units + tried[j] - 1) / tried[j]);
+                }
+                block_sums(need, warp_sums);
+            }
+            share = need[0] <= G ? tried[0] : need[1] <= G ? tried[1] : tried[2];
         }
-        if (lane == 31) warp_sums[0][warp] = sum;
-        __syncthreads();
-        uint32_t at = sum - mine;
-        for (int w = 0; w < warp; ++w) at += warp_sums[0][w];
-        const uint32_t want = few ? blockIdx.x : share * blockIdx.x;
-        if (threadIdx.x == kAttThreads - 1) {
-            prefix[p.c.seqs] = at + mine;
-            if (want >= at + mine) cursor_seq = -1;  // nothing left for this CTA
-        }
-        if (!few || (at <= want && want < at + mine)) {
+        // Prefix sum over the sequences: of CTAs, or of units.
+        {
+            auto wanted = [&](const Work& w) {
+                uint32_t each;
+                return w.chunks * heads * (few ? parts_of(w.units, share, each) : w.units);
+            };
+            uint32_t mine = 0;
 #pragma unroll 1
             for (int s = s0; s < s1; ++s) {
                 const Work w = sequence_work<NT>(p, s);
-                const uint32_t own = w.chunks ? wanted(w) : 0u;
-                prefix[s] = at;
-                if (at <= want && want < at + own) {
-                    cursor_seq = s;
-                    cursor_unit = want;
-                    if (few) {
-                        uint32_t each;
-                        const uint32_t parts = parts_of(w.units, share, each), local = want - at, item = quotient(local, parts), part = local - item * parts;
-                        set_seg<NT>(p, w, s, item, part * each, (part + 1) * each, int(blockIdx.x - part), int(blockIdx.x - part + parts - 1), segs[0]);
-                        nsegs = 1;
-                    }
-                }
-                at += own;
+                if (w.chunks) mine += wanted(w);
             }
+            uint32_t sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+                if (lane >= o) sum += v;
+            }
+            if (lane == 31) warp_sums[0][warp] = sum;
+            __syncthreads();
+            uint32_t at = sum - mine;
+            for (int w = 0; w < warp; ++w) at += warp_sums[0][w];
+            const uint32_t want = few ? blockIdx.x : share * blockIdx.x;
+            if (threadIdx.x == kAttThreads - 1) {
+                prefix[p.c.seqs] = at + mine;
+                if (want >= at + mine) cursor_seq = -1;  // nothing left for this CTA
+            }
+            if (!few || (at <= want && want < at + mine)) {
+#pragma unroll 1
+                for (int s = s0; s < s1; ++s) {
+                    const Work w = sequence_work<NT>(p, s);
+                    const uint32_t own = w.chunks ? wanted(w) : 0u;
+                    prefix[s] = at;
+                    if (at <= want && want < at + own) {
+                        cursor_seq = s;
+                        cursor_unit = want;
+                        if (few) {
+                            uint32_t each;
+                            const uint32_t parts = parts_of(w.units, share, each), local = want - at, item = quotient(local, parts), part = local - item * parts;
+                            set_seg<NT>(p, w, s, item, part * each, (part + 1) * each, int(blockIdx.x - part), int(blockIdx.x - part + parts - 1), segs[0]);
+                            nsegs = 1;
+                        }
+                    }
+                    at += own;
+                }
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
     if (cursor_seq < 0) return;
 
@@ -405,11 +465,11 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     const float by = __uint_as_float(scales.x) * p.scale, vs = __uint_as_float(scales.y);
                     float lv = lg2(vs);
                     lv = lv < kLeastLog ? kLeastLog : lv;  // NaN stays
-                    float x[NT][4];
+                    float x[NT][4], y[NT][4];  // two chains: a product waits for the one before it
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[nt][k] = 0.f;
+                        for (int k = 0; k < 4; ++k) x[nt][k] = y[nt][k] = 0.f;
 #pragma unroll
                     for (int j = 0; j < CHUNKS; ++j) {
                         const uint4 w = lds_uint4(at + j * 512 + lane16);
@@ -419,15 +479,15 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                         for (int nt = 0; nt < NT; ++nt) {
                             const uint4 b = NT == 1 ? qr[j] : reinterpret_cast<const uint4*>(qs)[(nt * CHUNKS + j) * 32 + lane];
                             mma16816(x[nt], a0, a1, a2, a3, b.x, b.y);
-                            mma16816(x[nt], c0, c1, c2, c3, b.z, b.w);
+                            mma16816(NT < 4 ? y[nt] : x[nt], c0, c1, c2, c3, b.z, b.w);
                         }
                     }
-                    const int token = int(rec * kKvBlock) + g;  // and 8 on
-                    bool over = false;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[nt][k] *= by;
+                        for (int k = 0; k < 4; ++k) x[nt][k] = (NT < 4 ? x[nt][k] + y[nt][k] : x[nt][k]) * by;
+                    const int token = int(rec * kKvBlock) + g;  // and 8 on
+                    bool over = false;
                     if (int(rec * kKvBlock) + kKvBlock - 1 > all_see) {  // the last blocks: some column does not see all of it
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
@@ -503,9 +563,13 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             };
 
             // The warps' sums become one: as many fragments as there are warps at a time, each warp adds one over all of them.
-            const bool whole = sg.first == sg.last;
-            // A piece of an item that several CTAs share: place 1 of the CTA that it begins in, place 0 of the others.
-            float4* piece = reinterpret_cast<float4*>(p.pieces + (size_t(blockIdx.x) * 2 + (int(blockIdx.x) == sg.first)) * C::PIECE);
+            // Of an item that several CTAs share, each leaves a piece: place 1 of the CTA that the item begins in, place 0 of the others.
+            const int me = blockIdx.x, shared_by = sg.last - sg.first + 1;
+            auto piece_at = [&](int cta, int place) { return reinterpret_cast<float4*>(p.pieces + (size_t(cta) * 4 + place) * C::PIECE); };
+            auto leave = [&](float4* piece, int f, const float (&v)[4], float r0, float r1, float u0, float u1) {
+                __stcg(piece + f * 32 + lane, make_float4(v[0], v[1], v[2], v[3]));
+                if (f % (D / 16) == 0 && g == 0) __stcg(piece + FRAGS * 32 + f / (D / 16) * 4 + t, make_float4(r0, r1, u0, u1));
+            };
             constexpr int SLOT = (ROUND + NT) * 32;
             float4* mine = merge + warp * SLOT + lane;
 #pragma unroll
@@ -543,39 +607,50 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                         v[2] = fmaf(x.z, f0, v[2]);
                         v[3] = fmaf(x.w, f1, v[3]);
                     }
-                    if (whole) {
-                        store(f, v, u0, u1);
-                    } else {
-                        __stcg(piece + f * 32 + lane, make_float4(v[0], v[1], v[2], v[3]));
-                        if (f % (D / 16) == 0 && g == 0) __stcg(piece + FRAGS * 32 + nt * 4 + t, make_float4(r0, r1, u0, u1));
-                    }
+                    if (shared_by == 1) store(f, v, u0, u1);
+                    else leave(piece_at(me, me == sg.first), f, v, r0, r1, u0, u1);
                 }
                 __syncthreads();
             }
-            if (!whole) {
-                if (threadIdx.x == 0) {
-                    uint32_t had;  // behind the barrier: releases the whole CTA's stores, and acquires the others'
-                    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(had) : "l"(p.arrived + sg.first) : "memory");
-                    is_last = had == uint32_t(sg.last - sg.first);
-                    if (is_last) p.arrived[sg.first] = 0u;  // for the next call
+            if (shared_by > 1) {
+                // The CTA that finds all of a group's pieces there adds them, in order; of many, the square root at a time, and then the
+                // groups' sums (places 2 and 3 of a group's first CTA): a load of what another CTA has just written takes long, and
+                // one after another so many of them.
+                int group = shared_by;
+                if (group > kAttBatch) {
+                    group = 3;
+                    while (group * group < shared_by) ++group;
                 }
-                __syncthreads();
-                if (is_last) {
-                    const float4* pieces = reinterpret_cast<const float4*>(p.pieces);
-                    constexpr int P4 = C::PIECE / 4;
+                const int groups = (shared_by + group - 1) / group, begin = sg.first + (me - sg.first) / group * group;
+#pragma unroll 1
+                for (int level = 0; level < 2; ++level) {
+                    const int from = level ? sg.first : begin, step = level ? group : 1, n = level ? groups : min(group, sg.last + 1 - begin);
+                    if (threadIdx.x == 0) {
+                        uint32_t* counter = p.arrived + (level ? 2 : from == sg.first) * kAttMaxCtas + from;
+                        uint32_t had;  // behind the barrier: releases the whole CTA's stores, and acquires the others'
+                        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(had) : "l"(counter) : "memory");
+                        is_last = had + 1 == uint32_t(n);
+                        if (is_last) *counter = 0u;  // for the next call
+                    }
+                    __syncthreads();
+                    const bool go_on = is_last;
+                    __syncthreads();
+                    if (!go_on) break;
+                    const bool final = level == 1 || groups == 1;
+#pragma unroll 1
                     for (int f = warp; f < FRAGS; f += kAttWarps) {
                         const int nt = f / (D / 16);
                         float r0 = kNoRef, r1 = kNoRef, u0 = 0.f, u1 = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-                        for (int b = sg.first; b <= sg.last; b += kAttBatch) {
+                        for (int at = 0; at < n; at += kAttBatch) {
                             float4 u[kAttBatch], m[kAttBatch];
 #pragma unroll
                             for (int k = 0; k < kAttBatch; ++k) {
-                                const int c = min(b + k, sg.last);
-                                const float4* at = pieces + (size_t(c) * 2 + (c == sg.first)) * P4;
-                                u[k] = __ldcg(at + f * 32 + lane);
-                                m[k] = __ldcg(at + FRAGS * 32 + nt * 4 + t);
-                                if (b + k > sg.last) m[k] = make_float4(kNoRef, kNoRef, 0.f, 0.f), u[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                const int cta = from + min(at + k, n - 1) * step;
+                                const float4* piece = piece_at(cta, 2 * level + (cta == sg.first));
+                                u[k] = __ldcg(piece + f * 32 + lane);
+                                m[k] = __ldcg(piece + FRAGS * 32 + nt * 4 + t);
+                                if (at + k >= n) m[k] = make_float4(kNoRef, kNoRef, 0.f, 0.f), u[k] = make_float4(0.f, 0.f, 0.f, 0.f);
                             }
                             float q0 = r0, q1 = r1;
 #pragma unroll
@@ -595,10 +670,12 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                             r0 = q0;
                             r1 = q1;
                         }
-                        store(f, v, u0, u1);
+                        if (final) store(f, v, u0, u1);
+                        else leave(piece_at(begin, 2 + (begin == sg.first)), f, v, r0, r1, u0, u1);
                     }
+                    if (final) break;
+                    __syncthreads();  // the stores are all before the next arrival
                 }
-                __syncthreads();  // is_last
             }
         }
         if (few) return;
@@ -606,11 +683,11 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     }
 }
 
-constexpr int kAttCounters = kAttMaxCtas * 4;  // bytes
+constexpr int kAttCounters = kAttMaxCtas * 3 * 4;  // bytes
 template <int D>
 constexpr int att_most_columns() { return D == 256 ? 2 : 4; }
 template <int D>
-constexpr size_t att_workspace() { return size_t(kAttCounters) + size_t(kAttMaxCtas) * 2 * AttCfg<D, att_most_columns<D>()>::PIECE * 4; }
+constexpr size_t att_workspace() { return size_t(kAttCounters) + size_t(kAttMaxCtas) * 4 * AttCfg<D, att_most_columns<D>()>::PIECE * 4; }
 
 template <int D, int NT>
 cudaError_t launch_attend(AttParams p, int sms, cudaStream_t s) {

@@ -272,7 +272,7 @@ def attend_check(tt, st, heads, scale=None, q=None, workspace=None, plain=None):
     worst = np.abs(have - want)[finite] / np.maximum(bound[finite], 1e-300)
     worst[np.abs(have - want)[finite] == 0] = 0
     assert worst.size == 0 or worst.max() <= 1, worst.max()
-    assert not ws[:2048].any()  # the counters are zero again
+    assert not ws[:4608].any()  # the counters are zero again
     again = torch.full_like(out, 7.5)
     tt.tetra_kv_attend(d, *st.args(), again, ws, scale)
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))
