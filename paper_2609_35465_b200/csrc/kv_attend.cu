@@ -204,7 +204,8 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     __shared__ int nsegs, cursor_seq;
     __shared__ uint32_t cursor_unit, is_last, the_share, are_few, warp_sums[4][kAttWarps];
 
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    // (What all lanes of a warp have alike is taken from lane 0 here and below: branches on it need no reconvergence.)
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0), g = lane >> 2, t = lane & 3;
     const int heads = p.c.kv_heads, heads_all = heads * p.group;
     pdl_wait();
     pdl_release();
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             }
             __syncthreads();
         }
-        const int count = nsegs;
+        const int count = __shfl_sync(0xFFFFFFFFu, nsegs, 0);
         if (count == 0) return;
 
         // The warp's stream of records over these parts: lane l looks up the place of the l-th of the next 32.
@@ -381,8 +382,8 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             if (++ahead_lane < 32 && ahead_rec < ahead_end) return;
             while (ahead_rec >= ahead_end) {
                 if (++ahead_seg >= count) return;
-                ahead_rec = segs[ahead_seg].r0 + warp;
-                ahead_end = segs[ahead_seg].r1;
+                ahead_rec = __shfl_sync(0xFFFFFFFFu, segs[ahead_seg].r0, 0) + warp;
+                ahead_end = __shfl_sync(0xFFFFFFFFu, segs[ahead_seg].r1, 0);
             }
             ahead_lane = 0;
             const uint32_t mine = ahead_rec + lane * kAttWarps;
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             placed &= ~(1u << to);
             if (ahead_seg < count) {
                 const unsigned char* from = reinterpret_cast<const unsigned char*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<uint64_t>(ahead_at), ahead_lane));
-                if (from) {
+                if (__ballot_sync(0xFFFFFFFFu, ahead_at != nullptr) >> ahead_lane & 1u) {
                     placed |= 1u << to;
                     const uint32_t dst = my_ring + to * REC;
 #pragma unroll
@@ -456,7 +457,8 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) ref[nt][0] = ref[nt][1] = kNoRef, sum[nt][0] = sum[nt][1] = 0.f;
 
-            for (uint32_t rec = sg.r0 + warp; rec < sg.r1; rec += kAttWarps) {
+            const uint32_t end = __shfl_sync(0xFFFFFFFFu, sg.r1, 0);
+            for (uint32_t rec = __shfl_sync(0xFFFFFFFFu, sg.r0, 0) + warp; rec < end; rec += kAttWarps) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
                 __syncwarp();  // the scales were copied by lane 0
                 if (placed >> stage & 1u) {
@@ -710,7 +712,7 @@ template <int D>
 cudaError_t launch_attend_for(const AttParams& p, int sms, cudaStream_t s) {
     const int64_t columns = (int64_t(p.c.rows) * p.group + p.c.seqs - 1) / p.c.seqs;
     if (columns <= 8) return launch_attend<D, 1>(p, sms, s);
-    if (D == 256 || columns <= 16) return launch_attend<D, 2>(p, sms, s);
+    if (D == 256 || columns <= 24) return launch_attend<D, 2>(p, sms, s);
     return launch_attend<D, att_most_columns<D>()>(p, sms, s);
 }
 
