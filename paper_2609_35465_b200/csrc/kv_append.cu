@@ -7,7 +7,8 @@
 // a rotated pair lie in one lane.
 // Norm and rotation are in 64 bits: a key next to the border of two codes, or of two scales, then goes where the
 // formulas put it whatever the order of the sum of squares, and the angle of a far position (10^5 rad) keeps its fraction.
-// The work is small (4096 float64 sines for 64 rows of 128) and latency bounds the kernel.
+// The work is small (4096 float64 sines for 64 rows of 128, made once for all heads of a CTA) and latency bounds the kernel:
+// the row's sequence, its length, its page and the block's scales are loads that depend on one another.
 #include "kv_common.cuh"
 
 namespace tetra {
@@ -26,21 +27,22 @@ struct KvRows {
     int32_t group;  // query heads to a kv head
 };
 
-// The sequence of row r (the CTA's threads look through row_start side by side), or -1; its rows [a, b).
-__device__ __forceinline__ int sequence_of(const KvCache& c, int r, int& a, int& b) {
-    __shared__ int found;
-    if (threadIdx.x == 0) found = INT32_MAX;
-    __syncthreads();
-    for (int s = threadIdx.x; s < c.seqs; s += blockDim.x) {
-        int x, y;
-        c.rows_of(s, x, y);
-        if (x <= r && r < y) atomicMin(&found, s);
+// The sequence of row r, or -1; its rows [a, b).  row_start does not decrease: a warp finds the place in two steps, among every
+// so many entries and then among those between two of them.
+static_assert(TETRA_KV_MAX_SEQS < 32 * 33, "two steps of 32 lanes");
+__device__ __forceinline__ int sequence_of(const KvCache& c, int r, int lane, int& a, int& b) {
+    const int entries = c.seqs + 1, stride = (entries + 31) / 32;
+    int at = lane * stride;
+    int s = __popc(__ballot_sync(0xFFFFFFFFu, at < entries && __ldg(c.row_start + at) <= r));
+    if (s == 0) return -1;
+    s = (s - 1) * stride;
+    if (stride > 1) {
+        at = s + 1 + lane;
+        s += __popc(__ballot_sync(0xFFFFFFFFu, lane < stride - 1 && at < entries && __ldg(c.row_start + at) <= r));
     }
-    __syncthreads();
-    const int s = found;
-    if (s == INT32_MAX) return -1;
+    if (s >= c.seqs) return -1;
     c.rows_of(s, a, b);
-    return s;
+    return a <= r && r < b ? s : -1;
 }
 
 template <typename T, int E>
@@ -50,9 +52,9 @@ __device__ __forceinline__ void load_row(const void* base, int64_t at, int lane,
     for (int i = 0; i < E; ++i) x[i] = float(src[lane + 32 * i]);
 }
 
-// Head norm and rotation of one head's row.
+// Head norm and rotation of one head's row; `turns`: cosine and sine for each pair, or nullptr.
 template <int E>
-__device__ __forceinline__ void turn(const float (&x)[E], const float* weight, const KvRows& p, int64_t pos, int lane, double (&z)[E]) {
+__device__ __forceinline__ void turn(const float (&x)[E], const float* weight, double eps, const double2* turns, int lane, double (&z)[E]) {
 #pragma unroll
     for (int i = 0; i < E; ++i) z[i] = double(x[i]);
     if (weight) {
@@ -61,18 +63,17 @@ __device__ __forceinline__ void turn(const float (&x)[E], const float* weight, c
         for (int i = 0; i < E; ++i) sum = fma(z[i], z[i], sum);
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        const double by = 1. / sqrt(sum * (1. / (32 * E)) + p.eps);
+        const double by = 1. / sqrt(sum * (1. / (32 * E)) + eps);
 #pragma unroll
         for (int i = 0; i < E; ++i) z[i] *= by * double(__ldg(weight + lane + 32 * i));
     }
-    if (p.inv_freq) {
+    if (turns) {
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-            double sn, cs;
-            sincospi(double(pos) * __ldg(p.inv_freq + lane + 32 * i) * 0.318309886183790671538, &sn, &cs);  // 1 / pi
+            const double2 t = turns[lane + 32 * i];
             const double u = z[i], w = z[i + E / 2];
-            z[i] = u * cs - w * sn;
-            z[i + E / 2] = w * cs + u * sn;
+            z[i] = u * t.x - w * t.y;
+            z[i + E / 2] = w * t.x + u * t.y;
         }
     }
 }
@@ -89,19 +90,33 @@ __device__ __forceinline__ float scale_for(uint32_t amax) {
 template <int D, typename T>
 __global__ void __launch_bounds__(kAppendThreads) k_kv_append(KvCache c, KvRows p) {
     constexpr int E = D / 32, TASKS = 2 * kKvBlock / kAppendWarps;
-    __shared__ uint32_t amax[2];  // keys, values
+    extern __shared__ __align__(16) unsigned char smem[];
+    double2* turns = reinterpret_cast<double2*>(smem);  // [rows of the block][D / 2]
+    __shared__ uint32_t amax[2];                        // keys, values
     pdl_wait();
     pdl_release();
-    const int r = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int r = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
+    // The first query of the warp: nothing that is looked up below decides where it lies.
+    const int own = kAppendWarps - 1 - warp;
+    float xq[E];
+    if (own < p.group) load_row<T>(p.q, r * p.q_stride + int64_t(head * p.group + own) * D, lane, xq);
     if (threadIdx.x < 2) amax[threadIdx.x] = 0u;
     int a, b;
-    const int s = sequence_of(c, r, a, b);
+    const int s = sequence_of(c, r, lane, a, b);
     if (s < 0) return;
     const int64_t pos = int64_t(__ldg(c.lengths + s)) + (r - a);
     const int first = int(pos & (kKvBlock - 1));
     const bool leader = r == a || first == 0;
     unsigned char* rec = leader ? c.record<D>(s, pos >> 4, head) : nullptr;
     const int n = rec ? min(kKvBlock - first, b - r) : 0;  // rows of the call in this block
+    if (p.inv_freq) {
+        for (int i = threadIdx.x; i < max(n, 1) * (D / 2); i += kAppendThreads) {
+            double sn, cs;
+            sincospi(double(pos + i / (D / 2)) * __ldg(p.inv_freq + i % (D / 2)) * 0.318309886183790671538, &sn, &cs);  // 1 / pi
+            turns[i] = make_double2(cs, sn);
+        }
+    }
+    __syncthreads();
 
     // Tasks: the block's keys, then its values, a warp each; the queries from the other end of the warps.
     float x[TASKS][E];
@@ -114,7 +129,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append(KvCache c, KvRows 
         if (key) {
             double z[E];
             load_row<T>(p.k, (r + row) * p.k_stride + head * D, lane, x[k]);
-            turn<E>(x[k], p.k_weight, p, pos + row, lane, z);
+            turn<E>(x[k], p.k_weight, p.eps, p.inv_freq ? turns + row * (D / 2) : nullptr, lane, z);
 #pragma unroll
             for (int i = 0; i < E; ++i) x[k][i] = float(z[i]);
         } else {
@@ -126,17 +141,14 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append(KvCache c, KvRows 
         top = __reduce_max_sync(0xFFFFFFFFu, top);
         if (lane == 0) atomicMax(&amax[key ? 0 : 1], top);
     }
-    if (p.q) {
-        for (int j = kAppendWarps - 1 - warp; j < p.group; j += kAppendWarps) {
-            const int h = head * p.group + j;
-            float xq[E];
-            double z[E];
-            load_row<T>(p.q, r * p.q_stride + int64_t(h) * D, lane, xq);
-            turn<E>(xq, p.q_weight, p, pos, lane, z);
-            __half* out = p.q_out + (int64_t(r) * c.kv_heads * p.group + h) * D;
+    for (int j = own; j < p.group; j += kAppendWarps) {  // none without q
+        const int h = head * p.group + j;
+        if (j > own) load_row<T>(p.q, r * p.q_stride + int64_t(h) * D, lane, xq);
+        double z[E];
+        turn<E>(xq, p.q_weight, p.eps, p.inv_freq ? turns : nullptr, lane, z);
+        __half* out = p.q_out + (int64_t(r) * c.kv_heads * p.group + h) * D;
 #pragma unroll
-            for (int i = 0; i < E; ++i) out[lane + 32 * i] = __double2half(z[i]);
-        }
+        for (int i = 0; i < E; ++i) out[lane + 32 * i] = __double2half(z[i]);
     }
     if (!rec) return;
 
@@ -199,55 +211,77 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append(KvCache c, KvRows 
     }
 }
 
-// One CTA per (row, kv head); the first row of a block brings the block's record into shared memory and writes all of the
-// call's rows of it.
-constexpr int kReadThreads = 128;
+// Two warps per (row, kv head): those of the first row of a block write all of the call's rows of it, each half of the dims.
+// A lane turns the bytes that it loads into the values that it stores: eight dims of two tokens, or four of four.
+constexpr int kReadRows = 4;  // of a CTA
 
 template <int D>
-__global__ void __launch_bounds__(kReadThreads) k_kv_read(KvCache c, __half* k_out, __half* v_out) {
-    constexpr int REC = kv_record_bytes(D);
-    __shared__ __align__(16) unsigned char held[REC];
+__global__ void __launch_bounds__(64 * kReadRows) k_kv_read(KvCache c, __half* k_out, __half* v_out) {
     pdl_wait();
     pdl_release();
-    const int r = blockIdx.x, head = blockIdx.y;
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0), g = lane >> 2, t = lane & 3;
+    const int r = blockIdx.x * kReadRows + (warp >> 1), head = blockIdx.y, half = warp & 1;
     int a, b;
-    const int s = sequence_of(c, r, a, b);
+    const int s = r < c.rows ? sequence_of(c, r, lane, a, b) : -1;
     if (s < 0) return;
     const int64_t pos = int64_t(__ldg(c.lengths + s)) + (r - a);
     const int first = int(pos & (kKvBlock - 1));
     if (r != a && first != 0) return;
     const int n = min(kKvBlock - first, b - r);
     const unsigned char* rec = c.record<D>(s, pos >> 4, head);
+    constexpr int MINE = D / 64;  // chunks of 32 dims
+    uint4 kw[MINE], vw[MINE];
+    float ks = 0.f, vs = 0.f;
     if (rec) {
-        for (int i = threadIdx.x; i < REC / 16; i += kReadThreads) reinterpret_cast<uint4*>(held)[i] = reinterpret_cast<const uint4*>(rec)[i];
-    }
-    __syncthreads();
-    const float ks = rec ? *reinterpret_cast<const float*>(held + 2 * kKvBlock * D) : 0.f;
-    const float vs = rec ? *reinterpret_cast<const float*>(held + 2 * kKvBlock * D + 4) : 0.f;
-    for (int i = threadIdx.x; i < n * (D / 8); i += kReadThreads) {  // eight dims of a token
-        const int row = i / (D / 8), d = i % (D / 8) * 8, t = first + row;
-        const unsigned char* kp = held + d / 32 * 512 + ((t & 7) * 4 + (d & 31) / 8) * 16 + (t >> 3) * 8;
-        const unsigned char* vp = held + kKvBlock * D + d / 32 * 512 + ((d & 31) / 4 * 4 + (t & 7) / 2) * 16 + (t >> 3) * 2 + (t & 1);
-        __align__(16) __half kh[8], vh[8];
+        const uint4* at = reinterpret_cast<const uint4*>(rec) + half * MINE * 32 + lane;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            kh[e] = __float2half_rn(rec ? float(int(kp[e]) - 128) * ks : 0.f);
-            vh[e] = __float2half_rn(rec ? float(int(vp[(e >> 2) * 64 + (e & 3) * 4]) - 128) * vs : 0.f);
+        for (int j = 0; j < MINE; ++j) {
+            kw[j] = at[j * 32];
+            vw[j] = at[j * 32 + D];
         }
-        const size_t at = (size_t(r + row) * c.kv_heads + head) * D + d;
-        *reinterpret_cast<uint4*>(k_out + at) = *reinterpret_cast<const uint4*>(kh);
-        *reinterpret_cast<uint4*>(v_out + at) = *reinterpret_cast<const uint4*>(vh);
+        const float2 scales = *reinterpret_cast<const float2*>(rec + 2 * kKvBlock * D);
+        ks = scales.x;
+        vs = scales.y;
+    } else {
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) kw[j] = vw[j] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+    }
+    auto value = [](uint32_t word, int k, float scale) { return float(int(word >> (8 * k) & 255u) - 128) * scale; };
+    auto pair = [](float x, float y) {
+        const __half2 h = __floats2half2_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    };
+#pragma unroll
+    for (int j = 0; j < MINE; ++j) {
+        const int d = (half * MINE + j) * 32;
+        const uint32_t kb[4] = {kw[j].x, kw[j].y, kw[j].z, kw[j].w}, vb[4] = {vw[j].x, vw[j].y, vw[j].z, vw[j].w};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = g + 8 * i - first;
+            if (row >= 0 && row < n)
+                *reinterpret_cast<uint4*>(k_out + (size_t(r + row) * c.kv_heads + head) * D + d + 8 * t) =
+                    make_uint4(pair(value(kb[2 * i], 0, ks), value(kb[2 * i], 1, ks)), pair(value(kb[2 * i], 2, ks), value(kb[2 * i], 3, ks)),
+                               pair(value(kb[2 * i + 1], 0, ks), value(kb[2 * i + 1], 1, ks)), pair(value(kb[2 * i + 1], 2, ks), value(kb[2 * i + 1], 3, ks)));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = 2 * t + (i & 1) + 8 * (i >> 1) - first;
+            if (row >= 0 && row < n)
+                *reinterpret_cast<uint2*>(v_out + (size_t(r + row) * c.kv_heads + head) * D + d + 4 * g) =
+                    make_uint2(pair(value(vb[0], i, vs), value(vb[1], i, vs)), pair(value(vb[2], i, vs), value(vb[3], i, vs)));
+        }
     }
 }
 
 template <typename K, typename... Args>
-int launch_rows(K kernel, int rows, int heads, int threads, void* stream, Args... args) {
+int launch_rows(K kernel, int rows, int heads, int threads, size_t smem, void* stream, Args... args) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(rows), unsigned(heads));
     cfg.blockDim = dim3(unsigned(threads));
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = static_cast<cudaStream_t>(stream);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
@@ -286,7 +320,7 @@ int tetra_kv_append(const tetra_kv_cache* cache, const tetra_kv_rows* rows, void
     if (c.rows == 0) return TETRA_OK;
     const KvRows p{rows->q, rows->k, rows->v, static_cast<__half*>(rows->q_out), rows->inv_freq, rows->q_weight, rows->k_weight,
                    rows->q_stride, rows->k_stride, rows->v_stride, rows->eps, rows->q ? rows->q_heads / c.kv_heads : 0};
-    auto launch = [&](auto kernel) { return launch_rows(kernel, c.rows, c.kv_heads, kAppendThreads, stream, c, p); };
+    auto launch = [&](auto kernel) { return launch_rows(kernel, c.rows, c.kv_heads, kAppendThreads, p.inv_freq ? size_t(kKvBlock) * D / 2 * sizeof(double2) : 0, stream, c, p); };
     if (rows->half_type) return launch(D == 64 ? k_kv_append<64, __half> : D == 128 ? k_kv_append<128, __half> : k_kv_append<256, __half>);
     return launch(D == 64 ? k_kv_append<64, float> : D == 128 ? k_kv_append<128, float> : k_kv_append<256, float>);
 }
@@ -299,7 +333,7 @@ int tetra_kv_read(const tetra_kv_cache* cache, void* k_out, void* v_out, int row
     if (!kv_aligned(k_out, 16) || !kv_aligned(v_out, 16)) return TETRA_ERR_ALIGN;
     if (rows == 0) return TETRA_OK;
     const int D = cache->head_dim;
-    return launch_rows(D == 64 ? k_kv_read<64> : D == 128 ? k_kv_read<128> : k_kv_read<256>, c.rows, c.kv_heads, kReadThreads, stream, c,
+    return launch_rows(D == 64 ? k_kv_read<64> : D == 128 ? k_kv_read<128> : k_kv_read<256>, (c.rows + kReadRows - 1) / kReadRows, c.kv_heads, 64 * kReadRows, 0, stream, c,
                        static_cast<__half*>(k_out), static_cast<__half*>(v_out));
 }
 
