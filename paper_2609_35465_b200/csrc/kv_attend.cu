@@ -42,8 +42,10 @@ struct AttCfg {
     static constexpr int REC = kv_record_bytes(D);
     static constexpr int CHUNKS = D / 32;                      // 512-byte chunks of the keys, and of the values
     static constexpr int FRAGS = NT * D / 16;                  // accumulators, four floats a lane each
-    static constexpr int ROUND = FRAGS < kAttWarps ? FRAGS : kAttWarps;  // of them that are merged at a time, one a warp
     static constexpr int CTAS = D == 256 || (D == 128 && NT == 4) ? 1 : 2;  // of an SM
+    static constexpr int EACH = CTAS == 1 ? 2 : 1;             // of them that a warp adds at a time
+    static constexpr int ROUND = FRAGS < EACH * kAttWarps ? FRAGS : EACH * kAttWarps;
+    static constexpr int TURNS = (FRAGS + kAttWarps - 1) / kAttWarps;  // of them that are a warp's
     static constexpr int STAGES = D == 64 || CTAS == 1 && D == 128 ? 3 : 2;
     static constexpr int RING = kAttWarps * STAGES * REC;
     static constexpr int MERGE = kAttWarps * 512 * (ROUND + NT);
@@ -407,10 +409,6 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         advance();
-        if (NT > 1) {
-#pragma unroll
-            for (int i = 0; i < STAGES; ++i) issue(i);
-        }
 
         for (int i = 0; i < count; ++i) {
             const Seg& sg = segs[i];
@@ -428,16 +426,25 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     for (int k = 0; k < STAGES; ++k) issue(k);
                 }
             } else {
-                for (int k = threadIdx.x; k < NT * CHUNKS * 32; k += kAttThreads) {
-                    const int l = k & 31, j = k / 32 % CHUNKS;
+                constexpr int EACH = (NT * CHUNKS * 32 + kAttThreads - 1) / kAttThreads;
+                uint4 v[EACH];
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) {
+                    const int k = threadIdx.x + e * kAttThreads, l = k & 31, j = k / 32 % CHUNKS;
                     const uint32_t col = sg.col0 + k / (32 * CHUNKS) * 8 + (l >> 2);
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (int(col) < sg.cols) {
+                    v[e] = make_uint4(0, 0, 0, 0);
+                    if (k < NT * CHUNKS * 32 && int(col) < sg.cols) {
                         const uint32_t row = quotient(col, p.group), h = col - row * p.group;
-                        v = __ldg(reinterpret_cast<const uint4*>(p.q + int64_t(sg.row0 + row) * p.q_stride + (sg.head * p.group + h) * D + 32 * j + 8 * (l & 3)));
+                        v[e] = __ldg(reinterpret_cast<const uint4*>(p.q + int64_t(sg.row0 + row) * p.q_stride + (sg.head * p.group + h) * D + 32 * j + 8 * (l & 3)));
                     }
-                    reinterpret_cast<uint4*>(qs)[k] = v;
                 }
+                if (i == 0) {
+#pragma unroll
+                    for (int k = 0; k < STAGES; ++k) issue(k);
+                }
+#pragma unroll
+                for (int e = 0; e < EACH; ++e)
+                    if (int(threadIdx.x) + e * kAttThreads < NT * CHUNKS * 32) reinterpret_cast<uint4*>(qs)[threadIdx.x + e * kAttThreads] = v[e];
                 __syncthreads();
             }
             // Last position of the lane's columns (2 t, 2 t + 1 of each eight), and of the item's first.
@@ -587,30 +594,33 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
 #pragma unroll
                 for (int f = 0; f < ROUND; ++f) mine[f * 32] = make_float4(o[at + f][0], o[at + f][1], o[at + f][2], o[at + f][3]);
                 __syncthreads();
-                if (warp < ROUND) {
-                    const int f = at + warp, nt = f / (D / 16);
-                    const float4* all = merge + lane;
-                    float4 m[kAttWarps];
-                    float r0 = kNoRef, r1 = kNoRef, u0 = 0.f, u1 = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int w = 0; w < kAttWarps; ++w) {
-                        m[w] = all[w * SLOT + (ROUND + nt) * 32];
-                        r0 = fmaxf(r0, m[w].x);
-                        r1 = fmaxf(r1, m[w].y);
-                    }
+                for (int turn = 0; turn < C::EACH; ++turn) {
+                    const int slot = warp + turn * kAttWarps, f = at + slot, nt = f / (D / 16);
+                    if (slot < ROUND) {
+                        const float4* all = merge + lane;
+                        float4 m[kAttWarps];
+                        float r0 = kNoRef, r1 = kNoRef, u0 = 0.f, u1 = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int w = 0; w < kAttWarps; ++w) {
-                        const float4 x = all[w * SLOT + warp * 32];
-                        const float f0 = ex2(m[w].x - r0), f1 = ex2(m[w].y - r1);
-                        u0 = fmaf(m[w].z, f0, u0);
-                        u1 = fmaf(m[w].w, f1, u1);
-                        v[0] = fmaf(x.x, f0, v[0]);
-                        v[1] = fmaf(x.y, f1, v[1]);
-                        v[2] = fmaf(x.z, f0, v[2]);
-                        v[3] = fmaf(x.w, f1, v[3]);
+                        for (int w = 0; w < kAttWarps; ++w) {
+                            m[w] = all[w * SLOT + (ROUND + nt) * 32];
+                            r0 = fmaxf(r0, m[w].x);
+                            r1 = fmaxf(r1, m[w].y);
+                        }
+#pragma unroll
+                        for (int w = 0; w < kAttWarps; ++w) {
+                            const float4 x = all[w * SLOT + slot * 32];
+                            const float f0 = ex2(m[w].x - r0), f1 = ex2(m[w].y - r1);
+                            u0 = fmaf(m[w].z, f0, u0);
+                            u1 = fmaf(m[w].w, f1, u1);
+                            v[0] = fmaf(x.x, f0, v[0]);
+                            v[1] = fmaf(x.y, f1, v[1]);
+                            v[2] = fmaf(x.z, f0, v[2]);
+                            v[3] = fmaf(x.w, f1, v[3]);
+                        }
+                        if (shared_by == 1) store(f, v, u0, u1);
+                        else leave(piece_at(me, me == sg.first), f, v, r0, r1, u0, u1);
                     }
-                    if (shared_by == 1) store(f, v, u0, u1);
-                    else leave(piece_at(me, me == sg.first), f, v, r0, r1, u0, u1);
                 }
                 __syncthreads();
             }
@@ -639,41 +649,52 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     __syncthreads();
                     if (!go_on) break;
                     const bool final = level == 1 || groups == 1;
+                    constexpr int TURNS = C::TURNS, BATCH = kAttBatch / TURNS;
+                    float r0[TURNS], r1[TURNS], u0[TURNS], u1[TURNS], v[TURNS][4];
+#pragma unroll
+                    for (int k = 0; k < TURNS; ++k) r0[k] = r1[k] = kNoRef, u0[k] = u1[k] = v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0.f;
 #pragma unroll 1
-                    for (int f = warp; f < FRAGS; f += kAttWarps) {
-                        const int nt = f / (D / 16);
-                        float r0 = kNoRef, r1 = kNoRef, u0 = 0.f, u1 = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-                        for (int at = 0; at < n; at += kAttBatch) {
-                            float4 u[kAttBatch], m[kAttBatch];
+                    for (int at = 0; at < n; at += BATCH) {
+                        float4 u[TURNS][BATCH], m[TURNS][BATCH];
 #pragma unroll
-                            for (int k = 0; k < kAttBatch; ++k) {
-                                const int cta = from + min(at + k, n - 1) * step;
-                                const float4* piece = piece_at(cta, 2 * level + (cta == sg.first));
-                                u[k] = __ldcg(piece + f * 32 + lane);
-                                m[k] = __ldcg(piece + FRAGS * 32 + nt * 4 + t);
-                                if (at + k >= n) m[k] = make_float4(kNoRef, kNoRef, 0.f, 0.f), u[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int k = 0; k < BATCH; ++k) {
+                            const int cta = from + min(at + k, n - 1) * step;
+                            const float4* piece = piece_at(cta, 2 * level + (cta == sg.first));
+#pragma unroll
+                            for (int i = 0; i < TURNS; ++i) {
+                                const int f = warp + i * kAttWarps;
+                                const bool is = at + k < n && f < FRAGS;
+                                u[i][k] = is ? __ldcg(piece + f * 32 + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+                                m[i][k] = is ? __ldcg(piece + FRAGS * 32 + f / (D / 16) * 4 + t) : make_float4(kNoRef, kNoRef, 0.f, 0.f);
                             }
-                            float q0 = r0, q1 = r1;
-#pragma unroll
-                            for (int k = 0; k < kAttBatch; ++k) q0 = fmaxf(q0, m[k].x), q1 = fmaxf(q1, m[k].y);
-                            const float f0 = ex2(r0 - q0), f1 = ex2(r1 - q1);
-                            u0 *= f0, u1 *= f1, v[0] *= f0, v[1] *= f1, v[2] *= f0, v[3] *= f1;
-#pragma unroll
-                            for (int k = 0; k < kAttBatch; ++k) {
-                                const float n0 = ex2(m[k].x - q0), n1 = ex2(m[k].y - q1);
-                                u0 = fmaf(m[k].z, n0, u0);
-                                u1 = fmaf(m[k].w, n1, u1);
-                                v[0] = fmaf(u[k].x, n0, v[0]);
-                                v[1] = fmaf(u[k].y, n1, v[1]);
-                                v[2] = fmaf(u[k].z, n0, v[2]);
-                                v[3] = fmaf(u[k].w, n1, v[3]);
-                            }
-                            r0 = q0;
-                            r1 = q1;
                         }
-                        if (final) store(f, v, u0, u1);
-                        else leave(piece_at(begin, 2 + (begin == sg.first)), f, v, r0, r1, u0, u1);
+#pragma unroll
+                        for (int i = 0; i < TURNS; ++i) {
+                            float q0 = r0[i], q1 = r1[i];
+#pragma unroll
+                            for (int k = 0; k < BATCH; ++k) q0 = fmaxf(q0, m[i][k].x), q1 = fmaxf(q1, m[i][k].y);
+                            const float f0 = ex2(r0[i] - q0), f1 = ex2(r1[i] - q1);
+                            u0[i] *= f0, u1[i] *= f1, v[i][0] *= f0, v[i][1] *= f1, v[i][2] *= f0, v[i][3] *= f1;
+#pragma unroll
+                            for (int k = 0; k < BATCH; ++k) {
+                                const float n0 = ex2(m[i][k].x - q0), n1 = ex2(m[i][k].y - q1);
+                                u0[i] = fmaf(m[i][k].z, n0, u0[i]);
+                                u1[i] = fmaf(m[i][k].w, n1, u1[i]);
+                                v[i][0] = fmaf(u[i][k].x, n0, v[i][0]);
+                                v[i][1] = fmaf(u[i][k].y, n1, v[i][1]);
+                                v[i][2] = fmaf(u[i][k].z, n0, v[i][2]);
+                                v[i][3] = fmaf(u[i][k].w, n1, v[i][3]);
+                            }
+                            r0[i] = q0;
+                            r1[i] = q1;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < TURNS; ++i) {
+                        const int f = warp + i * kAttWarps;
+                        if (f >= FRAGS) break;
+                        if (final) store(f, v[i], u0[i], u1[i]);
+                        else leave(piece_at(begin, 2 + (begin == sg.first)), f, v[i], r0[i], r1[i], u0[i], u1[i]);
                     }
                     if (final) break;
                     __syncthreads();  // the stores are all before the next arrival
