@@ -98,6 +98,13 @@ __device__ __forceinline__ Tally warp_scan(Tally v, int lane) {
     }
     return v;
 }
+struct Settings {
+    uint64_t k;       // entries that stay
+    float p;          // 1 and above: off
+    uint64_t floor_w; // least weight
+    float u;
+};
+
 // What a CTA of so many threads does.
 template <int kSmpThreads>
 struct Sampler {
@@ -239,6 +246,18 @@ static __device__ __forceinline__ uint32_t local_bin(SmpShared& sm, uint64_t k) 
 template <bool MASS>
 static __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
     SmpShared& sm = row.sm;
+    __syncthreads();
+    if (row.rank != 0) {
+        SmpShared* first = row.cluster.map_shared_rank(&sm, 0);
+#pragma unroll
+        for (int i = 0; i < kSmpBins / kSmpThreads; ++i) {
+            const int b = threadIdx.x + i * kSmpThreads;
+            if (!MASS || b < kSmpCounted) {
+                if (sm.count[b]) atomicAdd(first->count + b, sm.count[b]);
+            }
+            if (MASS && (sm.lo[b] | sm.hi[b])) add_mass(first->lo + b, first->hi + b, (uint64_t(sm.hi[b]) << 32) + sm.lo[b]);
+        }
+    }
     row.cluster.sync();
     if (row.rank == 0) {
         constexpr int PER = kSmpBins / kSmpThreads;
@@ -246,12 +265,7 @@ static __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int b = threadIdx.x * PER + i;
-            own[i] = {0, 0};
-#pragma unroll
-            for (int c = 0; c < kSmpCtas; ++c) {
-                const SmpShared* other = row.cluster.map_shared_rank(&sm, c);
-                own[i] = own[i] + Tally{MASS ? (uint64_t(other->hi[b]) << 32) + other->lo[b] : 0ull, other->count[b]};
-            }
+            own[i] = {MASS ? (uint64_t(sm.hi[b]) << 32) + sm.lo[b] : 0ull, sm.count[b]};
             sum = sum + own[i];
         }
         Tally upto = block_scan(sm, sum, total);
@@ -428,13 +442,6 @@ static __device__ __forceinline__ uint64_t find_cut(Row& row, const Bins& bins, 
     }
     return c;
 }
-
-struct Settings {
-    uint64_t k;       // entries that stay
-    float p;          // 1 and above: off
-    uint64_t floor_w; // least weight
-    float u;
-};
 
 // All of the filters and the draw among sm.list[0 .. n), which holds the first n entries in the order, 1 <= n <= kSmpFew: one CTA.
 // `need`: the mass that top-p wants where that is known, or 0: then the list holds all that top-k leaves.  An entry counts
@@ -641,7 +648,8 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
         const Tally* all = row.tell({own_best, sm.listed});
         const bool fits = __all_sync(0xFFFFFFFFu, all[lane % kSmpCtas].count <= kSmpRegion);
         if (fits) {
-            if (rank == 0) finish_parts(sm, all, by, T_row, set, token, prob);
+            // A quarter of the threads is enough, and fewer warps meet sooner at a barrier.
+            if (rank == 0 && threadIdx.x < kSmpFew) Sampler<kSmpFew>::finish_parts(sm, all, by, T_row, set, token, prob);
             return;
         }
         for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = 0;
@@ -685,7 +693,7 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
         }
         if (sm.entries <= kSmpFew && (top_k || sm.bin < kSmpCounted)) {
             const uint32_t n = gather(row, bins, 0, min(uint32_t(sm.bin), uint32_t(kSmpBins - 1)), 0);
-            if (rank == 0) finish(sm, weigh, n, set, top_k ? 0 : sm.need, token, prob);
+            if (rank == 0 && threadIdx.x < kSmpFew) Sampler<kSmpFew>::finish(sm, weigh, n, set, top_k ? 0 : sm.need, token, prob);
             return;
         }
         if (top_k) {
