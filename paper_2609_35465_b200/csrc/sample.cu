@@ -487,13 +487,16 @@ static __device__ __forceinline__ void finish(SmpShared& sm, const Weigh& weigh,
     }
 }
 
-// The same from the CTAs' parts: all[c].count entries at sm.list + c * kSmpRegion, all[c].mass the largest of the CTA; top-k is on.
+// The same from the CTAs' parts, top-k being on: all[c].count has how many entries lie at sm.list + c * kSmpRegion, and above that
+// the key below which the CTA has k entries at least (so have all: the largest of these keys is a bound for all); all[c].mass
+// is the CTA's largest.
 static __device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* all, double by, float T, const Settings& set, int32_t* token, float* prob) {
     constexpr int PER = kSmpCtas * kSmpRegion / kSmpThreads;
+    const int lane = threadIdx.x & 31;
     uint64_t best = 0, entry[PER];
-    uint32_t n = 0;
+    uint32_t bound = 0;
 #pragma unroll
-    for (int c = 0; c < kSmpCtas; ++c) best = max(best, all[c].mass), n += uint32_t(all[c].count);
+    for (int c = 0; c < kSmpCtas; ++c) best = max(best, all[c].mass), bound = max(bound, uint32_t(all[c].count >> 32));
     const float top = value_of(uint32_t(best >> 32));
     const Weigh weigh{double(top), by, reach_of(T), sm.powers};
     if (top == -INFINITY) {
@@ -503,21 +506,30 @@ static __device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* 
         }
         return;
     }
+    uint32_t own = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const uint32_t at = threadIdx.x + i * kSmpThreads;
-        entry[i] = at % kSmpRegion < all[at / kSmpRegion].count ? sm.list[at] : 0;
+        entry[i] = at % kSmpRegion < uint32_t(all[at / kSmpRegion].count) ? sm.list[at] : 0;
+        if (entry[i] >> 32 < bound) entry[i] = 0;
+        own += entry[i] != 0;
     }
+    if (threadIdx.x == 0) sm.few = 0;
     __syncthreads();
+    uint32_t place = own;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const uint32_t at = threadIdx.x + i * kSmpThreads;
-        uint32_t place = at % kSmpRegion;
-#pragma unroll
-        for (int c = 0; c < kSmpCtas - 1; ++c)
-            if (c < int(at / kSmpRegion)) place += uint32_t(all[c].count);
-        if (entry[i]) sm.list[place] = entry[i];
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, place, o);
+        if (lane >= o) place += v;
     }
+    const uint32_t before = place - own;
+    if (lane == 31) place = atomicAdd(&sm.few, place);
+    place = __shfl_sync(0xFFFFFFFFu, place, 31) + before;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (entry[i]) sm.list[place++] = entry[i];
+    __syncthreads();
+    uint32_t n = sm.few;
     __syncthreads();
     if (n > kSmpFew) {
         cut_list<false>(sm, Bins(top, -INFINITY, T), weigh, n, 0.f, 1.f, 0, set.k, &sm.cut);
@@ -645,8 +657,8 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
             }
         });
         __syncthreads();
-        const Tally* all = row.tell({own_best, sm.listed});
-        const bool fits = __all_sync(0xFFFFFFFFu, all[lane % kSmpCtas].count <= kSmpRegion);
+        const Tally* all = row.tell({own_best, uint64_t(sm.sub < kSmpBins ? sm.least_key : 0u) << 32 | sm.listed});
+        const bool fits = __all_sync(0xFFFFFFFFu, uint32_t(all[lane % kSmpCtas].count) <= kSmpRegion);
         if (fits) {
             // A quarter of the threads is enough, and fewer warps meet sooner at a barrier.
             if (rank == 0 && threadIdx.x < kSmpFew) Sampler<kSmpFew>::finish_parts(sm, all, by, T_row, set, token, prob);
