@@ -19,7 +19,8 @@
  *     launch).  tetra_pack_codes, tetra_q4_pack, the plan calls, copies and
  *     ordinary kernels do not allow it, so a product that follows one of them
  *     directly, in a captured graph too, multiplies what it wrote.  The products,
- *     tetra_decode_packed and tetra_q4_rows do allow it: use a result of theirs (y,
+ *     tetra_decode_packed, tetra_q4_rows and the calls of tetra_kv.h and
+ *     tetra_sample.h do allow it: use a result of theirs (y,
  *     coordinates, rows) as activations as it is, but as row scales, tail or codes
  *     only behind a copy, an ordinary kernel or a synchronisation; the same goes for
  *     a kernel of the caller's that executes griddepcontrol.launch_dependents;

@@ -17,7 +17,8 @@
  *   scales  2 float32    s_K, s_V, and 8 bytes that are not used
  * A byte holds code + 128, code in [-127, 127]; the value it stands for is code * scale.  (The orders are those in
  * which the lanes of a warp hold the operands of a tensor-core product: a lane's bytes are contiguous.)
- * tetra_kv_append writes powers of two as scales, the attention takes any finite scale.
+ * tetra_kv_append writes powers of two as scales, the attention takes any finite scale that is not
+ * negative.
  *
  * Rows.  A step has `rows` rows of q, k and v.  Those of sequence s are row_start[s] .. row_start[s+1] - 1, its
  * next tokens in order; lengths[s] tokens of it are in the cache before this step, so row row_start[s] + i is at

@@ -38,8 +38,9 @@ typedef struct {
  *   token   the smallest index i, among those that are left, with the sum of w_j over j <= i above u times their
  *           whole mass M; prob = w_i / M.
  * u lies in [0, 1) (values outside are taken as the nearest inside, NaN as 0).  T that is not above zero takes the first
- * of the largest logits, with prob 1.  NaN counts as minus infinity, which is never taken; where a logit is plus infinity only
- * those have mass.  A row without a logit above minus infinity gives token -1 and prob 0.
+ * of the largest logits, with prob 1.  NaN counts as minus infinity, which is never taken, plus infinity as float32's largest
+ * number; magnitudes below 2^-126 count as zero, and a distance from the largest logit that float32 cannot hold as infinite.
+ * A row without a logit above minus infinity gives token -1 and prob 0.
  * The weights are whole multiples of 2^-44, off by no more than that (the least have none), and every sum of them is exact:
  * the result does not depend on any order of summation and is the same from run to run.  One launch, no scratch memory. */
 int tetra_sample(const tetra_sample_rows *rows, void *stream);

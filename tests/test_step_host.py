@@ -172,3 +172,13 @@ def test_sampling_by_hand():
     assert ref.sample(x, 0.99, m=0.6)[0] == 2 and ref.sample(x, 0.99, m=2.0)[0] == 0
     assert ref.sample(x, 0.99, T=0)[0] == 0 and ref.sample(np.full(4, -np.inf), 0.5)[0] == -1
     assert ref.sample(np.array([1.0, 1, 1]), 0.99, k=2)[0] == 1  # equal logits: by index
+
+
+def test_kernels_wait_before_they_release():
+    """A kernel's end implies that of all before it, and its operands may come from any call before it on the stream."""
+    import os
+    import re
+    csrc = os.path.join(os.path.dirname(tbuild.__file__), "csrc")
+    for f, kernels in (("kv_append.cu", 2), ("kv_attend.cu", 1), ("sample.cu", 1)):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, f)).read())
+        assert len(re.findall(r"pdl_wait\(\);\s*pdl_release\(\);", text)) == kernels == text.count("pdl_release") == text.count("pdl_wait")
