@@ -168,12 +168,15 @@ __device__ __forceinline__ uint32_t parts_of(uint32_t units, uint32_t share, uin
     return (units + each - 1) / each;
 }
 
-// Units of a part that may do for so many items on G CTAs: a quarter or half of the items' last parts are thought to be short, then
-// all: that one does, since items * 2 <= G.
+// Units of a part that may do for so many items on G CTAs, items <= G: a quarter or half of the items' last parts are thought to be
+// short, then all: that one does.
 __device__ __forceinline__ uint32_t tried_share(uint32_t G, uint32_t items, uint32_t units, int j) {
-    const uint32_t over = G - (j == 0 ? items >> 2 : j == 1 ? items >> 1 : items);
+    const uint32_t over = max(1u, G - (j == 0 ? items >> 2 : j == 1 ? items >> 1 : items));
     return max(kAttLeastUnits, (units + over - 1) / over);
 }
+// A CTA with one part of one item has neither to look up its items one after another nor to begin anew, which takes as long as
+// about five units (16 sequences of 2048: 19.4 us so, 22.5 us with even ranges of 7 units instead of 8).
+__device__ __forceinline__ bool worth_it(uint32_t share, uint32_t even) { return share <= even + even / 8 + 5; }
 
 template <int N>
 __device__ __forceinline__ void block_sums(uint32_t (&v)[N], uint32_t (*warp_sums)[kAttWarps]) {
@@ -218,8 +221,8 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
         if (at < entries) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.c.table + at));
     }
     // How the work is cut.  Every CTA finds out for itself.  With few items each gets CTAs of its own, as many parts as leave the
-    // longest part short: part sizes are tried from one that may need too many CTAs to one that cannot.  With many, a CTA
-    // takes a range of the sequence of all units.  Up to 32 sequences are one warp's work, without a barrier.
+    // longest part short: part sizes are tried from one that may need too many CTAs to one that cannot.  With many, or where
+    // that would leave CTAs idle for long, a CTA takes a range of the sequence of all units.  Up to 32 sequences are one warp's work, without a barrier.
     const uint32_t G = gridDim.x;
     bool few;
     uint32_t share;
@@ -228,15 +231,16 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             const bool is = lane < p.c.seqs;
             Work w = is ? sequence_work<NT>(p, lane) : Work{0, 0, 0, 0, 0, 1};
             const uint32_t items = w.chunks * heads, all_items = __reduce_add_sync(0xFFFFFFFFu, items), all_units = __reduce_add_sync(0xFFFFFFFFu, items * w.units);
-            few = 2 * all_items <= G;
-            share = max(kAttLeastUnits, (all_units + G - 1) / G);
-            if (few) {
+            const uint32_t even = max(kAttLeastUnits, (all_units + G - 1) / G);
+            if (all_items <= G) {
 #pragma unroll 1
                 for (int j = 0; j < 3; ++j) {
                     share = tried_share(G, all_items, all_units, j);
                     if (__reduce_add_sync(0xFFFFFFFFu, items * ((w.units + share - 1) / share)) <= G) break;
                 }
             }
+            few = all_items <= G && worth_it(share, even);
+            if (!few) share = even;
             uint32_t each = 0, parts = 1;
             if (few) parts = parts_of(w.units, share, each);
             const uint32_t own = items * (few ? parts : w.units);
@@ -280,22 +284,23 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             total[1] += w.chunks * heads * w.units;
         }
         block_sums(total, warp_sums);
-        few = 2 * total[0] <= G;
-        share = max(kAttLeastUnits, (total[1] + G - 1) / G);
+        const uint32_t even = max(kAttLeastUnits, (total[1] + G - 1) / G);
+        share = even;
+        few = total[0] <= G;
         if (few) {
             uint32_t tried[3], need[3] = {0, 0, 0};
 #pragma unroll
             for (int j = 0; j < 3; ++j) tried[j] = tried_share(G, total[0], total[1], j);
-            if (tried[0] > kAttLeastUnits) {
 #pragma unroll 1
-                for (int s = s0; s < s1; ++s) {
-                    const Work w = sequence_work<NT>(p, s);
+            for (int s = s0; s < s1; ++s) {
+                const Work w = sequence_work<NT>(p, s);
 #pragma unroll
-                    for (int j = 0; j < 3; ++j) need[j] += w.chunks * heads * ((w.units + tried[j] - 1) / tried[j]);
-                }
-                block_sums(need, warp_sums);
+                for (int j = 0; j < 3; ++j) need[j] += w.chunks * heads * ((w.units + tried[j] - 1) / tried[j]);
             }
+            block_sums(need, warp_sums);
             share = need[0] <= G ? tried[0] : need[1] <= G ? tried[1] : tried[2];
+            few = worth_it(share, even);
+            if (!few) share = even;
         }
         // Prefix sum over the sequences: of CTAs, or of units.
         {

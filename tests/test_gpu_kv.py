@@ -305,6 +305,12 @@ def test_attend_many_sequences(tt):
     attend_check(tt, Step(27, 128, 8, 16, rng.integers(0, 100, 300).tolist(), [1] * 300), 32)
 
 
+@pytest.mark.parametrize("seqs,H,long,short", [(95, 2, 640, 640), (74, 2, 600, 1100), (100, 1, 513, 1100), (37, 8, 520, 500), (148, 2, 300, 1030), (50, 5, 40, 40), (33, 4, 3000, 10), (20, 7, 600, 1200), (32, 9, 640, 640)])
+def test_attend_at_every_way_to_cut(tt, seqs, H, long, short):
+    """Items about as many as CTAs, parts that just fit or just do not, equal and ragged ones."""
+    attend_check(tt, Step(37 + seqs, 64, H, 64, [long - 3 * i % 17 if i % 2 else short for i in range(seqs)], [1] * seqs), 2 * H)
+
+
 def test_attend_rows_that_see_nothing(tt):
     st = Step(28, 128, 2, 16, [-1, -5, 20, 7, -2], [1, 3, 1, 1, 5], width=2)
     st.table[2] = [-1, 10 ** 6]
