@@ -178,6 +178,15 @@ __device__ __forceinline__ uint32_t tried_share(uint32_t G, uint32_t items, uint
 // about five units (16 sequences of 2048: 19.4 us so, 22.5 us with even ranges of 7 units instead of 8).
 __device__ __forceinline__ bool worth_it(uint32_t share, uint32_t even) { return share <= even + even / 8 + 5; }
 
+// Whether a warp for each item is faster than ranges of units, items being of so many blocks at most.  In hundreds of cycles: a part
+// of an item takes a CTA 45 and 22 for each of its units, an item a warp 25 and 13 for each block.  Measured, 8 heads, ranges
+// against warps: 64 sequences of 3 tokens 9.3 and 7.9 us, of 100 11.2 and 11.3, of 300 15.9 and 19.4; 500 of 3 tokens 46
+// and 17 us, of 700 138 and 126.
+__device__ __forceinline__ bool short_items(uint32_t G, uint32_t items, uint32_t blocks) {
+    const uint32_t rounds = (items + kAttWarps * G - 1) / (kAttWarps * G), parts = (items + G - 1) / G;
+    return blocks < 64 && rounds * (25 + 13 * blocks) < parts * (45 + 22 * ((blocks + kAttWarps - 1) / kAttWarps));
+}
+
 template <int N>
 __device__ __forceinline__ void block_sums(uint32_t (&v)[N], uint32_t (*warp_sums)[kAttWarps]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -207,7 +216,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + C::RING + C::MERGE + C::QBYTES); // [seqs + 1]
     __shared__ Seg segs[kAttSegs];
     __shared__ int nsegs, cursor_seq;
-    __shared__ uint32_t cursor_unit, is_last, the_share, are_few, warp_sums[4][kAttWarps];
+    __shared__ uint32_t cursor_unit, is_last, the_share, are_few, are_tiny, warp_sums[4][kAttWarps];
 
     // (What all lanes of a warp have alike is taken from lane 0 here and below: branches on it need no reconvergence.)
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0), g = lane >> 2, t = lane & 3;
@@ -222,16 +231,17 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     }
     // How the work is cut.  Every CTA finds out for itself.  With few items each gets CTAs of its own, as many parts as leave the
     // longest part short: part sizes are tried from one that may need too many CTAs to one that cannot.  With many, or where
-    // that would leave CTAs idle for long, a CTA takes a range of the sequence of all units.  Up to 32 sequences are one warp's work, without a barrier.
+    // that would leave CTAs idle for long, a CTA takes a range of the sequence of all units; but of very short items each is a
+    // warp's own.  Up to 32 sequences are one warp's work to cut, without a barrier.
     const uint32_t G = gridDim.x;
-    bool few;
+    bool few, tiny = false;
     uint32_t share;
     if (p.c.seqs <= 32) {
         if (warp == 0) {
             const bool is = lane < p.c.seqs;
             Work w = is ? sequence_work<NT>(p, lane) : Work{0, 0, 0, 0, 0, 1};
             const uint32_t items = w.chunks * heads, all_items = __reduce_add_sync(0xFFFFFFFFu, items), all_units = __reduce_add_sync(0xFFFFFFFFu, items * w.units);
-            const uint32_t even = max(kAttLeastUnits, (all_units + G - 1) / G);
+            const uint32_t even = (all_units + G - 1) / G;
             if (all_items <= G) {
 #pragma unroll 1
                 for (int j = 0; j < 3; ++j) {
@@ -241,21 +251,23 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             }
             few = all_items <= G && worth_it(share, even);
             if (!few) share = even;
+            if (NT == 1 && !few) tiny = short_items(G, all_items, __reduce_max_sync(0xFFFFFFFFu, items ? w.blocks : 0u));
             uint32_t each = 0, parts = 1;
             if (few) parts = parts_of(w.units, share, each);
-            const uint32_t own = items * (few ? parts : w.units);
+            const uint32_t own = items * (few ? parts : tiny ? 1u : w.units);
             uint32_t at = own;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, at, o);
                 if (lane >= o) at += v;
             }
-            const uint32_t want = few ? blockIdx.x : share * blockIdx.x;
+            const uint32_t want = few || tiny ? blockIdx.x : share * blockIdx.x;
             if (lane == 31) {
                 prefix[p.c.seqs] = at;
                 if (want >= at) cursor_seq = -1;  // nothing left for this CTA
                 the_share = share;
                 are_few = few;
+                are_tiny = tiny;
             }
             at -= own;
             if (is) prefix[lane] = at;
@@ -271,20 +283,23 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
         }
         __syncthreads();
         few = are_few;
+        tiny = are_tiny;
         share = the_share;
     } else {
         // ... otherwise all threads', in loops that have one turn for up to 256 sequences (kept as loops: instructions that
         // run once a launch cost their fetch).
         const int per = (p.c.seqs + kAttThreads - 1) / kAttThreads, s0 = threadIdx.x * per, s1 = min(s0 + per, p.c.seqs);
-        uint32_t total[2] = {0, 0};
+        uint32_t total[2] = {0, 0}, longest = 0;
+        if (threadIdx.x == 0) cursor_unit = 0;
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) {
             const Work w = sequence_work<NT>(p, s);
             total[0] += w.chunks * heads;
             total[1] += w.chunks * heads * w.units;
+            if (w.chunks) longest = max(longest, w.blocks);
         }
         block_sums(total, warp_sums);
-        const uint32_t even = max(kAttLeastUnits, (total[1] + G - 1) / G);
+        const uint32_t even = (total[1] + G - 1) / G;
         share = even;
         few = total[0] <= G;
         if (few) {
@@ -302,11 +317,18 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             few = worth_it(share, even);
             if (!few) share = even;
         }
-        // Prefix sum over the sequences: of CTAs, or of units.
+        if (NT == 1 && !few) {
+            longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+            if (lane == 0) atomicMax(&cursor_unit, longest);
+            __syncthreads();
+            tiny = short_items(G, total[0], cursor_unit);
+            __syncthreads();
+        }
+        // Prefix sum over the sequences: of CTAs, of items, or of units.
         {
             auto wanted = [&](const Work& w) {
                 uint32_t each;
-                return w.chunks * heads * (few ? parts_of(w.units, share, each) : w.units);
+                return w.chunks * heads * (few ? parts_of(w.units, share, each) : tiny ? 1u : w.units);
             };
             uint32_t mine = 0;
 #pragma unroll 1
@@ -324,7 +346,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             __syncthreads();
             uint32_t at = sum - mine;
             for (int w = 0; w < warp; ++w) at += warp_sums[0][w];
-            const uint32_t want = few ? blockIdx.x : share * blockIdx.x;
+            const uint32_t want = few || tiny ? blockIdx.x : share * blockIdx.x;
             if (threadIdx.x == kAttThreads - 1) {
                 prefix[p.c.seqs] = at + mine;
                 if (want >= at + mine) cursor_seq = -1;  // nothing left for this CTA
@@ -354,8 +376,23 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     if (cursor_seq < 0) return;
 
     const uint32_t my_ring = smem_u32(ring) + warp * STAGES * REC, lane16 = lane * 16;
-    for (;;) {
-        if (!few) {  // the next parts of items of this CTA's range
+    // A warp's records of a part: every eighth, or all.
+    const uint32_t offset = tiny ? 0 : warp, step = tiny ? 1 : kAttWarps;
+    const Seg* list = tiny ? segs + warp : segs;
+    for (uint32_t item = warp * G + blockIdx.x;; item += kAttWarps * G) {
+        if (tiny) {  // the warp's next item
+            if (item >= prefix[p.c.seqs]) return;
+            int s = 0;
+            for (uint32_t who = 0; !who; s += 32) {
+                const int at = s + lane;
+                who = __ballot_sync(0xFFFFFFFFu, at < p.c.seqs && prefix[at] <= item && item < prefix[at + 1]);
+                if (who) s += __ffs(who) - 33;
+            }
+            const Work w = sequence_work<NT>(p, s);
+            __syncwarp();
+            if (lane == 0) set_seg<NT>(p, w, s, item - prefix[s], 0, w.units, 0, 0, segs[warp]);
+            __syncwarp();
+        } else if (!few) {  // the next parts of items of this CTA's range
             if (threadIdx.x == 0) {
                 int n = 0, s = cursor_seq;
                 uint32_t u = cursor_unit;
@@ -377,7 +414,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             }
             __syncthreads();
         }
-        const int count = __shfl_sync(0xFFFFFFFFu, nsegs, 0);
+        const int count = tiny ? 1 : __shfl_sync(0xFFFFFFFFu, nsegs, 0);
         if (count == 0) return;
 
         // The warp's stream of records over these parts: lane l looks up the place of the l-th of the next 32.
@@ -385,16 +422,16 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
         uint32_t ahead_rec = 0, ahead_end = 0;
         const unsigned char* ahead_at = nullptr;  // of the lane's record
         auto advance = [&] {
-            ahead_rec += kAttWarps;
+            ahead_rec += step;
             if (++ahead_lane < 32 && ahead_rec < ahead_end) return;
             while (ahead_rec >= ahead_end) {
                 if (++ahead_seg >= count) return;
-                ahead_rec = __shfl_sync(0xFFFFFFFFu, segs[ahead_seg].r0, 0) + warp;
-                ahead_end = __shfl_sync(0xFFFFFFFFu, segs[ahead_seg].r1, 0);
+                ahead_rec = __shfl_sync(0xFFFFFFFFu, list[ahead_seg].r0, 0) + offset;
+                ahead_end = __shfl_sync(0xFFFFFFFFu, list[ahead_seg].r1, 0);
             }
             ahead_lane = 0;
-            const uint32_t mine = ahead_rec + lane * kAttWarps;
-            ahead_at = mine < ahead_end ? p.c.template record<D>(segs[ahead_seg].seq, mine, segs[ahead_seg].head) : nullptr;
+            const uint32_t mine = ahead_rec + lane * step;
+            ahead_at = mine < ahead_end ? p.c.template record<D>(list[ahead_seg].seq, mine, list[ahead_seg].head) : nullptr;
         };
         uint32_t placed = 0;  // bit per stage: its record has a place
         int stage = 0;
@@ -416,7 +453,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
         advance();
 
         for (int i = 0; i < count; ++i) {
-            const Seg& sg = segs[i];
+            const Seg& sg = list[i];
             // Queries: lane (g, t) holds column g's dims 32 j + 8 t .. + 7 of every chunk j.
             uint4 qr[NT == 1 ? CHUNKS : 1];
             if (NT == 1) {
@@ -470,7 +507,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             for (int nt = 0; nt < NT; ++nt) ref[nt][0] = ref[nt][1] = kNoRef, sum[nt][0] = sum[nt][1] = 0.f;
 
             const uint32_t end = __shfl_sync(0xFFFFFFFFu, sg.r1, 0);
-            for (uint32_t rec = __shfl_sync(0xFFFFFFFFu, sg.r0, 0) + warp; rec < end; rec += kAttWarps) {
+            for (uint32_t rec = __shfl_sync(0xFFFFFFFFu, sg.r0, 0) + offset; rec < end; rec += step) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
                 __syncwarp();  // the scales were copied by lane 0
                 if (placed >> stage & 1u) {
@@ -592,8 +629,14 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int m = 4; m <= 16; m <<= 1) sum[nt][k] += __shfl_xor_sync(0xFFFFFFFFu, sum[nt][k], m);
-                mine[(ROUND + nt) * 32] = make_float4(ref[nt][0], ref[nt][1], sum[nt][0], sum[nt][1]);
             }
+            if (tiny) {
+#pragma unroll
+                for (int f = 0; f < FRAGS; ++f) store(f, o[f], sum[f / (D / 16)][0], sum[f / (D / 16)][1]);
+                break;  // count is one
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mine[(ROUND + nt) * 32] = make_float4(ref[nt][0], ref[nt][1], sum[nt][0], sum[nt][1]);
 #pragma unroll
             for (int at = 0; at < FRAGS; at += ROUND) {
 #pragma unroll
@@ -707,7 +750,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             }
         }
         if (few) return;
-        __syncthreads();  // segs
+        if (!tiny) __syncthreads();  // segs
     }
 }
 

@@ -305,7 +305,8 @@ def test_attend_many_sequences(tt):
     attend_check(tt, Step(27, 128, 8, 16, rng.integers(0, 100, 300).tolist(), [1] * 300), 32)
 
 
-@pytest.mark.parametrize("seqs,H,long,short", [(95, 2, 640, 640), (74, 2, 600, 1100), (100, 1, 513, 1100), (37, 8, 520, 500), (148, 2, 300, 1030), (50, 5, 40, 40), (33, 4, 3000, 10), (20, 7, 600, 1200), (32, 9, 640, 640)])
+@pytest.mark.parametrize("seqs,H,long,short", [(95, 2, 640, 640), (74, 2, 600, 1100), (100, 1, 513, 1100), (37, 8, 520, 500), (148, 2, 300, 1030), (50, 5, 40, 40), (33, 4, 3000, 10), (20, 7, 600, 1200), (32, 9, 640, 640),
+                                                   (400, 3, 40, 17), (64, 8, 3, 3), (30, 16, 100, 1), (64, 8, 130, 200), (700, 7, 20, 33)])
 def test_attend_at_every_way_to_cut(tt, seqs, H, long, short):
     """Items about as many as CTAs, parts that just fit or just do not, equal and ragged ones."""
     attend_check(tt, Step(37 + seqs, 64, H, 64, [long - 3 * i % 17 if i % 2 else short for i in range(seqs)], [1] * seqs), 2 * H)
