@@ -3,14 +3,14 @@
 // A step has one or a few rows a sequence and reads each sequence's keys and values once: 2 D bytes a token and kv head
 // against 4 D multiply-adds for each query head of the group, so HBM bounds it and the arrangement serves the stream.
 //
-// Work.  An item is (sequence, kv head, chunk of 8 NT columns); a column is one (row, query head of the group).  The
-// blocks of 16 tokens of all items form one sequence of units that the CTAs of a persistent grid cut into equal
-// contiguous ranges, whatever the lengths: a CTA finds its range from a prefix sum over the sequences that each CTA makes for
-// itself (lengths are on the device and change from step to step of a captured graph).  Of its part of an item the eight
-// warps take every eighth record; each warp streams its records through a cp.async ring of its own that goes on over the
-// ends of items.  A lane copies the very bytes that it will use, so nothing but a warp-wide fence stands between
-// a copy and its use.  The warps' sums meet in shared memory; an item cut by ranges leaves a piece per CTA in the
-// workspace, and the CTA that finds the others there adds them in order of the CTAs.  Nothing waits for another CTA.
+// Work.  An item is (sequence, kv head, chunk of 8 NT columns); a column is one (row, query head of the group).  The lengths are
+// on the device and change from step to step of a captured graph, so every CTA of a persistent grid finds its work from
+// them: one part of one item where items are few, so many parts each that all are of about the same size; a contiguous
+// range of the blocks of all items where they are many; and where they are many and very short, a warp takes an item.  Of a
+// CTA's part of an item the eight warps take every eighth record; each warp streams its records through a cp.async ring of its
+// own that goes on over the ends of items.  A lane copies the very bytes that it will use, so nothing but a warp-wide fence
+// stands between a copy and its use.  The warps' sums meet in shared memory; of an item that several CTAs share each leaves a piece in
+// the workspace, and the CTA that finds the others there adds them in order of the CTAs.  Nothing waits for another CTA.
 //
 // Arithmetic.  S^T = K Q^T and O^T = V^T P^T by mma.sync m16n8k16: tokens, then dims, fill the 16 rows and up to eight
 // columns of a group the 8 columns, where Q K^T would leave 12 of 16 rows empty.  (tcgen05 wants 64 or 128 rows of one

@@ -1,7 +1,7 @@
 // The next token of each row of logits: temperature, top-k, top-p and min-p, from given uniform numbers (tetra_sample).
 //
-// A cluster of eight CTAs takes a row.  Each CTA reads an eighth of it once into shared memory; everything after that
-// happens there and in the cluster's distributed shared memory.
+// A cluster of eight CTAs takes a row, or one CTA a short one.  Each CTA reads an eighth of it once into shared memory; everything after
+// that happens there and in the cluster's distributed shared memory.
 //   * Weights are fixed-point numbers (units of 2^-44 of the largest), so sums are exact in whatever order, and what
 //     is found by a histogram here, by counting there and by a scan at the end agrees to the last bit.
 //   * The three filters all keep a prefix of the order (logit down, index up), so they come to one cut: the last entry
@@ -25,12 +25,12 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kSmpCtas = 8, kSmpMaxWarps = 32;
+constexpr int kSmpMostCtas = 8, kSmpMaxWarps = 32;
 constexpr int kSmpBins = 1024;
 constexpr int kSmpCounted = kSmpBins / 4;                       // bins of masses whose entries are counted too: few are so near
 constexpr int kSmpList = 2048;                                  // entries that one CTA takes
-constexpr int kSmpRegion = kSmpList / kSmpCtas;                // ... an equal share of each
 constexpr int kSmpFew = 256;                                    // ... and compares each with each
+constexpr int kSmpAlone = 8192, kSmpAloneMany = 32768;           // logits that one CTA takes; of more rows than clusters run at once
 constexpr int kSmpBits = 44;                                    // a weight of 1 is 2^44
 
 static_assert(TETRA_SAMPLE_MAX_VOCAB <= 1 << 19, "sums of weights stay below 2^63");
@@ -46,7 +46,7 @@ struct alignas(16) SmpShared {
     uint32_t ahead_of[kSmpFew];
     double powers[64];                    // 2^(44 + j / 64)
     uint32_t count[kSmpBins], lo[kSmpBins], hi[kSmpBins];  // of the bins: entries, mass in two words
-    Tally slots[2][kSmpCtas];             // what the CTAs tell each other
+    Tally slots[2][kSmpMostCtas];           // what the CTAs tell each other
     Tally warp[kSmpMaxWarps], whole;
     uint64_t bin, ahead, need, entries;   // a crossing: its bin, the sum before it, what is needed, entries up to its end
     uint64_t cut;
@@ -106,10 +106,19 @@ struct Settings {
 };
 
 // What a CTA of so many threads does.
-template <int kSmpThreads>
+template <int kSmpThreads, int kSmpCtas>
 struct Sampler {
 
 static constexpr int kSmpWarps = kSmpThreads / 32;
+static constexpr int kSmpRegion = kSmpList / kSmpCtas;  // entries of a CTA, in equal shares
+
+// The cluster, which may be a CTA alone.
+static __device__ __forceinline__ void sync() {
+    if (kSmpCtas == 1) __syncthreads();
+    else cg::this_cluster().sync();
+}
+template <typename P>
+static __device__ __forceinline__ P* of(P* mine, int rank) { return kSmpCtas == 1 ? mine : cg::this_cluster().map_shared_rank(mine, rank); }
 
 // ... over the CTA's threads up to this one; `total` is the CTA's.  The warps' sums are added by one warp: each thread adding them
 // for itself takes more cycles than all the rest.
@@ -180,15 +189,14 @@ struct Row {
     const float* x;   // this CTA's part, minus infinity up to a multiple of four
     int count;
     uint32_t index;   // of its first token
-    cg::cluster_group cluster;
     int rank, turn;
 
     // Every CTA's value for every CTA, in the order of their ranks.  The first warp's lanes bring the CTA's.
     __device__ __forceinline__ const Tally* tell(Tally mine) {
         Tally* slots = sm.slots[turn & 1];
         ++turn;
-        if (threadIdx.x < kSmpCtas) cluster.map_shared_rank(slots, threadIdx.x)[rank] = mine;
-        cluster.sync();
+        if (threadIdx.x < kSmpCtas) of(slots, threadIdx.x)[rank] = mine;
+        sync();
         return slots;
     }
     __device__ __forceinline__ uint64_t entry(int i, float v) const { return uint64_t(key_of(v)) << 32 | uint32_t(~(index + uint32_t(i))); }
@@ -248,7 +256,7 @@ static __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
     SmpShared& sm = row.sm;
     __syncthreads();
     if (row.rank != 0) {
-        SmpShared* first = row.cluster.map_shared_rank(&sm, 0);
+        SmpShared* first = of(&sm, 0);
 #pragma unroll
         for (int i = 0; i < kSmpBins / kSmpThreads; ++i) {
             const int b = threadIdx.x + i * kSmpThreads;
@@ -258,7 +266,7 @@ static __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
             if (MASS && (sm.lo[b] | sm.hi[b])) add_mass(first->lo + b, first->hi + b, (uint64_t(sm.hi[b]) << 32) + sm.lo[b]);
         }
     }
-    row.cluster.sync();
+    sync();
     if (row.rank == 0) {
         constexpr int PER = kSmpBins / kSmpThreads;
         Tally own[PER], sum{0, 0}, total;
@@ -280,7 +288,7 @@ static __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
             const bool all = !MASS && need >= whole && threadIdx.x == kSmpThreads - 1 && i == PER - 1;
             if (all || ((MASS || need < whole) && a < need && need <= b))
                 for (int r = 0; r < kSmpCtas; ++r) {
-                    SmpShared* other = row.cluster.map_shared_rank(&sm, r);
+                    SmpShared* other = of(&sm, r);
                     other->bin = all ? kSmpBins : uint64_t(threadIdx.x * PER + i);
                     other->ahead = a;
                     other->need = need;
@@ -288,7 +296,7 @@ static __device__ __forceinline__ void find_bin(Row& row, uint64_t k, float p) {
                 }
         }
     }
-    row.cluster.sync();
+    sync();
 }
 
 // Entries of the bins [low, high] that are not below `cut`: how many there are in the cluster, and all of them in the list of
@@ -314,10 +322,10 @@ static __device__ __forceinline__ uint32_t gather(Row& row, const Bins& bins, ui
     if (threadIdx.x == 0) sm.listed = 0;
     if (total <= kSmpList) {
         if (row.rank != 0) {
-            uint64_t* list = row.cluster.map_shared_rank(sm.list, 0) + before;
+            uint64_t* list = of(sm.list, 0) + before;
             for (uint32_t i = threadIdx.x; i < mine; i += kSmpThreads) list[i] = sm.list[i];
         }
-        row.cluster.sync();
+        sync();
     }
     return total;
 }
@@ -418,9 +426,9 @@ static __device__ __forceinline__ uint64_t find_cut(Row& row, const Bins& bins, 
     if (entries <= kSmpList) {
         if (row.rank == 0) {
             cut_list<MASS>(sm, bins, weigh, entries, float(bin), float(kSmpBins), ahead, need, &sm.cut);
-            if (threadIdx.x < kSmpCtas) *row.cluster.map_shared_rank(&sm.cut, threadIdx.x) = sm.cut;
+            if (threadIdx.x < kSmpCtas) *of(&sm.cut, threadIdx.x) = sm.cut;
         }
-        row.cluster.sync();
+        sync();
         // What is read here is written again behind a barrier of the cluster that follows.
         return sm.cut;
     }
@@ -553,7 +561,7 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
     static_assert(sizeof(SmpShared) % 16 == 0, "the part lies behind it");
     const int r = blockIdx.x / kSmpCtas, rank = blockIdx.x % kSmpCtas, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int begin = min(part * rank, p.vocab), count = min(part, p.vocab - begin);
-    Row row{sm, held, count, uint32_t(begin), cg::this_cluster(), rank, 0};
+    Row row{sm, held, count, uint32_t(begin), rank, 0};
     if (threadIdx.x == 0) sm.listed = 0;
     if (threadIdx.x < 64) sm.powers[threadIdx.x] = exp2(kSmpBits + threadIdx.x / 64.);
     for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = sm.lo[i] = sm.hi[i] = 0;
@@ -636,7 +644,7 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
 
     // Few of many: each CTA sends what may be among its own first k to the first CTA, and that is all they tell each other.  The
     // bin that holds the k-th of its threads' largest logits is not before that of the k-th of its part, and hardly behind it.
-    if (T_row > 0.f && !one && k_row > 0 && k_row <= kSmpRegion / 2) {
+    if (T_row > 0.f && !one && k_row > 0 && k_row <= kSmpFew / 2) {
         if (threadIdx.x == 0) sm.whole = first;
         __syncthreads();
         const uint64_t own_best = sm.whole.mass;
@@ -649,7 +657,7 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
         __syncthreads();
         // Below k threads' largest there is nothing to find; where there are not so many, all that have mass are sent.
         const float least_sent = sm.sub < kSmpBins ? value_of(sm.least_key) : fmaxf(own_top - bins.range, -FLT_MAX);
-        uint64_t* list = row.cluster.map_shared_rank(sm.list, 0) + rank * kSmpRegion;
+        uint64_t* list = of(sm.list, 0) + rank * kSmpRegion;
         row.each([&](int i, float v) {
             if (v >= least_sent) {
                 const uint32_t at = atomicAdd(&sm.listed, 1u);
@@ -661,7 +669,7 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
         const bool fits = __all_sync(0xFFFFFFFFu, uint32_t(all[lane % kSmpCtas].count) <= kSmpRegion);
         if (fits) {
             // A quarter of the threads is enough, and fewer warps meet sooner at a barrier.
-            if (rank == 0 && threadIdx.x < kSmpFew) Sampler<kSmpFew>::finish_parts(sm, all, by, T_row, set, token, prob);
+            if (rank == 0 && threadIdx.x < kSmpFew) Sampler<kSmpFew, kSmpCtas>::finish_parts(sm, all, by, T_row, set, token, prob);
             return;
         }
         for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = 0;
@@ -705,14 +713,14 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
         }
         if (sm.entries <= kSmpFew && (top_k || sm.bin < kSmpCounted)) {
             const uint32_t n = gather(row, bins, 0, min(uint32_t(sm.bin), uint32_t(kSmpBins - 1)), 0);
-            if (rank == 0 && threadIdx.x < kSmpFew) Sampler<kSmpFew>::finish(sm, weigh, n, set, top_k ? 0 : sm.need, token, prob);
+            if (rank == 0 && threadIdx.x < kSmpFew) Sampler<kSmpFew, kSmpCtas>::finish(sm, weigh, n, set, top_k ? 0 : sm.need, token, prob);
             return;
         }
         if (top_k) {
             if (sm.bin < kSmpBins) cut = find_cut<false>(row, bins, weigh, 0);
             if (nucleus) {  // again, of masses and of what is left
                 for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = sm.lo[i] = sm.hi[i] = 0;
-                row.cluster.sync();
+                sync();
                 row.each([&](int i, float v) {
                     if (row.entry(i, v) >= cut) add(v);
                 });
@@ -808,9 +816,9 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
 
 };  // Sampler
 
-template <typename T, int THREADS>
-__cluster_dims__(kSmpCtas, 1, 1) __global__ void __launch_bounds__(THREADS) k_sample(tetra_sample_rows p, int part) {
-    Sampler<THREADS>::template run<T>(p, part);
+template <typename T, int THREADS, int CTAS>
+__cluster_dims__(CTAS, 1, 1) __global__ void __launch_bounds__(THREADS) k_sample(tetra_sample_rows p, int part) {
+    Sampler<THREADS, CTAS>::template run<T>(p, part);
 }
 
 }  // namespace
@@ -831,16 +839,20 @@ int tetra_sample(const tetra_sample_rows* p, void* stream) {
     if (off(p->logits, p->half_type ? 2 : 4) || off(p->u, 4) || off(p->temperature, 4) || off(p->top_k, 4) || off(p->top_p, 4) || off(p->min_p, 4) ||
         off(p->tokens, 4) || off(p->prob, 4))
         return TETRA_ERR_ALIGN;
-    const int part = ((p->vocab + kSmpCtas - 1) / kSmpCtas + 7) / 8 * 8;
-    const size_t smem = sizeof(SmpShared) + 4 * size_t(part);
-    constexpr size_t most = sizeof(SmpShared) + 4 * (size_t(TETRA_SAMPLE_MAX_VOCAB) / kSmpCtas);
-    static_assert(most <= 232448, "a CTA's shared memory");
     int sms = 0;
     if (device_sms(&sms) != cudaSuccess) return TETRA_ERR_CUDA;
+    // A barrier of a cluster takes ten times as long as a CTA's: a short row is one CTA's.  Measured, a cluster against one CTA,
+    // us for top-k 50 with top-p 0.9 / for top-p alone / for neither: 1 row of 8000 9.0 and 6.4 / 8.5 and 8.4 / 6.6 and
+    // 8.0, of 16000 9.0 and 7.2 / 8.5 and 10.8 / 6.7 and 11.2; 64 rows of 32000 19 and 9 / 30 and 29 / 19 and 20.
+    const int ctas = p->vocab <= (p->rows * kSmpMostCtas > 2 * sms ? kSmpAloneMany : kSmpAlone) ? 1 : kSmpMostCtas;
+    const int part = ((p->vocab + ctas - 1) / ctas + 7) / 8 * 8;
+    const size_t smem = sizeof(SmpShared) + 4 * size_t(part);
+    constexpr size_t most = sizeof(SmpShared) + 4 * (size_t(TETRA_SAMPLE_MAX_VOCAB) / kSmpMostCtas);
+    static_assert(most <= 232448, "a CTA's shared memory");
     static PerDeviceOnce once;
     const cudaError_t e = once.run([] {
         cudaError_t worst = cudaSuccess;
-        for (auto kernel : {k_sample<float, 512>, k_sample<float, 1024>, k_sample<__half, 512>, k_sample<__half, 1024>}) {
+        for (auto kernel : {k_sample<float, 512, 8>, k_sample<float, 1024, 8>, k_sample<float, 1024, 1>, k_sample<__half, 512, 8>, k_sample<__half, 1024, 8>, k_sample<__half, 1024, 1>}) {
             const cudaError_t got = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
             if (got != cudaSuccess) worst = got;
         }
@@ -848,12 +860,13 @@ int tetra_sample(const tetra_sample_rows* p, void* stream) {
     });
     if (e != cudaSuccess) return TETRA_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int grid = p->rows * kSmpCtas;
+    const int grid = p->rows * ctas;
     // A CTA on an SM of its own wants more warps to hide its latencies; where there are more clusters than that, two CTAs share an
     // SM (a seventh of the SMs stay empty: clusters do not cross the boundaries of their groups).
-    const bool alone = grid <= sms - sms / 7;
-    auto kernel = p->half_type ? alone ? k_sample<__half, 1024> : k_sample<__half, 512> : alone ? k_sample<float, 1024> : k_sample<float, 512>;
-    return launch_pdl(kernel, grid, alone ? 1024 : 512, smem, s, *p, part) == cudaSuccess ? TETRA_OK : TETRA_ERR_CUDA;
+    const bool wide = ctas == 1 || grid <= sms - sms / 7;
+    auto kernel = p->half_type ? (ctas == 1 ? k_sample<__half, 1024, 1> : wide ? k_sample<__half, 1024, 8> : k_sample<__half, 512, 8>)
+                               : (ctas == 1 ? k_sample<float, 1024, 1> : wide ? k_sample<float, 1024, 8> : k_sample<float, 512, 8>);
+    return launch_pdl(kernel, grid, wide ? 1024 : 512, smem, s, *p, part) == cudaSuccess ? TETRA_OK : TETRA_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -64,6 +64,15 @@ def test_rows_with_settings_of_their_own(tt):
           np.where(rng.random(n) < 0.3, 1.0, rng.random(n)), np.where(rng.random(n) < 0.5, 0, 0.1 * rng.random(n)))
 
 
+@pytest.mark.parametrize("rows,vocab", [(2, 8191), (2, 8192), (2, 8193), (40, 32767), (40, 32768), (40, 32769), (90, 8200)])
+def test_where_one_cta_takes_a_row(tt, rows, vocab):
+    rng = np.random.default_rng(vocab)
+    x = head_logits(rng, rows, vocab)
+    for k, p, m in ((40, 0.9, None), (None, 0.9, None), (None, None, 0.001), (700, 0.97, None)):
+        check(tt, x, rng.random(rows), 1.1, k, p, m)
+    check(tt, np.zeros((rows, vocab), np.float32), rng.random(rows), 1.0, vocab // 2, 0.3)
+
+
 def test_largest_vocabulary(tt):
     rng = np.random.default_rng(2)
     check(tt, head_logits(rng, 2, 393216), rng.random(2), 1.0, None, 0.9)
