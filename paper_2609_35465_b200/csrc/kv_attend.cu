@@ -630,9 +630,19 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
 #pragma unroll
                     for (int m = 4; m <= 16; m <<= 1) sum[nt][k] += __shfl_xor_sync(0xFFFFFFFFu, sum[nt][k], m);
             }
-            if (tiny) {
+            if (tiny) {  // all of a column's dims that the lane has, four at a time
 #pragma unroll
-                for (int f = 0; f < FRAGS; ++f) store(f, o[f], sum[f / (D / 16)][0], sum[f / (D / 16)][1]);
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t col = sg.col0 + 2 * t + k, row = quotient(col, p.group), h = col - row * p.group;
+                    const float s = sum[0][k], by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
+                    if (int(col) >= sg.cols) continue;
+                    __half* out = p.out + (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D + 4 * g;
+#pragma unroll
+                    for (int j = 0; j < CHUNKS; ++j) {
+                        const __half2 lo = __floats2half2_rn(o[2 * j][k] * by, o[2 * j][k + 2] * by), hi = __floats2half2_rn(o[2 * j + 1][k] * by, o[2 * j + 1][k + 2] * by);
+                        *reinterpret_cast<uint2*>(out + 32 * j) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+                    }
+                }
                 break;  // count is one
             }
 #pragma unroll
