@@ -216,6 +216,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + C::RING + C::MERGE + C::QBYTES); // [seqs + 1]
     __shared__ Seg segs[kAttSegs];
     __shared__ int nsegs, cursor_seq;
+    __shared__ int64_t places[2][8 * NT];  // of an item's columns in the output, or -1; the next item's apart
     __shared__ uint32_t cursor_unit, is_last, the_share, are_few, are_tiny, warp_sums[4][kAttWarps];
 
     // (What all lanes of a warp have alike is taken from lane 0 here and below: branches on it need no reconvergence.)
@@ -489,6 +490,10 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     if (int(threadIdx.x) + e * kAttThreads < NT * CHUNKS * 32) reinterpret_cast<uint4*>(qs)[threadIdx.x + e * kAttThreads] = v[e];
                 __syncthreads();
             }
+            if (!tiny && threadIdx.x < 8 * NT) {  // read behind the merge's barrier
+                const uint32_t col = sg.col0 + threadIdx.x, row = quotient(col, p.group), h = col - row * p.group;
+                places[i & 1][threadIdx.x] = int(col) < sg.cols ? (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D : -1;
+            }
             // Last position of the lane's columns (2 t, 2 t + 1 of each eight), and of the item's first.
             int sees[NT][2];
 #pragma unroll
@@ -606,10 +611,9 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                 const int nt = f / (D / 16), m = f % (D / 16), d = m / 2 * 32 + 4 * g + (m & 1) * 2;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const uint32_t col = sg.col0 + nt * 8 + 2 * t + k, row = quotient(col, p.group), h = col - row * p.group;
+                    const int64_t at = places[i & 1][nt * 8 + 2 * t + k];
                     const float s = k ? s_odd : s_even, by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
-                    if (int(col) < sg.cols)
-                        *reinterpret_cast<__half2*>(p.out + (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D + d) = __floats2half2_rn(v[k] * by, v[k + 2] * by);
+                    if (at >= 0) *reinterpret_cast<__half2*>(p.out + at + d) = __floats2half2_rn(v[k] * by, v[k + 2] * by);
                 }
             };
 
