@@ -491,16 +491,23 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                 __syncthreads();
             }
             if (!tiny && threadIdx.x < 8 * NT) {  // read behind the merge's barrier
-                const uint32_t col = sg.col0 + threadIdx.x, row = quotient(col, p.group), h = col - row * p.group;
-                places[i & 1][threadIdx.x] = int(col) < sg.cols ? (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D : -1;
+                const uint32_t col = sg.col0 + threadIdx.x;
+                int64_t at = -1;
+                if (int(col) < sg.cols) {
+                    const uint32_t row = quotient(col, p.group), h = col - row * p.group;
+                    at = (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D;
+                }
+                places[i & 1][threadIdx.x] = at;
             }
             // Last position of the lane's columns (2 t, 2 t + 1 of each eight), and of the item's first.
             int sees[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    sees[nt][k] = int(min(int64_t(INT32_MAX), int64_t(sg.before) + quotient(sg.col0 + nt * 8 + 2 * t + k, p.group)));
+                for (int k = 0; k < 2; ++k) {
+                    const int col = sg.col0 + nt * 8 + 2 * t + k;
+                    sees[nt][k] = int(min(int64_t(INT32_MAX), int64_t(sg.before) + (col < sg.cols ? quotient(col, p.group) : 0u)));
+                }
             const int all_see = int(min(int64_t(INT32_MAX), int64_t(sg.before) + quotient(sg.col0, p.group)));
 
             float o[FRAGS][4], ref[NT][2], sum[NT][2];
