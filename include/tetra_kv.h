@@ -27,8 +27,8 @@
  * a sequence whose range is not 0 <= row_start[s] <= row_start[s+1] <= rows counts as one without rows.  A position below zero (lengths
  * below zero: a slot without a sequence), a position at or behind width * page_tokens, and one whose page number is
  * not in [0, pages) has no place: nothing is stored there, nothing is read from there, and it has no part in an
- * attention.  None of that is an error the host can see without a copy.  Two sequences may share pages for reading;
- * a block that rows are appended to must belong to one sequence.
+ * attention.  None of that is an error the host can see without a copy.  Sequences may share pages for reading, and a
+ * page may stand in a sequence twice; a block that rows are appended to must stand at one place of one sequence.
  */
 #ifndef TETRA_KV_H
 #define TETRA_KV_H
@@ -99,7 +99,8 @@ size_t tetra_kv_workspace_bytes(int head_dim);
 
 /* out[r][n] = sum_p softmax_p(scale * q[r][n] . k[p][n / (q_heads / kv_heads)]) v[p][...] over the positions
  * p <= lengths[s] + i that have a place, for row r = row_start[s] + i; zero for a row that has none.  The rows' own
- * keys and values are in the cache already (tetra_kv_append with the same row_start and lengths).
+ * keys and values are in the cache already (tetra_kv_append with the same row_start and lengths).  out may be q, where
+ * its rows are contiguous.
  * q: float16, rows q_stride elements apart, 16-byte aligned, q_stride a multiple of 8; out: float16
  * [rows][q_heads][head_dim], 16-byte aligned; q_heads a multiple of kv_heads; seqs * rows * q_heads up to 2^32.  One launch.  Products are of float16
  * values that are exact but for the weights, which are rounded to float16 next to a running maximum of weight times

@@ -312,6 +312,26 @@ def test_attend_at_every_way_to_cut(tt, seqs, H, long, short):
     attend_check(tt, Step(37 + seqs, 64, H, 64, [long - 3 * i % 17 if i % 2 else short for i in range(seqs)], [1] * seqs), 2 * H)
 
 
+@pytest.mark.parametrize("D,H,heads,seqs,rows", [(64, 8, 64, 700, 4), (256, 4, 48, 200, 3), (128, 6, 60, 300, 2)])
+def test_attend_many_chunks(tt, D, H, heads, seqs, rows):
+    """More parts of items to a CTA than it looks up at a time."""
+    attend_check(tt, Step(38 + D, D, H, 16, [i * 7 % 23 for i in range(seqs)], [rows - (i % 11 == 0) for i in range(seqs)], spare=2), heads)
+
+
+def test_a_long_prompt_in_one_call(tt):
+    """Far more rows of a sequence than a product takes: slow, and right."""
+    attend_check(tt, Step(39, 64, 2, 64, [100, 3], [700, 1]), 6)
+
+
+def test_attend_in_place(tt):
+    """The output may lie where the queries were: a column is read before it is written."""
+    st = Step(43, 128, 2, 32, [3000, 5, 400], [1, 2, 16])
+    q = st.rng.standard_normal((19, 8, 128)).astype(np.float16)
+    ws, d = tt.tetra_kv_workspace(128), dev(q)
+    want = tt.tetra_kv_attend(d, *st.args(), torch.empty_like(d), ws)
+    assert torch.equal(tt.tetra_kv_attend(d, *st.args(), d, ws), want)
+
+
 def test_attend_rows_that_see_nothing(tt):
     st = Step(28, 128, 2, 16, [-1, -5, 20, 7, -2], [1, 3, 1, 1, 5], width=2)
     st.table[2] = [-1, 10 ** 6]

@@ -115,3 +115,53 @@ def test_a_captured_decode_loop(tt):
     assert torch.equal(torch.stack(seen[0]), torch.stack(seen[1]))
     assert torch.equal(eager.cache, graphed.cache) and torch.equal(eager.prob, graphed.prob)
     assert not graphed.ws[:4608].any()
+
+
+def test_first_calls_of_several_threads(tmp_path):
+    """Four host threads, each with a stream and a workspace of its own, make the process's first calls at once."""
+    import subprocess
+    import sys
+    program = tmp_path / "first.py"
+    program.write_text("""
+import threading
+import torch
+from paper_2609_35465_b200 import tetra
+tetra._native()
+torch.zeros(1, device="cuda")
+gate, got, failed = threading.Barrier(4), [None] * 4, []
+
+def work(i):
+    try:
+        torch.manual_seed(7)
+        g = torch.Generator("cuda").manual_seed(7)
+        with torch.cuda.stream(torch.cuda.Stream()):
+            whole = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+            where = (tetra.tetra_kv_cache(8, 64, 2, 128), whole([[3, 1, 6, 0]]), whole([0, 250]), whole([0]))
+            x = torch.randn((250, 12, 128), device="cuda", generator=g)
+            q, out = torch.empty((2, 250, 8, 128), dtype=torch.float16, device="cuda")
+            ws, logits, u, tokens = tetra.tetra_kv_workspace(128), torch.randn((5, 20000), device="cuda", generator=g), torch.rand(5, device="cuda", generator=g), whole([0] * 5)
+            torch.cuda.current_stream().synchronize()
+            gate.wait()
+            tetra.tetra_kv_append(x[:, :8], x[:, 8:10], x[:, 10:], *where, q)
+            tetra.tetra_kv_attend(q, *where, out, ws)
+            tetra.tetra_sample(logits, u, tokens)
+            torch.cuda.current_stream().synchronize()
+            got[i] = out.cpu(), tokens.cpu()
+    except Exception as e:
+        failed.append(repr(e))
+        gate.abort()
+
+threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+for t in threads:
+    t.start()
+for t in threads:
+    t.join()
+assert not failed, failed
+for o, t in got[1:]:
+    assert torch.equal(o, got[0][0]) and torch.equal(t, got[0][1])
+print("equal")
+""")
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, str(program)], cwd=root, env=dict(os.environ, PYTHONPATH=root), capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "equal" in run.stdout, run.stdout + run.stderr
