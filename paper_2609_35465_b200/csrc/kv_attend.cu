@@ -178,13 +178,13 @@ __device__ __forceinline__ uint32_t tried_share(uint32_t G, uint32_t items, uint
 // about five units (16 sequences of 2048: 19.4 us so, 22.5 us with even ranges of 7 units instead of 8).
 __device__ __forceinline__ bool worth_it(uint32_t share, uint32_t even) { return share <= even + even / 8 + 5; }
 
-// Whether a warp for each item is faster than ranges of units, items being of so many blocks at most.  In hundreds of cycles: a part
-// of an item takes a CTA 45 and 22 for each of its units, an item a warp 25 and 13 for each block.  Measured, 8 heads, ranges
-// against warps: 64 sequences of 3 tokens 9.3 and 7.9 us, of 100 11.2 and 11.3, of 300 15.9 and 19.4; 500 of 3 tokens 46
-// and 17 us, of 700 138 and 126.
+// Whether a warp for each item is faster than parts or ranges of units, items being of so many blocks at most.  In hundreds of
+// cycles: a part of an item takes a CTA 45 and 22 for each of its units, an item a warp 5 and 13 for each block.  Measured, 8
+// heads, without against with: 40 sequences of 3 tokens 8.9 and 5.3 us, of 250 13.9 and 13.1, of 500 18.2 and 23.4; 128 of 700 41.6
+// and 36.5; 500 of 3 tokens 42 and 12 us, of 700 133 and 120.
 __device__ __forceinline__ bool short_items(uint32_t G, uint32_t items, uint32_t blocks) {
     const uint32_t rounds = (items + kAttWarps * G - 1) / (kAttWarps * G), parts = (items + G - 1) / G;
-    return blocks < 64 && rounds * (25 + 13 * blocks) < parts * (45 + 22 * ((blocks + kAttWarps - 1) / kAttWarps));
+    return blocks < 64 && rounds * (5 + 13 * blocks) < parts * (45 + 22 * ((blocks + kAttWarps - 1) / kAttWarps));
 }
 
 template <int N>
