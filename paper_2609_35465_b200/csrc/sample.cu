@@ -56,6 +56,7 @@ struct alignas(16) SmpShared {
 // Logits are compared as integers in the order of the floats; NaN is minus infinity, plus infinity the largest float32, zeros
 // (and what is below 2^-126) are equal.
 __device__ __forceinline__ float clean(float x) { return __fadd_rn(fminf(fmaxf(x, -INFINITY), FLT_MAX), 0.f); }
+__device__ __forceinline__ float distance_up(float a, float b) { return __fsub_ru(a, b); }
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t b = __float_as_uint(x);
     return b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
@@ -176,7 +177,8 @@ static __device__ __forceinline__ float reach_of(float T) { return fminf(31.25f 
 // Distance bins: logit -> bin, the largest in bin 0; kSmpBins for one without mass.
 struct Bins {
     float top, range, by;
-    __device__ __forceinline__ Bins(float top_, float least, float T) : top(top_), range(fminf(top_ - least, reach_of(T))) {
+    // Rounded up, so that neither `least` nor top - range leaves the least logit out.
+    __device__ __forceinline__ Bins(float top_, float least, float T) : top(top_), range(fminf(distance_up(top_, least), reach_of(T))) {
         by = range > 1e-30f ? float(kSmpBins) / range : 0.f;
     }
     __device__ __forceinline__ bool has(float x) const { return top - x <= range; }

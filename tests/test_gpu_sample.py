@@ -115,6 +115,20 @@ def test_outliers_and_masks(tt):
     check(tt, x, [0.3, 0.7], 1e38, 10, 0.9)
 
 
+@pytest.mark.parametrize("vocab,last", [(40, 39), (9001, 9000), (9001, 39), (151936, 151935), (151936, 39)])
+def test_fewer_tokens_than_top_k(tt, vocab, last):
+    """Two or three logits above minus infinity, of any fractions: the least, whose distance from the largest is not a float32,
+    has its mass too."""
+    rng = np.random.default_rng(5)
+    n = 24
+    x = np.full((n, vocab), -np.inf, np.float32)
+    x[:, 3] = 8 + 8 * rng.random(n)
+    x[:, last] = rng.random(n)
+    x[::2, 20] = 4 + rng.random(n // 2)
+    check(tt, x, np.full(n, 0.999), 8.0, 30)
+    check(tt, x, np.full(n, 0.999), 8.0, 30, None, 0.01)
+
+
 def test_flat_distributions(tt):
     """High temperatures and small logits: everything lies within a few bins of the largest."""
     rng = np.random.default_rng(5)
