@@ -118,6 +118,14 @@ static __device__ __forceinline__ void sync() {
     if (kSmpCtas == 1) __syncthreads();
     else cg::this_cluster().sync();
 }
+// Nothing may be written to a CTA that has not begun: each tells so at its first instruction, and before the first such
+// write waits for the others' word, which is long there by then.
+static __device__ __forceinline__ void begun() {
+    if (kSmpCtas > 1) cg::this_cluster().barrier_arrive();
+}
+static __device__ __forceinline__ void all_begun() {
+    if (kSmpCtas > 1) cg::this_cluster().barrier_wait();
+}
 template <typename P>
 static __device__ __forceinline__ P* of(P* mine, int rank) { return kSmpCtas == 1 ? mine : cg::this_cluster().map_shared_rank(mine, rank); }
 
@@ -564,6 +572,7 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
     const int r = blockIdx.x / kSmpCtas, rank = blockIdx.x % kSmpCtas, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int begin = min(part * rank, p.vocab), count = min(part, p.vocab - begin);
     Row row{sm, held, count, uint32_t(begin), rank, 0};
+    begun();
     if (threadIdx.x == 0) sm.listed = 0;
     if (threadIdx.x < 64) sm.powers[threadIdx.x] = exp2(kSmpBits + threadIdx.x / 64.);
     for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = sm.lo[i] = sm.hi[i] = 0;
@@ -640,6 +649,7 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
         if (lane < kSmpWarps) first = sm.warp[lane];
         first = extremes<32>(first);
     }
+    all_begun();
     const Settings set{k_row > 0 ? uint64_t(k_row) : ~0ull, p_row, m_row > 0.f ? uint64_t(ceil(double(m_row) * double(1ull << kSmpBits))) : 0ull, p.u[r]};
     const double by = 64. * 1.4426950408889634074 / double(T_row);
     const bool one = p_row <= 0.f || m_row > 1.f || k_row == 1;  // the first alone stays

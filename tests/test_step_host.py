@@ -182,3 +182,15 @@ def test_kernels_wait_before_they_release():
     for f, kernels in (("kv_append.cu", 2), ("kv_attend.cu", 1), ("sample.cu", 1)):
         text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, f)).read())
         assert len(re.findall(r"pdl_wait\(\);\s*pdl_release\(\);", text)) == kernels == text.count("pdl_release") == text.count("pdl_wait")
+
+
+def test_no_cta_of_a_cluster_is_written_to_before_it_has_begun():
+    """In the sampler's kernel a word is given at the start and awaited before anything that reaches another CTA."""
+    import os
+    import re
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(os.path.dirname(tbuild.__file__), "csrc", "sample.cu")).read())
+    body = text[text.index("void run(const tetra_sample_rows& p"):]
+    reaches = [m.start() for m in re.finditer(r"\bof\(|\btell\(|\bfind_bin<|\bgather\(|\bfind_cut<|\bsync\(\)", body)]
+    assert body.count(" begun();") == body.count(" all_begun();") == 1 and reaches
+    assert body.index(" begun();") < body.index("pdl_wait()") < body.index(" all_begun();") < min(reaches)
+    assert "return" not in body[:body.index(" all_begun();")]
