@@ -111,6 +111,15 @@ class Cache:
             there[pos:pos + m] = True
         return out, there
 
+    def value_scales(self, table, s, n):
+        """The scale of the values at each of the first n positions, float64 [n, heads]."""
+        out = np.zeros((max(n, 0), self.codes.shape[2]))
+        for pos in range(0, n, BLOCK):
+            at = self.place(table, s, pos)
+            if at is not None:
+                out[pos:pos + BLOCK] = self.scales[at[0], :, at[1], 1]
+        return out
+
 
 def attend(cache, q, table, starts, lengths, scale):
     """(float64 [rows, heads, D], the bound of its error, NaN for rows that belong to nobody).
@@ -126,6 +135,7 @@ def attend(cache, q, table, starts, lengths, scale):
         a, b = int(starts[s]), int(starts[s + 1])
         n = max(0, min(int(lengths[s]) + b - a, table.shape[1] * cache.P)) if b > a else 0
         kv, there = cache.tokens(table, s, n)
+        steps = cache.value_scales(table, s, n)
         for r in range(a, b):
             m = max(0, min(int(lengths[s]) + r - a + 1, n))
             use = np.flatnonzero(there[:m])
@@ -141,7 +151,7 @@ def attend(cache, q, table, starts, lengths, scale):
                 p /= p.sum(-1, keepdims=True)
                 o, mean = np.einsum("hgp,phd->hgd", p, v), np.einsum("hgp,phd->hgd", p, np.abs(v))
                 off = 2 * ((cache.D + 16) * 2.0 ** -23 * size + 2.0 ** -17)
-                most = (p * np.abs(v).max(-1).T[:, None]).max(-1)
+                most = (p * steps[use].T[:, None]).max(-1)
                 e = 2.0 ** -11 * np.abs(o) + (2.0 ** -11 + off[..., None]) * mean + len(use) * 2.0 ** -32 * 127 * most[..., None] + 2.0 ** -25
             out[r], bound[r] = o.reshape(q.shape[1:]), e.reshape(q.shape[1:])
     return out, bound
