@@ -1,6 +1,6 @@
 // The next token of each row of logits: temperature, top-k, top-p and min-p, from given uniform numbers (tetra_sample).
 //
-// A cluster of eight CTAs takes a row, or one CTA a short one.  Each CTA reads an eighth of it once into shared memory; everything after
+// A cluster of four to eight CTAs takes a row, or one CTA a short one.  Each CTA reads its part of it once into shared memory; everything after
 // that happens there and in the cluster's distributed shared memory.
 //   * Weights are fixed-point numbers (units of 2^-44 of the largest), so sums are exact in whatever order, and what
 //     is found by a histogram here, by counting there and by a scan at the end agrees to the last bit.
@@ -509,7 +509,7 @@ static __device__ __forceinline__ void finish(SmpShared& sm, const Weigh& weigh,
 // the key below which the CTA has k entries at least (so have all: the largest of these keys is a bound for all); all[c].mass
 // is the CTA's largest.
 static __device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* all, double by, float T, const Settings& set, int32_t* token, float* prob) {
-    constexpr int PER = kSmpCtas * kSmpRegion / kSmpThreads;
+    constexpr int ALL = kSmpCtas * kSmpRegion, PER = (ALL + kSmpThreads - 1) / kSmpThreads;
     const int lane = threadIdx.x & 31;
     uint64_t best = 0, entry[PER];
     uint32_t bound = 0;
@@ -528,7 +528,7 @@ static __device__ __forceinline__ void finish_parts(SmpShared& sm, const Tally* 
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const uint32_t at = threadIdx.x + i * kSmpThreads;
-        entry[i] = at % kSmpRegion < uint32_t(all[at / kSmpRegion].count) ? sm.list[at] : 0;
+        entry[i] = at < ALL && at % kSmpRegion < uint32_t(all[at / kSmpRegion].count) ? sm.list[at] : 0;
         if (entry[i] >> 32 < bound) entry[i] = 0;
         own += entry[i] != 0;
     }
@@ -688,7 +688,7 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
         if (threadIdx.x == 0) sm.listed = 0;
     }
     const Tally* all = row.tell(first);
-    first = extremes<kSmpCtas>(all[lane % kSmpCtas]);
+    first = extremes<kSmpMostCtas>(all[min(lane % kSmpMostCtas, kSmpCtas - 1)]);
     const uint64_t best = first.mass;
     const uint32_t low = uint32_t(first.count);
     const float top = value_of(uint32_t(best >> 32));
@@ -833,6 +833,50 @@ __cluster_dims__(CTAS, 1, 1) __global__ void __launch_bounds__(THREADS) k_sample
     Sampler<THREADS, CTAS>::template run<T>(p, part);
 }
 
+using SampleKernel = void (*)(tetra_sample_rows, int);
+// ctas: of a row.  wide: a CTA has its SM for itself.
+template <typename T>
+SampleKernel sample_kernel(int ctas, bool wide) {
+    switch (ctas) {
+        case 1: return k_sample<T, 1024, 1>;
+        case 4: return k_sample<T, 1024, 4>;
+        case 5: return k_sample<T, 1024, 5>;
+        case 6: return k_sample<T, 1024, 6>;
+        default: return wide ? k_sample<T, 1024, kSmpMostCtas> : k_sample<T, 512, kSmpMostCtas>;
+    }
+}
+constexpr int kSmpClusters[] = {kSmpMostCtas, 6, 5, 4};  // of seven no more run at once than of eight
+constexpr int kSmpMostBytes = 232448;  // a CTA's shared memory
+static_assert(sizeof(SmpShared) + 4 * (size_t(TETRA_SAMPLE_MAX_VOCAB) / kSmpMostCtas) <= kSmpMostBytes, "a row of the largest vocabulary fits a cluster");
+
+// How many clusters, each CTA with an SM for itself, the current device runs at once: by the number of CTAs.
+cudaError_t wide_clusters(const int** found) {
+    static int counts[64][kSmpMostCtas + 1];
+    static PerDeviceOnce once;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    e = once.run([dev] {
+        for (int c : {1, 4, 5, 6, kSmpMostCtas})
+            for (bool wide : {false, true})
+                for (SampleKernel kernel : {sample_kernel<float>(c, wide), sample_kernel<__half>(c, wide)}) {
+                    const cudaError_t got = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmpMostBytes);
+                    if (got != cudaSuccess) return got;
+                }
+        for (int c : kSmpClusters) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(unsigned(c));
+            cfg.blockDim = dim3(1024);
+            cfg.dynamicSmemBytes = kSmpMostBytes;
+            const cudaError_t got = cudaOccupancyMaxActiveClusters(&counts[dev][c], sample_kernel<float>(c, true), &cfg);
+            if (got != cudaSuccess) return got;
+        }
+        return cudaSuccess;
+    });
+    *found = e == cudaSuccess ? counts[dev] : nullptr;
+    return e;
+}
+
 }  // namespace
 }  // namespace tetra
 
@@ -856,29 +900,25 @@ int tetra_sample(const tetra_sample_rows* p, void* stream) {
     // A barrier of a cluster takes ten times as long as a CTA's: a short row is one CTA's.  Measured, a cluster against one CTA,
     // us for top-k 50 with top-p 0.9 / for top-p alone / for neither: 1 row of 8000 9.0 and 6.4 / 8.5 and 8.4 / 6.6 and
     // 8.0, of 16000 9.0 and 7.2 / 8.5 and 10.8 / 6.7 and 11.2; 64 rows of 32000 19 and 9 / 30 and 29 / 19 and 20.
-    const int ctas = p->vocab <= (p->rows * kSmpMostCtas > 2 * sms ? kSmpAloneMany : kSmpAlone) ? 1 : kSmpMostCtas;
-    const int part = ((p->vocab + ctas - 1) / ctas + 7) / 8 * 8;
-    const size_t smem = sizeof(SmpShared) + 4 * size_t(part);
-    constexpr size_t most = sizeof(SmpShared) + 4 * (size_t(TETRA_SAMPLE_MAX_VOCAB) / kSmpMostCtas);
-    static_assert(most <= 232448, "a CTA's shared memory");
-    static PerDeviceOnce once;
-    const cudaError_t e = once.run([] {
-        cudaError_t worst = cudaSuccess;
-        for (auto kernel : {k_sample<float, 512, 8>, k_sample<float, 1024, 8>, k_sample<float, 1024, 1>, k_sample<__half, 512, 8>, k_sample<__half, 1024, 8>, k_sample<__half, 1024, 1>}) {
-            const cudaError_t got = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
-            if (got != cudaSuccess) worst = got;
-        }
-        return worst;
-    });
-    if (e != cudaSuccess) return TETRA_ERR_CUDA;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int grid = p->rows * ctas;
-    // A CTA on an SM of its own wants more warps to hide its latencies; where there are more clusters than that, two CTAs share an
-    // SM (a seventh of the SMs stay empty: clusters do not cross the boundaries of their groups).
-    const bool wide = ctas == 1 || grid <= sms - sms / 7;
-    auto kernel = p->half_type ? (ctas == 1 ? k_sample<__half, 1024, 1> : wide ? k_sample<__half, 1024, 8> : k_sample<__half, 512, 8>)
-                               : (ctas == 1 ? k_sample<float, 1024, 1> : wide ? k_sample<float, 1024, 8> : k_sample<float, 512, 8>);
-    return launch_pdl(kernel, grid, wide ? 1024 : 512, smem, s, *p, part) == cudaSuccess ? TETRA_OK : TETRA_ERR_CUDA;
+    const bool alone = p->vocab <= (p->rows * kSmpMostCtas > 2 * sms ? kSmpAloneMany : kSmpAlone);
+    auto part_of = [&](int ctas) { return ((p->vocab + ctas - 1) / ctas + 7) / 8 * 8; };
+    auto bytes_of = [&](int ctas) { return sizeof(SmpShared) + 4 * size_t(part_of(ctas)); };
+    // A CTA on an SM of its own has twice the warps to hide its latencies and all of the SM's units, so of the clusters that
+    // leave each CTA its SM the largest is taken; where none does, two CTAs of clusters of eight share an SM.  Clusters do not cross the
+    // boundaries of the SMs' groups, so the device says how many run at once (15, 22, 26 and 33 of eight, six, five and four
+    // on one).  Measured, two CTAs of eight to an SM against so, 151936 logits, us for top-k 40 with top-p 0.9 / for top-p alone /
+    // for neither: 16 rows 13.2 and 11.7 / 36.7 and 32.6 / 21.5 and 17.9 (six), 24 rows 14.4 and 12.1 / 40.5 and 37.2 / 24.7
+    // and 21.6 (five), 32 rows 19.9 and 13.2 / 43.0 and 43.7 / 26.4 and 25.3 (four); 40 rows in two rounds of four 24.6 and 22.1 /
+    // 61.4 and 66.5 / 36.3 and 41.2.
+    int ctas = alone ? 1 : kSmpMostCtas;
+    bool wide = alone;
+    const int* at_once = nullptr;
+    if (wide_clusters(&at_once) != cudaSuccess) return TETRA_ERR_CUDA;
+    for (int c : kSmpClusters)
+        if (!wide && bytes_of(c) <= kSmpMostBytes && p->rows <= at_once[c]) ctas = c, wide = true;
+    auto kernel = p->half_type ? sample_kernel<__half>(ctas, wide) : sample_kernel<float>(ctas, wide);
+    return launch_pdl(kernel, p->rows * ctas, wide ? 1024 : 512, bytes_of(ctas), static_cast<cudaStream_t>(stream), *p, part_of(ctas)) == cudaSuccess
+               ? TETRA_OK : TETRA_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -73,6 +73,21 @@ def test_where_one_cta_takes_a_row(tt, rows, vocab):
     check(tt, np.zeros((rows, vocab), np.float32), rng.random(rows), 1.0, vocab // 2, 0.3)
 
 
+@pytest.mark.parametrize("rows,vocab", [(14, 33000), (16, 33000), (21, 33001), (24, 33003), (30, 33000), (33, 40000), (45, 33000), (20, 262144), (18, 350001)])
+def test_clusters_of_every_size(tt, rows, vocab):
+    """Numbers of rows for which clusters of eight, six, five, four and again eight CTAs are taken, and rows too long for the smaller ones."""
+    rng = np.random.default_rng(rows)
+    x = head_logits(rng, rows, vocab)
+    for k, p, m in ((40, 0.9, None), (128, None, 0.01), (None, 0.9, None), (None, None, 0.001), (700, 0.97, None)):
+        check(tt, x, rng.random(rows), 1.1, k, p, m)
+    few = np.full((rows, vocab), -np.inf, np.float32)
+    few[:, rng.integers(0, vocab, 40)] = 3 * rng.standard_normal((rows, 40))
+    check(tt, few, rng.random(rows), 2.0, 60, 0.95)
+    if vocab < 50000:  # more equal logits than a part's share of the list
+        check(tt, np.zeros((rows, vocab), np.float32), rng.random(rows), 1.0, 100, 0.3)
+        check(tt, np.zeros((rows, vocab), np.float32), rng.random(rows), 1.0, None, 0.3)
+
+
 def test_largest_vocabulary(tt):
     rng = np.random.default_rng(2)
     check(tt, head_logits(rng, 2, 393216), rng.random(2), 1.0, None, 0.9)
