@@ -30,6 +30,7 @@ constexpr int kSmpBins = 1024;
 constexpr int kSmpCounted = kSmpBins / 4;                       // bins of masses whose entries are counted too: few are so near
 constexpr int kSmpList = 2048;                                  // entries that one CTA takes
 constexpr int kSmpFew = 256;                                    // ... and compares each with each
+constexpr int kSmpNear = 128;                                   // ... and does so at once to find a cut: 256 such take as long as a histogram
 constexpr int kSmpAlone = 8192, kSmpAloneMany = 32768;           // logits that one CTA takes; of more rows than clusters run at once
 constexpr int kSmpBits = 44;                                    // a weight of 1 is 2^44
 
@@ -346,7 +347,7 @@ template <bool MASS>
 static __device__ __noinline__ void cut_list(SmpShared& sm, const Bins bins, const Weigh weigh, uint32_t n, float bin, float scale, uint64_t ahead, uint64_t need, uint64_t* cut) {
     constexpr int PER = kSmpBins / kSmpThreads;
     auto weight = [&](uint64_t entry) { return MASS ? weigh.any(value_of(uint32_t(entry >> 32))) : 1ull; };
-    if (n > kSmpFew) {  // a histogram of their own
+    if (n > kSmpNear) {  // a histogram of their own
         for (int i = threadIdx.x; i < kSmpBins; i += kSmpThreads) sm.count[i] = sm.lo[i] = sm.hi[i] = 0;
         if (threadIdx.x == 0) sm.few = 0;
         __syncthreads();
