@@ -775,9 +775,9 @@ static __device__ __forceinline__ void run(const tetra_sample_rows& p, int part)
                     const uint64_t w = weigh(queue[lane]);
                     sum += w >= set.floor_w ? w : 0;
                     const float rest = queue[32 + lane];
-                    __syncwarp();
-                    queue[lane] = rest;
                     queued -= 32;
+                    __syncwarp();
+                    if (lane < queued) queue[lane] = rest;  // the places from there on are the next ones', filled without a barrier in between
                 }
             }
         }
