@@ -21,6 +21,7 @@
 // largest weight TIMES SCALE of V, not the largest weight, so that a block of large values keeps no block of small ones
 // that is attended to from its bits, and 2^-32 of the largest is still seen.  The denominator sums 2^(score - m) in float32.
 // m moves only when a weight would pass 2^15: a vote per block, a reduction when it does.
+#include <cfloat>
 #include <cmath>
 
 #include "kv_common.cuh"
@@ -33,7 +34,7 @@ constexpr uint32_t kAttLeastUnits = 4;     // of a CTA: what sharing an item cos
 constexpr int kAttSegs = 32;              // parts of items that a CTA looks up at a time
 constexpr int kAttMaxCtas = 384;          // of a launch: pieces in the workspace
 constexpr int kAttBatch = 8;               // pieces that are loaded at a time
-constexpr float kNoRef = -1e30f;          // reference of a column that has seen nothing
+constexpr float kNoRef = -FLT_MAX;        // reference of a column that has seen nothing: below every finite score
 constexpr float kLeastLog = -60.f;        // log2 of the least s_V that counts: 127 * 2^-60 is zero in float16
 constexpr float kHigh = 15.f, kBase = 7.f; // a weight reaches 2^kHigh at most, a new reference puts the largest at 2^kBase
 
