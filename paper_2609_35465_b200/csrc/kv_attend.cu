@@ -529,6 +529,9 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     const float by = __uint_as_float(scales.x) * p.scale, vs = __uint_as_float(scales.y);
                     float lv = lg2(vs);
                     lv = lv < kLeastLog ? kLeastLog : lv;  // NaN stays
+                    // A score of 2^24 or more has no fractions, and what is added to it is rounded away: it is its difference from the
+                    // reference, which is exact where it matters, that is held against the room for a weight.
+                    const float room = kHigh - lv;
                     float x[NT][4], y[NT][4];  // two chains: a product waits for the one before it
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -561,7 +564,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
-                        over |= fmaxf(x[nt][0], x[nt][2]) + lv > ref[nt][0] + kHigh || fmaxf(x[nt][1], x[nt][3]) + lv > ref[nt][1] + kHigh;
+                        over |= fmaxf(x[nt][0], x[nt][2]) - ref[nt][0] > room || fmaxf(x[nt][1], x[nt][3]) - ref[nt][1] > room;
                     if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
@@ -570,7 +573,8 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                                 float top = fmaxf(x[nt][k], x[nt][k + 2]);
 #pragma unroll
                                 for (int m = 4; m <= 16; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, m));
-                                const float now = top + lv - kBase;
+                                float now = top + lv - kBase;
+                                if (top - now > room) now = top;  // a step of so large scores is more than the room there is
                                 if (now > ref[nt][k]) {
                                     const float f = ex2(ref[nt][k] - now);
                                     ref[nt][k] = now;
