@@ -102,9 +102,11 @@ size_t tetra_kv_workspace_bytes(int head_dim);
  * keys and values are in the cache already (tetra_kv_append with the same row_start and lengths).  out may be q, where
  * its rows are contiguous.
  * q: float16, rows q_stride elements apart, 16-byte aligned, q_stride a multiple of 8; out: float16
- * [rows][q_heads][head_dim], 16-byte aligned; q_heads a multiple of kv_heads; seqs * rows * q_heads up to 2^32.  One launch.  Products are of float16
- * values that are exact but for the weights, which are rounded to float16 next to a running maximum of weight times
- * scale; sums are float32.  Any number of rows a sequence is right; the kernel is made for up to 16. */
+ * [rows][q_heads][head_dim], 16-byte aligned; q_heads a multiple of kv_heads; seqs * rows * q_heads up to 2^32; scale below
+ * 2^127 in size.  One launch.  Products are of float16 values that are exact but for the weights, which are rounded to float16 next to a
+ * running maximum of weight times scale; sums are float32, scores of any size that it holds among them (scale * s_K has to be a
+ * float32 number too).  Any number of rows a sequence is right; the kernel is made for up to 16 (a step's mixture of such and of
+ * single tokens is right too, but has one kernel for all, by the average). */
 int tetra_kv_attend(const tetra_kv_cache *cache, const void *q, int64_t q_stride, void *out, int rows, int q_heads,
                     float scale, void *workspace, size_t workspace_bytes, void *stream);
 

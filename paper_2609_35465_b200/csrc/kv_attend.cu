@@ -830,7 +830,8 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const void* q, int64_t q_stride
     const int D = cache->head_dim;
     if (!q || !out || !workspace) return TETRA_ERR_NULL;
     if (q_heads < 1 || q_heads % p.c.kv_heads || q_heads > 4096 || q_stride < int64_t(q_heads) * D) return TETRA_ERR_SHAPE;
-    if (!std::isfinite(scale) || int64_t(cache->seqs) * rows * q_heads > (1ll << 32)) return TETRA_ERR_SHAPE;
+    const float scale_log2 = scale * 1.4426950408889634f;  // times log2 e
+    if (!std::isfinite(scale_log2) || int64_t(cache->seqs) * rows * q_heads > (1ll << 32)) return TETRA_ERR_SHAPE;
     if (!kv_aligned(q, 16) || q_stride % 8 || !kv_aligned(out, 16) || !kv_aligned(workspace, 256)) return TETRA_ERR_ALIGN;
     if (workspace_bytes < tetra_kv_workspace_bytes(D)) return TETRA_ERR_SIZE;
     if (rows == 0) return TETRA_OK;
@@ -839,7 +840,7 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const void* q, int64_t q_stride
     p.q = static_cast<const __half*>(q);
     p.out = static_cast<__half*>(out);
     p.q_stride = q_stride;
-    p.scale = scale * 1.4426950408889634f;
+    p.scale = scale_log2;
     p.group = q_heads / p.c.kv_heads;
     p.unit_shift = 0;
     p.arrived = static_cast<uint32_t*>(workspace);

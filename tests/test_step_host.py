@@ -96,6 +96,14 @@ def test_read_and_attend_refuse(tt):
         assert got == rc, change
 
 
+def test_attend_refuses_a_scale_that_no_score_has(tt):
+    """The kernel works in powers of two: the scale times log2(e) has to be finite as well."""
+    L, c = tt.lib(), view(tt)
+    for scale in (2.4e38, -2.4e38, float(np.finfo(np.float32).max)):
+        assert L.tetra_kv_attend(C.byref(c), 256, 512, 256, 1, 4, scale, 256, L.tetra_kv_workspace_bytes(128), None) == -2
+    assert L.tetra_kv_attend(C.byref(c), 256, 512, 256, 0, 4, 2.0 ** 127, 256, L.tetra_kv_workspace_bytes(128), None) == 0  # no rows, no launch
+
+
 def test_sample_refuses(tt):
     L = tt.lib()
     good = dict(logits=256, u=256, tokens=256, row_stride=100, rows=1, vocab=100)
