@@ -838,7 +838,8 @@ __cluster_dims__(CTAS, 1, 1) __global__ void __launch_bounds__(THREADS) k_sample
 }
 
 using SampleKernel = void (*)(tetra_sample_rows, int);
-// ctas: of a row.  wide: a CTA has its SM for itself.
+// ctas: of a row.  wide: a CTA has its SM for itself; otherwise two of 512 threads share its registers, 64 a thread either way (the
+// narrow ones spill 28 bytes).
 template <typename T>
 SampleKernel sample_kernel(int ctas, bool wide) {
     switch (ctas) {
