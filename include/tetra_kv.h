@@ -110,6 +110,29 @@ size_t tetra_kv_workspace_bytes(int head_dim);
 int tetra_kv_attend(const tetra_kv_cache *cache, const void *q, int64_t q_stride, void *out, int rows, int q_heads,
                     float scale, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Groups of sequences that begin with the same tokens (several answers to one prompt).  Group g is the sequences
+ * group_start[g] .. group_start[g+1] - 1; their first shared[g] tokens have the same pages, that is, equal entries of
+ * page_table.  group_start int32 [groups + 1], shared int32 [groups], device memory; groups up to TETRA_KV_MAX_SEQS, or none
+ * (then both may be NULL).  group_start does not decrease; a group whose range is not 0 <= a <= b <= seqs counts as empty.  Sequences
+ * may be in no group. */
+typedef struct {
+    const int32_t *group_start, *shared;
+    int32_t groups;
+} tetra_kv_groups;
+
+/* Bytes of the workspace of tetra_kv_attend_shared for so many rows, heads and groups at most (more of any take no less);
+ * 0 for what is rejected.  As with tetra_kv_attend, the caller zeroes it once, and calls that share it must not overlap. */
+size_t tetra_kv_shared_workspace_bytes(int head_dim, int rows, int q_heads, int kv_heads, int groups);
+
+/* What tetra_kv_attend gives, with the same arguments and limits, but for the rounding: tokens that a group shares are read once for
+ * all of its rows, through the page table of the first of its sequences that take part.  Whole blocks are shared, the tokens
+ * behind them are read by each sequence.  A sequence takes part where it has rows and lengths[s] is not below the shared
+ * tokens of whole blocks; the others of the group, and a group with fewer than two that do, read all of their tokens
+ * themselves.  Two launches. */
+int tetra_kv_attend_shared(const tetra_kv_cache *cache, const tetra_kv_groups *groups, const void *q, int64_t q_stride,
+                           void *out, int rows, int q_heads, float scale, void *workspace, size_t workspace_bytes,
+                           void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -49,6 +49,7 @@ struct Api {
     decltype(&tetra_kv_append) kv_append;
     decltype(&tetra_kv_read) kv_read;
     decltype(&tetra_kv_attend) kv_attend;
+    decltype(&tetra_kv_attend_shared) kv_attend_shared;
     decltype(&tetra_sample) sample;
 } api;
 PyObject* tetra_error = nullptr;  // the exception class
@@ -481,6 +482,31 @@ FASTCALL(py_kv_attend) {
     });
 }
 
+// cache, page_table, row_start, lengths, group_start, shared, q, out, scale, workspace, stream
+FASTCALL(py_kv_attend_shared) {
+    return guarded(n, 11, [&] {
+        const char* what = "tetra_kv_attend_shared";
+        const tetra_kv_cache c = kv_cache_of(a, what);
+        tetra_kv_groups g = {};
+        const int64_t groups = tensor(a[5]).dim() == 1 ? tensor(a[5]).size(0) : 0;
+        g.group_start = static_cast<const int32_t*>(shaped(a[4], at::kInt, {groups + 1}, what, "group_start"));
+        g.shared = static_cast<const int32_t*>(shaped(a[5], at::kInt, {groups}, what, "shared"));
+        g.groups = narrow(groups, what, "shared");
+        const int64_t rows = tensor(a[6]).dim() == 3 ? tensor(a[6]).size(0) : 0;
+        int64_t heads = 0, stride = 0;
+        void* q = rows_of_heads(a[6], at::kHalf, rows, c.head_dim, what, "q", heads, stride);
+        void* out = shaped(a[7], at::kHalf, {rows, heads, c.head_dim}, what, "out");
+        const int q_heads = narrow(heads, what, "q"), count = narrow(rows, what, "q");
+        const float scale = a[8] == Py_None ? float(1. / std::sqrt(double(c.head_dim))) : float(real(a[8]));
+        const at::Tensor& ws = typed(a[9], at::kByte, what, "workspace");
+        if (!ws.is_contiguous()) fail(tetra_error, "%s workspace: tensor is not contiguous", what);
+        void *wp = ws.data_ptr(), *s = stream_of(a[10]);
+        const size_t wn = size_t(ws.numel());
+        if (rows > 0) check(unlocked([&] { return api.kv_attend_shared(&c, &g, q, stride, out, count, q_heads, scale, wp, wn, s); }), what);
+        return same(a[7]);
+    });
+}
+
 // logits, u, tokens, prob, temperature, top_k, top_p, min_p, stream
 FASTCALL(py_sample) {
     return guarded(n, 9, [&] {
@@ -540,6 +566,7 @@ FASTCALL(py_setup) {
         get(api.kv_append, "tetra_kv_append");
         get(api.kv_read, "tetra_kv_read");
         get(api.kv_attend, "tetra_kv_attend");
+        get(api.kv_attend_shared, "tetra_kv_attend_shared");
         get(api.sample, "tetra_sample");
         Py_XDECREF(tetra_error);
         tetra_error = same(a[1]);
@@ -551,7 +578,8 @@ FASTCALL(py_setup) {
 PyMethodDef methods[] = {METHOD(setup),        METHOD(gemv),          METHOD(gemv_tail), METHOD(gemv_noalloc), METHOD(gemv_batched),
                          METHOD(gemv_list),    METHOD(grouped_run),   METHOD(pack_codes), METHOD(decode_packed), METHOD(encode_blocks),
                          METHOD(q4_pack),      METHOD(q4_gemv),       METHOD(q4_rows),   METHOD(q4_list_run),  METHOD(kv_append),
-                         METHOD(kv_read),      METHOD(kv_attend),     METHOD(sample),  {nullptr, nullptr, 0, nullptr}};
+                         METHOD(kv_read),      METHOD(kv_attend),     METHOD(kv_attend_shared), METHOD(sample),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of the Tetra C ABI.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

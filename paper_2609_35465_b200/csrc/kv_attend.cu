@@ -21,10 +21,13 @@
 // largest weight TIMES SCALE of V, not the largest weight, so that a block of large values keeps no block of small ones
 // that is attended to from its bits, and 2^-32 of the largest is still seen.  The denominator sums 2^(score - m) in float32.
 // m moves only when a weight would pass 2^15: a vote per block, a reduction when it does.
+//
+// SHARED: the second kernel of tetra_kv_attend_shared.  The first blocks of a sequence that shares them with others are in pieces that
+// k_kv_prefix left: here they are not read, and the pieces are added to a column's sums before it is stored.
 #include <cfloat>
 #include <cmath>
 
-#include "kv_common.cuh"
+#include "kv_shared.cuh"
 
 namespace tetra {
 namespace {
@@ -60,7 +63,7 @@ struct Seg {
     int32_t seq, head;
     int32_t row0;          // first row of the sequence
     int32_t col0, cols;    // the item's first column, and the sequence's columns
-    uint32_t r0, r1;       // blocks, of those that the item's last row sees
+    uint32_t r0, r1;       // blocks, of those that the item's last row sees (SHARED: behind the shared ones)
     int32_t first, last;   // CTAs that the item begins and ends in
     int32_t before;        // tokens before the step
 };
@@ -76,6 +79,8 @@ struct AttParams {
     // A CTA may be an item's last and the next one's first: what it keeps for either is apart (second: of the item that begins in it).
     float* pieces;         // [CTA][4][PIECE]: pieces, then groups' sums, two each
     uint32_t* arrived;     // [3][CTA]: pieces of the groups that begin in this CTA, two; groups of the item that begins in it
+    const SharedSeq* shared;      // SHARED: by sequence,
+    const float* shared_pieces;   // and what k_kv_prefix left
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -123,8 +128,9 @@ __device__ __forceinline__ uint32_t quotient(uint32_t a, uint32_t b) { return a 
 struct Work {
     int32_t row0, rows, before;
     uint32_t chunks, blocks, units;
+    uint32_t first;  // SHARED: blocks that are not read here
 };
-template <int NT>
+template <int NT, bool SHARED>
 __device__ __forceinline__ Work sequence_work(const AttParams& p, int s) {
     Work w;
     int b;
@@ -136,11 +142,16 @@ __device__ __forceinline__ Work sequence_work(const AttParams& p, int s) {
     const int64_t seen = int64_t(w.before) + w.rows;
     const uint32_t n = seen <= 0 ? 0u : uint32_t((seen + kKvBlock - 1) / kKvBlock);
     w.blocks = min(n, most);
+    w.first = 0;
+    if (SHARED) {
+        w.first = min(uint32_t(__ldcg(&p.shared[s].first)), w.blocks);
+        w.blocks -= w.first;
+    }
     w.units = max(1u, (w.blocks + (kAttWarps << p.unit_shift) - 1) / (kAttWarps << p.unit_shift));
     return w;
 }
 // The part of units [u0, u1) of an item.
-template <int NT>
+template <int NT, bool SHARED>
 __device__ __forceinline__ void set_seg(const AttParams& p, const Work& w, int s, uint32_t item, uint32_t u0, uint32_t u1, int first, int last, Seg& q) {
     q.seq = s;
     const uint32_t head = quotient(item, w.chunks);
@@ -153,9 +164,9 @@ __device__ __forceinline__ void set_seg(const AttParams& p, const Work& w, int s
     q.last = last;
     const uint32_t rows = q.col0 + 8 * NT >= q.cols ? w.rows : (q.col0 + 8 * NT - 1) / uint32_t(p.group) + 1;  // up to the item's last
     const int64_t seen = int64_t(w.before) + rows;
-    const uint32_t n = seen <= 0 ? 0u : min(w.blocks, uint32_t((seen + kKvBlock - 1) / kKvBlock));
-    q.r0 = u0 * (kAttWarps << p.unit_shift);
-    q.r1 = min(n, u1 * (kAttWarps << p.unit_shift));
+    const uint32_t n = seen <= 0 ? 0u : min(SHARED ? w.first + w.blocks : w.blocks, uint32_t((seen + kKvBlock - 1) / kKvBlock));
+    q.r0 = (SHARED ? w.first : 0u) + u0 * (kAttWarps << p.unit_shift);
+    q.r1 = min(n, (SHARED ? w.first : 0u) + u1 * (kAttWarps << p.unit_shift));
 }
 
 // Parts of an item of so many units when a CTA takes `share` at most, and units of a part.
@@ -206,7 +217,62 @@ __device__ __forceinline__ void block_sums(uint32_t (&v)[N], uint32_t (*warp_sum
     __syncthreads();
 }
 
-template <int D, int NT>
+// SHARED: adds to a column's sums (v, of `N` values from float `at` of a piece's column; reference r, denominator u) those of its pieces,
+// in order; four at a time are on the way.
+template <int N>
+__device__ __forceinline__ void add_pieces(const AttParams& p, int D, const PieceRange& range, int at, float (&v)[N], float& r, float& u) {
+    constexpr int BATCH = 4;
+    const size_t piece = size_t(pre_piece(D));
+    const float* from = p.shared_pieces + size_t(range.first) * piece + range.column * 4 + at / 4 * (4 * kPreColumns) + at % 4;
+    const float* ends = p.shared_pieces + size_t(range.first) * piece + kPreColumns * D + range.column * 2;
+#pragma unroll 1
+    for (int i = 0; i < range.count; i += BATCH) {
+        float x[BATCH][N];
+        float2 m[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const size_t to = size_t(min(i + k, range.count - 1)) * range.step * piece;
+            m[k] = __ldcg(reinterpret_cast<const float2*>(ends + to));
+            if (N == 2) {
+                const float2 y = __ldcg(reinterpret_cast<const float2*>(from + to));
+                x[k][0] = y.x, x[k][1] = y.y;
+            } else {
+                const float4 y = __ldcg(reinterpret_cast<const float4*>(from + to));
+                x[k][0] = y.x, x[k][1] = y.y, x[k][N - 2] = y.z, x[k][N - 1] = y.w;
+            }
+        }
+        float now = r;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            if (i + k >= range.count) m[k].y = 0.f;
+            if (m[k].y != 0.f) now = fmaxf(now, m[k].x);  // 0: nothing seen, and nothing written
+        }
+        const float f = ex2(r - now);
+        u *= f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] *= f;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const bool is = m[k].y != 0.f;
+            const float g = is ? ex2(m[k].x - now) : 0.f;
+            u = is ? fmaf(m[k].y, g, u) : u;
+#pragma unroll
+            for (int n = 0; n < N; ++n) v[n] = is ? fmaf(x[k][n], g, v[n]) : v[n];
+        }
+        r = now;
+    }
+}
+
+template <int D>
+__device__ __forceinline__ PieceRange range_of(const AttParams& p, const Seg& sg, uint32_t col) {
+    const uint4* at = reinterpret_cast<const uint4*>(p.shared + sg.seq);
+    const uint4 a = __ldcg(at), b = __ldcg(at + 1);
+    const SharedSeq s{int32_t(a.x), int32_t(a.y), int32_t(a.z), int32_t(a.w), int32_t(b.x), int32_t(b.y), {0, 0}};
+    if (s.first == 0) return PieceRange{0, 0, 0, 0};
+    return pieces_of<D>(s, sg.head, uint32_t(sg.row0 - s.row0) * p.group + col);
+}
+
+template <int D, int NT, bool SHARED>
 __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(AttParams p) {
     using C = AttCfg<D, NT>;
     constexpr int CHUNKS = C::CHUNKS, STAGES = C::STAGES, REC = C::REC, FRAGS = C::FRAGS, ROUND = C::ROUND;
@@ -218,6 +284,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     __shared__ Seg segs[kAttSegs];
     __shared__ int nsegs, cursor_seq;
     __shared__ int64_t places[2][8 * NT];  // of an item's columns in the output, or -1; the next item's apart
+    __shared__ PieceRange ranges[2][SHARED ? 8 * NT : 1];
     __shared__ uint32_t cursor_unit, is_last, the_share, are_few, are_tiny, warp_sums[4][kAttWarps];
 
     // (What all lanes of a warp have alike is taken from lane 0 here and below: branches on it need no reconvergence.)
@@ -241,7 +308,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     if (p.c.seqs <= 32) {
         if (warp == 0) {
             const bool is = lane < p.c.seqs;
-            Work w = is ? sequence_work<NT>(p, lane) : Work{0, 0, 0, 0, 0, 1};
+            Work w = is ? sequence_work<NT, SHARED>(p, lane) : Work{0, 0, 0, 0, 0, 1, 0};
             const uint32_t items = w.chunks * heads, all_items = __reduce_add_sync(0xFFFFFFFFu, items), all_units = __reduce_add_sync(0xFFFFFFFFu, items * w.units);
             const uint32_t even = (all_units + G - 1) / G;
             if (all_items <= G) {
@@ -278,7 +345,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                 cursor_unit = want;
                 if (few) {
                     const uint32_t local = want - at, item = quotient(local, parts), part = local - item * parts;
-                    set_seg<NT>(p, w, lane, item, part * each, (part + 1) * each, int(blockIdx.x - part), int(blockIdx.x - part + parts - 1), segs[0]);
+                    set_seg<NT, SHARED>(p, w, lane, item, part * each, (part + 1) * each, int(blockIdx.x - part), int(blockIdx.x - part + parts - 1), segs[0]);
                     nsegs = 1;
                 }
             }
@@ -295,7 +362,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
         if (threadIdx.x == 0) cursor_unit = 0;
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) {
-            const Work w = sequence_work<NT>(p, s);
+            const Work w = sequence_work<NT, SHARED>(p, s);
             total[0] += w.chunks * heads;
             total[1] += w.chunks * heads * w.units;
             if (w.chunks) longest = max(longest, w.blocks);
@@ -310,7 +377,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             for (int j = 0; j < 3; ++j) tried[j] = tried_share(G, total[0], total[1], j);
 #pragma unroll 1
             for (int s = s0; s < s1; ++s) {
-                const Work w = sequence_work<NT>(p, s);
+                const Work w = sequence_work<NT, SHARED>(p, s);
 #pragma unroll
                 for (int j = 0; j < 3; ++j) need[j] += w.chunks * heads * ((w.units + tried[j] - 1) / tried[j]);
             }
@@ -335,7 +402,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             uint32_t mine = 0;
 #pragma unroll 1
             for (int s = s0; s < s1; ++s) {
-                const Work w = sequence_work<NT>(p, s);
+                const Work w = sequence_work<NT, SHARED>(p, s);
                 if (w.chunks) mine += wanted(w);
             }
             uint32_t sum = mine;
@@ -356,7 +423,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             if (!few || (at <= want && want < at + mine)) {
 #pragma unroll 1
                 for (int s = s0; s < s1; ++s) {
-                    const Work w = sequence_work<NT>(p, s);
+                    const Work w = sequence_work<NT, SHARED>(p, s);
                     const uint32_t own = w.chunks ? wanted(w) : 0u;
                     prefix[s] = at;
                     if (at <= want && want < at + own) {
@@ -365,7 +432,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                         if (few) {
                             uint32_t each;
                             const uint32_t parts = parts_of(w.units, share, each), local = want - at, item = quotient(local, parts), part = local - item * parts;
-                            set_seg<NT>(p, w, s, item, part * each, (part + 1) * each, int(blockIdx.x - part), int(blockIdx.x - part + parts - 1), segs[0]);
+                            set_seg<NT, SHARED>(p, w, s, item, part * each, (part + 1) * each, int(blockIdx.x - part), int(blockIdx.x - part + parts - 1), segs[0]);
                             nsegs = 1;
                         }
                     }
@@ -390,9 +457,9 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                 who = __ballot_sync(0xFFFFFFFFu, at < p.c.seqs && prefix[at] <= item && item < prefix[at + 1]);
                 if (who) s += __ffs(who) - 33;
             }
-            const Work w = sequence_work<NT>(p, s);
+            const Work w = sequence_work<NT, SHARED>(p, s);
             __syncwarp();
-            if (lane == 0) set_seg<NT>(p, w, s, item - prefix[s], 0, w.units, 0, 0, segs[warp]);
+            if (lane == 0) set_seg<NT, SHARED>(p, w, s, item - prefix[s], 0, w.units, 0, 0, segs[warp]);
             __syncwarp();
         } else if (!few) {  // the next parts of items of this CTA's range
             if (threadIdx.x == 0) {
@@ -401,11 +468,11 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                 const uint32_t end = min(prefix[p.c.seqs], share * (blockIdx.x + 1));
                 while (n < kAttSegs && u < end) {
                     while (u >= prefix[s + 1]) ++s;
-                    const Work w = sequence_work<NT>(p, s);
+                    const Work w = sequence_work<NT, SHARED>(p, s);
                     uint32_t item = (u - prefix[s]) / w.units;
                     while (n < kAttSegs && u < end && u < prefix[s + 1]) {
                         const uint32_t at = prefix[s] + item * w.units, stop = min(at + w.units, end);
-                        set_seg<NT>(p, w, s, item, u - at, stop - at, int(at / share), int((at + w.units - 1) / share), segs[n++]);
+                        set_seg<NT, SHARED>(p, w, s, item, u - at, stop - at, int(at / share), int((at + w.units - 1) / share), segs[n++]);
                         u = stop;
                         ++item;
                     }
@@ -499,6 +566,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     at = (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D;
                 }
                 places[i & 1][threadIdx.x] = at;
+                if (SHARED) ranges[i & 1][threadIdx.x] = at < 0 ? PieceRange{0, 0, 0, 0} : range_of<D>(p, sg, col);
             }
             // Last position of the lane's columns (2 t, 2 t + 1 of each eight), and of the item's first.
             int sees[NT][2];
@@ -619,13 +687,18 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
             }
 
             // Two of a fragment's values belong to column 2 t (2 t + 1) and dims d, d + 1.
-            auto store = [&](int f, const float (&v)[4], float s_even, float s_odd) {
+            auto store = [&](int f, const float (&v)[4], float r_even, float r_odd, float s_even, float s_odd) {
                 const int nt = f / (D / 16), m = f % (D / 16), d = m / 2 * 32 + 4 * g + (m & 1) * 2;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int64_t at = places[i & 1][nt * 8 + 2 * t + k];
-                    const float s = k ? s_odd : s_even, by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
-                    if (at >= 0) *reinterpret_cast<__half2*>(p.out + at + d) = __floats2half2_rn(v[k] * by, v[k + 2] * by);
+                    float s = k ? s_odd : s_even, x[2] = {v[k], v[k + 2]};
+                    if (SHARED) {
+                        float r = k ? r_odd : r_even;
+                        add_pieces<2>(p, D, ranges[i & 1][nt * 8 + 2 * t + k], d, x, r, s);
+                    }
+                    const float by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
+                    if (at >= 0) *reinterpret_cast<__half2*>(p.out + at + d) = __floats2half2_rn(x[0] * by, x[1] * by);
                 }
             };
 
@@ -650,12 +723,21 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const uint32_t col = sg.col0 + 2 * t + k, row = quotient(col, p.group), h = col - row * p.group;
-                    const float s = sum[0][k], by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
+                    float s = sum[0][k], by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
                     if (int(col) >= sg.cols) continue;
                     __half* out = p.out + (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D + 4 * g;
+                    PieceRange range;
+                    if (SHARED) range = range_of<D>(p, sg, col);
 #pragma unroll
                     for (int j = 0; j < CHUNKS; ++j) {
-                        const __half2 lo = __floats2half2_rn(o[2 * j][k] * by, o[2 * j][k + 2] * by), hi = __floats2half2_rn(o[2 * j + 1][k] * by, o[2 * j + 1][k + 2] * by);
+                        float x[4] = {o[2 * j][k], o[2 * j][k + 2], o[2 * j + 1][k], o[2 * j + 1][k + 2]};
+                        if (SHARED) {
+                            float r = ref[0][k];
+                            s = sum[0][k];
+                            add_pieces<4>(p, D, range, 32 * j + 4 * g, x, r, s);
+                            by = s == 0.f ? 0.f : 1.f / s;
+                        }
+                        const __half2 lo = __floats2half2_rn(x[0] * by, x[1] * by), hi = __floats2half2_rn(x[2] * by, x[3] * by);
                         *reinterpret_cast<uint2*>(out + 32 * j) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
                     }
                 }
@@ -692,7 +774,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                             v[2] = fmaf(x.z, f0, v[2]);
                             v[3] = fmaf(x.w, f1, v[3]);
                         }
-                        if (shared_by == 1) store(f, v, u0, u1);
+                        if (shared_by == 1) store(f, v, r0, r1, u0, u1);
                         else leave(piece_at(me, me == sg.first), f, v, r0, r1, u0, u1);
                     }
                 }
@@ -767,7 +849,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     for (int i = 0; i < TURNS; ++i) {
                         const int f = warp + i * kAttWarps;
                         if (f >= FRAGS) break;
-                        if (final) store(f, v[i], u0[i], u1[i]);
+                        if (final) store(f, v[i], r0[i], r1[i], u0[i], u1[i]);
                         else leave(piece_at(begin, 2 + (begin == sg.first)), f, v[i], r0[i], r1[i], u0[i], u1[i]);
                     }
                     if (final) break;
@@ -786,19 +868,19 @@ constexpr int att_most_columns() { return D == 256 ? 2 : 4; }
 template <int D>
 constexpr size_t att_workspace() { return size_t(kAttCounters) + size_t(kAttMaxCtas) * 4 * AttCfg<D, att_most_columns<D>()>::PIECE * 4; }
 
-template <int D, int NT>
+template <int D, int NT, bool SHARED>
 cudaError_t launch_attend(AttParams p, int sms, cudaStream_t s) {
     using C = AttCfg<D, NT>;
     constexpr int most = C::SMEM + 4 * (TETRA_KV_MAX_SEQS + 1);
     static PerDeviceOnce once;  // per instantiation
-    cudaError_t e = once.run([] { return cudaFuncSetAttribute(k_kv_attend<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, most); });
+    cudaError_t e = once.run([] { return cudaFuncSetAttribute(k_kv_attend<D, NT, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, most); });
     if (e != cudaSuccess) return e;
     const int grid = C::CTAS * sms < kAttMaxCtas ? C::CTAS * sms : kAttMaxCtas;
     // Units are counted in 32 bits, a grid's rounding with them: larger ones where all sequences, as long as the table and with
     // all of the rows (row_start is not known here), could pass that.
     const int64_t items = (int64_t(p.c.rows) * p.group / (8 * NT) + 1) * p.c.seqs * p.c.kv_heads, blocks = int64_t(p.c.width) * p.c.blocks_per_page;
     while (items * (blocks / (kAttWarps << p.unit_shift) + 1) > (1ll << 30) && blocks > (kAttWarps << p.unit_shift)) ++p.unit_shift;
-    return launch_pdl(k_kv_attend<D, NT>, grid, kAttThreads, size_t(C::SMEM) + 4 * (p.c.seqs + 1), s, p);
+    return launch_pdl(k_kv_attend<D, NT, SHARED>, grid, kAttThreads, size_t(C::SMEM) + 4 * (p.c.seqs + 1), s, p);
 }
 
 // Columns of an item by what a sequence has on average: more of them read a block's codes once for more rows, but an
@@ -808,12 +890,46 @@ cudaError_t launch_attend(AttParams p, int sms, cudaStream_t s) {
 // 1000 and 8000 47 / 57 / 78, 2000 and 8000 64 / 76 / 101; one row in the piece's place 15, 20, 33 and 57 with 8.
 // (At the cap of 128 registers two CTAs to an SM leave 16 columns of 128 dims with 100 bytes spilt a thread, 32 of 64 with 12:
 // 64 sequences of 4 rows behind 4000 tokens, 16 columns of 128, take 106 us, 5.0 TB/s.)
-template <int D>
+template <int D, bool SHARED>
 cudaError_t launch_attend_for(const AttParams& p, int sms, cudaStream_t s) {
     const int64_t columns = (int64_t(p.c.rows) * p.group + p.c.seqs - 1) / p.c.seqs;
-    if (columns <= 8) return launch_attend<D, 1>(p, sms, s);
-    if (D == 256 || columns <= 24) return launch_attend<D, 2>(p, sms, s);
-    return launch_attend<D, att_most_columns<D>()>(p, sms, s);
+    if (columns <= 8) return launch_attend<D, 1, SHARED>(p, sms, s);
+    if (D == 256 || columns <= 24) return launch_attend<D, 2, SHARED>(p, sms, s);
+    return launch_attend<D, att_most_columns<D>(), SHARED>(p, sms, s);
+}
+template <bool SHARED>
+cudaError_t launch_attend_all(const AttParams& p, int D, int sms, cudaStream_t s) {
+    return D == 64 ? launch_attend_for<64, SHARED>(p, sms, s) : D == 128 ? launch_attend_for<128, SHARED>(p, sms, s) : launch_attend_for<256, SHARED>(p, sms, s);
+}
+
+// What both calls check, in the order in which they say so.
+int attend_params(const tetra_kv_cache* cache, const void* q, int64_t q_stride, void* out, int rows, int q_heads, float scale, void* workspace, size_t workspace_bytes,
+                  size_t wanted_bytes, AttParams& p) {
+    const int rc = kv_check(cache, rows, p.c);
+    if (rc != TETRA_OK) return rc;
+    const int D = cache->head_dim;
+    if (!q || !out || !workspace) return TETRA_ERR_NULL;
+    if (q_heads < 1 || q_heads % p.c.kv_heads || q_heads > 4096 || q_stride < int64_t(q_heads) * D) return TETRA_ERR_SHAPE;
+    p.scale = scale * 1.4426950408889634f;  // times log2 e
+    if (!std::isfinite(p.scale) || int64_t(cache->seqs) * rows * q_heads > (1ll << 32)) return TETRA_ERR_SHAPE;
+    if (!kv_aligned(q, 16) || q_stride % 8 || !kv_aligned(out, 16) || !kv_aligned(workspace, 256)) return TETRA_ERR_ALIGN;
+    if (workspace_bytes < wanted_bytes) return TETRA_ERR_SIZE;
+    p.q = static_cast<const __half*>(q);
+    p.out = static_cast<__half*>(out);
+    p.q_stride = q_stride;
+    p.group = q_heads / p.c.kv_heads;
+    p.unit_shift = 0;
+    p.arrived = static_cast<uint32_t*>(workspace);
+    p.pieces = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + kAttCounters);
+    p.shared = nullptr;
+    p.shared_pieces = nullptr;
+    return TETRA_OK;
+}
+
+// The workspace of tetra_kv_attend_shared: that of tetra_kv_attend, the sequences' shares, the pieces.
+constexpr size_t kSharedSeqs = size_t(TETRA_KV_MAX_SEQS) * sizeof(SharedSeq);
+size_t shared_workspace(int D, int64_t rows, int q_heads, int kv_heads, int groups) {
+    return (tetra_kv_workspace_bytes(D) + 255) / 256 * 256 + kSharedSeqs + prefix_bytes(D, prefix_parts_most(D, rows, q_heads, kv_heads, groups));
 }
 
 }  // namespace
@@ -830,28 +946,41 @@ size_t tetra_kv_workspace_bytes(int head_dim) {
 int tetra_kv_attend(const tetra_kv_cache* cache, const void* q, int64_t q_stride, void* out, int rows, int q_heads, float scale, void* workspace,
                     size_t workspace_bytes, void* stream) {
     AttParams p;
-    const int rc = kv_check(cache, rows, p.c);
-    if (rc != TETRA_OK) return rc;
-    const int D = cache->head_dim;
-    if (!q || !out || !workspace) return TETRA_ERR_NULL;
-    if (q_heads < 1 || q_heads % p.c.kv_heads || q_heads > 4096 || q_stride < int64_t(q_heads) * D) return TETRA_ERR_SHAPE;
-    const float scale_log2 = scale * 1.4426950408889634f;  // times log2 e
-    if (!std::isfinite(scale_log2) || int64_t(cache->seqs) * rows * q_heads > (1ll << 32)) return TETRA_ERR_SHAPE;
-    if (!kv_aligned(q, 16) || q_stride % 8 || !kv_aligned(out, 16) || !kv_aligned(workspace, 256)) return TETRA_ERR_ALIGN;
-    if (workspace_bytes < tetra_kv_workspace_bytes(D)) return TETRA_ERR_SIZE;
-    if (rows == 0) return TETRA_OK;
+    const int rc = attend_params(cache, q, q_stride, out, rows, q_heads, scale, workspace, workspace_bytes, cache ? tetra_kv_workspace_bytes(cache->head_dim) : 0, p);
+    if (rc != TETRA_OK || rows == 0) return rc;
     int sms = 0;
     if (device_sms(&sms) != cudaSuccess) return TETRA_ERR_CUDA;
-    p.q = static_cast<const __half*>(q);
-    p.out = static_cast<__half*>(out);
-    p.q_stride = q_stride;
-    p.scale = scale_log2;
-    p.group = q_heads / p.c.kv_heads;
-    p.unit_shift = 0;
-    p.arrived = static_cast<uint32_t*>(workspace);
-    p.pieces = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + kAttCounters);
+    return kv_status(launch_attend_all<false>(p, cache->head_dim, sms, static_cast<cudaStream_t>(stream)));
+}
+
+size_t tetra_kv_shared_workspace_bytes(int head_dim, int rows, int q_heads, int kv_heads, int groups) {
+    if (tetra_kv_workspace_bytes(head_dim) == 0 || rows < 0 || rows > TETRA_KV_MAX_ROWS || kv_heads < 1 || kv_heads > 1024 || q_heads < 1 || q_heads > 4096 ||
+        q_heads % kv_heads || groups < 0 || groups > TETRA_KV_MAX_SEQS)
+        return 0;
+    return shared_workspace(head_dim, rows, q_heads, kv_heads, groups);
+}
+
+int tetra_kv_attend_shared(const tetra_kv_cache* cache, const tetra_kv_groups* groups, const void* q, int64_t q_stride, void* out, int rows, int q_heads, float scale,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+    AttParams p;
+    if (!groups || (groups->groups > 0 && (!groups->group_start || !groups->shared))) return TETRA_ERR_NULL;
+    if (groups->groups < 0 || groups->groups > TETRA_KV_MAX_SEQS) return TETRA_ERR_SHAPE;
+    if (!kv_aligned(groups->group_start, 4) || !kv_aligned(groups->shared, 4)) return TETRA_ERR_ALIGN;
+    const size_t wanted = cache ? tetra_kv_shared_workspace_bytes(cache->head_dim, rows, q_heads, cache->kv_heads, groups->groups) : 0;
+    const int rc = attend_params(cache, q, q_stride, out, rows, q_heads, scale, workspace, workspace_bytes, wanted, p);
+    if (rc != TETRA_OK || rows == 0) return rc;
+    int sms = 0;
+    if (device_sms(&sms) != cudaSuccess) return TETRA_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return kv_status(D == 64 ? launch_attend_for<64>(p, sms, s) : D == 128 ? launch_attend_for<128>(p, sms, s) : launch_attend_for<256>(p, sms, s));
+    const int D = cache->head_dim;
+    if (groups->groups == 0) return kv_status(launch_attend_all<false>(p, D, sms, s));
+    unsigned char* at = static_cast<unsigned char*>(workspace) + (tetra_kv_workspace_bytes(D) + 255) / 256 * 256;
+    p.shared = reinterpret_cast<const SharedSeq*>(at);
+    p.shared_pieces = reinterpret_cast<const float*>(at + kSharedSeqs);
+    const cudaError_t e = launch_prefix(*cache, rows, PrefixGroups{groups->group_start, groups->shared, groups->groups}, q, q_stride, p.scale, p.group, D, at,
+                                        reinterpret_cast<float*>(at + kSharedSeqs), prefix_parts_most(D, rows, q_heads, cache->kv_heads, groups->groups), s);
+    if (e != cudaSuccess) return TETRA_ERR_CUDA;
+    return kv_status(launch_attend_all<true>(p, D, sms, s));
 }
 
 }  // extern "C"

@@ -1,0 +1,713 @@
+// Attention of a group's rows to the tokens that its sequences share (the first kernel of tetra_kv_attend_shared).
+//
+// S answers behind one prompt are S times the query heads of a group as columns for the same keys: 256 columns a kv head for 64
+// answers of a model with four query heads to a kv head.  2 D bytes a token and kv head stand against 4 D multiply-adds a column, so
+// from about 100 columns on the tensor cores bound it, not HBM, and tcgen05 pays: a tile of 128 columns is one operand's 128 rows.
+//
+// Work.  An item is (group, kv head, tile of 256 columns; 128 with heads of 256), its tokens come in steps of 64 (four records) and
+// are cut into parts; what a CTA does is found by each CTA from the lengths, which are on the device.  A part leaves its sums in the
+// workspace; k_kv_attend, which does the sequences' own tokens, adds them.  No atomics on memory: bit-identical from run to run.
+//
+// A CTA.  One thread copies records by cp.async.bulk into a ring.  Four warps turn their bytes into float16 (exact: codes are small
+// integers) and lay them out for the tensor cores: keys as [token][dim], values as [dim][token], rows of 128 bytes, swizzled; the
+// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  One thread issues the products:
+// S = Q K^T (Q from tensor memory, 128 columns x 64 tokens) and O += P V (P from tensor memory, over S).  Two groups of four warps
+// ("slots"), a thread a column, turn S into weights: no value of a column is in another thread, so there are no exchanges.  The
+// slots take the two halves of a tile's columns, or, where a tile has no more than 128, every other step, so that the products of
+// one run beside the exponentials of the other.
+//
+// Arithmetic is that of k_kv_attend: scores are exact products summed in float32, times s_K; weights enter as
+// float16(2^(score - m) s_V) with m a running reference that moves only when a weight would pass 2^15 (a vote a step); the
+// denominator sums 2^(score - m) in float32.
+#include <cfloat>
+#include <climits>
+#include <cmath>
+
+#include "kv_shared.cuh"
+
+namespace tetra {
+namespace {
+
+constexpr int kPreStep = 64;                              // tokens of a step
+constexpr int kPreBlocks = kPreStep / kKvBlock;
+constexpr int kPreSoft = 8, kPreConvert = 4;              // warps
+constexpr int kPreConvertAt = kPreSoft, kPreCopyWarp = kPreSoft + kPreConvert, kPreMmaWarp = kPreCopyWarp + 1;
+constexpr int kPreThreads = (kPreMmaWarp + 1) * 32;
+constexpr int kPreScales = 8;                             // steps whose scales are kept
+constexpr int kPreMostCtas = 160, kPreWaves = 2;          // of a launch; parts a CTA where items are few
+constexpr uint32_t kPrePartCost = 6;                      // steps that a part's beginning and end take
+constexpr uint32_t kPreTries = 1u << 22;                  // of a wait: then the call's results are NaN
+constexpr float kPreNoRef = -FLT_MAX, kPreLeastLog = -60.f, kPreHigh = 15.f, kPreBase = 7.f;  // as in k_kv_attend
+
+template <int D>
+struct PreCfg {
+    static constexpr int SLOTS = pre_slots(D);
+    static constexpr int REC = kv_record_bytes(D), STAGE = kPreBlocks * REC;
+    static constexpr int STAGES = D == 256 ? 2 : 6;
+    static constexpr int TILE = kPreStep * D * 2;         // bytes of a step's keys, or values, in float16
+    static constexpr int RING = 4 * TILE;                 // behind two of each
+    static constexpr int SMEM = RING + STAGES * STAGE + 1024;  // 1024: alignment; and the plan
+    // Columns of tensor memory: a slot's queries, scores (weights over them) and sums.
+    static constexpr int QCOLS = D / 2, SLOT = QCOLS + kPreStep + D;
+    static_assert(SLOTS * SLOT <= 512, "tensor memory");
+};
+
+struct PreParams {
+    KvCache c;
+    PrefixGroups g;
+    const __half* q;
+    int64_t q_stride;
+    float scale;        // times log2 e
+    int32_t group;      // query heads to a kv head
+    SharedSeq* seqs;
+    float* pieces;
+    uint32_t most;      // parts
+};
+
+// The plan, in shared memory, by group.
+struct PrePlan {
+    int32_t *start, *part0, *count, *leader, *row0, *rows_end, *blocks, *parts;
+    static __host__ __device__ size_t bytes(int groups) { return (size_t(groups) * 8 + 2) * 4; }
+};
+
+struct PrePart {
+    int32_t leader, head, col0, cols;  // the sequence whose pages are read; first column of the tile, and columns of it
+    int32_t row0;
+    uint32_t begin, end, blocks;       // steps; blocks that are shared
+    bool both;                         // the slots share the columns
+};
+
+__device__ __forceinline__ float pre_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float pre_lg2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Bytes 0, 1 (HIGH: 2, 3) of w as float16 codes: 1024 + byte, minus 1152.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t pre_codes(uint32_t w) {
+    const uint32_t u = prmt(w, 0x64646464u, HIGH ? 0x4342u : 0x4140u);
+    uint32_t h;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h) : "r"(u), "r"(0x64806480u));
+    return h;
+}
+__device__ __forceinline__ uint4 pre_lds(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ void pre_sts(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void pre_sts(uint32_t at, uint32_t a, uint32_t b) {
+    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(a), "r"(b) : "memory");
+}
+
+// ---- barriers --------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// Every wait ends: after so many tries, or when another one has given up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < kPreTries; ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (done) return true;
+        if (*failed) return false;
+    }
+    *failed = 1;
+    return false;
+}
+__device__ __forceinline__ void copy_record(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+
+// ---- tensor cores ------------------------------------------------------------------------------------------------------
+// Rows of 128 bytes in groups of eight (1024 bytes), 16-byte pieces of a row exchanged by the row's place in its group.
+__device__ __forceinline__ uint64_t tile_descriptor(uint32_t at) {
+    return uint64_t((at & 0x3FFFFu) >> 4) | uint64_t(1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+// float16 x float16 -> float32, 128 rows, n columns, both operands with k running fastest.
+__host__ __device__ constexpr uint32_t product_kind(int n) { return 1u << 4 | uint32_t(n / 8) << 17 | uint32_t(128 / 16) << 24; }
+__device__ __forceinline__ void tensor_product(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, bool add) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"(uint32_t(add))
+        : "memory");
+}
+__device__ __forceinline__ void tensor_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+#define TETRA_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
+#define TETRA_W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
+// 32 columns of the lane's row.
+__device__ __forceinline__ void tensor_load(uint32_t at, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : TETRA_R8(r, 0), TETRA_R8(r, 8), TETRA_R8(r, 16), TETRA_R8(r, 24)
+        : "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::TETRA_W8(r, 0),
+        TETRA_W8(r, 8), TETRA_W8(r, 16), TETRA_W8(r, 24), "r"(at)
+        : "memory");
+}
+#undef TETRA_R8
+#undef TETRA_W8
+
+// ---- the plan ------------------------------------------------------------------------------------------------------------
+// The group of sequence s, or -1.
+__device__ __forceinline__ int group_of(const PrePlan& plan, int groups, int seqs, int s) {
+    int lo = 0, hi = groups;  // the last g with start[g] <= s
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (plan.start[mid] <= s) lo = mid;
+        else hi = mid;
+    }
+    const int a = plan.start[lo], b = plan.start[lo + 1];
+    return a >= 0 && b <= seqs && a <= s && s < b ? lo : -1;
+}
+// A sequence shares where all of its rows see all of the shared blocks and none of its own tokens is in them.
+__device__ __forceinline__ bool shares(int a, int b, int before, int blocks) { return b > a && blocks > 0 && int64_t(before) >= int64_t(blocks) * kKvBlock; }
+
+struct PreGroup {
+    uint32_t items, steps;
+};
+template <int D>
+__device__ __forceinline__ PreGroup group_work(const PreParams& p, const PrePlan& plan, int g) {
+    PreGroup w{0, 1};
+    if (g < p.g.groups && plan.count[g] >= 2) {
+        const uint32_t cols = uint32_t(plan.rows_end[g] - plan.row0[g]) * p.group;
+        w.items = (cols + pre_tile(D) - 1) / pre_tile(D) * p.c.kv_heads;
+        w.steps = (uint32_t(plan.blocks[g]) + kPreBlocks - 1) / kPreBlocks;
+    }
+    return w;
+}
+// Parts of an item when none has more than `share` steps.
+__device__ __forceinline__ uint32_t pre_parts(uint32_t steps, uint32_t share) {
+    const uint32_t each = (steps + (steps + share - 1) / share - 1) / ((steps + share - 1) / share);
+    return (steps + each - 1) / each;
+}
+
+// Every CTA finds out for itself how the work is cut.  The longest part decides, so the share of a part is the least with which
+// there are no more parts than CTAs, or twice as many, whichever takes less.  Returns the number of parts.
+template <int D>
+__device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan& plan, uint32_t* total) {
+    const int groups = p.g.groups, seqs = p.c.seqs, tid = threadIdx.x, lane = tid & 31;
+    const int64_t most_tokens = int64_t(p.c.width) * p.c.blocks_per_page * kKvBlock;
+    for (int g = tid; g < groups; g += kPreThreads) {
+        plan.start[g] = __ldg(p.g.start + g);
+        const int tokens = __ldg(p.g.shared + g);
+        plan.blocks[g] = int(min(int64_t(max(tokens, 0)), most_tokens) / kKvBlock);
+        plan.count[g] = 0;
+        plan.leader[g] = plan.row0[g] = INT_MAX;
+        plan.rows_end[g] = 0;
+    }
+    if (tid == 0) plan.start[groups] = __ldg(p.g.start + groups);
+    __syncthreads();
+#pragma unroll 1
+    for (int s = tid; s < seqs; s += kPreThreads) {
+        int a, b;
+        p.c.rows_of(s, a, b);
+        const int before = __ldg(p.c.lengths + s), g = group_of(plan, groups, seqs, s);
+        if (g >= 0 && shares(a, b, before, plan.blocks[g])) {
+            atomicAdd(plan.count + g, 1);
+            atomicMin(plan.leader + g, s);
+            atomicMin(plan.row0 + g, a);
+            atomicMax(plan.rows_end + g, b);
+        }
+    }
+    __syncthreads();
+    if (tid < 32) {
+        const uint32_t G = gridDim.x;
+        uint32_t items = 0, work = 0, longest = 1;
+        for (int g = lane; g < groups; g += 32) {
+            const PreGroup w = group_work<D>(p, plan, g);
+            items += w.items;
+            work += w.items * w.steps;
+            longest = max(longest, w.steps);
+        }
+        items = __reduce_add_sync(0xFFFFFFFFu, items);
+        work = __reduce_add_sync(0xFFFFFFFFu, work);
+        longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+        uint32_t share = longest, cost = ~0u;
+#pragma unroll 1
+        for (uint32_t k = 1; k <= kPreWaves && items; ++k) {
+            const uint32_t may = min(k * G, p.most);
+            if (items > may) continue;
+            uint32_t tried = max(1u, (work + may - 1) / may);
+#pragma unroll 1
+            while (tried < longest) {
+                uint32_t need = 0;
+                for (int g = lane; g < groups; g += 32) {
+                    const PreGroup w = group_work<D>(p, plan, g);
+                    need += w.items * pre_parts(w.steps, tried);
+                }
+                if (__reduce_add_sync(0xFFFFFFFFu, need) <= may) break;
+                tried += max(1u, tried >> 4);
+            }
+            tried = min(tried, longest);
+            if (k * (tried + kPrePartCost) < cost) cost = k * (tried + kPrePartCost), share = tried;
+        }
+        // A group whose parts have no place (which takes sequences that have rows in common) is not shared.
+        uint32_t at = 0;
+        for (int g0 = 0; g0 < groups; g0 += 32) {
+            const int g = g0 + lane;
+            const PreGroup w = group_work<D>(p, plan, g);
+            const uint32_t parts = w.items ? pre_parts(w.steps, share) : 0u;
+            uint32_t own = w.items * parts, sum = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+                if (lane >= o) sum += v;
+            }
+            if (g < groups) {
+                const bool fits = at + sum <= p.most;
+                plan.part0[g] = int(min(at + sum - own, p.most));
+                plan.parts[g] = fits ? int(parts) : 0;
+            }
+            at += __shfl_sync(0xFFFFFFFFu, sum, 31);
+        }
+        if (lane == 0) {
+            *total = min(at, p.most);
+            plan.part0[groups] = int(min(at, p.most));
+        }
+    }
+    __syncthreads();
+    if (blockIdx.x == 0) {
+#pragma unroll 1
+        for (int s = tid; s < seqs; s += kPreThreads) {
+            int a, b;
+            p.c.rows_of(s, a, b);
+            const int before = __ldg(p.c.lengths + s), g = group_of(plan, groups, seqs, s);
+            SharedSeq out = {};
+            if (g >= 0 && plan.count[g] >= 2 && plan.parts[g] > 0 && shares(a, b, before, plan.blocks[g])) {
+                out.first = plan.blocks[g];
+                out.part0 = plan.part0[g];
+                out.parts = plan.parts[g];
+                out.row0 = plan.row0[g];
+                out.cols = (plan.rows_end[g] - plan.row0[g]) * p.group;
+                out.tiles = (out.cols + pre_tile(D) - 1) / pre_tile(D);
+            }
+            p.seqs[s] = out;
+        }
+    }
+    return *total;
+}
+
+// Part number n of the plan; false: of a group that is not shared.
+template <int D>
+__device__ __forceinline__ bool part_of(const PreParams& p, const PrePlan& plan, uint32_t n, PrePart& q) {
+    int lo = 0, hi = p.g.groups;
+    while (hi - lo > 1) {  // the last group whose parts begin at or before n
+        const int mid = (lo + hi) >> 1;
+        if (uint32_t(plan.part0[mid]) <= n) lo = mid;
+        else hi = mid;
+    }
+    const uint32_t parts = uint32_t(plan.parts[lo]);
+    if (parts == 0) return false;
+    const uint32_t local = n - uint32_t(plan.part0[lo]), item = local / parts, part = local - item * parts;
+    const uint32_t cols = uint32_t(plan.rows_end[lo] - plan.row0[lo]) * p.group, tiles = (cols + pre_tile(D) - 1) / pre_tile(D);
+    const uint32_t head = item / tiles, steps = (uint32_t(plan.blocks[lo]) + kPreBlocks - 1) / kPreBlocks, each = (steps + parts - 1) / parts;
+    q.leader = plan.leader[lo];
+    q.head = int(head);
+    q.col0 = int(item - head * tiles) * pre_tile(D);
+    q.cols = min(int(cols) - q.col0, pre_tile(D));
+    q.row0 = plan.row0[lo];
+    q.blocks = uint32_t(plan.blocks[lo]);
+    q.begin = part * each;
+    q.end = min(steps, q.begin + each);
+    q.both = pre_slots(D) == 2 && q.cols <= kPreColumns;
+    return int(head) < p.c.kv_heads;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
+    using C = PreCfg<D>;
+    constexpr int SLOTS = C::SLOTS, STAGES = C::STAGES, CHUNKS = D / 32;
+    extern __shared__ unsigned char raw[];
+    __shared__ __align__(8) uint64_t raw_full[STAGES], raw_empty[STAGES], k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2], p_ready[2], o_done[2],
+        scales_full[kPreScales], drained;
+    __shared__ __align__(16) float4 scales[kPreScales][kPreBlocks];  // s_K times the call's, s_V, log2 s_V, whether there is such a block
+    __shared__ uint32_t placed[STAGES], total, tensor_base;
+    __shared__ int failed;
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
+    pdl_wait();
+    pdl_release();
+
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    PrePlan plan;
+    {
+        int32_t* at = reinterpret_cast<int32_t*>(raw + (base - smem_u32(raw)) + C::RING + STAGES * C::STAGE);
+        const int n = p.g.groups;
+        plan = PrePlan{at, at + n + 1, at + 2 * n + 2, at + 3 * n + 2, at + 4 * n + 2, at + 5 * n + 2, at + 6 * n + 2, at + 7 * n + 2};
+    }
+    const uint32_t parts = make_plan<D>(p, plan, &total);
+    if (parts <= blockIdx.x) return;
+
+    if (threadIdx.x == 0) {
+        failed = 0;
+        for (int i = 0; i < STAGES; ++i) bar_init(smem_u32(raw_full + i), 1), bar_init(smem_u32(raw_empty + i), kPreConvert);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_u32(k_full + i), kPreConvert), bar_init(smem_u32(v_full + i), kPreConvert);
+            bar_init(smem_u32(k_empty + i), 1), bar_init(smem_u32(v_empty + i), 1);
+            bar_init(smem_u32(q_ready + i), 4), bar_init(smem_u32(p_ready + i), 4);
+            bar_init(smem_u32(s_full + i), 1), bar_init(smem_u32(o_done + i), 1);
+        }
+        for (int i = 0; i < kPreScales; ++i) bar_init(smem_u32(scales_full + i), 1);
+        bar_init(smem_u32(&drained), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kPreMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tensor_base)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tensor = tensor_base;
+    volatile int* gave_up = &failed;
+    const uint32_t ring = base + C::RING;
+    uint32_t n0 = 0;  // steps before the part
+
+    if (warp == kPreCopyWarp) {
+        // ---- records into the ring: lane l looks up the place of the l-th of the next 32, a batch ahead
+        bool ok = true;
+        uint32_t n = 0;
+        for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
+            PrePart q;
+            if (!part_of<D>(p, plan, at, q)) continue;
+            const uint32_t end = min(q.end * kPreBlocks, q.blocks);
+            auto look = [&](uint32_t first) { return first + lane < end ? p.c.template record<D>(q.leader, first + lane, q.head) : nullptr; };
+            const unsigned char *now = look(q.begin * kPreBlocks), *next = look(q.begin * kPreBlocks + 32);
+            for (uint32_t step = q.begin; ok && step < q.end; ++step, ++n) {
+                const uint32_t k = (step - q.begin) * kPreBlocks & 31u, stage = n % STAGES;
+                if (k == 0 && step > q.begin) now = next, next = look(step * kPreBlocks + 32);
+                ok = bar_wait(smem_u32(raw_empty + stage), (n / STAGES & 1u) ^ 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                const unsigned char* from = reinterpret_cast<const unsigned char*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<uint64_t>(now), k + (lane & 3)));
+                const uint32_t there = __ballot_sync(0xFFFFFFFFu, lane < kPreBlocks && from != nullptr);
+                const uint32_t bar = smem_u32(raw_full + stage);
+                if (lane == 0) {
+                    placed[stage] = there;
+                    if (there) bar_expect(bar, __popc(there) * C::REC);
+                    else bar_arrive(bar);
+                }
+                __syncwarp();
+                if (there >> lane & 1u) copy_record(ring + stage * C::STAGE + lane * C::REC, from, C::REC, bar);
+            }
+        }
+        // Nothing is in flight when the CTA ends: what was copied has been waited for by who converts it, unless that gave up.
+        if (!ok) {
+            int none = 0;
+            for (uint32_t back = 1; back <= STAGES && back <= n; ++back) bar_wait(smem_u32(raw_full + (n - back) % STAGES), (n - back) / STAGES & 1u, &none);
+        }
+    } else if (warp >= kPreConvertAt && warp < kPreCopyWarp) {
+        // ---- bytes to operands
+        const int w = warp - kPreConvertAt;
+        bool ok = true;
+        uint32_t n = 0;
+        // Keys: a unit of 16 bytes is 8 dims (tt of a chunk of 32) of tokens g and g + 8.  A quarter of the warp takes tokens g, g ^ 1 of
+        // two chunks, which no two lanes read or write through the same bank.
+        const int odd = lane >> 2 & 1, tt = lane & 3;
+        // Values: a unit is dims 4 dq .. + 3 of tokens 2 tq, 2 tq + 1, and 8 on; half a warp takes two blocks.
+        const int vblock = (w >> 1) * 2 + (lane >> 3 & 1), e = lane >> 2 & 1, tq = lane & 3;
+        for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
+            PrePart q;
+            if (!part_of<D>(p, plan, at, q)) continue;
+            for (uint32_t step = q.begin; step < q.end; ++step, ++n) {
+                const uint32_t stage = n % STAGES, from = ring + stage * C::STAGE, two = n & 1u, parity = (n >> 1 & 1u) ^ 1u;
+                ok = bar_wait(smem_u32(raw_full + stage), n / STAGES & 1u, gave_up) && bar_wait(smem_u32(k_empty + two), parity, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                if (w == 0) {
+                    if (lane < kPreBlocks) {
+                        const bool is = placed[stage] >> lane & 1u;
+                        const uint4 raw4 = pre_lds(from + lane * C::REC + 32 * D);
+                        const float vs = __uint_as_float(raw4.y);
+                        float lv = pre_lg2(vs);
+                        lv = lv < kPreLeastLog ? kPreLeastLog : lv;  // NaN stays
+                        scales[n % kPreScales][lane] = is ? make_float4(__uint_as_float(raw4.x) * p.scale, vs, lv, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(scales_full + n % kPreScales));
+                }
+                {
+                    const uint32_t to = base + two * C::TILE;
+#pragma unroll
+                    for (int pair = 0; pair < CHUNKS / 2; ++pair) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int g = (2 * (lane >> 3) + h) ^ odd, row = w * kKvBlock + (g >> 1) * 4 + (g & 1);
+                            const uint4 u = pre_lds(from + w * C::REC + (2 * pair + odd) * 512 + (g * 4 + tt) * 16);
+                            const uint32_t chunk = odd * 4 + tt, line = to + pair * (kPreStep * 128) + row * 128;
+                            pre_sts(line + ((chunk ^ (row & 7)) << 4), pre_codes<false>(u.x), pre_codes<true>(u.x), pre_codes<false>(u.y), pre_codes<true>(u.y));
+                            pre_sts(line + 256 + ((chunk ^ ((row + 2) & 7)) << 4), pre_codes<false>(u.z), pre_codes<true>(u.z), pre_codes<false>(u.w), pre_codes<true>(u.w));
+                        }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(k_full + two));
+                ok = bar_wait(smem_u32(v_empty + two), parity, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                {
+                    const uint32_t to = base + (2 + two) * C::TILE;
+#pragma unroll
+                    for (int it = 0; it < D / 32; ++it) {
+                        const int chunk = (w & 1) + 2 * (it >> 1), dq = ((it & 1) * 2 + (lane >> 4)) * 2 + e;
+                        const uint4 u = pre_lds(from + vblock * C::REC + 16 * D + chunk * 512 + (dq * 4 + tq) * 16);
+                        const uint32_t word[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int d = chunk * 32 + dq * 4 + i;
+                            pre_sts(to + d * 128 + (((2 * vblock + (tq >> 1)) ^ (d & 7)) << 4) + (tq & 1) * 8, pre_codes<false>(word[i]), pre_codes<true>(word[i]));
+                        }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    bar_arrive(smem_u32(v_full + two));
+                    bar_arrive(smem_u32(raw_empty + stage));
+                }
+            }
+        }
+    } else if (warp == kPreMmaWarp) {
+        // ---- products, issued by one thread
+        if (lane == 0) {
+            bool ok = true;
+            uint32_t jobs_of[2] = {0, 0}, q_of[2] = {0, 0};
+            for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
+                PrePart q;
+                if (!part_of<D>(p, plan, at, q)) continue;
+                const uint32_t steps = q.end - q.begin;
+                const bool halves = SLOTS == 2 && !q.both;  // each step is both slots' work
+                const uint32_t jobs = halves ? 2 * steps : steps;
+                auto step_of = [&](uint32_t job) { return n0 + (halves ? job >> 1 : job); };
+                auto scores = [&](uint32_t job) {
+                    const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, n = step_of(job), two = n & 1u;
+                    if (job < uint32_t(SLOTS)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_of[slot]++ & 1u, gave_up);
+                    ok = ok && bar_wait(smem_u32(k_full + two), n >> 1 & 1u, gave_up);
+                    if (!ok) return;
+                    fence_after();
+                    const uint32_t to = tensor + slot * C::SLOT + C::QCOLS, a = tensor + slot * C::SLOT;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        tensor_product(to, a + k * 8, tile_descriptor(base + two * C::TILE + k / 4 * (kPreStep * 128) + k % 4 * 32), product_kind(kPreStep), k > 0);
+                    tensor_commit(smem_u32(s_full + slot));
+                    if (!halves || slot == 1) tensor_commit(smem_u32(k_empty + two));
+                };
+                for (uint32_t job = 0; ok && job < uint32_t(SLOTS) && job < jobs; ++job) scores(job);
+                for (uint32_t job = 0; ok && job < jobs; ++job) {
+                    const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, n = step_of(job), two = n & 1u;
+                    ok = ok && bar_wait(smem_u32(v_full + two), n >> 1 & 1u, gave_up);
+                    ok = ok && bar_wait(smem_u32(p_ready + slot), jobs_of[slot]++ & 1u, gave_up);
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t a = tensor + slot * C::SLOT + C::QCOLS, to = a + kPreStep;
+#pragma unroll
+                    for (int k = 0; k < kPreStep / 16; ++k)
+                        tensor_product(to, a + k * 8, tile_descriptor(base + (2 + two) * C::TILE + k * 32), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
+                    tensor_commit(smem_u32(o_done + slot));
+                    if (!halves || slot == 1) tensor_commit(smem_u32(v_empty + two));
+                    if (job + SLOTS < jobs) scores(job + SLOTS);
+                }
+                n0 += steps;
+            }
+            // What was issued has ended when the tensor memory is given back.
+            int none = 0;
+            tensor_commit(smem_u32(&drained));
+            bar_wait(smem_u32(&drained), 0, &none);
+        }
+        __syncwarp();
+    } else if (warp < 4 * SLOTS) {
+        // ---- weights: a thread a column
+        const uint32_t slot = warp >> 2, column = threadIdx.x & 127;
+        const uint32_t at_q = tensor + slot * C::SLOT + ((warp & 3u) << 21), at_s = at_q + C::QCOLS, at_o = at_s + kPreStep;  // lanes from bit 16 on
+        uint32_t jobs = 0;
+        bool ok = true;
+        for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
+            PrePart q;
+            if (!part_of<D>(p, plan, at, q)) continue;
+            const uint32_t steps = q.end - q.begin, first = q.both ? slot : 0u, by = q.both ? 2u : 1u;
+            const int col = q.col0 + (q.both || SLOTS == 1 ? 0 : int(slot) * kPreColumns) + int(column);
+            const bool live = col < q.col0 + q.cols;
+            float ref = kPreNoRef, sum = 0.f;
+            if (first < steps) {
+                const uint32_t row = live ? uint32_t(col) / uint32_t(p.group) : 0u, h = live ? uint32_t(col) - row * p.group : 0u;
+                const uint4* src = reinterpret_cast<const uint4*>(p.q + int64_t(q.row0 + row) * p.q_stride + (int64_t(q.head) * p.group + h) * D);
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) {
+                    uint32_t r[32];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint4 v = live ? __ldg(src + j * 8 + i) : make_uint4(0, 0, 0, 0);
+                        r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
+                    }
+                    tensor_store(at_q + j * 32, r);
+                }
+                wait_stores();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(q_ready + slot));
+            }
+            for (uint32_t i = first; i < steps; i += by, ++jobs) {
+                const uint32_t n = n0 + i;
+                ok = bar_wait(smem_u32(scales_full + n % kPreScales), n / kPreScales & 1u, gave_up) && bar_wait(smem_u32(s_full + slot), jobs & 1u, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                fence_after();
+                uint32_t r[64];
+                tensor_load(at_s, r);
+                tensor_load(at_s + 32, r + 32);
+                wait_loads();
+                float4 c[kPreBlocks];
+                float top[kPreBlocks];
+                bool over = false;
+#pragma unroll
+                for (int b = 0; b < kPreBlocks; ++b) {
+                    c[b] = scales[n % kPreScales][b];
+                    top[b] = -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float x = c[b].w != 0.f ? __uint_as_float(r[16 * b + k]) * c[b].x : -INFINITY;
+                        r[16 * b + k] = __float_as_uint(x);
+                        top[b] = fmaxf(top[b], x);
+                    }
+                    over |= top[b] - ref > kPreHigh - c[b].z;
+                }
+                if (__any_sync(0xFFFFFFFFu, over)) {
+                    float now = ref;
+#pragma unroll
+                    for (int b = 0; b < kPreBlocks; ++b) {
+                        float want = top[b] + c[b].z - kPreBase;
+                        if (top[b] - want > kPreHigh - c[b].z) want = top[b];  // a step of so large scores is more than the room there is
+                        if (want > now) now = want;
+                    }
+                    const float f = pre_ex2(ref - now);
+                    ref = now;
+                    sum *= f;
+                    if (i > first) {
+                        ok = bar_wait(smem_u32(o_done + slot), (jobs - 1) & 1u, gave_up);
+                        if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                        fence_after();
+#pragma unroll 1
+                        for (int j = 0; j < D; j += 32) {
+                            uint32_t o[32];
+                            tensor_load(at_o + j, o);
+                            wait_loads();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tensor_store(at_o + j, o);
+                        }
+                    }
+                }
+                uint32_t w[32];
+#pragma unroll
+                for (int b = 0; b < kPreBlocks; ++b) {
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) {
+                        const float x0 = __uint_as_float(r[16 * b + k]), x1 = __uint_as_float(r[16 * b + k + 1]);
+                        const float e0 = pre_ex2(x0 - ref), e1 = pre_ex2(x1 - ref);
+                        sum += e0 + e1;
+                        const __half2 h = __floats2half2_rn(e0 * c[b].y, e1 * c[b].y);
+                        w[8 * b + k / 2] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                }
+                tensor_store(at_s, w);
+                wait_stores();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(p_ready + slot));
+            }
+            // The piece: sums as [D / 4][column][4], then references and denominators.
+            float* piece = p.pieces + (size_t(at) * SLOTS + slot) * pre_piece(D);
+            if (ok && first < steps) {
+                ok = bar_wait(smem_u32(o_done + slot), (jobs - 1) & 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (ok) {
+                    fence_after();
+#pragma unroll 1
+                    for (int j = 0; j < D; j += 32) {
+                        uint32_t o[32];
+                        tensor_load(at_o + j, o);
+                        wait_loads();
+                        if (live) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                __stcg(reinterpret_cast<uint4*>(piece) + (j / 4 + k) * kPreColumns + column, make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
+                        }
+                    }
+                    fence_before();
+                }
+            }
+            if (live) __stcg(reinterpret_cast<float2*>(piece + kPreColumns * D) + column, make_float2(ref, ok ? sum : __uint_as_float(0x7FC00000u)));
+            n0 += steps;
+        }
+        // A wait that gave up: all that the CTA had still to do becomes NaN.
+        if (!ok) {
+            for (uint32_t at = blockIdx.x; at < parts; at += gridDim.x) {
+                float* piece = p.pieces + (size_t(at) * SLOTS + slot) * pre_piece(D);
+                __stcg(reinterpret_cast<float2*>(piece + kPreColumns * D) + column, make_float2(0.f, __uint_as_float(0x7FC00000u)));
+            }
+        }
+    }
+    __syncthreads();
+    if (warp == kPreMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
+}
+
+template <int D>
+cudaError_t launch_prefix_for(const PreParams& p, int sms, cudaStream_t s) {
+    using C = PreCfg<D>;
+    const size_t most = C::SMEM + PrePlan::bytes(TETRA_KV_MAX_SEQS);
+    static PerDeviceOnce once;  // per instantiation
+    const cudaError_t e = once.run([&] { return cudaFuncSetAttribute(k_kv_prefix<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)); });
+    if (e != cudaSuccess) return e;
+    return launch_pdl(k_kv_prefix<D>, sms < kPreMostCtas ? sms : kPreMostCtas, kPreThreads, C::SMEM + PrePlan::bytes(p.g.groups), s, p);
+}
+
+}  // namespace
+
+size_t prefix_parts_most(int head_dim, int64_t rows, int q_heads, int kv_heads, int groups) {
+    const int64_t tile = pre_tile(head_dim), sharing = groups < rows / 2 ? groups : rows / 2;  // two sequences with a row each, at least
+    const int64_t items = (rows * (q_heads / kv_heads) / tile + sharing) * kv_heads, few = kPreWaves * kPreMostCtas;
+    return size_t(items > few ? items : few);
+}
+size_t prefix_bytes(int head_dim, size_t parts) { return parts * pre_slots(head_dim) * pre_piece(head_dim) * sizeof(float); }
+
+cudaError_t launch_prefix(const tetra_kv_cache& cache, int rows, const PrefixGroups& groups, const void* q, int64_t q_stride, float scale_log2, int q_group, int head_dim,
+                          void* seqs, float* pieces, size_t parts, cudaStream_t s) {
+    int sms = 0;
+    const cudaError_t e = device_sms(&sms);
+    if (e != cudaSuccess) return e;
+    PreParams p;
+    if (kv_check(&cache, rows, p.c) != TETRA_OK) return cudaErrorInvalidValue;
+    p.g = groups;
+    p.q = static_cast<const __half*>(q);
+    p.q_stride = q_stride;
+    p.scale = scale_log2;
+    p.group = q_group;
+    p.seqs = static_cast<SharedSeq*>(seqs);
+    p.pieces = pieces;
+    p.most = uint32_t(parts);
+    return head_dim == 64 ? launch_prefix_for<64>(p, sms, s) : head_dim == 128 ? launch_prefix_for<128>(p, sms, s) : launch_prefix_for<256>(p, sms, s);
+}
+
+}  // namespace tetra

@@ -115,6 +115,9 @@ def lib():
         L.tetra_kv_read.argtypes = [vp, vp, vp, i32, vp]
         L.tetra_sample.argtypes = [vp, vp]
         L.tetra_kv_attend.argtypes = [vp, vp, C.c_int64, vp, i32, i32, C.c_float, vp, sz, vp]
+        L.tetra_kv_shared_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.tetra_kv_shared_workspace_bytes.restype = sz
+        L.tetra_kv_attend_shared.argtypes = [vp, vp, vp, C.c_int64, vp, i32, i32, C.c_float, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -407,6 +410,11 @@ class KvRows(C.Structure):
                 ("v_stride", C.c_int64), ("eps", C.c_double), ("rows", C.c_int32), ("q_heads", C.c_int32), ("half_type", C.c_int32)]
 
 
+class KvGroups(C.Structure):
+    """Mirror of tetra_kv_groups."""
+    _fields_ = [("group_start", C.c_void_p), ("shared", C.c_void_p), ("groups", C.c_int32)]
+
+
 KV_BLOCK = 16
 
 
@@ -448,6 +456,24 @@ def tetra_kv_attend(q, cache, page_table, row_start, lengths, out, workspace, sc
 
     Same page_table, row_start and lengths as the tetra_kv_append before it; scale: 1 / sqrt(D) unless given."""
     return (_nat or _native()).kv_attend(cache, page_table, row_start, lengths, q, out, scale, workspace, stream)
+
+
+def tetra_kv_shared_workspace(head_dim: int, rows: int, q_heads: int, kv_heads: int, groups: int, device="cuda") -> torch.Tensor:
+    """The workspace of tetra_kv_attend_shared for so many rows, heads and groups at most, zeroed; calls that share one must not
+    overlap on the GPU."""
+    n = lib().tetra_kv_shared_workspace_bytes(head_dim, rows, q_heads, kv_heads, groups)
+    if n == 0:
+        raise TetraError("tetra_kv_shared_workspace_bytes: rejected (head_dim %d, %d rows, %d and %d heads, %d groups)"
+                         % (head_dim, rows, q_heads, kv_heads, groups))
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def tetra_kv_attend_shared(q, cache, page_table, row_start, lengths, group_start, shared, out, workspace, scale=None, stream=None):
+    """tetra_kv_attend for sequences that begin with the same tokens, which are read once for a group of them; returns out.
+
+    Group g is the sequences group_start[g] .. group_start[g + 1] - 1 (int32 [groups + 1]); their first shared[g] tokens (int32
+    [groups]) have the same pages.  Everything else as in tetra_kv_attend; the workspace is tetra_kv_shared_workspace's."""
+    return (_nat or _native()).kv_attend_shared(cache, page_table, row_start, lengths, group_start, shared, q, out, scale, workspace, stream)
 
 
 # ---------------------------------------------------------------------------
