@@ -43,7 +43,8 @@ extern "C" {
 enum {
     TETRA_KV_BLOCK = 16,      /* tokens that share a scale */
     TETRA_KV_MAX_SEQS = 1024, /* sequences of one call */
-    TETRA_KV_MAX_ROWS = 65536 /* rows of one call */
+    TETRA_KV_MAX_ROWS = 65536, /* rows of one call */
+    TETRA_KV_MAX_AXES = 8      /* axes of a row's position */
 };
 
 /* A cache and the step's sequences.  cache: 16-byte aligned; page_table int32 [seqs][table_stride], of which `width`
@@ -88,6 +89,20 @@ size_t tetra_kv_cache_bytes(int pages, int page_tokens, int kv_heads, int head_d
  * attends to it is NaN, other blocks are untouched. */
 int tetra_kv_append(const tetra_kv_cache *cache, const tetra_kv_rows *rows, void *stream);
 
+/* Positions apart from slots, on several axes (time, height and width of pictures): positions int32 [rows][axes], rows `stride`
+ * elements apart; axis uint8 [head_dim / 2], below axes; device memory.  axes: 1 to TETRA_KV_MAX_AXES. */
+typedef struct {
+    const int32_t *positions;
+    const uint8_t *axis;
+    int64_t stride;
+    int32_t axes;
+} tetra_kv_axes;
+
+/* tetra_kv_append, but for the angle: row r turns pair i by positions[r][axis[i]] * inv_freq[i], in 64 bits.  Positions may be
+ * negative; an axis that is not below axes does not turn its pairs.  Where a row's key and value go is, as there, the next
+ * slot of its sequence (row_start, lengths).  inv_freq is required.  One launch. */
+int tetra_kv_append_at(const tetra_kv_cache *cache, const tetra_kv_rows *rows, const tetra_kv_axes *axes, void *stream);
+
 /* What the cache holds for the rows' positions, as values: k_out, v_out float16 [rows][kv_heads][head_dim] (16-byte
  * aligned), code * scale rounded once; zero for a position without a place.  The rows are given by row_start and
  * lengths alone: reading a whole sequence takes lengths 0 and as many rows as it has tokens. */
@@ -128,7 +143,7 @@ size_t tetra_kv_shared_workspace_bytes(int head_dim, int rows, int q_heads, int 
  * all of its rows, through the page table of the first of its sequences that take part.  Whole blocks are shared, the tokens
  * behind them are read by each sequence.  A sequence takes part where it has rows and lengths[s] is not below the shared
  * tokens of whole blocks; the others of the group, and a group with fewer than two that do, read all of their tokens
- * themselves.  Two launches. */
+themselves.  Three launches. */
 int tetra_kv_attend_shared(const tetra_kv_cache *cache, const tetra_kv_groups *groups, const void *q, int64_t q_stride,
                            void *out, int rows, int q_heads, float scale, void *workspace, size_t workspace_bytes,
                            void *stream);

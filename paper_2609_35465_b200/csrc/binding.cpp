@@ -47,6 +47,7 @@ struct Api {
     decltype(&tetra_q4_rows) q4_rows;
     decltype(&tetra_q4_list_run) q4_list_run;
     decltype(&tetra_kv_append) kv_append;
+    decltype(&tetra_kv_append_at) kv_append_at;
     decltype(&tetra_kv_read) kv_read;
     decltype(&tetra_kv_attend) kv_attend;
     decltype(&tetra_kv_attend_shared) kv_attend_shared;
@@ -417,34 +418,57 @@ double real(PyObject* o) {
     return v;
 }
 
+// a: q, k, v, q_out, inv_freq, q_weight, k_weight, eps
+tetra_kv_rows kv_rows_of(PyObject* const* a, const tetra_kv_cache& c, const char* what) {
+    const at::ScalarType type = tensor(a[1]).scalar_type();
+    if (type != at::kFloat && type != at::kHalf) fail(tetra_error, "%s k: %s, the call takes Float or Half", what, c10::toString(type));
+    const int64_t rows = tensor(a[1]).dim() == 3 ? tensor(a[1]).size(0) : 0, D = c.head_dim;
+    tetra_kv_rows r = {};
+    int64_t heads = 0;
+    r.k = rows_of_heads(a[1], type, rows, D, what, "k", heads, r.k_stride);
+    if (heads != c.kv_heads) fail(tetra_error, "%s k: wrong shape", what);
+    r.v = rows_of_heads(a[2], type, rows, D, what, "v", heads, r.v_stride);
+    if (heads != c.kv_heads) fail(tetra_error, "%s v: wrong shape", what);
+    if ((a[0] == Py_None) != (a[3] == Py_None)) fail(tetra_error, "%s: q and q_out are given together", what);
+    if (a[0] != Py_None) {
+        r.q = rows_of_heads(a[0], type, rows, D, what, "q", heads, r.q_stride);
+        r.q_heads = narrow(heads, what, "q");
+        r.q_out = shaped(a[3], at::kHalf, {rows, heads, D}, what, "q_out");
+    }
+    if (a[4] != Py_None) r.inv_freq = static_cast<const double*>(shaped(a[4], at::kDouble, {D / 2}, what, "inv_freq"));
+    if (a[5] != Py_None) r.q_weight = static_cast<const float*>(shaped(a[5], at::kFloat, {D}, what, "q_weight"));
+    if (a[6] != Py_None) r.k_weight = static_cast<const float*>(shaped(a[6], at::kFloat, {D}, what, "k_weight"));
+    r.eps = real(a[7]);
+    r.rows = narrow(rows, what, "k");
+    r.half_type = type == at::kHalf;
+    return r;
+}
 // cache, page_table, row_start, lengths, q, k, v, q_out, inv_freq, q_weight, k_weight, eps, stream
 FASTCALL(py_kv_append) {
     return guarded(n, 13, [&] {
         const char* what = "tetra_kv_append";
         const tetra_kv_cache c = kv_cache_of(a, what);
-        const at::ScalarType type = tensor(a[5]).scalar_type();
-        if (type != at::kFloat && type != at::kHalf) fail(tetra_error, "%s k: %s, the call takes Float or Half", what, c10::toString(type));
-        const int64_t rows = tensor(a[5]).dim() == 3 ? tensor(a[5]).size(0) : 0, D = c.head_dim;
-        tetra_kv_rows r = {};
-        int64_t heads = 0;
-        r.k = rows_of_heads(a[5], type, rows, D, what, "k", heads, r.k_stride);
-        if (heads != c.kv_heads) fail(tetra_error, "%s k: wrong shape", what);
-        r.v = rows_of_heads(a[6], type, rows, D, what, "v", heads, r.v_stride);
-        if (heads != c.kv_heads) fail(tetra_error, "%s v: wrong shape", what);
-        if ((a[4] == Py_None) != (a[7] == Py_None)) fail(tetra_error, "%s: q and q_out are given together", what);
-        if (a[4] != Py_None) {
-            r.q = rows_of_heads(a[4], type, rows, D, what, "q", heads, r.q_stride);
-            r.q_heads = narrow(heads, what, "q");
-            r.q_out = shaped(a[7], at::kHalf, {rows, heads, D}, what, "q_out");
-        }
-        if (a[8] != Py_None) r.inv_freq = static_cast<const double*>(shaped(a[8], at::kDouble, {D / 2}, what, "inv_freq"));
-        if (a[9] != Py_None) r.q_weight = static_cast<const float*>(shaped(a[9], at::kFloat, {D}, what, "q_weight"));
-        if (a[10] != Py_None) r.k_weight = static_cast<const float*>(shaped(a[10], at::kFloat, {D}, what, "k_weight"));
-        r.eps = real(a[11]);
-        r.rows = narrow(rows, what, "k");
-        r.half_type = type == at::kHalf;
+        const tetra_kv_rows r = kv_rows_of(a + 4, c, what);
         void* s = stream_of(a[12]);
-        if (rows > 0) check(unlocked([&] { return api.kv_append(&c, &r, s); }), what);
+        if (r.rows > 0) check(unlocked([&] { return api.kv_append(&c, &r, s); }), what);
+        return same(a[7]);
+    });
+}
+// cache, page_table, row_start, lengths, q, k, v, q_out, inv_freq, q_weight, k_weight, eps, positions, axis, stream
+FASTCALL(py_kv_append_at) {
+    return guarded(n, 15, [&] {
+        const char* what = "tetra_kv_append_at";
+        const tetra_kv_cache c = kv_cache_of(a, what);
+        const tetra_kv_rows r = kv_rows_of(a + 4, c, what);
+        const at::Tensor& p = typed(a[12], at::kInt, what, "positions");
+        if (p.dim() != 2 || p.size(0) != r.rows || (p.stride(1) != 1 && p.size(1) > 1)) fail(tetra_error, "%s positions: wrong shape", what);
+        tetra_kv_axes t;
+        t.positions = static_cast<const int32_t*>(p.data_ptr());
+        t.axes = narrow(p.size(1), what, "positions");
+        t.stride = r.rows > 1 ? p.stride(0) : p.size(1);
+        t.axis = static_cast<const uint8_t*>(shaped(a[13], at::kByte, {c.head_dim / 2}, what, "axis"));
+        void* s = stream_of(a[14]);
+        if (r.rows > 0) check(unlocked([&] { return api.kv_append_at(&c, &r, &t, s); }), what);
         return same(a[7]);
     });
 }
@@ -564,6 +588,7 @@ FASTCALL(py_setup) {
         get(api.q4_rows, "tetra_q4_rows");
         get(api.q4_list_run, "tetra_q4_list_run");
         get(api.kv_append, "tetra_kv_append");
+        get(api.kv_append_at, "tetra_kv_append_at");
         get(api.kv_read, "tetra_kv_read");
         get(api.kv_attend, "tetra_kv_attend");
         get(api.kv_attend_shared, "tetra_kv_attend_shared");
@@ -577,7 +602,7 @@ FASTCALL(py_setup) {
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(setup),        METHOD(gemv),          METHOD(gemv_tail), METHOD(gemv_noalloc), METHOD(gemv_batched),
                          METHOD(gemv_list),    METHOD(grouped_run),   METHOD(pack_codes), METHOD(decode_packed), METHOD(encode_blocks),
-                         METHOD(q4_pack),      METHOD(q4_gemv),       METHOD(q4_rows),   METHOD(q4_list_run),  METHOD(kv_append),
+                         METHOD(q4_pack),      METHOD(q4_gemv),       METHOD(q4_rows),   METHOD(q4_list_run),  METHOD(kv_append), METHOD(kv_append_at),
                          METHOD(kv_read),      METHOD(kv_attend),     METHOD(kv_attend_shared), METHOD(sample),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of the Tetra C ABI.", -1, methods,

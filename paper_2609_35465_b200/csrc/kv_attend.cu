@@ -22,8 +22,8 @@
 // that is attended to from its bits, and 2^-32 of the largest is still seen.  The denominator sums 2^(score - m) in float32.
 // m moves only when a weight would pass 2^15: a vote per block, a reduction when it does.
 //
-// SHARED: the second kernel of tetra_kv_attend_shared.  The first blocks of a sequence that shares them with others are in pieces that
-// k_kv_prefix left: here they are not read, and the pieces are added to a column's sums before it is stored.
+// SHARED: the second kernel of tetra_kv_attend_shared.  The first blocks of a sequence that shares them with others are k_kv_prefix's:
+// here they are not read, and the columns' sums are left for k_kv_join.
 #include <cfloat>
 #include <cmath>
 
@@ -66,6 +66,7 @@ struct Seg {
     uint32_t r0, r1;       // blocks, of those that the item's last row sees (SHARED: behind the shared ones)
     int32_t first, last;   // CTAs that the item begins and ends in
     int32_t before;        // tokens before the step
+    bool joined;           // SHARED: what is stored are sums, which others are added to
 };
 
 struct AttParams {
@@ -79,8 +80,9 @@ struct AttParams {
     // A CTA may be an item's last and the next one's first: what it keeps for either is apart (second: of the item that begins in it).
     float* pieces;         // [CTA][4][PIECE]: pieces, then groups' sums, two each
     uint32_t* arrived;     // [3][CTA]: pieces of the groups that begin in this CTA, two; groups of the item that begins in it
-    const SharedSeq* shared;      // SHARED: by sequence,
-    const float* shared_pieces;   // and what k_kv_prefix left
+    const SharedSeq* shared;  // SHARED: by sequence
+    float* own;               // SHARED: [row][head][D] sums and, behind them, [row][head][2] references and denominators
+    int64_t own_ends;         // where these begin
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -129,6 +131,7 @@ struct Work {
     int32_t row0, rows, before;
     uint32_t chunks, blocks, units;
     uint32_t first;  // SHARED: blocks that are not read here
+    bool joined;
 };
 template <int NT, bool SHARED>
 __device__ __forceinline__ Work sequence_work(const AttParams& p, int s) {
@@ -143,8 +146,11 @@ __device__ __forceinline__ Work sequence_work(const AttParams& p, int s) {
     const uint32_t n = seen <= 0 ? 0u : uint32_t((seen + kKvBlock - 1) / kKvBlock);
     w.blocks = min(n, most);
     w.first = 0;
+    w.joined = false;
     if (SHARED) {
-        w.first = min(uint32_t(__ldcg(&p.shared[s].first)), w.blocks);
+        const uint32_t first = uint32_t(__ldg(&p.shared[s].first));
+        w.joined = first > 0;
+        w.first = min(first, w.blocks);
         w.blocks -= w.first;
     }
     w.units = max(1u, (w.blocks + (kAttWarps << p.unit_shift) - 1) / (kAttWarps << p.unit_shift));
@@ -160,6 +166,7 @@ __device__ __forceinline__ void set_seg(const AttParams& p, const Work& w, int s
     q.col0 = int(item - head * w.chunks) * 8 * NT;
     q.cols = w.rows * p.group;
     q.before = w.before;
+    q.joined = w.joined;
     q.first = first;
     q.last = last;
     const uint32_t rows = q.col0 + 8 * NT >= q.cols ? w.rows : (q.col0 + 8 * NT - 1) / uint32_t(p.group) + 1;  // up to the item's last
@@ -217,61 +224,6 @@ __device__ __forceinline__ void block_sums(uint32_t (&v)[N], uint32_t (*warp_sum
     __syncthreads();
 }
 
-// SHARED: adds to a column's sums (v, of `N` values from float `at` of a piece's column; reference r, denominator u) those of its pieces,
-// in order; four at a time are on the way.
-template <int N>
-__device__ __forceinline__ void add_pieces(const AttParams& p, int D, const PieceRange& range, int at, float (&v)[N], float& r, float& u) {
-    constexpr int BATCH = 4;
-    const size_t piece = size_t(pre_piece(D));
-    const float* from = p.shared_pieces + size_t(range.first) * piece + range.column * 4 + at / 4 * (4 * kPreColumns) + at % 4;
-    const float* ends = p.shared_pieces + size_t(range.first) * piece + kPreColumns * D + range.column * 2;
-#pragma unroll 1
-    for (int i = 0; i < range.count; i += BATCH) {
-        float x[BATCH][N];
-        float2 m[BATCH];
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            const size_t to = size_t(min(i + k, range.count - 1)) * range.step * piece;
-            m[k] = __ldcg(reinterpret_cast<const float2*>(ends + to));
-            if (N == 2) {
-                const float2 y = __ldcg(reinterpret_cast<const float2*>(from + to));
-                x[k][0] = y.x, x[k][1] = y.y;
-            } else {
-                const float4 y = __ldcg(reinterpret_cast<const float4*>(from + to));
-                x[k][0] = y.x, x[k][1] = y.y, x[k][N - 2] = y.z, x[k][N - 1] = y.w;
-            }
-        }
-        float now = r;
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            if (i + k >= range.count) m[k].y = 0.f;
-            if (m[k].y != 0.f) now = fmaxf(now, m[k].x);  // 0: nothing seen, and nothing written
-        }
-        const float f = ex2(r - now);
-        u *= f;
-#pragma unroll
-        for (int n = 0; n < N; ++n) v[n] *= f;
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            const bool is = m[k].y != 0.f;
-            const float g = is ? ex2(m[k].x - now) : 0.f;
-            u = is ? fmaf(m[k].y, g, u) : u;
-#pragma unroll
-            for (int n = 0; n < N; ++n) v[n] = is ? fmaf(x[k][n], g, v[n]) : v[n];
-        }
-        r = now;
-    }
-}
-
-template <int D>
-__device__ __forceinline__ PieceRange range_of(const AttParams& p, const Seg& sg, uint32_t col) {
-    const uint4* at = reinterpret_cast<const uint4*>(p.shared + sg.seq);
-    const uint4 a = __ldcg(at), b = __ldcg(at + 1);
-    const SharedSeq s{int32_t(a.x), int32_t(a.y), int32_t(a.z), int32_t(a.w), int32_t(b.x), int32_t(b.y), {0, 0}};
-    if (s.first == 0) return PieceRange{0, 0, 0, 0};
-    return pieces_of<D>(s, sg.head, uint32_t(sg.row0 - s.row0) * p.group + col);
-}
-
 template <int D, int NT, bool SHARED>
 __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(AttParams p) {
     using C = AttCfg<D, NT>;
@@ -284,7 +236,6 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     __shared__ Seg segs[kAttSegs];
     __shared__ int nsegs, cursor_seq;
     __shared__ int64_t places[2][8 * NT];  // of an item's columns in the output, or -1; the next item's apart
-    __shared__ PieceRange ranges[2][SHARED ? 8 * NT : 1];
     __shared__ uint32_t cursor_unit, is_last, the_share, are_few, are_tiny, warp_sums[4][kAttWarps];
 
     // (What all lanes of a warp have alike is taken from lane 0 here and below: branches on it need no reconvergence.)
@@ -308,7 +259,7 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     if (p.c.seqs <= 32) {
         if (warp == 0) {
             const bool is = lane < p.c.seqs;
-            Work w = is ? sequence_work<NT, SHARED>(p, lane) : Work{0, 0, 0, 0, 0, 1, 0};
+            Work w = is ? sequence_work<NT, SHARED>(p, lane) : Work{0, 0, 0, 0, 0, 1, 0, false};
             const uint32_t items = w.chunks * heads, all_items = __reduce_add_sync(0xFFFFFFFFu, items), all_units = __reduce_add_sync(0xFFFFFFFFu, items * w.units);
             const uint32_t even = (all_units + G - 1) / G;
             if (all_items <= G) {
@@ -566,7 +517,6 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
                     at = (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D;
                 }
                 places[i & 1][threadIdx.x] = at;
-                if (SHARED) ranges[i & 1][threadIdx.x] = at < 0 ? PieceRange{0, 0, 0, 0} : range_of<D>(p, sg, col);
             }
             // Last position of the lane's columns (2 t, 2 t + 1 of each eight), and of the item's first.
             int sees[NT][2];
@@ -692,13 +642,13 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int64_t at = places[i & 1][nt * 8 + 2 * t + k];
-                    float s = k ? s_odd : s_even, x[2] = {v[k], v[k + 2]};
-                    if (SHARED) {
-                        float r = k ? r_odd : r_even;
-                        add_pieces<2>(p, D, ranges[i & 1][nt * 8 + 2 * t + k], d, x, r, s);
+                    const float s = k ? s_odd : s_even, by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
+                    if (SHARED && sg.joined && at >= 0) {
+                        __stcg(reinterpret_cast<float2*>(p.own + at + d), make_float2(v[k], v[k + 2]));
+                        if (d == 0) __stcg(reinterpret_cast<float2*>(p.own + p.own_ends) + at / D, make_float2(k ? r_odd : r_even, s));
+                        continue;
                     }
-                    const float by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
-                    if (at >= 0) *reinterpret_cast<__half2*>(p.out + at + d) = __floats2half2_rn(x[0] * by, x[1] * by);
+                    if (at >= 0) *reinterpret_cast<__half2*>(p.out + at + d) = __floats2half2_rn(v[k] * by, v[k + 2] * by);
                 }
             };
 
@@ -723,21 +673,20 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const uint32_t col = sg.col0 + 2 * t + k, row = quotient(col, p.group), h = col - row * p.group;
-                    float s = sum[0][k], by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
+                    const float s = sum[0][k], by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
                     if (int(col) >= sg.cols) continue;
-                    __half* out = p.out + (int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h) * D + 4 * g;
-                    PieceRange range;
-                    if (SHARED) range = range_of<D>(p, sg, col);
+                    const int64_t at = int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h;
+                    if (SHARED && sg.joined) {
+#pragma unroll
+                        for (int j = 0; j < CHUNKS; ++j)
+                            __stcg(reinterpret_cast<float4*>(p.own + at * D + 4 * g + 32 * j), make_float4(o[2 * j][k], o[2 * j][k + 2], o[2 * j + 1][k], o[2 * j + 1][k + 2]));
+                        if (g == 0) __stcg(reinterpret_cast<float2*>(p.own + p.own_ends) + at, make_float2(ref[0][k], s));
+                        continue;
+                    }
+                    __half* out = p.out + at * D + 4 * g;
 #pragma unroll
                     for (int j = 0; j < CHUNKS; ++j) {
-                        float x[4] = {o[2 * j][k], o[2 * j][k + 2], o[2 * j + 1][k], o[2 * j + 1][k + 2]};
-                        if (SHARED) {
-                            float r = ref[0][k];
-                            s = sum[0][k];
-                            add_pieces<4>(p, D, range, 32 * j + 4 * g, x, r, s);
-                            by = s == 0.f ? 0.f : 1.f / s;
-                        }
-                        const __half2 lo = __floats2half2_rn(x[0] * by, x[1] * by), hi = __floats2half2_rn(x[2] * by, x[3] * by);
+                        const __half2 lo = __floats2half2_rn(o[2 * j][k] * by, o[2 * j][k + 2] * by), hi = __floats2half2_rn(o[2 * j + 1][k] * by, o[2 * j + 1][k + 2] * by);
                         *reinterpret_cast<uint2*>(out + 32 * j) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
                     }
                 }
@@ -922,14 +871,9 @@ int attend_params(const tetra_kv_cache* cache, const void* q, int64_t q_stride, 
     p.arrived = static_cast<uint32_t*>(workspace);
     p.pieces = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + kAttCounters);
     p.shared = nullptr;
-    p.shared_pieces = nullptr;
+    p.own = nullptr;
+    p.own_ends = 0;
     return TETRA_OK;
-}
-
-// The workspace of tetra_kv_attend_shared: that of tetra_kv_attend, the sequences' shares, the pieces.
-constexpr size_t kSharedSeqs = size_t(TETRA_KV_MAX_SEQS) * sizeof(SharedSeq);
-size_t shared_workspace(int D, int64_t rows, int q_heads, int kv_heads, int groups) {
-    return (tetra_kv_workspace_bytes(D) + 255) / 256 * 256 + kSharedSeqs + prefix_bytes(D, prefix_parts_most(D, rows, q_heads, kv_heads, groups));
 }
 
 }  // namespace
@@ -957,7 +901,7 @@ size_t tetra_kv_shared_workspace_bytes(int head_dim, int rows, int q_heads, int 
     if (tetra_kv_workspace_bytes(head_dim) == 0 || rows < 0 || rows > TETRA_KV_MAX_ROWS || kv_heads < 1 || kv_heads > 1024 || q_heads < 1 || q_heads > 4096 ||
         q_heads % kv_heads || groups < 0 || groups > TETRA_KV_MAX_SEQS)
         return 0;
-    return shared_workspace(head_dim, rows, q_heads, kv_heads, groups);
+    return SharedPlaces(head_dim, rows, q_heads, kv_heads, groups).end;
 }
 
 int tetra_kv_attend_shared(const tetra_kv_cache* cache, const tetra_kv_groups* groups, const void* q, int64_t q_stride, void* out, int rows, int q_heads, float scale,
@@ -974,13 +918,28 @@ int tetra_kv_attend_shared(const tetra_kv_cache* cache, const tetra_kv_groups* g
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int D = cache->head_dim;
     if (groups->groups == 0) return kv_status(launch_attend_all<false>(p, D, sms, s));
-    unsigned char* at = static_cast<unsigned char*>(workspace) + (tetra_kv_workspace_bytes(D) + 255) / 256 * 256;
-    p.shared = reinterpret_cast<const SharedSeq*>(at);
-    p.shared_pieces = reinterpret_cast<const float*>(at + kSharedSeqs);
-    const cudaError_t e = launch_prefix(*cache, rows, PrefixGroups{groups->group_start, groups->shared, groups->groups}, q, q_stride, p.scale, p.group, D, at,
-                                        reinterpret_cast<float*>(at + kSharedSeqs), prefix_parts_most(D, rows, q_heads, cache->kv_heads, groups->groups), s);
-    if (e != cudaSuccess) return TETRA_ERR_CUDA;
-    return kv_status(launch_attend_all<true>(p, D, sms, s));
+    const SharedPlaces at(D, rows, q_heads, cache->kv_heads, groups->groups);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    SharedCall call;
+    call.c = p.c;
+    call.g = *groups;
+    call.q = p.q;
+    call.out = p.out;
+    call.q_stride = q_stride;
+    call.scale = p.scale;
+    call.group = p.group;
+    call.seqs = reinterpret_cast<SharedSeq*>(ws + at.seqs);
+    call.own = reinterpret_cast<float*>(ws + at.own);
+    call.own_ends = int64_t(rows) * q_heads * D;
+    call.pieces = reinterpret_cast<float*>(ws + at.pieces);
+    call.most = uint32_t(at.parts);
+    p.shared = call.seqs;
+    p.own = call.own;
+    p.own_ends = call.own_ends;
+    cudaError_t e = launch_prefix(call, D, sms, s);
+    if (e == cudaSuccess) e = launch_attend_all<true>(p, D, sms, s);
+    if (e == cudaSuccess) e = launch_join(call, D, s);
+    return kv_status(e);
 }
 
 }  // extern "C"

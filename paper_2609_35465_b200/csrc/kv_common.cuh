@@ -40,6 +40,24 @@ struct KvCache {
     }
 };
 
+// The sequence of row r, or -1; its rows [a, b).  row_start does not decrease: a warp finds the place in two steps, among every
+// so many entries and then among those between two of them.
+static_assert(TETRA_KV_MAX_SEQS < 32 * 33, "two steps of 32 lanes");
+__device__ __forceinline__ int sequence_of(const KvCache& c, int r, int lane, int& a, int& b) {
+    const int entries = c.seqs + 1, stride = (entries + 31) / 32;
+    int at = lane * stride;
+    int s = __popc(__ballot_sync(0xFFFFFFFFu, at < entries && __ldg(c.row_start + at) <= r));
+    if (s == 0) return -1;
+    s = (s - 1) * stride;
+    if (stride > 1) {
+        at = s + 1 + lane;
+        s += __popc(__ballot_sync(0xFFFFFFFFu, lane < stride - 1 && at < entries && __ldg(c.row_start + at) <= r));
+    }
+    if (s >= c.seqs) return -1;
+    c.rows_of(s, a, b);
+    return a <= r && r < b ? s : -1;
+}
+
 inline bool kv_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 inline bool kv_shape_ok(int pages, int page_tokens, int kv_heads, int D) {

@@ -34,10 +34,10 @@ constexpr int kPreSoft = 8, kPreConvert = 4;              // warps
 constexpr int kPreConvertAt = kPreSoft, kPreCopyWarp = kPreSoft + kPreConvert, kPreMmaWarp = kPreCopyWarp + 1;
 constexpr int kPreThreads = (kPreMmaWarp + 1) * 32;
 constexpr int kPreScales = 8;                             // steps whose scales are kept
-constexpr int kPreMostCtas = 160, kPreWaves = 2;          // of a launch; parts a CTA where items are few
 constexpr uint32_t kPrePartCost = 6;                      // steps that a part's beginning and end take
 constexpr uint32_t kPreTries = 1u << 22;                  // of a wait: then the call's results are NaN
 constexpr float kPreNoRef = -FLT_MAX, kPreLeastLog = -60.f, kPreHigh = 15.f, kPreBase = 7.f;  // as in k_kv_attend
+constexpr float kPreMost = 32768.f;                       // 2^15
 
 template <int D>
 struct PreCfg {
@@ -52,17 +52,7 @@ struct PreCfg {
     static_assert(SLOTS * SLOT <= 512, "tensor memory");
 };
 
-struct PreParams {
-    KvCache c;
-    PrefixGroups g;
-    const __half* q;
-    int64_t q_stride;
-    float scale;        // times log2 e
-    int32_t group;      // query heads to a kv head
-    SharedSeq* seqs;
-    float* pieces;
-    uint32_t most;      // parts
-};
+using PreParams = SharedCall;
 
 // The plan, in shared memory, by group.
 struct PrePlan {
@@ -148,6 +138,13 @@ __device__ __forceinline__ void tensor_product(uint32_t d, uint32_t a, uint64_t 
 __device__ __forceinline__ void tensor_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// One lane of a whole warp, always the same.  (The compiler knows it to be one: with `lane == 0` in its place each product is issued
+// in a loop over the lanes that may be active, 140 cycles a product where it takes 45.)
+__device__ __forceinline__ bool elected() {
+    uint32_t is;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(is));
+    return is != 0;
+}
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -213,14 +210,14 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
     const int groups = p.g.groups, seqs = p.c.seqs, tid = threadIdx.x, lane = tid & 31;
     const int64_t most_tokens = int64_t(p.c.width) * p.c.blocks_per_page * kKvBlock;
     for (int g = tid; g < groups; g += kPreThreads) {
-        plan.start[g] = __ldg(p.g.start + g);
+        plan.start[g] = __ldg(p.g.group_start + g);
         const int tokens = __ldg(p.g.shared + g);
         plan.blocks[g] = int(min(int64_t(max(tokens, 0)), most_tokens) / kKvBlock);
         plan.count[g] = 0;
         plan.leader[g] = plan.row0[g] = INT_MAX;
         plan.rows_end[g] = 0;
     }
-    if (tid == 0) plan.start[groups] = __ldg(p.g.start + groups);
+    if (tid == 0) plan.start[groups] = __ldg(p.g.group_start + groups);
     __syncthreads();
 #pragma unroll 1
     for (int s = tid; s < seqs; s += kPreThreads) {
@@ -338,12 +335,46 @@ __device__ __forceinline__ bool part_of(const PreParams& p, const PrePlan& plan,
     return int(head) < p.c.kv_heads;
 }
 
+__device__ __forceinline__ uint64_t two_floats(float a, float b) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ void two_floats(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+// Weights of a block of 16 tokens, two and two as float16; returns the sum of 2^(score - ref).  scale: s_K times the call's, s_V, log2 s_V,
+// whether there is such a block.
+__device__ __forceinline__ float block_weights(const uint32_t* scores, const float4& scale, float ref, uint32_t* weights) {
+    if (scale.w == 0.f) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) weights[k] = 0u;
+        return 0.f;
+    }
+    const uint64_t by = two_floats(scale.x, scale.x), from = two_floats(-ref, -ref), times = two_floats(scale.y, scale.y);
+    uint64_t sum = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        uint64_t x, e, w;
+        float a, b;
+        asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(two_floats(__uint_as_float(scores[2 * k]), __uint_as_float(scores[2 * k + 1]))), "l"(by), "l"(from));
+        two_floats(x, a, b);
+        e = two_floats(pre_ex2(a), pre_ex2(b));
+        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(sum) : "l"(sum), "l"(e));
+        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(w) : "l"(e), "l"(times));
+        two_floats(w, a, b);
+        const __half2 h = __floats2half2_rn(a, b);
+        weights[k] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    float a, b;
+    two_floats(sum, a, b);
+    return a + b;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     using C = PreCfg<D>;
     constexpr int SLOTS = C::SLOTS, STAGES = C::STAGES, CHUNKS = D / 32;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t raw_full[STAGES], raw_empty[STAGES], k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2], p_ready[2], o_done[2],
+    __shared__ __align__(8) uint64_t raw_full[STAGES], raw_empty[STAGES], tile_full[2], tile_empty[2], q_ready[2], s_full[2], p_ready[2], o_done[2],
         scales_full[kPreScales], drained;
     __shared__ __align__(16) float4 scales[kPreScales][kPreBlocks];  // s_K times the call's, s_V, log2 s_V, whether there is such a block
     __shared__ uint32_t placed[STAGES], total, tensor_base;
@@ -366,8 +397,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         failed = 0;
         for (int i = 0; i < STAGES; ++i) bar_init(smem_u32(raw_full + i), 1), bar_init(smem_u32(raw_empty + i), kPreConvert);
         for (int i = 0; i < 2; ++i) {
-            bar_init(smem_u32(k_full + i), kPreConvert), bar_init(smem_u32(v_full + i), kPreConvert);
-            bar_init(smem_u32(k_empty + i), 1), bar_init(smem_u32(v_empty + i), 1);
+            bar_init(smem_u32(tile_full + i), kPreConvert), bar_init(smem_u32(tile_empty + i), 1);
             bar_init(smem_u32(q_ready + i), 4), bar_init(smem_u32(p_ready + i), 4);
             bar_init(smem_u32(s_full + i), 1), bar_init(smem_u32(o_done + i), 1);
         }
@@ -435,7 +465,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
             if (!part_of<D>(p, plan, at, q)) continue;
             for (uint32_t step = q.begin; step < q.end; ++step, ++n) {
                 const uint32_t stage = n % STAGES, from = ring + stage * C::STAGE, two = n & 1u, parity = (n >> 1 & 1u) ^ 1u;
-                ok = bar_wait(smem_u32(raw_full + stage), n / STAGES & 1u, gave_up) && bar_wait(smem_u32(k_empty + two), parity, gave_up);
+                ok = bar_wait(smem_u32(raw_full + stage), n / STAGES & 1u, gave_up) && bar_wait(smem_u32(tile_empty + two), parity, gave_up);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 if (w == 0) {
                     if (lane < kPreBlocks) {
@@ -463,11 +493,6 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                         }
                     }
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_u32(k_full + two));
-                ok = bar_wait(smem_u32(v_empty + two), parity, gave_up);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 {
                     const uint32_t to = base + (2 + two) * C::TILE;
 #pragma unroll
@@ -485,64 +510,67 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    bar_arrive(smem_u32(v_full + two));
+                    bar_arrive(smem_u32(tile_full + two));
                     bar_arrive(smem_u32(raw_empty + stage));
                 }
             }
         }
     } else if (warp == kPreMmaWarp) {
         // ---- products, issued by one thread
-        if (lane == 0) {
-            bool ok = true;
-            uint32_t jobs_of[2] = {0, 0}, q_of[2] = {0, 0};
-            for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
-                PrePart q;
-                if (!part_of<D>(p, plan, at, q)) continue;
-                const uint32_t steps = q.end - q.begin;
-                const bool halves = SLOTS == 2 && !q.both;  // each step is both slots' work
-                const uint32_t jobs = halves ? 2 * steps : steps;
-                auto step_of = [&](uint32_t job) { return n0 + (halves ? job >> 1 : job); };
-                auto scores = [&](uint32_t job) {
-                    const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, n = step_of(job), two = n & 1u;
-                    if (job < uint32_t(SLOTS)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_of[slot]++ & 1u, gave_up);
-                    ok = ok && bar_wait(smem_u32(k_full + two), n >> 1 & 1u, gave_up);
-                    if (!ok) return;
-                    fence_after();
-                    const uint32_t to = tensor + slot * C::SLOT + C::QCOLS, a = tensor + slot * C::SLOT;
+        bool ok = true;
+        uint32_t jobs_of[2] = {0, 0}, q_of[2] = {0, 0};
+        const uint64_t tiles = tile_descriptor(base);
+        for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
+            PrePart q;
+            if (!part_of<D>(p, plan, at, q)) continue;
+            const uint32_t steps = q.end - q.begin;
+            const bool halves = SLOTS == 2 && !q.both;  // each step is both slots' work
+            const uint32_t jobs = halves ? 2 * steps : steps;
+            auto step_of = [&](uint32_t job) { return n0 + (halves ? job >> 1 : job); };
+            auto scores = [&](uint32_t job) {
+                const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, n = step_of(job), two = n & 1u;
+                if (job < uint32_t(SLOTS)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_of[slot]++ & 1u, gave_up);
+                if (!halves || slot == 0) ok = ok && bar_wait(smem_u32(tile_full + two), n >> 1 & 1u, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; return; }
+                fence_after();
+                if (elected()) {
+                    const uint32_t a = tensor + slot * C::SLOT, to = a + C::QCOLS;
+                    const uint64_t b = tiles + (two * C::TILE >> 4);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        tensor_product(to, a + k * 8, tile_descriptor(base + two * C::TILE + k / 4 * (kPreStep * 128) + k % 4 * 32), product_kind(kPreStep), k > 0);
+                    for (int k = 0; k < D / 16; ++k) tensor_product(to, a + k * 8, b + ((k / 4 * (kPreStep * 128) + k % 4 * 32) >> 4), product_kind(kPreStep), k > 0);
                     tensor_commit(smem_u32(s_full + slot));
-                    if (!halves || slot == 1) tensor_commit(smem_u32(k_empty + two));
-                };
-                for (uint32_t job = 0; ok && job < uint32_t(SLOTS) && job < jobs; ++job) scores(job);
-                for (uint32_t job = 0; ok && job < jobs; ++job) {
-                    const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, n = step_of(job), two = n & 1u;
-                    ok = ok && bar_wait(smem_u32(v_full + two), n >> 1 & 1u, gave_up);
-                    ok = ok && bar_wait(smem_u32(p_ready + slot), jobs_of[slot]++ & 1u, gave_up);
-                    if (!ok) break;
-                    fence_after();
-                    const uint32_t a = tensor + slot * C::SLOT + C::QCOLS, to = a + kPreStep;
-#pragma unroll
-                    for (int k = 0; k < kPreStep / 16; ++k)
-                        tensor_product(to, a + k * 8, tile_descriptor(base + (2 + two) * C::TILE + k * 32), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
-                    tensor_commit(smem_u32(o_done + slot));
-                    if (!halves || slot == 1) tensor_commit(smem_u32(v_empty + two));
-                    if (job + SLOTS < jobs) scores(job + SLOTS);
                 }
-                n0 += steps;
+                __syncwarp();
+            };
+            for (uint32_t job = 0; ok && job < uint32_t(SLOTS) && job < jobs; ++job) scores(job);
+            for (uint32_t job = 0; ok && job < jobs; ++job) {
+                const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, n = step_of(job), two = n & 1u;
+                ok = bar_wait(smem_u32(p_ready + slot), jobs_of[slot]++ & 1u, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                fence_after();
+                if (elected()) {
+                    const uint32_t a = tensor + slot * C::SLOT + C::QCOLS, to = a + kPreStep;
+                    const uint64_t b = tiles + ((2 + two) * C::TILE >> 4);
+#pragma unroll
+                    for (int k = 0; k < kPreStep / 16; ++k) tensor_product(to, a + k * 8, b + (k * 32 >> 4), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
+                    if (job + SLOTS >= jobs) tensor_commit(smem_u32(o_done + slot));  // the slot's last of the part
+                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + two));
+                }
+                __syncwarp();
+                if (job + SLOTS < jobs) scores(job + SLOTS);
             }
-            // What was issued has ended when the tensor memory is given back.
-            int none = 0;
-            tensor_commit(smem_u32(&drained));
-            bar_wait(smem_u32(&drained), 0, &none);
+            n0 += steps;
         }
+        // What was issued has ended when the tensor memory is given back.
+        if (elected()) tensor_commit(smem_u32(&drained));
+        int none = 0;
+        bar_wait(smem_u32(&drained), 0, &none);
         __syncwarp();
     } else if (warp < 4 * SLOTS) {
         // ---- weights: a thread a column
         const uint32_t slot = warp >> 2, column = threadIdx.x & 127;
         const uint32_t at_q = tensor + slot * C::SLOT + ((warp & 3u) << 21), at_s = at_q + C::QCOLS, at_o = at_s + kPreStep;  // lanes from bit 16 on
-        uint32_t jobs = 0;
+        uint32_t jobs = 0, pieces_done = 0;
         bool ok = true;
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
@@ -578,36 +606,35 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 tensor_load(at_s, r);
                 tensor_load(at_s + 32, r + 32);
                 wait_loads();
-                float4 c[kPreBlocks];
-                float top[kPreBlocks];
+                // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
+                // column) call for a new one; as long as none does, no maximum is looked for.
+                uint32_t w[32];
+                float now[kPreBlocks];
+                const float4* c = scales[n % kPreScales];
                 bool over = false;
 #pragma unroll
                 for (int b = 0; b < kPreBlocks; ++b) {
-                    c[b] = scales[n % kPreScales][b];
-                    top[b] = -INFINITY;
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const float x = c[b].w != 0.f ? __uint_as_float(r[16 * b + k]) * c[b].x : -INFINITY;
-                        r[16 * b + k] = __float_as_uint(x);
-                        top[b] = fmaxf(top[b], x);
-                    }
-                    over |= top[b] - ref > kPreHigh - c[b].z;
+                    now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
+                    over |= now[b] * c[b].y > kPreMost;
                 }
                 if (__any_sync(0xFFFFFFFFu, over)) {
-                    float now = ref;
+                    float next = ref;
 #pragma unroll
                     for (int b = 0; b < kPreBlocks; ++b) {
-                        float want = top[b] + c[b].z - kPreBase;
-                        if (top[b] - want > kPreHigh - c[b].z) want = top[b];  // a step of so large scores is more than the room there is
-                        if (want > now) now = want;
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) top = fmaxf(top, __uint_as_float(r[16 * b + k]) * c[b].x);
+                        if (c[b].w == 0.f) top = -INFINITY;
+                        float want = top + c[b].z - kPreBase;
+                        if (top - want > kPreHigh - c[b].z) want = top;  // a step of so large scores is more than the room there is
+                        if (over && want > next) next = want;
                     }
-                    const float f = pre_ex2(ref - now);
-                    ref = now;
+                    const float f = pre_ex2(ref - next);
+                    ref = next;
                     sum *= f;
-                    if (i > first) {
-                        ok = bar_wait(smem_u32(o_done + slot), (jobs - 1) & 1u, gave_up);
-                        if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                        fence_after();
+#pragma unroll
+                    for (int b = 0; b < kPreBlocks; ++b) now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
+                    if (i > first) {  // the products before this step's scores have ended with them
 #pragma unroll 1
                         for (int j = 0; j < D; j += 32) {
                             uint32_t o[32];
@@ -619,28 +646,18 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                         }
                     }
                 }
-                uint32_t w[32];
 #pragma unroll
-                for (int b = 0; b < kPreBlocks; ++b) {
-#pragma unroll
-                    for (int k = 0; k < 16; k += 2) {
-                        const float x0 = __uint_as_float(r[16 * b + k]), x1 = __uint_as_float(r[16 * b + k + 1]);
-                        const float e0 = pre_ex2(x0 - ref), e1 = pre_ex2(x1 - ref);
-                        sum += e0 + e1;
-                        const __half2 h = __floats2half2_rn(e0 * c[b].y, e1 * c[b].y);
-                        w[8 * b + k / 2] = *reinterpret_cast<const uint32_t*>(&h);
-                    }
-                }
+                for (int b = 0; b < kPreBlocks; ++b) sum += now[b];
                 tensor_store(at_s, w);
                 wait_stores();
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_u32(p_ready + slot));
             }
-            // The piece: sums as [D / 4][column][4], then references and denominators.
+            // The piece: sums, then references and denominators.
             float* piece = p.pieces + (size_t(at) * SLOTS + slot) * pre_piece(D);
             if (ok && first < steps) {
-                ok = bar_wait(smem_u32(o_done + slot), (jobs - 1) & 1u, gave_up);
+                ok = bar_wait(smem_u32(o_done + slot), pieces_done++ & 1u, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (ok) {
                     fence_after();
@@ -651,8 +668,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                         wait_loads();
                         if (live) {
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                __stcg(reinterpret_cast<uint4*>(piece) + (j / 4 + k) * kPreColumns + column, make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
+                            for (int k = 0; k < 4; ++k)
+                                asm volatile("st.global.cg.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(piece + column * D + j + 8 * k), "r"(o[8 * k]), "r"(o[8 * k + 1]),
+                                             "r"(o[8 * k + 2]), "r"(o[8 * k + 3]), "r"(o[8 * k + 4]), "r"(o[8 * k + 5]), "r"(o[8 * k + 6]), "r"(o[8 * k + 7])
+                                             : "memory");
                         }
                     }
                     fence_before();
@@ -673,6 +692,81 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     if (warp == kPreMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
 }
 
+// A column's sums: of its own tokens and of its pieces, in this order, a warp a column.  A lane has D / 32 dims.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+
+// Four floats, or the two that there are.
+template <int E>
+__device__ __forceinline__ void load_four(const float* from, float* to) {
+    if constexpr (E == 2) {
+        const float2 v = __ldcg(reinterpret_cast<const float2*>(from));
+        to[0] = v.x, to[1] = v.y;
+    } else {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(from));
+        to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
+    }
+}
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) k_kv_join(PreParams p) {
+    constexpr int E = D / 32, BATCH = 32 / E;  // dims a lane; pieces that are on the way
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
+    pdl_wait();
+    pdl_release();
+    const int heads = p.c.kv_heads * p.group, h = blockIdx.y * kJoinWarps + warp, r = blockIdx.x;
+    int a, b;
+    const int s = h < heads ? sequence_of(p.c, r, lane, a, b) : -1;
+    if (s < 0) return;
+    const uint4 s0 = __ldcg(reinterpret_cast<const uint4*>(p.seqs + s)), s1 = __ldcg(reinterpret_cast<const uint4*>(p.seqs + s) + 1);
+    const SharedSeq share{int32_t(s0.x), int32_t(s0.y), int32_t(s0.z), int32_t(s0.w), int32_t(s1.x), int32_t(s1.y), {0, 0}};
+    if (share.first == 0) return;  // stored already
+    const int head = h / p.group;
+    const PieceRange range = pieces_of<D>(share, head, uint32_t(r - share.row0) * p.group + uint32_t(h - head * p.group));
+    const size_t piece = size_t(pre_piece(D)), step = piece * range.step;
+    const int64_t row = int64_t(r) * heads + h;
+    const float* from = p.pieces + size_t(range.first) * piece + range.column * D + lane * E;
+    const float* ends = p.pieces + size_t(range.first) * piece + kPreColumns * D + range.column * 2;
+    float v[E], ref, sum;
+    {
+        const float2 end = __ldcg(reinterpret_cast<const float2*>(p.own + p.own_ends) + row);
+#pragma unroll
+        for (int k = 0; k < E; k += 4) load_four<E>(p.own + row * D + lane * E + k, v + k);
+        ref = end.x;
+        sum = end.y;
+    }
+#pragma unroll 1
+    for (int i = 0; i < range.count; i += BATCH) {
+        float x[BATCH][E];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+#pragma unroll
+            for (int j = 0; j < E; j += 4) load_four<E>(from + size_t(min(i + k, range.count - 1)) * step + j, x[k] + j);
+        const bool mine = lane < BATCH && i + lane < range.count;
+        const float2 end = mine ? __ldcg(reinterpret_cast<const float2*>(ends + size_t(i + lane) * step)) : make_float2(kPreNoRef, 0.f);
+        // A denominator of zero: nothing seen, and no sums written.
+        float top = end.y != 0.f ? end.x : kPreNoRef;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const float now = fmaxf(ref, top), f = pre_ex2(ref - now), g = end.y != 0.f ? pre_ex2(end.x - now) : 0.f, part = end.y != 0.f ? end.y * g : 0.f;
+        sum *= f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] *= f;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            if (i + k >= range.count) break;
+            const float by = __shfl_sync(0xFFFFFFFFu, g, k);
+            const bool is = __shfl_sync(0xFFFFFFFFu, end.y, k) != 0.f;
+            sum += __shfl_sync(0xFFFFFFFFu, part, k);
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[j] = is ? fmaf(x[k][j], by, v[j]) : v[j];
+        }
+        ref = now;
+    }
+    const float by = sum == 0.f ? 0.f : 1.f / sum;
+    __half* out = p.out + row * D + lane * E;
+#pragma unroll
+    for (int k = 0; k < E; k += 2) *reinterpret_cast<__half2*>(out + k) = __floats2half2_rn(v[k] * by, v[k + 1] * by);
+}
+
 template <int D>
 cudaError_t launch_prefix_for(const PreParams& p, int sms, cudaStream_t s) {
     using C = PreCfg<D>;
@@ -682,32 +776,27 @@ cudaError_t launch_prefix_for(const PreParams& p, int sms, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     return launch_pdl(k_kv_prefix<D>, sms < kPreMostCtas ? sms : kPreMostCtas, kPreThreads, C::SMEM + PrePlan::bytes(p.g.groups), s, p);
 }
+template <int D>
+cudaError_t launch_join_for(const PreParams& p, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(p.c.rows), unsigned((p.c.kv_heads * p.group + kJoinWarps - 1) / kJoinWarps));
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_kv_join<D>, p);
+}
 
 }  // namespace
 
-size_t prefix_parts_most(int head_dim, int64_t rows, int q_heads, int kv_heads, int groups) {
-    const int64_t tile = pre_tile(head_dim), sharing = groups < rows / 2 ? groups : rows / 2;  // two sequences with a row each, at least
-    const int64_t items = (rows * (q_heads / kv_heads) / tile + sharing) * kv_heads, few = kPreWaves * kPreMostCtas;
-    return size_t(items > few ? items : few);
-}
-size_t prefix_bytes(int head_dim, size_t parts) { return parts * pre_slots(head_dim) * pre_piece(head_dim) * sizeof(float); }
-
-cudaError_t launch_prefix(const tetra_kv_cache& cache, int rows, const PrefixGroups& groups, const void* q, int64_t q_stride, float scale_log2, int q_group, int head_dim,
-                          void* seqs, float* pieces, size_t parts, cudaStream_t s) {
-    int sms = 0;
-    const cudaError_t e = device_sms(&sms);
-    if (e != cudaSuccess) return e;
-    PreParams p;
-    if (kv_check(&cache, rows, p.c) != TETRA_OK) return cudaErrorInvalidValue;
-    p.g = groups;
-    p.q = static_cast<const __half*>(q);
-    p.q_stride = q_stride;
-    p.scale = scale_log2;
-    p.group = q_group;
-    p.seqs = static_cast<SharedSeq*>(seqs);
-    p.pieces = pieces;
-    p.most = uint32_t(parts);
+cudaError_t launch_prefix(const SharedCall& p, int head_dim, int sms, cudaStream_t s) {
     return head_dim == 64 ? launch_prefix_for<64>(p, sms, s) : head_dim == 128 ? launch_prefix_for<128>(p, sms, s) : launch_prefix_for<256>(p, sms, s);
+}
+cudaError_t launch_join(const SharedCall& p, int head_dim, cudaStream_t s) {
+    return head_dim == 64 ? launch_join_for<64>(p, s) : head_dim == 128 ? launch_join_for<128>(p, s) : launch_join_for<256>(p, s);
 }
 
 }  // namespace tetra

@@ -112,6 +112,7 @@ def lib():
         L.tetra_kv_workspace_bytes.argtypes = [i32]
         L.tetra_kv_workspace_bytes.restype = sz
         L.tetra_kv_append.argtypes = [vp, vp, vp]
+        L.tetra_kv_append_at.argtypes = [vp, vp, vp, vp]
         L.tetra_kv_read.argtypes = [vp, vp, vp, i32, vp]
         L.tetra_sample.argtypes = [vp, vp]
         L.tetra_kv_attend.argtypes = [vp, vp, C.c_int64, vp, i32, i32, C.c_float, vp, sz, vp]
@@ -410,6 +411,11 @@ class KvRows(C.Structure):
                 ("v_stride", C.c_int64), ("eps", C.c_double), ("rows", C.c_int32), ("q_heads", C.c_int32), ("half_type", C.c_int32)]
 
 
+class KvAxes(C.Structure):
+    """Mirror of tetra_kv_axes."""
+    _fields_ = [("positions", C.c_void_p), ("axis", C.c_void_p), ("stride", C.c_int64), ("axes", C.c_int32)]
+
+
 class KvGroups(C.Structure):
     """Mirror of tetra_kv_groups."""
     _fields_ = [("group_start", C.c_void_p), ("shared", C.c_void_p), ("groups", C.c_int32)]
@@ -444,6 +450,15 @@ def tetra_kv_append(q, k, v, cache, page_table, row_start, lengths, q_out, inv_f
     q_out (float16 [rows, q_heads, D]) may be None together.  page_table int32 [seqs, width], row_start int32 [seqs + 1],
     lengths int32 [seqs]: tokens before this step.  inv_freq float64 [D / 2]; q_weight, k_weight float32 [D]: head norms."""
     return (_nat or _native()).kv_append(cache, page_table, row_start, lengths, q, k, v, q_out, inv_freq, q_weight, k_weight, eps, stream)
+
+
+def tetra_kv_append_at(q, k, v, cache, page_table, row_start, lengths, positions, axis, q_out, inv_freq, q_weight=None, k_weight=None,
+                       eps: float = 1e-6, stream=None):
+    """tetra_kv_append with positions given apart from the slots, on several axes; returns q_out.
+
+    positions int32 [rows, axes] (rows may lie apart), axis uint8 [D / 2], below axes: row r turns pair i by
+    positions[r, axis[i]] * inv_freq[i].  Everything else as in tetra_kv_append; lengths say where the rows are stored."""
+    return (_nat or _native()).kv_append_at(cache, page_table, row_start, lengths, q, k, v, q_out, inv_freq, q_weight, k_weight, eps, positions, axis, stream)
 
 
 def tetra_kv_read(cache, page_table, row_start, lengths, k_out, v_out, stream=None):
