@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtetra_b200.so")
 BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["tetra_tables.cpp", "tetra_decode.cu", "tetra_gemv.cu", "tetra_list.cu", "tetra_batched.cu", "tetra_api.cu", "tetra_noalloc.cu", "q4_gemv.cu", "q4_list.cu", "tetra_encode.cu",
-           "kv_append.cu", "kv_append_at.cu", "kv_attend.cu", "kv_prefix.cu", "sample.cu"]
+           "kv_append.cu", "kv_append_at.cu", "kv_attend.cu", "kv_prefix.cu", "sample.cu", "logprobs.cu"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
          "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "--use_fast_math"]

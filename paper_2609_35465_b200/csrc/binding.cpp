@@ -22,6 +22,7 @@
 
 #include "../../include/tetra.h"
 #include "../../include/tetra_kv.h"
+#include "../../include/tetra_logprobs.h"
 #include "../../include/tetra_q4.h"
 #include "../../include/tetra_sample.h"
 
@@ -52,6 +53,7 @@ struct Api {
     decltype(&tetra_kv_attend) kv_attend;
     decltype(&tetra_kv_attend_shared) kv_attend_shared;
     decltype(&tetra_sample) sample;
+    decltype(&tetra_logprobs) logprobs;
 } api;
 PyObject* tetra_error = nullptr;  // the exception class
 
@@ -559,6 +561,46 @@ FASTCALL(py_sample) {
     });
 }
 
+// logits, tokens, logprob, rank, entropy, top_tokens, top_logprob, temperature, stream
+FASTCALL(py_logprobs) {
+    return guarded(n, 9, [&] {
+        const char* what = "tetra_logprobs";
+        const at::ScalarType type = tensor(a[0]).scalar_type();
+        if (type != at::kFloat && type != at::kHalf) fail(tetra_error, "%s logits: %s, the call takes Float or Half", what, c10::toString(type));
+        const at::Tensor& x = typed(a[0], type, what, "logits");
+        if (x.dim() != 2 || (x.stride(1) != 1 && x.size(1) > 1)) fail(tetra_error, "%s logits: wrong shape", what);
+        const int64_t rows = x.size(0);
+        tetra_logprobs_rows r = {};
+        r.logits = x.data_ptr();
+        r.rows = narrow(rows, what, "logits");
+        r.vocab = narrow(x.size(1), what, "logits");
+        r.row_stride = rows > 1 ? x.stride(0) : x.size(1);
+        r.half_type = type == at::kHalf;
+        if ((a[1] == Py_None) != (a[2] == Py_None)) fail(tetra_error, "%s: tokens and logprob are given together", what);
+        if (a[1] != Py_None) {
+            const int64_t given = tensor(a[1]).dim() == 2 ? tensor(a[1]).size(1) : 0;
+            r.tokens = static_cast<const int32_t*>(shaped(a[1], at::kInt, {rows, given}, what, "tokens"));
+            r.logprob = static_cast<float*>(shaped(a[2], at::kFloat, {rows, given}, what, "logprob"));
+            r.given = narrow(given, what, "tokens");
+            if (a[3] != Py_None) r.rank = static_cast<int32_t*>(shaped(a[3], at::kInt, {rows, given}, what, "rank"));
+        } else if (a[3] != Py_None) {
+            fail(tetra_error, "%s: rank is that of tokens", what);
+        }
+        if (a[4] != Py_None) r.entropy = static_cast<float*>(shaped(a[4], at::kFloat, {rows}, what, "entropy"));
+        if ((a[5] == Py_None) != (a[6] == Py_None)) fail(tetra_error, "%s: top_tokens and top_logprob are given together", what);
+        if (a[5] != Py_None) {
+            const int64_t top = tensor(a[5]).dim() == 2 ? tensor(a[5]).size(1) : 0;
+            r.top_tokens = static_cast<int32_t*>(shaped(a[5], at::kInt, {rows, top}, what, "top_tokens"));
+            r.top_logprob = static_cast<float*>(shaped(a[6], at::kFloat, {rows, top}, what, "top_logprob"));
+            r.top = narrow(top, what, "top_tokens");
+        }
+        if (a[7] != Py_None) r.temperature = static_cast<const float*>(shaped(a[7], at::kFloat, {rows}, what, "temperature"));
+        void* s = stream_of(a[8]);
+        if (rows > 0) check(unlocked([&] { return api.logprobs(&r, s); }), what);
+        return same(a[2]);
+    });
+}
+
 // library path, exception class
 FASTCALL(py_setup) {
     return guarded(n, 2, [&] {
@@ -593,6 +635,7 @@ FASTCALL(py_setup) {
         get(api.kv_attend, "tetra_kv_attend");
         get(api.kv_attend_shared, "tetra_kv_attend_shared");
         get(api.sample, "tetra_sample");
+        get(api.logprobs, "tetra_logprobs");
         Py_XDECREF(tetra_error);
         tetra_error = same(a[1]);
         return same(Py_None);
@@ -603,7 +646,7 @@ FASTCALL(py_setup) {
 PyMethodDef methods[] = {METHOD(setup),        METHOD(gemv),          METHOD(gemv_tail), METHOD(gemv_noalloc), METHOD(gemv_batched),
                          METHOD(gemv_list),    METHOD(grouped_run),   METHOD(pack_codes), METHOD(decode_packed), METHOD(encode_blocks),
                          METHOD(q4_pack),      METHOD(q4_gemv),       METHOD(q4_rows),   METHOD(q4_list_run),  METHOD(kv_append), METHOD(kv_append_at),
-                         METHOD(kv_read),      METHOD(kv_attend),     METHOD(kv_attend_shared), METHOD(sample),
+                         METHOD(kv_read),      METHOD(kv_attend),     METHOD(kv_attend_shared), METHOD(sample), METHOD(logprobs),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of the Tetra C ABI.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -115,6 +115,7 @@ def lib():
         L.tetra_kv_append_at.argtypes = [vp, vp, vp, vp]
         L.tetra_kv_read.argtypes = [vp, vp, vp, i32, vp]
         L.tetra_sample.argtypes = [vp, vp]
+        L.tetra_logprobs.argtypes = [vp, vp]
         L.tetra_kv_attend.argtypes = [vp, vp, C.c_int64, vp, i32, i32, C.c_float, vp, sz, vp]
         L.tetra_kv_shared_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
         L.tetra_kv_shared_workspace_bytes.restype = sz
@@ -507,3 +508,22 @@ def tetra_sample(logits, u, tokens, prob=None, temperature=None, top_k=None, top
     u float32 [rows]: uniform numbers of [0, 1).  Per row, or None: temperature float32 (1; 0 takes the largest logit), top_k
     int32, top_p float32, min_p float32 (off).  prob float32 [rows]: the probability with which the token was taken."""
     return (_nat or _native()).sample(logits, u, tokens, prob, temperature, top_k, top_p, min_p, stream)
+
+
+# ---------------------------------------------------------------------------
+# what tokens are worth (include/tetra_logprobs.h)
+# ---------------------------------------------------------------------------
+class LogprobsRows(C.Structure):
+    """Mirror of tetra_logprobs_rows."""
+    _fields_ = [("logits", C.c_void_p), ("temperature", C.c_void_p), ("tokens", C.c_void_p), ("logprob", C.c_void_p), ("rank", C.c_void_p),
+                ("entropy", C.c_void_p), ("top_tokens", C.c_void_p), ("top_logprob", C.c_void_p), ("row_stride", C.c_int64), ("rows", C.c_int32),
+                ("vocab", C.c_int32), ("half_type", C.c_int32), ("given", C.c_int32), ("top", C.c_int32)]
+
+
+def tetra_logprobs(logits, tokens, logprob, rank=None, entropy=None, top_tokens=None, top_logprob=None, temperature=None, stream=None):
+    """Log probabilities of given tokens under each row of logits (float32 or float16 [rows, vocab], rows may lie apart); returns logprob.
+
+    tokens int32 [rows, given] and logprob float32 [rows, given] (None together), rank int32 [rows, given]: tokens ahead of each;
+    entropy float32 [rows]; top_tokens int32 [rows, top] and top_logprob float32 [rows, top]: the likeliest tokens, in order.
+    temperature float32 [rows], or None for 1 (0: all of the probability is the largest logit's)."""
+    return (_nat or _native()).logprobs(logits, tokens, logprob, rank, entropy, top_tokens, top_logprob, temperature, stream)
