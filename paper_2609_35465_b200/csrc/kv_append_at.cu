@@ -3,8 +3,6 @@
 // As tetra_kv_append, but a pair is turned by the row's position on the pair's axis, and that has nothing to do with the row's slot.
 // A picture comes as one call of some thousand rows, so work is cut by blocks, not rows: a CTA per (block of 16 slots, kv head) makes
 // its rows' sines once for the block's keys and all queries of the head group.  Rows of a chat's step are a block each.
-#include <type_traits>
-
 #include "kv_rows.cuh"
 
 namespace tetra {
@@ -50,43 +48,18 @@ __device__ __forceinline__ int block_of(const KvCache& c, int at, int lane, int&
     return -1;
 }
 
-// BLOCKS: a CTA for each block; else one for each row, of which the first of a block does its work.
-template <int D, typename T, bool BLOCKS>
-__global__ void __launch_bounds__(kAppendThreads) k_kv_append_at(KvCache c, KvRows p, KvAxes t) {
-    constexpr int E = D / 32;
-    extern __shared__ __align__(16) unsigned char smem[];
-    double2* turns = reinterpret_cast<double2*>(smem);  // [rows of the block][D / 2]
-    __shared__ uint32_t amax[2];                        // keys, values
-    pdl_wait();
-    pdl_release();
-    const int head = blockIdx.y, lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
-    if (threadIdx.x < 2) amax[threadIdx.x] = 0u;
-    int r = blockIdx.x, a = 0, b = 0, s;
-    int64_t before = 0;
-    if (BLOCKS) {
-        s = block_of(c, blockIdx.x, lane, r, a, b, before);
-    } else {
-        s = sequence_of(c, r, lane, a, b);
-        if (s >= 0) before = __ldg(c.lengths + s);
-    }
-    if (s < 0) return;
-    const int64_t slot = before + (r - a);
-    const int first = int(slot & (kKvBlock - 1));
-    if (!BLOCKS && r != a && first != 0) return;
-    unsigned char* rec = c.record<D>(s, slot >> 4, head);
-    const int rows = min(kKvBlock - first, b - r), n = rec ? rows : 0;
-    for (int i = threadIdx.x; i < rows * (D / 2); i += kAppendThreads) {
-        const int row = i / (D / 2), pair = i % (D / 2);
-        const int axis = __ldg(t.axis + pair);
-        const int at = axis < t.axes ? __ldg(t.positions + int64_t(r + row) * t.stride + axis) : 0;
-        double sn, cs;
-        sincospi(double(at) * __ldg(p.inv_freq + pair) * 0.318309886183790671538, &sn, &cs);  // 1 / pi
-        turns[i] = make_double2(cs, sn);
-    }
-    __syncthreads();
+__device__ __forceinline__ double2 turn_of(const KvRows& p, const KvAxes& t, int row, int pair) {
+    const int axis = __ldg(t.axis + pair);
+    const int at = axis < t.axes ? __ldg(t.positions + row * t.stride + axis) : 0;
+    double sn, cs;
+    sincospi(double(at) * __ldg(p.inv_freq + pair) * 0.318309886183790671538, &sn, &cs);  // 1 / pi
+    return make_double2(cs, sn);
+}
 
-    // Tasks: the block's keys, then its values, a warp each; the queries from the other end of the warps.
-    float x[kAppendTasks][E];
+// The keys and values of n rows of a block, from row r on: a warp takes a row at a time (keys, then values).
+template <int D, typename T>
+__device__ __forceinline__ void load_block(const KvRows& p, int64_t r, int n, int head, const double2* turns, uint32_t* amax, float (&x)[kAppendTasks][D / 32], int lane, int warp) {
+    constexpr int E = D / 32;
 #pragma unroll
     for (int k = 0; k < kAppendTasks; ++k) {
         const int task = warp + kAppendWarps * k;
@@ -108,7 +81,32 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append_at(KvCache c, KvRo
         top = __reduce_max_sync(0xFFFFFFFFu, top);
         if (lane == 0) atomicMax(&amax[key ? 0 : 1], top);
     }
-    for (int j = kAppendWarps - 1 - warp; j < rows * p.group; j += kAppendWarps) {  // none without q
+}
+
+// Few rows a sequence: a CTA for each row, of which the first of a block does the block's work.
+template <int D, typename T>
+__global__ void __launch_bounds__(kAppendThreads) k_kv_append_at(KvCache c, KvRows p, KvAxes t) {
+    constexpr int E = D / 32;
+    extern __shared__ __align__(16) unsigned char smem[];
+    double2* turns = reinterpret_cast<double2*>(smem);  // [rows of the block][D / 2]
+    __shared__ uint32_t amax[2];                        // keys, values
+    pdl_wait();
+    pdl_release();
+    const int r = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
+    if (threadIdx.x < 2) amax[threadIdx.x] = 0u;
+    int a, b;
+    const int s = sequence_of(c, r, lane, a, b);
+    if (s < 0) return;
+    const int64_t slot = int64_t(__ldg(c.lengths + s)) + (r - a);
+    const int first = int(slot & (kKvBlock - 1));
+    if (r != a && first != 0) return;
+    unsigned char* rec = c.record<D>(s, slot >> 4, head);
+    const int rows = min(kKvBlock - first, b - r), n = rec ? rows : 0;
+    for (int i = threadIdx.x; i < rows * (D / 2); i += kAppendThreads) turns[i] = turn_of(p, t, r + i / (D / 2), i % (D / 2));
+    __syncthreads();
+    float x[kAppendTasks][E];
+    load_block<D, T>(p, r, n, head, turns, amax, x, lane, warp);
+    for (int j = kAppendWarps - 1 - warp; j < rows * p.group; j += kAppendWarps) {  // queries, from the other end of the warps; none without q
         const int row = j / p.group, h = head * p.group + j - row * p.group;
         float xq[E];
         double z[E];
@@ -120,6 +118,168 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append_at(KvCache c, KvRo
     }
     if (!rec) return;
     finish_block<D>(rec, first, n, amax, x, lane, warp);
+}
+
+// N values of a row that lie side by side.
+template <typename T, int N>
+__device__ __forceinline__ void load_side(const T* from, float (&x)[N]) {
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (N == 1) x[0] = from[0];
+        if constexpr (N == 2) {
+            const float2 v = *reinterpret_cast<const float2*>(from);
+            x[0] = v.x, x[1] = v.y;
+        }
+        if constexpr (N == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(from);
+            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        }
+    } else {
+        if constexpr (N == 1) x[0] = __half2float(from[0]);
+#pragma unroll
+        for (int i = 0; i + 1 < N; i += 2) {
+            const float2 v = __half22float2(reinterpret_cast<const __half2*>(from)[i / 2]);
+            x[i] = v.x, x[i + 1] = v.y;
+        }
+    }
+}
+
+// Many rows a sequence: a CTA for each block.  Queries are most of the work; they are rounded to float16 at the end, so from their
+// sines on (made in 64 bits, rounded to 32) they are in 32 bits, which moves a result by 2^-21 at most where float16 rounds by 2^-12; keys,
+// whose codes a last bit may decide, stay in 64.  SIDE: rows of q are aligned for loads of a lane's D / 64 neighbours at once.
+template <int D, typename T, bool SIDE>
+__global__ void __launch_bounds__(kAppendThreads) k_kv_append_blocks(KvCache c, KvRows p, KvAxes t) {
+    constexpr int E = D / 32, N = D / 64, PAIRS = D / 2;
+    extern __shared__ __align__(16) unsigned char smem[];
+    double2* turns = reinterpret_cast<double2*>(smem);                                                             // [16][D / 2]
+    float2* turns32 = reinterpret_cast<float2*>(smem + kKvBlock * PAIRS * sizeof(double2));                        // the same
+    unsigned char* made = smem + kKvBlock * PAIRS * (sizeof(double2) + sizeof(float2));                            // a record's codes
+    __shared__ uint32_t amax[2];
+    pdl_wait();
+    pdl_release();
+    const int head = blockIdx.y, lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
+    if (threadIdx.x < 2) amax[threadIdx.x] = 0u;
+    int r, a, b;
+    int64_t before;
+    const int s = block_of(c, blockIdx.x, lane, r, a, b, before);
+    if (s < 0) return;
+    const int64_t slot = before + (r - a);
+    const int first = int(slot & (kKvBlock - 1));
+    unsigned char* rec = c.record<D>(s, slot >> 4, head);
+    const int rows = min(kKvBlock - first, b - r), n = rec ? rows : 0;
+    for (int i = threadIdx.x; i < rows * PAIRS; i += kAppendThreads) {
+        const double2 v = turn_of(p, t, r + i / PAIRS, i % PAIRS);
+        turns[i] = v;
+        turns32[i] = make_float2(float(v.x), float(v.y));
+    }
+    __syncthreads();
+    float x[kAppendTasks][E];
+    load_block<D, T>(p, r, n, head, turns, amax, x, lane, warp);
+    __syncthreads();  // amax
+    if (n == kKvBlock) {
+        // A whole block: its scales are powers of two, of which the reciprocals are exact, and its bytes are put together here.
+        float scale[2], by[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const float made_for = scale_for(amax[w]);
+            scale[w] = amax[w] >= kInfBits ? __uint_as_float(kNanBits) : made_for;
+            by[w] = amax[w] >= kInfBits || made_for == 0.f ? 0.f : __uint_as_float((254u << 23) - __float_as_uint(made_for));
+        }
+#pragma unroll
+        for (int k = 0; k < kAppendTasks; ++k) {
+            const int task = warp + kAppendWarps * k, token = task & (kKvBlock - 1);
+            const bool key = task < kKvBlock;
+            const uint32_t at = key ? ((token & 7) * 4 + (lane >> 3)) * 16 + (token >> 3) * 8 + (lane & 7)
+                                    : kKvBlock * D + ((lane >> 2) * 4 + (token & 7) / 2) * 16 + (lane & 3) * 4 + (token >> 3) * 2 + (token & 1);
+            const float f = by[key ? 0 : 1];
+#pragma unroll
+            for (int i = 0; i < E; ++i) made[at + 512 * i] = static_cast<unsigned char>((f == 0.f ? 0 : __float2int_rn(x[k][i] * f)) + 128);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * D; i += kAppendThreads) reinterpret_cast<uint4*>(rec)[i] = reinterpret_cast<const uint4*>(made)[i];
+        if (threadIdx.x == 0) *reinterpret_cast<float2*>(rec + 2 * kKvBlock * D) = make_float2(scale[0], scale[1]);
+    } else if (rec) {
+        finish_block<D>(rec, first, n, amax, x, lane, warp);
+    }
+
+    // Queries: a lane has N neighbours of either half.
+    if (p.group == 0) return;
+    float weight[2][N];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < N; ++i) weight[k][i] = p.q_weight ? __ldg(p.q_weight + k * PAIRS + lane * N + i) : 1.f;
+    const int tasks = rows * p.group, heads = c.kv_heads * p.group;
+    float now[2][N], next[2][N];
+    auto load = [&](int j, float (&to)[2][N]) {
+        const int row = j / p.group;
+        const T* from = static_cast<const T*>(p.q) + (int64_t(r) + row) * p.q_stride + int64_t(head * p.group + j - row * p.group) * D + lane * N;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (SIDE) load_side<T, N>(from + k * PAIRS, to[k]);
+            else
+#pragma unroll
+                for (int i = 0; i < N; ++i) to[k][i] = float(from[k * PAIRS + i]);
+        }
+    };
+    if (warp < tasks) load(warp, next);
+    for (int j = warp; j < tasks; j += kAppendWarps) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < N; ++i) now[k][i] = next[k][i];
+        if (j + kAppendWarps < tasks) load(j + kAppendWarps, next);
+        const int row = j / p.group;
+        if (p.q_weight) {
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum = fmaf(now[k][i], now[k][i], sum);
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            const float by = rsqrtf(sum * (1.f / D) + float(p.eps));
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) now[k][i] *= by * weight[k][i];
+        }
+        __half* out = p.q_out + ((int64_t(r) + row) * heads + head * p.group + j - row * p.group) * D + lane * N;
+        float lo[N], hi[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float2 u = turns32[row * PAIRS + lane * N + i];
+            lo[i] = now[0][i] * u.x - now[1][i] * u.y;
+            hi[i] = now[1][i] * u.x + now[0][i] * u.y;
+        }
+        if constexpr (N == 1) {
+            out[0] = __float2half_rn(lo[0]);
+            out[PAIRS] = __float2half_rn(hi[0]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                if (SIDE) {
+                    *reinterpret_cast<__half2*>(out + i) = __floats2half2_rn(lo[i], lo[i + 1]);
+                    *reinterpret_cast<__half2*>(out + PAIRS + i) = __floats2half2_rn(hi[i], hi[i + 1]);
+                } else {
+                    out[i] = __float2half_rn(lo[i]), out[i + 1] = __float2half_rn(lo[i + 1]);
+                    out[PAIRS + i] = __float2half_rn(hi[i]), out[PAIRS + i + 1] = __float2half_rn(hi[i + 1]);
+                }
+            }
+        }
+    }
+}
+
+template <int D, typename T, bool SIDE>
+int launch_blocks_for(int blocks, const KvCache& c, const KvRows& p, const KvAxes& t, void* stream) {
+    constexpr size_t smem = size_t(kKvBlock) * D / 2 * (sizeof(double2) + sizeof(float2)) + 2 * kKvBlock * D;
+    static PerDeviceOnce once;  // per instantiation
+    if (smem > 48 * 1024 && once.run([] { return cudaFuncSetAttribute(k_kv_append_blocks<D, T, SIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)); }) != cudaSuccess)
+        return TETRA_ERR_CUDA;
+    return launch_rows(k_kv_append_blocks<D, T, SIDE>, blocks, c.kv_heads, kAppendThreads, smem, stream, c, p, t);
+}
+template <typename T, bool SIDE>
+int launch_blocks(int D, int blocks, const KvCache& c, const KvRows& p, const KvAxes& t, void* stream) {
+    return D == 64 ? launch_blocks_for<64, T, SIDE>(blocks, c, p, t, stream) : D == 128 ? launch_blocks_for<128, T, SIDE>(blocks, c, p, t, stream) : launch_blocks_for<256, T, SIDE>(blocks, c, p, t, stream);
 }
 
 }  // namespace
@@ -143,15 +303,14 @@ extern "C" int tetra_kv_append_at(const tetra_kv_cache* cache, const tetra_kv_ro
     const KvAxes t{axes->positions, axes->axis, axes->stride, axes->axes};
     // Blocks that the rows may fall in: each sequence's, and one more where it begins inside one.
     const int64_t blocks = int64_t(c.rows) / kKvBlock + 2 * int64_t(c.seqs);
-    const bool by_blocks = blocks < c.rows;
-    auto launch = [&](auto kernel) {
-        return launch_rows(kernel, by_blocks ? int(blocks) : c.rows, c.kv_heads, kAppendThreads, size_t(kKvBlock) * D / 2 * sizeof(double2), stream, c, p, t);
-    };
-    auto pick = [&](auto half, auto blocks_too) {
-        using T = decltype(half);
-        constexpr bool B = decltype(blocks_too)::value;
-        return launch(D == 64 ? k_kv_append_at<64, T, B> : D == 128 ? k_kv_append_at<128, T, B> : k_kv_append_at<256, T, B>);
-    };
-    if (rows->half_type) return by_blocks ? pick(__half(), std::true_type()) : pick(__half(), std::false_type());
-    return by_blocks ? pick(0.f, std::true_type()) : pick(0.f, std::false_type());
+    if (blocks >= c.rows) {
+        auto launch = [&](auto kernel) { return launch_rows(kernel, c.rows, c.kv_heads, kAppendThreads, size_t(kKvBlock) * D / 2 * sizeof(double2), stream, c, p, t); };
+        if (rows->half_type) return launch(D == 64 ? k_kv_append_at<64, __half> : D == 128 ? k_kv_append_at<128, __half> : k_kv_append_at<256, __half>);
+        return launch(D == 64 ? k_kv_append_at<64, float> : D == 128 ? k_kv_append_at<128, float> : k_kv_append_at<256, float>);
+    }
+    // What a lane loads and stores at once has to be aligned as one.
+    const size_t side = size_t(D / 64) * (rows->half_type ? 2 : 4);
+    const bool aligned = kv_aligned(p.q, side) && p.q_stride * (rows->half_type ? 2 : 4) % int64_t(side) == 0 && kv_aligned(p.q_out, 2 * size_t(D / 64));
+    return aligned ? (rows->half_type ? launch_blocks<__half, true>(D, int(blocks), c, p, t, stream) : launch_blocks<float, true>(D, int(blocks), c, p, t, stream))
+                   : (rows->half_type ? launch_blocks<__half, false>(D, int(blocks), c, p, t, stream) : launch_blocks<float, false>(D, int(blocks), c, p, t, stream));
 }
