@@ -84,22 +84,28 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append(KvCache c, KvRows 
     finish_block<D>(rec, first, n, amax, x, lane, warp);
 }
 
-// Two warps per (row, kv head): those of the first row of a block write all of the call's rows of it, each half of the dims.
+// Two warps per (row, kv head), or, where rows are many, per (block, kv head): those of the first row of a block write all of the call's rows of it, each half of the dims.
 // A lane turns the bytes that it loads into the values that it stores: eight dims of two tokens, or four of four.
 constexpr int kReadRows = 4;  // of a CTA
 
-template <int D>
+template <int D, bool BLOCKS>
 __global__ void __launch_bounds__(64 * kReadRows) k_kv_read(KvCache c, __half* k_out, __half* v_out) {
     pdl_wait();
     pdl_release();
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0), g = lane >> 2, t = lane & 3;
-    const int r = blockIdx.x * kReadRows + (warp >> 1), head = blockIdx.y, half = warp & 1;
-    int a, b;
-    const int s = r < c.rows ? sequence_of(c, r, lane, a, b) : -1;
+    const int head = blockIdx.y, half = warp & 1;
+    int r = blockIdx.x * kReadRows + (warp >> 1), a = 0, b = 0, s;
+    int64_t before = 0;
+    if (BLOCKS) {
+        s = block_of(c, r, lane, r, a, b, before);
+    } else {
+        s = r < c.rows ? sequence_of(c, r, lane, a, b) : -1;
+        if (s >= 0) before = __ldg(c.lengths + s);
+    }
     if (s < 0) return;
-    const int64_t pos = int64_t(__ldg(c.lengths + s)) + (r - a);
+    const int64_t pos = before + (r - a);
     const int first = int(pos & (kKvBlock - 1));
-    if (r != a && first != 0) return;
+    if (!BLOCKS && r != a && first != 0) return;
     const int n = min(kKvBlock - first, b - r);
     const unsigned char* rec = c.record<D>(s, pos >> 4, head);
     constexpr int MINE = D / 64;  // chunks of 32 dims
@@ -180,8 +186,15 @@ int tetra_kv_read(const tetra_kv_cache* cache, void* k_out, void* v_out, int row
     if (!kv_aligned(k_out, 16) || !kv_aligned(v_out, 16)) return TETRA_ERR_ALIGN;
     if (rows == 0) return TETRA_OK;
     const int D = cache->head_dim;
-    return launch_rows(D == 64 ? k_kv_read<64> : D == 128 ? k_kv_read<128> : k_kv_read<256>, (c.rows + kReadRows - 1) / kReadRows, c.kv_heads, 64 * kReadRows, 0, stream, c,
-                       static_cast<__half*>(k_out), static_cast<__half*>(v_out));
+    // Many rows a sequence: by blocks (2949 rows of one, 8 kv heads: 21 us by rows).
+    const int64_t blocks = kv_most_blocks(c);
+    const bool by_blocks = 32 * int64_t(c.seqs) <= c.rows;
+    const int items = by_blocks ? int(blocks) : c.rows;
+    auto launch = [&](auto kernel) {
+        return launch_rows(kernel, (items + kReadRows - 1) / kReadRows, c.kv_heads, 64 * kReadRows, 0, stream, c, static_cast<__half*>(k_out), static_cast<__half*>(v_out));
+    };
+    if (by_blocks) return launch(D == 64 ? k_kv_read<64, true> : D == 128 ? k_kv_read<128, true> : k_kv_read<256, true>);
+    return launch(D == 64 ? k_kv_read<64, false> : D == 128 ? k_kv_read<128, false> : k_kv_read<256, false>);
 }
 
 }  // extern "C"

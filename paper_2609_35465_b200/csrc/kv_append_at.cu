@@ -15,71 +15,57 @@ struct KvAxes {
     int32_t axes;
 };
 
-// Block number `at` among the blocks that the call's rows fall in, sequence after sequence: its sequence and the first of its rows.  A
-// warp looks at 32 sequences at a time.
-__device__ __forceinline__ int block_of(const KvCache& c, int at, int lane, int& r, int& a, int& b, int64_t& before) {
-    for (int s0 = 0; s0 < c.seqs; s0 += 32) {
-        const int s = s0 + lane;
-        int x = 0, y = 0, own = 0;
-        int64_t len = 0;
-        if (s < c.seqs) {
-            c.rows_of(s, x, y);
-            len = __ldg(c.lengths + s);
-            if (y > x) own = int(((len + (y - x - 1)) >> 4) - (len >> 4)) + 1;
-        }
-        int sum = own;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-            if (lane >= o) sum += v;
-        }
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, at < sum);
-        if (who) {
-            const int l = __ffs(who) - 1;
-            a = __shfl_sync(0xFFFFFFFFu, x, l);
-            b = __shfl_sync(0xFFFFFFFFu, y, l);
-            before = __shfl_sync(0xFFFFFFFFu, len, l);
-            const int local = at - (__shfl_sync(0xFFFFFFFFu, sum, l) - __shfl_sync(0xFFFFFFFFu, own, l));
-            r = local == 0 ? a : a + int((((before >> 4) + local) << 4) - before);
-            return s0 + l;
-        }
-        at -= __shfl_sync(0xFFFFFFFFu, sum, 31);
-    }
-    return -1;
+// Cosine and sine of so many turns, in 64 bits: the nearest quarter is taken off, what is left, pi/4 at most, goes into the two
+// Taylor series, which cut behind the 13th and 14th power are off by 2e-14 (pi/4)^15 / 15!.  That is 1e-10 of a key's code, where a general
+// function to the last bit costs four times as much, a quarter of the kernel.
+__device__ __forceinline__ double2 cosine_sine(double turns) {
+    const double quarters = rint(4. * turns), y = 6.283185307179586476925 * fma(-0.25, quarters, turns), z = y * y;
+    double s = fma(z, 1. / 6227020800., -1. / 39916800.), c = fma(z, -1. / 87178291200., 1. / 479001600.);
+    s = fma(s, z, 1. / 362880.), c = fma(c, z, -1. / 3628800.);
+    s = fma(s, z, -1. / 5040.), c = fma(c, z, 1. / 40320.);
+    s = fma(s, z, 1. / 120.), c = fma(c, z, -1. / 720.);
+    s = fma(s, z, -1. / 6.), c = fma(c, z, 1. / 24.);
+    s = fma(s * z, y, y), c = fma(fma(c, z, -0.5), z, 1.);
+    const int q = int(int64_t(quarters)) & 3;
+    const double u = q & 1 ? s : c, v = q & 1 ? c : s;
+    return make_double2(q == 1 || q == 2 ? -u : u, q >= 2 ? -v : v);
 }
 
 __device__ __forceinline__ double2 turn_of(const KvRows& p, const KvAxes& t, int row, int pair) {
     const int axis = __ldg(t.axis + pair);
     const int at = axis < t.axes ? __ldg(t.positions + row * t.stride + axis) : 0;
-    double sn, cs;
-    sincospi(double(at) * __ldg(p.inv_freq + pair) * 0.318309886183790671538, &sn, &cs);  // 1 / pi
-    return make_double2(cs, sn);
+    return cosine_sine(double(at) * __ldg(p.inv_freq + pair) * 0.159154943091895335769);  // 1 / 2 pi
 }
 
 // The keys and values of n rows of a block, from row r on: a warp takes a row at a time (keys, then values).
 template <int D, typename T>
-__device__ __forceinline__ void load_block(const KvRows& p, int64_t r, int n, int head, const double2* turns, uint32_t* amax, float (&x)[kAppendTasks][D / 32], int lane, int warp) {
+__device__ __forceinline__ void load_block(const KvRows& p, int64_t r, int n, int head, float (&x)[kAppendTasks][D / 32], int lane, int warp) {
+#pragma unroll
+    for (int k = 0; k < kAppendTasks; ++k) {
+        const int task = warp + kAppendWarps * k;
+        if (task >= 2 * n) continue;
+        if (task < n) load_row<T>(p.k, (r + task) * p.k_stride + head * D, lane, x[k]);
+        else load_row<T>(p.v, (r + task - n) * p.v_stride + head * D, lane, x[k]);
+    }
+}
+template <int D>
+__device__ __forceinline__ void turn_block(const KvRows& p, int n, const double2* turns, uint32_t* amax, float (&x)[kAppendTasks][D / 32], int lane, int warp) {
     constexpr int E = D / 32;
 #pragma unroll
     for (int k = 0; k < kAppendTasks; ++k) {
         const int task = warp + kAppendWarps * k;
-        if (task >= 2 * n) break;
-        const bool key = task < n;
-        const int row = key ? task : task - n;
-        if (key) {
+        if (task >= 2 * n) continue;
+        if (task < n) {
             double z[E];
-            load_row<T>(p.k, (r + row) * p.k_stride + head * D, lane, x[k]);
-            turn<E>(x[k], p.k_weight, p.eps, turns + row * (D / 2), lane, z);
+            turn<E>(x[k], p.k_weight, p.eps, turns + task * (D / 2), lane, z);
 #pragma unroll
             for (int i = 0; i < E; ++i) x[k][i] = float(z[i]);
-        } else {
-            load_row<T>(p.v, (r + row) * p.v_stride + head * D, lane, x[k]);
         }
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < E; ++i) top = max(top, __float_as_uint(x[k][i]) & 0x7FFFFFFFu);  // NaN is above infinity
         top = __reduce_max_sync(0xFFFFFFFFu, top);
-        if (lane == 0) atomicMax(&amax[key ? 0 : 1], top);
+        if (lane == 0) atomicMax(&amax[task < n ? 0 : 1], top);
     }
 }
 
@@ -105,7 +91,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append_at(KvCache c, KvRo
     for (int i = threadIdx.x; i < rows * (D / 2); i += kAppendThreads) turns[i] = turn_of(p, t, r + i / (D / 2), i % (D / 2));
     __syncthreads();
     float x[kAppendTasks][E];
-    load_block<D, T>(p, r, n, head, turns, amax, x, lane, warp);
+    load_block<D, T>(p, r, n, head, x, lane, warp);
+    turn_block<D>(p, n, turns, amax, x, lane, warp);
     for (int j = kAppendWarps - 1 - warp; j < rows * p.group; j += kAppendWarps) {  // queries, from the other end of the warps; none without q
         const int row = j / p.group, h = head * p.group + j - row * p.group;
         float xq[E];
@@ -166,14 +153,41 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append_blocks(KvCache c, 
     const int first = int(slot & (kKvBlock - 1));
     unsigned char* rec = c.record<D>(s, slot >> 4, head);
     const int rows = min(kKvBlock - first, b - r), n = rec ? rows : 0;
+    float x[kAppendTasks][E];
+    load_block<D, T>(p, r, n, head, x, lane, warp);
+    // Queries, some of a warp's at a time, the next ones on their way: a lane has N neighbours of either half.
+    constexpr int AT_ONCE = N == 4 ? 1 : 4;
+    const int heads = c.kv_heads * p.group, step_row = p.group ? kAppendWarps / p.group : 0, step_head = p.group ? kAppendWarps % p.group : 0;
+    float next[AT_ONCE][2][N];
+    int next_row = p.group ? warp / p.group : rows, next_head = p.group ? warp % p.group : 0;
+    auto advance = [&](int& row, int& j) {
+        row += step_row, j += step_head;
+        if (j >= p.group) j -= p.group, ++row;
+    };
+    auto load = [&](int row, int j) {
+#pragma unroll
+        for (int o = 0; o < AT_ONCE; ++o) {
+            if (row < rows) {
+                const T* from = static_cast<const T*>(p.q) + (int64_t(r) + row) * p.q_stride + int64_t(head * p.group + j) * D + lane * N;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if (SIDE) load_side<T, N>(from + k * PAIRS, next[o][k]);
+                    else
+#pragma unroll
+                        for (int i = 0; i < N; ++i) next[o][k][i] = float(from[k * PAIRS + i]);
+                }
+            }
+            advance(row, j);
+        }
+    };
+    load(next_row, next_head);
     for (int i = threadIdx.x; i < rows * PAIRS; i += kAppendThreads) {
         const double2 v = turn_of(p, t, r + i / PAIRS, i % PAIRS);
         turns[i] = v;
         turns32[i] = make_float2(float(v.x), float(v.y));
     }
     __syncthreads();
-    float x[kAppendTasks][E];
-    load_block<D, T>(p, r, n, head, turns, amax, x, lane, warp);
+    turn_block<D>(p, n, turns, amax, x, lane, warp);
     __syncthreads();  // amax
     if (n == kKvBlock) {
         // A whole block: its scales are powers of two, of which the reciprocals are exact, and its bytes are put together here.
@@ -201,34 +215,28 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append_blocks(KvCache c, 
         finish_block<D>(rec, first, n, amax, x, lane, warp);
     }
 
-    // Queries: a lane has N neighbours of either half.
     if (p.group == 0) return;
     float weight[2][N];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int i = 0; i < N; ++i) weight[k][i] = p.q_weight ? __ldg(p.q_weight + k * PAIRS + lane * N + i) : 1.f;
-    const int tasks = rows * p.group, heads = c.kv_heads * p.group;
-    float now[2][N], next[2][N];
-    auto load = [&](int j, float (&to)[2][N]) {
-        const int row = j / p.group;
-        const T* from = static_cast<const T*>(p.q) + (int64_t(r) + row) * p.q_stride + int64_t(head * p.group + j - row * p.group) * D + lane * N;
+    while (next_row < rows) {
+      float batch[AT_ONCE][2][N];
+      int row = next_row, j = next_head;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (SIDE) load_side<T, N>(from + k * PAIRS, to[k]);
-            else
-#pragma unroll
-                for (int i = 0; i < N; ++i) to[k][i] = float(from[k * PAIRS + i]);
-        }
-    };
-    if (warp < tasks) load(warp, next);
-    for (int j = warp; j < tasks; j += kAppendWarps) {
+      for (int o = 0; o < AT_ONCE; ++o) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) now[k][i] = next[k][i];
-        if (j + kAppendWarps < tasks) load(j + kAppendWarps, next);
-        const int row = j / p.group;
+            for (int i = 0; i < N; ++i) batch[o][k][i] = next[o][k][i];
+        advance(next_row, next_head);
+      }
+      if (next_row < rows) load(next_row, next_head);
+#pragma unroll
+      for (int o = 0; o < AT_ONCE; ++o, advance(row, j)) {
+        if (row >= rows) break;
+        float (&now)[2][N] = batch[o];
         if (p.q_weight) {
             float sum = 0.f;
 #pragma unroll
@@ -243,7 +251,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append_blocks(KvCache c, 
 #pragma unroll
                 for (int i = 0; i < N; ++i) now[k][i] *= by * weight[k][i];
         }
-        __half* out = p.q_out + ((int64_t(r) + row) * heads + head * p.group + j - row * p.group) * D + lane * N;
+        __half* out = p.q_out + ((int64_t(r) + row) * heads + head * p.group + j) * D + lane * N;
         float lo[N], hi[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -266,6 +274,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append_blocks(KvCache c, 
                 }
             }
         }
+    }
     }
 }
 
@@ -301,8 +310,7 @@ extern "C" int tetra_kv_append_at(const tetra_kv_cache* cache, const tetra_kv_ro
     if (!kv_aligned(axes->positions, 4)) return TETRA_ERR_ALIGN;
     if (c.rows == 0) return TETRA_OK;
     const KvAxes t{axes->positions, axes->axis, axes->stride, axes->axes};
-    // Blocks that the rows may fall in: each sequence's, and one more where it begins inside one.
-    const int64_t blocks = int64_t(c.rows) / kKvBlock + 2 * int64_t(c.seqs);
+    const int64_t blocks = kv_most_blocks(c);
     if (blocks >= c.rows) {
         auto launch = [&](auto kernel) { return launch_rows(kernel, c.rows, c.kv_heads, kAppendThreads, size_t(kKvBlock) * D / 2 * sizeof(double2), stream, c, p, t); };
         if (rows->half_type) return launch(D == 64 ? k_kv_append_at<64, __half> : D == 128 ? k_kv_append_at<128, __half> : k_kv_append_at<256, __half>);

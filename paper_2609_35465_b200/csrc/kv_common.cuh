@@ -58,6 +58,39 @@ __device__ __forceinline__ int sequence_of(const KvCache& c, int r, int lane, in
     return a <= r && r < b ? s : -1;
 }
 
+// Block number `at` among the blocks that the call's rows fall in, sequence after sequence: its sequence and the first of its rows.  A
+// warp looks at 32 sequences at a time.
+__device__ __forceinline__ int block_of(const KvCache& c, int at, int lane, int& r, int& a, int& b, int64_t& before) {
+    for (int s0 = 0; s0 < c.seqs; s0 += 32) {
+        const int s = s0 + lane;
+        int x = 0, y = 0, own = 0;
+        int64_t len = 0;
+        if (s < c.seqs) {
+            c.rows_of(s, x, y);
+            len = __ldg(c.lengths + s);
+            if (y > x) own = int(((len + (y - x - 1)) >> 4) - (len >> 4)) + 1;
+        }
+        int sum = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, at < sum);
+        if (who) {
+            const int l = __ffs(who) - 1;
+            a = __shfl_sync(0xFFFFFFFFu, x, l);
+            b = __shfl_sync(0xFFFFFFFFu, y, l);
+            before = __shfl_sync(0xFFFFFFFFu, len, l);
+            const int local = at - (__shfl_sync(0xFFFFFFFFu, sum, l) - __shfl_sync(0xFFFFFFFFu, own, l));
+            r = local == 0 ? a : a + int((((before >> 4) + local) << 4) - before);
+            return s0 + l;
+        }
+        at -= __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+    return -1;
+}
+
 inline bool kv_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 inline bool kv_shape_ok(int pages, int page_tokens, int kv_heads, int D) {
@@ -77,6 +110,9 @@ inline int kv_check(const tetra_kv_cache* c, int rows, KvCache& k) {
                 c->page_tokens / kKvBlock, c->kv_heads, c->seqs, c->width, rows};
     return TETRA_OK;
 }
+
+// Blocks that a call's rows may fall in: each sequence's, and one more where it begins inside one.
+inline int64_t kv_most_blocks(const KvCache& c) { return int64_t(c.rows) / kKvBlock + 2 * int64_t(c.seqs); }
 
 inline int kv_status(cudaError_t e) { return e == cudaSuccess ? TETRA_OK : TETRA_ERR_CUDA; }
 
