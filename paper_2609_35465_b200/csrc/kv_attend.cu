@@ -80,7 +80,7 @@ struct AttParams {
     // A CTA may be an item's last and the next one's first: what it keeps for either is apart (second: of the item that begins in it).
     float* pieces;         // [CTA][4][PIECE]: pieces, then groups' sums, two each
     uint32_t* arrived;     // [3][CTA]: pieces of the groups that begin in this CTA, two; groups of the item that begins in it
-    const SharedSeq* shared;  // SHARED: by sequence
+    SharedGroups shared;      // SHARED
     float* own;               // SHARED: [row][head][D] sums and, behind them, [row][head][2] references and denominators
     int64_t own_ends;         // where these begin
 };
@@ -148,7 +148,7 @@ __device__ __forceinline__ Work sequence_work(const AttParams& p, int s) {
     w.first = 0;
     w.joined = false;
     if (SHARED) {
-        const uint32_t first = uint32_t(__ldg(&p.shared[s].first));
+        const uint32_t first = uint32_t(shared_of(p.c, p.shared, s, w.row0, b, w.before));
         w.joined = first > 0;
         w.first = min(first, w.blocks);
         w.blocks -= w.first;
@@ -225,7 +225,7 @@ __device__ __forceinline__ void block_sums(uint32_t (&v)[N], uint32_t (*warp_sum
 }
 
 template <int D, int NT, bool SHARED>
-__global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(AttParams p) {
+__device__ __forceinline__ void attend(const AttParams& p) {
     using C = AttCfg<D, NT>;
     constexpr int CHUNKS = C::CHUNKS, STAGES = C::STAGES, REC = C::REC, FRAGS = C::FRAGS, ROUND = C::ROUND;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -241,9 +241,6 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     // (What all lanes of a warp have alike is taken from lane 0 here and below: branches on it need no reconvergence.)
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0), g = lane >> 2, t = lane & 3;
     const int heads = p.c.kv_heads, heads_all = heads * p.group;
-    pdl_wait();
-    pdl_release();
-
     // The first lines of the page table, which is wanted as soon as it is known whose it is.
     {
         const int64_t entries = (p.c.seqs - 1) * p.c.table_stride + p.c.width, at = int64_t(threadIdx.x) * 32;
@@ -811,6 +808,16 @@ __global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(
     }
 }
 
+template <int D, int NT, bool SHARED>
+__global__ void __launch_bounds__(kAttThreads, AttCfg<D, NT>::CTAS) k_kv_attend(AttParams p) {
+    if (!SHARED) {
+        pdl_wait();
+        pdl_release();
+    }
+    attend<D, NT, SHARED>(p);
+    if (SHARED) end_behind_prefix();
+}
+
 constexpr int kAttCounters = kAttMaxCtas * 3 * 4;  // bytes
 template <int D>
 constexpr int att_most_columns() { return D == 256 ? 2 : 4; }
@@ -870,7 +877,7 @@ int attend_params(const tetra_kv_cache* cache, const void* q, int64_t q_stride, 
     p.unit_shift = 0;
     p.arrived = static_cast<uint32_t*>(workspace);
     p.pieces = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + kAttCounters);
-    p.shared = nullptr;
+    p.shared = SharedGroups{nullptr, nullptr, 0};
     p.own = nullptr;
     p.own_ends = 0;
     return TETRA_OK;
@@ -922,7 +929,7 @@ int tetra_kv_attend_shared(const tetra_kv_cache* cache, const tetra_kv_groups* g
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     SharedCall call;
     call.c = p.c;
-    call.g = *groups;
+    call.g = SharedGroups{groups->group_start, groups->shared, groups->groups};
     call.q = p.q;
     call.out = p.out;
     call.q_stride = q_stride;
@@ -933,7 +940,7 @@ int tetra_kv_attend_shared(const tetra_kv_cache* cache, const tetra_kv_groups* g
     call.own_ends = int64_t(rows) * q_heads * D;
     call.pieces = reinterpret_cast<float*>(ws + at.pieces);
     call.most = uint32_t(at.parts);
-    p.shared = call.seqs;
+    p.shared = call.g;
     p.own = call.own;
     p.own_ends = call.own_ends;
     cudaError_t e = launch_prefix(call, D, sms, s);

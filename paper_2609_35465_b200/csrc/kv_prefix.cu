@@ -4,21 +4,23 @@
 // answers of a model with four query heads to a kv head.  2 D bytes a token and kv head stand against 4 D multiply-adds a column, so
 // from about 100 columns on the tensor cores bound it, not HBM, and tcgen05 pays: a tile of 128 columns is one operand's 128 rows.
 //
-// Work.  An item is (group, kv head, tile of 256 columns; 128 with heads of 256), its tokens come in steps of 64 (four records) and
-// are cut into parts; what a CTA does is found by each CTA from the lengths, which are on the device.  A part leaves its sums in the
-// workspace; k_kv_attend, which does the sequences' own tokens, adds them.  No atomics on memory: bit-identical from run to run.
+// Work.  An item is (group, kv head, tile of 256 columns; 128 with heads of 256), its tokens come in steps of 128 (64) and are cut into
+// parts; what a CTA does is found by each CTA from the lengths, which are on the device.  A part leaves its sums in the workspace;
+// k_kv_attend does the sequences' own tokens meanwhile, and k_kv_join adds both.  No atomics on memory: bit-identical from run to run.
 //
-// A CTA.  One thread copies records by cp.async.bulk into a ring.  Four warps turn their bytes into float16 (exact: codes are small
+// A CTA.  One warp copies records by cp.async.bulk into a ring.  Four warps turn their bytes into float16 (exact: codes are small
 // integers) and lay them out for the tensor cores: keys as [token][dim], values as [dim][token], rows of 128 bytes, swizzled; the
-// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  One thread issues the products:
-// S = Q K^T (Q from tensor memory, 128 columns x 64 tokens) and O += P V (P from tensor memory, over S).  Two groups of four warps
+// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  Three tiles of keys or values are in use
+// or being made.  One thread issues the products: S = Q K^T and O += P V (P from tensor memory, over S).  Two groups of four warps
 // ("slots"), a thread a column, turn S into weights: no value of a column is in another thread, so there are no exchanges.  The
 // slots take the two halves of a tile's columns, or, where a tile has no more than 128, every other step, so that the products of
-// one run beside the exponentials of the other.
+// one run beside the exponentials of the other.  (Steps of 64 tokens: what a slot waits for between its steps, two barriers, two
+// products, loads and stores of tensor memory, takes longer than its 64 exponentials a thread: 3300 cycles a step where the products
+// take 1024.)
 //
 // Arithmetic is that of k_kv_attend: scores are exact products summed in float32, times s_K; weights enter as
-// float16(2^(score - m) s_V) with m a running reference that moves only when a weight would pass 2^15 (a vote a step); the
-// denominator sums 2^(score - m) in float32.
+// float16(2^(score - m) s_V) with m a running reference, a whole number, that moves only when a block's weights together would pass
+// 2^15; the denominator sums 2^(score - m) in float32.
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -28,27 +30,31 @@
 namespace tetra {
 namespace {
 
-constexpr int kPreStep = 64;                              // tokens of a step
-constexpr int kPreBlocks = kPreStep / kKvBlock;
+constexpr int kPreHalf = 64;                              // tokens that are copied and converted at a time
+constexpr int kPreBlocks = kPreHalf / kKvBlock;
 constexpr int kPreSoft = 8, kPreConvert = 4;              // warps
 constexpr int kPreConvertAt = kPreSoft, kPreCopyWarp = kPreSoft + kPreConvert, kPreMmaWarp = kPreCopyWarp + 1;
 constexpr int kPreThreads = (kPreMmaWarp + 1) * 32;
-constexpr int kPreScales = 8;                             // steps whose scales are kept
-constexpr uint32_t kPrePartCost = 6;                      // steps that a part's beginning and end take
+constexpr int kPreScales = 8;                             // halves of a step whose scales are kept
+constexpr int kPreTiles = 3;                              // of keys or values
+constexpr uint32_t kPrePartCost = 4;                      // steps that a part's beginning and end take
 constexpr uint32_t kPreTries = 1u << 22;                  // of a wait: then the call's results are NaN
+constexpr int kPreSmem = 227 * 1024 - 2304;               // what a CTA may have, but for the barriers
 constexpr float kPreNoRef = -FLT_MAX, kPreLeastLog = -60.f, kPreHigh = 15.f, kPreBase = 7.f;  // as in k_kv_attend
 constexpr float kPreMost = 32768.f;                       // 2^15
 
 template <int D>
 struct PreCfg {
     static constexpr int SLOTS = pre_slots(D);
+    static constexpr int HALVES = D == 256 ? 1 : 2, STEP = HALVES * kPreHalf;  // tokens of a step
+    static constexpr bool QTENSOR = D == 256;             // queries in tensor memory, else in shared memory
     static constexpr int REC = kv_record_bytes(D), STAGE = kPreBlocks * REC;
-    static constexpr int STAGES = D == 256 ? 2 : 6;
-    static constexpr int TILE = kPreStep * D * 2;         // bytes of a step's keys, or values, in float16
-    static constexpr int RING = 4 * TILE;                 // behind two of each
-    static constexpr int SMEM = RING + STAGES * STAGE + 1024;  // 1024: alignment; and the plan
-    // Columns of tensor memory: a slot's queries, scores (weights over them) and sums.
-    static constexpr int QCOLS = D / 2, SLOT = QCOLS + kPreStep + D;
+    static constexpr int TILE = STEP * D * 2;             // bytes of a step's keys, or values, in float16
+    static constexpr int QTILE = QTENSOR ? 0 : kPreColumns * D * 2;
+    static constexpr int RING = kPreTiles * TILE + SLOTS * QTILE;  // the ring of records is behind the tiles and the queries
+    static constexpr int smem(int stages) { return RING + stages * STAGE + 1024; }  // 1024: alignment; and the plan
+    // Columns of tensor memory of a slot: queries, scores (weights over them), sums.
+    static constexpr int QCOLS = QTENSOR ? D / 2 : 0, SLOT = QCOLS + STEP + D;
     static_assert(SLOTS * SLOT <= 512, "tensor memory");
 };
 
@@ -56,8 +62,8 @@ using PreParams = SharedCall;
 
 // The plan, in shared memory, by group.
 struct PrePlan {
-    int32_t *start, *part0, *count, *leader, *row0, *rows_end, *blocks, *parts;
-    static __host__ __device__ size_t bytes(int groups) { return (size_t(groups) * 8 + 2) * 4; }
+    int32_t *part0, *leader, *row0, *rows_end, *blocks, *parts;
+    static __host__ __device__ size_t bytes(int groups) { return (size_t(groups) * 6 + 1) * 4; }
 };
 
 struct PrePart {
@@ -135,6 +141,11 @@ __device__ __forceinline__ void tensor_product(uint32_t d, uint32_t a, uint64_t 
         "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"(uint32_t(add))
         : "memory");
 }
+__device__ __forceinline__ void tensor_product(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"(uint32_t(add))
+        : "memory");
+}
 __device__ __forceinline__ void tensor_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -166,40 +177,34 @@ __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t* r) {
         TETRA_W8(r, 8), TETRA_W8(r, 16), TETRA_W8(r, 24), "r"(at)
         : "memory");
 }
+// 16 columns.
+__device__ __forceinline__ void tensor_load16(uint32_t at, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : TETRA_R8(r, 0), TETRA_R8(r, 8) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tensor_store16(uint32_t at, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::TETRA_W8(r, 0), TETRA_W8(r, 8), "r"(at) : "memory");
+}
 #undef TETRA_R8
 #undef TETRA_W8
 
 // ---- the plan ------------------------------------------------------------------------------------------------------------
-// The group of sequence s, or -1.
-__device__ __forceinline__ int group_of(const PrePlan& plan, int groups, int seqs, int s) {
-    int lo = 0, hi = groups;  // the last g with start[g] <= s
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (plan.start[mid] <= s) lo = mid;
-        else hi = mid;
-    }
-    const int a = plan.start[lo], b = plan.start[lo + 1];
-    return a >= 0 && b <= seqs && a <= s && s < b ? lo : -1;
-}
-// A sequence shares where all of its rows see all of the shared blocks and none of its own tokens is in them.
-__device__ __forceinline__ bool shares(int a, int b, int before, int blocks) { return b > a && blocks > 0 && int64_t(before) >= int64_t(blocks) * kKvBlock; }
-
 struct PreGroup {
     uint32_t items, steps;
 };
 template <int D>
 __device__ __forceinline__ PreGroup group_work(const PreParams& p, const PrePlan& plan, int g) {
     PreGroup w{0, 1};
-    if (g < p.g.groups && plan.count[g] >= 2) {
+    if (g < p.g.groups && plan.rows_end[g] > 0) {
         const uint32_t cols = uint32_t(plan.rows_end[g] - plan.row0[g]) * p.group;
         w.items = (cols + pre_tile(D) - 1) / pre_tile(D) * p.c.kv_heads;
-        w.steps = (uint32_t(plan.blocks[g]) + kPreBlocks - 1) / kPreBlocks;
+        w.steps = (uint32_t(plan.blocks[g]) * kKvBlock + PreCfg<D>::STEP - 1) / PreCfg<D>::STEP;
     }
     return w;
 }
 // Parts of an item when none has more than `share` steps.
 __device__ __forceinline__ uint32_t pre_parts(uint32_t steps, uint32_t share) {
-    const uint32_t each = (steps + (steps + share - 1) / share - 1) / ((steps + share - 1) / share);
+    if (steps <= share) return 1;
+    const uint32_t parts = (steps + share - 1) / share, each = (steps + parts - 1) / parts;
     return (steps + each - 1) / each;
 }
 
@@ -208,27 +213,30 @@ __device__ __forceinline__ uint32_t pre_parts(uint32_t steps, uint32_t share) {
 template <int D>
 __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan& plan, uint32_t* total) {
     const int groups = p.g.groups, seqs = p.c.seqs, tid = threadIdx.x, lane = tid & 31;
-    const int64_t most_tokens = int64_t(p.c.width) * p.c.blocks_per_page * kKvBlock;
     for (int g = tid; g < groups; g += kPreThreads) {
-        plan.start[g] = __ldg(p.g.group_start + g);
-        const int tokens = __ldg(p.g.shared + g);
-        plan.blocks[g] = int(min(int64_t(max(tokens, 0)), most_tokens) / kKvBlock);
-        plan.count[g] = 0;
         plan.leader[g] = plan.row0[g] = INT_MAX;
-        plan.rows_end[g] = 0;
+        plan.rows_end[g] = plan.blocks[g] = 0;
     }
-    if (tid == 0) plan.start[groups] = __ldg(p.g.group_start + groups);
+    // A sequence's rows and its group, 0 blocks if it does not take part.
+    auto look = [&](int s, int& group, int& a, int& b) {
+        p.c.rows_of(s, a, b);
+        const int before = __ldg(p.c.lengths + s);
+        int first, last;
+        group = group_of(p.g, seqs, s, first, last);
+        const int blocks = group < 0 ? 0 : shared_blocks(p.c, p.g, group);
+        return group >= 0 && takes_part(first, last, blocks, a, b, before) ? blocks : 0;
+    };
+    int group = -1, a = 0, b = 0, blocks = 0;
+    if (tid < seqs) blocks = look(tid, group, a, b);
     __syncthreads();
 #pragma unroll 1
     for (int s = tid; s < seqs; s += kPreThreads) {
-        int a, b;
-        p.c.rows_of(s, a, b);
-        const int before = __ldg(p.c.lengths + s), g = group_of(plan, groups, seqs, s);
-        if (g >= 0 && shares(a, b, before, plan.blocks[g])) {
-            atomicAdd(plan.count + g, 1);
-            atomicMin(plan.leader + g, s);
-            atomicMin(plan.row0 + g, a);
-            atomicMax(plan.rows_end + g, b);
+        if (s != tid) blocks = look(s, group, a, b);
+        if (blocks > 0) {
+            plan.blocks[group] = blocks;
+            atomicMin(plan.leader + group, s);
+            atomicMin(plan.row0 + group, a);
+            atomicMax(plan.rows_end + group, b);
         }
     }
     __syncthreads();
@@ -248,14 +256,14 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
 #pragma unroll 1
         for (uint32_t k = 1; k <= kPreWaves && items; ++k) {
             const uint32_t may = min(k * G, p.most);
-            if (items > may) continue;
+            if (items > may || (k > 1 && 2 * items <= G)) continue;
             uint32_t tried = max(1u, (work + may - 1) / may);
 #pragma unroll 1
             while (tried < longest) {
                 uint32_t need = 0;
                 for (int g = lane; g < groups; g += 32) {
                     const PreGroup w = group_work<D>(p, plan, g);
-                    need += w.items * pre_parts(w.steps, tried);
+                    need += w.items * ((w.steps + tried - 1) / tried);
                 }
                 if (__reduce_add_sync(0xFFFFFFFFu, need) <= may) break;
                 tried += max(1u, tried >> 4);
@@ -263,7 +271,7 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
             tried = min(tried, longest);
             if (k * (tried + kPrePartCost) < cost) cost = k * (tried + kPrePartCost), share = tried;
         }
-        // A group whose parts have no place (which takes sequences that have rows in common) is not shared.
+        // A group whose parts have no place (which takes sequences that have rows in common) has no parts.
         uint32_t at = 0;
         for (int g0 = 0; g0 < groups; g0 += 32) {
             const int g = g0 + lane;
@@ -276,31 +284,25 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
                 if (lane >= o) sum += v;
             }
             if (g < groups) {
-                const bool fits = at + sum <= p.most;
                 plan.part0[g] = int(min(at + sum - own, p.most));
-                plan.parts[g] = fits ? int(parts) : 0;
+                plan.parts[g] = at + sum <= p.most ? int(parts) : 0;
             }
             at += __shfl_sync(0xFFFFFFFFu, sum, 31);
         }
-        if (lane == 0) {
-            *total = min(at, p.most);
-            plan.part0[groups] = int(min(at, p.most));
-        }
+        if (lane == 0) *total = plan.part0[groups] = int(min(at, p.most));
     }
     __syncthreads();
     if (blockIdx.x == 0) {
 #pragma unroll 1
         for (int s = tid; s < seqs; s += kPreThreads) {
-            int a, b;
-            p.c.rows_of(s, a, b);
-            const int before = __ldg(p.c.lengths + s), g = group_of(plan, groups, seqs, s);
             SharedSeq out = {};
-            if (g >= 0 && plan.count[g] >= 2 && plan.parts[g] > 0 && shares(a, b, before, plan.blocks[g])) {
-                out.first = plan.blocks[g];
-                out.part0 = plan.part0[g];
-                out.parts = plan.parts[g];
-                out.row0 = plan.row0[g];
-                out.cols = (plan.rows_end[g] - plan.row0[g]) * p.group;
+            const int blocks = look(s, group, a, b);
+            if (blocks > 0) {
+                out.first = blocks;
+                out.part0 = plan.part0[group];
+                out.parts = plan.parts[group];
+                out.row0 = plan.row0[group];
+                out.cols = (plan.rows_end[group] - plan.row0[group]) * p.group;
                 out.tiles = (out.cols + pre_tile(D) - 1) / pre_tile(D);
             }
             p.seqs[s] = out;
@@ -309,7 +311,7 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
     return *total;
 }
 
-// Part number n of the plan; false: of a group that is not shared.
+// Part number n of the plan; false: of a group that has none.
 template <int D>
 __device__ __forceinline__ bool part_of(const PreParams& p, const PrePlan& plan, uint32_t n, PrePart& q) {
     int lo = 0, hi = p.g.groups;
@@ -322,7 +324,7 @@ __device__ __forceinline__ bool part_of(const PreParams& p, const PrePlan& plan,
     if (parts == 0) return false;
     const uint32_t local = n - uint32_t(plan.part0[lo]), item = local / parts, part = local - item * parts;
     const uint32_t cols = uint32_t(plan.rows_end[lo] - plan.row0[lo]) * p.group, tiles = (cols + pre_tile(D) - 1) / pre_tile(D);
-    const uint32_t head = item / tiles, steps = (uint32_t(plan.blocks[lo]) + kPreBlocks - 1) / kPreBlocks, each = (steps + parts - 1) / parts;
+    const uint32_t head = item / tiles, steps = (uint32_t(plan.blocks[lo]) * kKvBlock + PreCfg<D>::STEP - 1) / PreCfg<D>::STEP, each = (steps + parts - 1) / parts;
     q.leader = plan.leader[lo];
     q.head = int(head);
     q.col0 = int(item - head * tiles) * pre_tile(D);
@@ -372,36 +374,38 @@ __device__ __forceinline__ float block_weights(const uint32_t* scores, const flo
 template <int D>
 __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     using C = PreCfg<D>;
-    constexpr int SLOTS = C::SLOTS, STAGES = C::STAGES, CHUNKS = D / 32;
+    constexpr int SLOTS = C::SLOTS, HALVES = C::HALVES, STEP = C::STEP, CHUNKS = D / 32;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t raw_full[STAGES], raw_empty[STAGES], tile_full[2], tile_empty[2], q_ready[2], s_full[2], p_ready[2], o_done[2],
-        scales_full[kPreScales], drained;
+    __shared__ __align__(8) uint64_t raw_full[8], raw_empty[8], tile_full[kPreTiles], tile_empty[kPreTiles], q_ready[2], s_full[2], p_ready[2], o_done[2], scales_full[kPreScales],
+        other_ready, other_free, drained;
     __shared__ __align__(16) float4 scales[kPreScales][kPreBlocks];  // s_K times the call's, s_V, log2 s_V, whether there is such a block
-    __shared__ uint32_t placed[STAGES], total, tensor_base;
+    __shared__ float2 other[kPreColumns];                            // of the slots that share columns: the second one's references and denominators
+    __shared__ uint32_t placed[8], total, tensor_base;
     __shared__ int failed;
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
     pdl_wait();
     pdl_release();
 
-    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u, stages = uint32_t(p.stages);
     PrePlan plan;
     {
-        int32_t* at = reinterpret_cast<int32_t*>(raw + (base - smem_u32(raw)) + C::RING + STAGES * C::STAGE);
+        int32_t* at = reinterpret_cast<int32_t*>(raw + (base - smem_u32(raw)) + C::RING + p.stages * C::STAGE);
         const int n = p.g.groups;
-        plan = PrePlan{at, at + n + 1, at + 2 * n + 2, at + 3 * n + 2, at + 4 * n + 2, at + 5 * n + 2, at + 6 * n + 2, at + 7 * n + 2};
+        plan = PrePlan{at, at + n + 1, at + 2 * n + 1, at + 3 * n + 1, at + 4 * n + 1, at + 5 * n + 1};
     }
     const uint32_t parts = make_plan<D>(p, plan, &total);
     if (parts <= blockIdx.x) return;
 
     if (threadIdx.x == 0) {
         failed = 0;
-        for (int i = 0; i < STAGES; ++i) bar_init(smem_u32(raw_full + i), 1), bar_init(smem_u32(raw_empty + i), kPreConvert);
+        for (uint32_t i = 0; i < stages; ++i) bar_init(smem_u32(raw_full + i), 1), bar_init(smem_u32(raw_empty + i), kPreConvert);
+        for (int i = 0; i < kPreTiles; ++i) bar_init(smem_u32(tile_full + i), kPreConvert * HALVES), bar_init(smem_u32(tile_empty + i), 1);
         for (int i = 0; i < 2; ++i) {
-            bar_init(smem_u32(tile_full + i), kPreConvert), bar_init(smem_u32(tile_empty + i), 1);
             bar_init(smem_u32(q_ready + i), 4), bar_init(smem_u32(p_ready + i), 4);
             bar_init(smem_u32(s_full + i), 1), bar_init(smem_u32(o_done + i), 1);
         }
         for (int i = 0; i < kPreScales; ++i) bar_init(smem_u32(scales_full + i), 1);
+        bar_init(smem_u32(&other_ready), 4), bar_init(smem_u32(&other_free), 4);
         bar_init(smem_u32(&drained), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -414,25 +418,24 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     fence_after();
     const uint32_t tensor = tensor_base;
     volatile int* gave_up = &failed;
-    const uint32_t ring = base + C::RING;
+    const uint32_t queries = base + kPreTiles * C::TILE, ring = base + C::RING;
     uint32_t n0 = 0;  // steps before the part
 
     if (warp == kPreCopyWarp) {
         // ---- records into the ring: lane l looks up the place of the l-th of the next 32, a batch ahead
         bool ok = true;
-        uint32_t n = 0;
+        uint32_t stage = 0, turn = 0, issued = 0;
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
             if (!part_of<D>(p, plan, at, q)) continue;
-            const uint32_t end = min(q.end * kPreBlocks, q.blocks);
+            const uint32_t begin = q.begin * HALVES, last = q.end * HALVES, end = min(last * kPreBlocks, q.blocks);
             auto look = [&](uint32_t first) { return first + lane < end ? p.c.template record<D>(q.leader, first + lane, q.head) : nullptr; };
-            const unsigned char *now = look(q.begin * kPreBlocks), *next = look(q.begin * kPreBlocks + 32);
-            for (uint32_t step = q.begin; ok && step < q.end; ++step, ++n) {
-                const uint32_t k = (step - q.begin) * kPreBlocks & 31u, stage = n % STAGES;
-                if (k == 0 && step > q.begin) now = next, next = look(step * kPreBlocks + 32);
-                ok = bar_wait(smem_u32(raw_empty + stage), (n / STAGES & 1u) ^ 1u, gave_up);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
+            const unsigned char *now = look(begin * kPreBlocks), *next = look(begin * kPreBlocks + 32);
+            for (uint32_t half = begin; half < last; ++half) {
+                const uint32_t k = (half - begin) * kPreBlocks & 31u;
+                if (k == 0 && half > begin) now = next, next = look(half * kPreBlocks + 32);
+                ok = bar_wait(smem_u32(raw_empty + stage), (turn & 1u) ^ 1u, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 const unsigned char* from = reinterpret_cast<const unsigned char*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<uint64_t>(now), k + (lane & 3)));
                 const uint32_t there = __ballot_sync(0xFFFFFFFFu, lane < kPreBlocks && from != nullptr);
                 const uint32_t bar = smem_u32(raw_full + stage);
@@ -443,18 +446,23 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 }
                 __syncwarp();
                 if (there >> lane & 1u) copy_record(ring + stage * C::STAGE + lane * C::REC, from, C::REC, bar);
+                ++issued;
+                if (++stage == stages) stage = 0, ++turn;
             }
         }
         // Nothing is in flight when the CTA ends: what was copied has been waited for by who converts it, unless that gave up.
         if (!ok) {
             int none = 0;
-            for (uint32_t back = 1; back <= STAGES && back <= n; ++back) bar_wait(smem_u32(raw_full + (n - back) % STAGES), (n - back) / STAGES & 1u, &none);
+            for (uint32_t back = 0; back < stages && back < issued; ++back) {
+                if (stage == 0) stage = stages, --turn;
+                bar_wait(smem_u32(raw_full + --stage), turn & 1u, &none);
+            }
         }
     } else if (warp >= kPreConvertAt && warp < kPreCopyWarp) {
         // ---- bytes to operands
         const int w = warp - kPreConvertAt;
         bool ok = true;
-        uint32_t n = 0;
+        uint32_t stage = 0, turn = 0, tile = 0, tile_turn = 0, n = 0;
         // Keys: a unit of 16 bytes is 8 dims (tt of a chunk of 32) of tokens g and g + 8.  A quarter of the warp takes tokens g, g ^ 1 of
         // two chunks, which no two lanes read or write through the same bank.
         const int odd = lane >> 2 & 1, tt = lane & 3;
@@ -463,55 +471,70 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
             if (!part_of<D>(p, plan, at, q)) continue;
-            for (uint32_t step = q.begin; step < q.end; ++step, ++n) {
-                const uint32_t stage = n % STAGES, from = ring + stage * C::STAGE, two = n & 1u, parity = (n >> 1 & 1u) ^ 1u;
-                ok = bar_wait(smem_u32(raw_full + stage), n / STAGES & 1u, gave_up) && bar_wait(smem_u32(tile_empty + two), parity, gave_up);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                if (w == 0) {
-                    if (lane < kPreBlocks) {
-                        const bool is = placed[stage] >> lane & 1u;
-                        const uint4 raw4 = pre_lds(from + lane * C::REC + 32 * D);
-                        const float vs = __uint_as_float(raw4.y);
-                        float lv = pre_lg2(vs);
-                        lv = lv < kPreLeastLog ? kPreLeastLog : lv;  // NaN stays
-                        scales[n % kPreScales][lane] = is ? make_float4(__uint_as_float(raw4.x) * p.scale, vs, lv, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (uint32_t step = q.begin; ok && step < q.end; ++step) {
+                const uint32_t key_tile = tile, key_turn = tile_turn;
+                if (++tile == kPreTiles) tile = 0, ++tile_turn;
+                const uint32_t value_tile = tile, value_turn = tile_turn;
+                if (++tile == kPreTiles) tile = 0, ++tile_turn;
+#pragma unroll 1
+                for (int half = 0; half < HALVES; ++half, ++n) {
+                    const uint32_t from = ring + stage * C::STAGE;
+                    ok = bar_wait(smem_u32(raw_full + stage), turn & 1u, gave_up) && (half > 0 || bar_wait(smem_u32(tile_empty + key_tile), (key_turn & 1u) ^ 1u, gave_up));
+                    if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                    if (w == 0) {
+                        if (lane < kPreBlocks) {
+                            const bool is = placed[stage] >> lane & 1u;
+                            const uint4 raw4 = pre_lds(from + lane * C::REC + 32 * D);
+                            const float vs = __uint_as_float(raw4.y);
+                            float lv = pre_lg2(vs);
+                            lv = lv < kPreLeastLog ? kPreLeastLog : lv;  // NaN stays
+                            scales[n % kPreScales][lane] = is ? make_float4(__uint_as_float(raw4.x) * p.scale, vs, lv, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_u32(scales_full + n % kPreScales));
                     }
+                    {
+                        const uint32_t to = base + key_tile * C::TILE + half * (kPreHalf * 128);
+#pragma unroll
+                        for (int pair = 0; pair < CHUNKS / 2; ++pair) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const int g = (2 * (lane >> 3) + h) ^ odd, row = w * kKvBlock + (g >> 1) * 4 + (g & 1);
+                                const uint4 u = pre_lds(from + w * C::REC + (2 * pair + odd) * 512 + (g * 4 + tt) * 16);
+                                const uint32_t chunk = odd * 4 + tt, line = to + pair * (STEP * 128) + row * 128;
+                                pre_sts(line + ((chunk ^ (row & 7)) << 4), pre_codes<false>(u.x), pre_codes<true>(u.x), pre_codes<false>(u.y), pre_codes<true>(u.y));
+                                pre_sts(line + 256 + ((chunk ^ ((row + 2) & 7)) << 4), pre_codes<false>(u.z), pre_codes<true>(u.z), pre_codes<false>(u.w), pre_codes<true>(u.w));
+                            }
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) bar_arrive(smem_u32(scales_full + n % kPreScales));
-                }
-                {
-                    const uint32_t to = base + two * C::TILE;
+                    if (lane == 0) bar_arrive(smem_u32(tile_full + key_tile));
+                    if (half == 0) {
+                        ok = bar_wait(smem_u32(tile_empty + value_tile), (value_turn & 1u) ^ 1u, gave_up);
+                        if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                    }
+                    {
+                        const uint32_t to = base + value_tile * C::TILE + half * (D * 128);
 #pragma unroll
-                    for (int pair = 0; pair < CHUNKS / 2; ++pair) {
+                        for (int it = 0; it < D / 32; ++it) {
+                            const int chunk = (w & 1) + 2 * (it >> 1), dq = ((it & 1) * 2 + (lane >> 4)) * 2 + e;
+                            const uint4 u = pre_lds(from + vblock * C::REC + 16 * D + chunk * 512 + (dq * 4 + tq) * 16);
+                            const uint32_t word[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int g = (2 * (lane >> 3) + h) ^ odd, row = w * kKvBlock + (g >> 1) * 4 + (g & 1);
-                            const uint4 u = pre_lds(from + w * C::REC + (2 * pair + odd) * 512 + (g * 4 + tt) * 16);
-                            const uint32_t chunk = odd * 4 + tt, line = to + pair * (kPreStep * 128) + row * 128;
-                            pre_sts(line + ((chunk ^ (row & 7)) << 4), pre_codes<false>(u.x), pre_codes<true>(u.x), pre_codes<false>(u.y), pre_codes<true>(u.y));
-                            pre_sts(line + 256 + ((chunk ^ ((row + 2) & 7)) << 4), pre_codes<false>(u.z), pre_codes<true>(u.z), pre_codes<false>(u.w), pre_codes<true>(u.w));
+                            for (int i = 0; i < 4; ++i) {
+                                const int d = chunk * 32 + dq * 4 + i;
+                                pre_sts(to + d * 128 + (((2 * vblock + (tq >> 1)) ^ (d & 7)) << 4) + (tq & 1) * 8, pre_codes<false>(word[i]), pre_codes<true>(word[i]));
+                            }
                         }
                     }
-                }
-                {
-                    const uint32_t to = base + (2 + two) * C::TILE;
-#pragma unroll
-                    for (int it = 0; it < D / 32; ++it) {
-                        const int chunk = (w & 1) + 2 * (it >> 1), dq = ((it & 1) * 2 + (lane >> 4)) * 2 + e;
-                        const uint4 u = pre_lds(from + vblock * C::REC + 16 * D + chunk * 512 + (dq * 4 + tq) * 16);
-                        const uint32_t word[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int d = chunk * 32 + dq * 4 + i;
-                            pre_sts(to + d * 128 + (((2 * vblock + (tq >> 1)) ^ (d & 7)) << 4) + (tq & 1) * 8, pre_codes<false>(word[i]), pre_codes<true>(word[i]));
-                        }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        bar_arrive(smem_u32(tile_full + value_tile));
+                        bar_arrive(smem_u32(raw_empty + stage));
                     }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {
-                    bar_arrive(smem_u32(tile_full + two));
-                    bar_arrive(smem_u32(raw_empty + stage));
+                    if (++stage == stages) stage = 0, ++turn;
                 }
             }
         }
@@ -519,7 +542,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         // ---- products, issued by one thread
         bool ok = true;
         uint32_t jobs_of[2] = {0, 0}, q_of[2] = {0, 0};
-        const uint64_t tiles = tile_descriptor(base);
+        const uint64_t tiles = tile_descriptor(base), q_tiles = tile_descriptor(queries);
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
             if (!part_of<D>(p, plan, at, q)) continue;
@@ -528,38 +551,48 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
             const uint32_t jobs = halves ? 2 * steps : steps;
             auto step_of = [&](uint32_t job) { return n0 + (halves ? job >> 1 : job); };
             auto scores = [&](uint32_t job) {
-                const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, n = step_of(job), two = n & 1u;
-                if (job < uint32_t(SLOTS)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_of[slot]++ & 1u, gave_up);
-                if (!halves || slot == 0) ok = ok && bar_wait(smem_u32(tile_full + two), n >> 1 & 1u, gave_up);
+                const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, number = 2 * step_of(job), tile = number % kPreTiles;
+                if (job < (halves || SLOTS == 1 ? uint32_t(SLOTS) : 1u)) {  // (slots that share columns share the first one's queries)
+                    ok = ok && bar_wait(smem_u32(q_ready + slot), q_of[0] & 1u, gave_up);
+                }
+                if (!halves || slot == 0) ok = ok && bar_wait(smem_u32(tile_full + tile), number / kPreTiles & 1u, gave_up);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; return; }
                 fence_after();
                 if (elected()) {
-                    const uint32_t a = tensor + slot * C::SLOT, to = a + C::QCOLS;
-                    const uint64_t b = tiles + (two * C::TILE >> 4);
+                    const uint32_t to = tensor + slot * C::SLOT + C::QCOLS;
+                    const uint64_t b = tiles + (tile * C::TILE >> 4);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) tensor_product(to, a + k * 8, b + ((k / 4 * (kPreStep * 128) + k % 4 * 32) >> 4), product_kind(kPreStep), k > 0);
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint64_t keys = b + ((k / 4 * (STEP * 128) + k % 4 * 32) >> 4);
+                        if constexpr (C::QTENSOR) tensor_product(to, tensor + slot * C::SLOT + k * 8, keys, product_kind(STEP), k > 0);
+                        else tensor_product(to, q_tiles + (((halves ? slot : 0) * C::QTILE + k / 4 * (kPreColumns * 128) + k % 4 * 32) >> 4), keys, product_kind(STEP), k > 0);
+                    }
                     tensor_commit(smem_u32(s_full + slot));
+                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + tile));
                 }
                 __syncwarp();
             };
             for (uint32_t job = 0; ok && job < uint32_t(SLOTS) && job < jobs; ++job) scores(job);
             for (uint32_t job = 0; ok && job < jobs; ++job) {
-                const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, n = step_of(job), two = n & 1u;
-                ok = bar_wait(smem_u32(p_ready + slot), jobs_of[slot]++ & 1u, gave_up);
+                const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, number = 2 * step_of(job) + 1, tile = number % kPreTiles;
+                if (!halves || slot == 0) ok = bar_wait(smem_u32(tile_full + tile), number / kPreTiles & 1u, gave_up);
+                ok = ok && bar_wait(smem_u32(p_ready + slot), jobs_of[slot]++ & 1u, gave_up);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 fence_after();
                 if (elected()) {
-                    const uint32_t a = tensor + slot * C::SLOT + C::QCOLS, to = a + kPreStep;
-                    const uint64_t b = tiles + ((2 + two) * C::TILE >> 4);
+                    const uint32_t a = tensor + slot * C::SLOT + C::QCOLS, to = a + STEP;
+                    const uint64_t b = tiles + (tile * C::TILE >> 4);
 #pragma unroll
-                    for (int k = 0; k < kPreStep / 16; ++k) tensor_product(to, a + k * 8, b + (k * 32 >> 4), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
+                    for (int k = 0; k < STEP / 16; ++k)
+                        tensor_product(to, a + k * 8, b + ((k / 4 * (D * 128) + k % 4 * 32) >> 4), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
                     if (job + SLOTS >= jobs) tensor_commit(smem_u32(o_done + slot));  // the slot's last of the part
-                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + two));
+                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + tile));
                 }
                 __syncwarp();
                 if (job + SLOTS < jobs) scores(job + SLOTS);
             }
             n0 += steps;
+            ++q_of[0];
         }
         // What was issued has ended when the tensor memory is given back.
         if (elected()) tensor_commit(smem_u32(&drained));
@@ -569,17 +602,17 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     } else if (warp < 4 * SLOTS) {
         // ---- weights: a thread a column
         const uint32_t slot = warp >> 2, column = threadIdx.x & 127;
-        const uint32_t at_q = tensor + slot * C::SLOT + ((warp & 3u) << 21), at_s = at_q + C::QCOLS, at_o = at_s + kPreStep;  // lanes from bit 16 on
-        uint32_t jobs = 0, pieces_done = 0;
+        const uint32_t at_q = tensor + slot * C::SLOT + ((warp & 3u) << 21), at_s = at_q + C::QCOLS, at_o = at_s + STEP;  // lanes from bit 16 on
+        uint32_t jobs = 0, ends = 0, shared_parts = 0, freed = 0;
         bool ok = true;
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
             if (!part_of<D>(p, plan, at, q)) continue;
             const uint32_t steps = q.end - q.begin, first = q.both ? slot : 0u, by = q.both ? 2u : 1u;
             const int col = q.col0 + (q.both || SLOTS == 1 ? 0 : int(slot) * kPreColumns) + int(column);
-            const bool live = col < q.col0 + q.cols;
+            const bool live = col < q.col0 + q.cols, mine = !q.both || slot == 0;  // whose queries these are, and who leaves the piece
             float ref = kPreNoRef, sum = 0.f;
-            if (first < steps) {
+            if (mine) {
                 const uint32_t row = live ? uint32_t(col) / uint32_t(p.group) : 0u, h = live ? uint32_t(col) - row * p.group : 0u;
                 const uint4* src = reinterpret_cast<const uint4*>(p.q + int64_t(q.row0 + row) * p.q_stride + (int64_t(q.head) * p.group + h) * D);
 #pragma unroll
@@ -590,95 +623,153 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                         const uint4 v = live ? __ldg(src + j * 8 + i) : make_uint4(0, 0, 0, 0);
                         r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
                     }
-                    tensor_store(at_q + j * 32, r);
+                    if constexpr (C::QTENSOR) {
+                        tensor_store(at_q + j * 32, r);
+                    } else {
+                        const uint32_t line = queries + slot * C::QTILE + j * (kPreColumns * 128) + column * 128;
+#pragma unroll
+                        for (uint32_t i = 0; i < 8; ++i) pre_sts(line + ((i ^ (column & 7u)) << 4), r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                    }
                 }
-                wait_stores();
-                fence_before();
+                if constexpr (C::QTENSOR) {
+                    wait_stores();
+                    fence_before();
+                } else {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_u32(q_ready + slot));
+            } else if (lane == 0) {
+                bar_arrive(smem_u32(q_ready + slot));
             }
-            for (uint32_t i = first; i < steps; i += by, ++jobs) {
-                const uint32_t n = n0 + i;
-                ok = bar_wait(smem_u32(scales_full + n % kPreScales), n / kPreScales & 1u, gave_up) && bar_wait(smem_u32(s_full + slot), jobs & 1u, gave_up);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                fence_after();
-                uint32_t r[64];
-                tensor_load(at_s, r);
-                tensor_load(at_s + 32, r + 32);
-                wait_loads();
-                // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
-                // column) call for a new one; as long as none does, no maximum is looked for.
-                uint32_t w[32];
-                float now[kPreBlocks];
-                const float4* c = scales[n % kPreScales];
-                bool over = false;
-#pragma unroll
-                for (int b = 0; b < kPreBlocks; ++b) {
-                    now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
-                    over |= now[b] * c[b].y > kPreMost;
-                }
-                if (__any_sync(0xFFFFFFFFu, over)) {
-                    float next = ref;
-#pragma unroll
-                    for (int b = 0; b < kPreBlocks; ++b) {
-                        float top = -INFINITY;
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) top = fmaxf(top, __uint_as_float(r[16 * b + k]) * c[b].x);
-                        if (c[b].w == 0.f) top = -INFINITY;
-                        float want = top + c[b].z - kPreBase;
-                        if (top - want > kPreHigh - c[b].z) want = top;  // a step of so large scores is more than the room there is
-                        if (over && want > next) next = want;
-                    }
-                    const float f = pre_ex2(ref - next);
-                    ref = next;
-                    sum *= f;
-#pragma unroll
-                    for (int b = 0; b < kPreBlocks; ++b) now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
-                    if (i > first) {  // the products before this step's scores have ended with them
+            if (slot == 1 && freed < shared_parts) {  // the first slot has yet to read the sums of the last part that they shared
+                ok = bar_wait(smem_u32(&other_free), (shared_parts - 1) & 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                freed = shared_parts;
+            }
+            for (uint32_t i = first; ok && i < steps; i += by, ++jobs) {
+                ok = bar_wait(smem_u32(s_full + slot), jobs & 1u, gave_up);
 #pragma unroll 1
-                        for (int j = 0; j < D; j += 32) {
-                            uint32_t o[32];
-                            tensor_load(at_o + j, o);
+                for (int chunk = 0; chunk < STEP / 32; ++chunk) {  // 32 tokens at a time: what registers hold
+                    const uint32_t n = (n0 + i) * HALVES + (chunk >> 1);
+                    if ((chunk & 1) == 0) {
+                        ok = ok && bar_wait(smem_u32(scales_full + n % kPreScales), n / kPreScales & 1u, gave_up);
+                        if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                        fence_after();
+                    }
+                    uint32_t r[32], w[16];
+                    tensor_load(at_s + chunk * 32, r);
+                    const float4 c[2] = {scales[n % kPreScales][(chunk & 1) * 2], scales[n % kPreScales][(chunk & 1) * 2 + 1]};
+                    wait_loads();
+                    // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
+                    // column) call for a new one; as long as none does, no maximum is looked for.
+                    float now[2];
+                    bool over = false;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
+                        over |= now[b] * c[b].y > kPreMost;
+                    }
+                    if (__any_sync(0xFFFFFFFFu, over)) {
+                        float next = ref;
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            float top = -INFINITY;
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) top = fmaxf(top, __uint_as_float(r[16 * b + k]) * c[b].x);
+                            if (c[b].w == 0.f) top = -INFINITY;
+                            float want = rintf(top + c[b].z - kPreBase);
+                            if (top - want > kPreHigh - c[b].z) want = top;  // a step of so large scores is more than the room there is
+                            if (over && want > next) next = want;
+                        }
+                        const float f = pre_ex2(ref - next);  // a power of two
+                        ref = next;
+                        sum *= f;
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
+                        if (i > first) {  // the products before this step's scores have ended with them
+#pragma unroll 1
+                            for (int j = 0; j < D; j += 32) {
+                                tensor_load(at_o + j, r);
+                                wait_loads();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
+                                tensor_store(at_o + j, r);
+                            }
+                        }
+#pragma unroll 1
+                        for (int j = 0; j < chunk; ++j) {  // the step's weights so far
+                            tensor_load16(at_s + j * 16, r);
                             wait_loads();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            tensor_store(at_o + j, o);
+                            for (int k = 0; k < 16; ++k) {
+                                const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&r[k]));
+                                const __half2 h = __floats2half2_rn(v.x * f, v.y * f);
+                                r[k] = *reinterpret_cast<const uint32_t*>(&h);
+                            }
+                            tensor_store16(at_s + j * 16, r);
                         }
                     }
+                    sum += now[0] + now[1];
+                    tensor_store16(at_s + chunk * 16, w);
                 }
-#pragma unroll
-                for (int b = 0; b < kPreBlocks; ++b) sum += now[b];
-                tensor_store(at_s, w);
                 wait_stores();
+                if (!ok) break;
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_u32(p_ready + slot));
             }
             // The piece: sums, then references and denominators.
-            float* piece = p.pieces + (size_t(at) * SLOTS + slot) * pre_piece(D);
+            float* piece = p.pieces + (size_t(at) * SLOTS + (mine ? slot : 0u)) * pre_piece(D);
             if (ok && first < steps) {
-                ok = bar_wait(smem_u32(o_done + slot), pieces_done++ & 1u, gave_up);
+                ok = bar_wait(smem_u32(o_done + slot), ends++ & 1u, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
-                if (ok) {
+                if (ok) fence_after();
+            }
+            if (!mine) {
+                other[column] = make_float2(ref, ok ? sum : __uint_as_float(0x7FC00000u));
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(&other_ready));
+            } else if (ok) {
+                float2 end{kPreNoRef, 0.f};
+                if (q.both) {
+                    ok = bar_wait(smem_u32(&other_ready), shared_parts & 1u, gave_up);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
                     fence_after();
+                    end = other[column];
+                }
+                const float top = fmaxf(ref, end.x), f0 = pre_ex2(ref - top), f1 = pre_ex2(end.x - top);
+                const bool two = q.both && steps > 1;  // else the other slot has nothing
+                sum = two ? fmaf(sum, f0, end.y * f1) : sum;
+                ref = two ? top : ref;
 #pragma unroll 1
-                    for (int j = 0; j < D; j += 32) {
-                        uint32_t o[32];
-                        tensor_load(at_o + j, o);
-                        wait_loads();
-                        if (live) {
+                for (int j = 0; ok && j < D; j += 32) {
+                    uint32_t o[32], u[32];
+                    tensor_load(at_o + j, o);
+                    if (two) tensor_load(at_o + C::SLOT + j, u);
+                    wait_loads();
+                    if (two) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                asm volatile("st.global.cg.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(piece + column * D + j + 8 * k), "r"(o[8 * k]), "r"(o[8 * k + 1]),
-                                             "r"(o[8 * k + 2]), "r"(o[8 * k + 3]), "r"(o[8 * k + 4]), "r"(o[8 * k + 5]), "r"(o[8 * k + 6]), "r"(o[8 * k + 7])
-                                             : "memory");
-                        }
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o[k]), f0, __uint_as_float(u[k]) * f1));
                     }
-                    fence_before();
+                    if (live) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            asm volatile("st.global.cg.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(piece + column * D + j + 8 * k), "r"(o[8 * k]), "r"(o[8 * k + 1]),
+                                         "r"(o[8 * k + 2]), "r"(o[8 * k + 3]), "r"(o[8 * k + 4]), "r"(o[8 * k + 5]), "r"(o[8 * k + 6]), "r"(o[8 * k + 7])
+                                         : "memory");
+                    }
+                }
+                fence_before();
+                if (q.both) {
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(&other_free));
                 }
             }
-            if (live) __stcg(reinterpret_cast<float2*>(piece + kPreColumns * D) + column, make_float2(ref, ok ? sum : __uint_as_float(0x7FC00000u)));
+            if (mine && live) __stcg(reinterpret_cast<float2*>(piece + kPreColumns * D) + column, make_float2(ref, ok ? sum : __uint_as_float(0x7FC00000u)));
             n0 += steps;
+            shared_parts += q.both;
         }
         // A wait that gave up: all that the CTA had still to do becomes NaN.
         if (!ok) {
@@ -692,74 +783,94 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     if (warp == kPreMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
 }
 
-// A column's sums: of its own tokens and of its pieces, in this order, a warp a column.  A lane has D / 32 dims.
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+// A column's sums: of its own tokens and of its pieces, in this order.  A CTA has four columns of a row, two warps a column, which take every
+// other piece and have all of theirs on the way at once (one warp and eight at a time: 14 us where 18 pieces of 2048 columns take 6).
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinColumns = kJoinWarps / 2;
 
-// Four floats, or the two that there are.
+// Four floats, or the two that there are.  (Volatile: these loads stay where they are, side by side.)
 template <int E>
 __device__ __forceinline__ void load_four(const float* from, float* to) {
-    if constexpr (E == 2) {
-        const float2 v = __ldcg(reinterpret_cast<const float2*>(from));
-        to[0] = v.x, to[1] = v.y;
-    } else {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(from));
-        to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
-    }
+    if constexpr (E == 2) asm volatile("ld.global.cg.v2.f32 {%0,%1}, [%2];" : "=f"(to[0]), "=f"(to[1]) : "l"(from));
+    else asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(to[0]), "=f"(to[1]), "=f"(to[2]), "=f"(to[3]) : "l"(from));
 }
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) k_kv_join(PreParams p) {
-    constexpr int E = D / 32, BATCH = 32 / E;  // dims a lane; pieces that are on the way
-    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
+    constexpr int E = D / 32, BATCH = D == 256 ? 8 : 12;  // dims a lane; pieces of a warp that are on the way
+    __shared__ float halves[kJoinColumns][D + 2];
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0), column = warp >> 1, second = warp & 1;
+    const int heads = p.c.kv_heads * p.group, h = blockIdx.y * kJoinColumns + column, r = blockIdx.x;
+    // What came before the three kernels is complete (each starts behind the one before it has waited).
+    int a = 0, b = 0;
+    const int s = sequence_of(p.c, r, lane, a, b);
     pdl_wait();
     pdl_release();
-    const int heads = p.c.kv_heads * p.group, h = blockIdx.y * kJoinWarps + warp, r = blockIdx.x;
-    int a, b;
-    const int s = h < heads ? sequence_of(p.c, r, lane, a, b) : -1;
     if (s < 0) return;
-    const uint4 s0 = __ldcg(reinterpret_cast<const uint4*>(p.seqs + s)), s1 = __ldcg(reinterpret_cast<const uint4*>(p.seqs + s) + 1);
-    const SharedSeq share{int32_t(s0.x), int32_t(s0.y), int32_t(s0.z), int32_t(s0.w), int32_t(s1.x), int32_t(s1.y), {0, 0}};
-    if (share.first == 0) return;  // stored already
-    const int head = h / p.group;
-    const PieceRange range = pieces_of<D>(share, head, uint32_t(r - share.row0) * p.group + uint32_t(h - head * p.group));
-    const size_t piece = size_t(pre_piece(D)), step = piece * range.step;
+    const uint4 s0 = __ldcg(reinterpret_cast<const uint4*>(p.seqs + s));
+    if (s0.x == 0) return;  // stored already
+    const int row0 = __ldcg(&p.seqs[s].row0);
+    const bool is = h < heads;
+    float v[E], ref = kPreNoRef, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = 0.f;
     const int64_t row = int64_t(r) * heads + h;
-    const float* from = p.pieces + size_t(range.first) * piece + range.column * D + lane * E;
-    const float* ends = p.pieces + size_t(range.first) * piece + kPreColumns * D + range.column * 2;
-    float v[E], ref, sum;
-    {
-        const float2 end = __ldcg(reinterpret_cast<const float2*>(p.own + p.own_ends) + row);
+    if (is) {
+        constexpr uint32_t TILE = pre_tile(D);
+        const uint32_t head = uint32_t(h) / uint32_t(p.group), at = uint32_t(r - row0) * p.group + (uint32_t(h) - head * p.group), tile = at / TILE, in = at % TILE;
+        const uint32_t cols = uint32_t(__ldcg(&p.seqs[s].cols));
+        const bool both = pre_slots(D) == 2 && cols - tile * TILE <= kPreColumns;
+        const size_t piece = size_t(pre_piece(D)), step = piece * pre_slots(D);
+        const float* from = p.pieces + (size_t(s0.y) + (size_t(head) * s0.w + tile) * s0.z) * step + (both ? 0 : in / kPreColumns) * piece;
+        const float* ends = from + kPreColumns * D + in % kPreColumns * 2;
+        from += in % kPreColumns * D + lane * E;
+        const int count = int(s0.z);
+        if (!second) {
+            const float2 end = __ldcg(reinterpret_cast<const float2*>(p.own + p.own_ends) + row);
 #pragma unroll
-        for (int k = 0; k < E; k += 4) load_four<E>(p.own + row * D + lane * E + k, v + k);
-        ref = end.x;
-        sum = end.y;
-    }
-#pragma unroll 1
-    for (int i = 0; i < range.count; i += BATCH) {
-        float x[BATCH][E];
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k)
-#pragma unroll
-            for (int j = 0; j < E; j += 4) load_four<E>(from + size_t(min(i + k, range.count - 1)) * step + j, x[k] + j);
-        const bool mine = lane < BATCH && i + lane < range.count;
-        const float2 end = mine ? __ldcg(reinterpret_cast<const float2*>(ends + size_t(i + lane) * step)) : make_float2(kPreNoRef, 0.f);
-        // A denominator of zero: nothing seen, and no sums written.
-        float top = end.y != 0.f ? end.x : kPreNoRef;
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        const float now = fmaxf(ref, top), f = pre_ex2(ref - now), g = end.y != 0.f ? pre_ex2(end.x - now) : 0.f, part = end.y != 0.f ? end.y * g : 0.f;
-        sum *= f;
-#pragma unroll
-        for (int j = 0; j < E; ++j) v[j] *= f;
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            if (i + k >= range.count) break;
-            const float by = __shfl_sync(0xFFFFFFFFu, g, k);
-            const bool is = __shfl_sync(0xFFFFFFFFu, end.y, k) != 0.f;
-            sum += __shfl_sync(0xFFFFFFFFu, part, k);
-#pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = is ? fmaf(x[k][j], by, v[j]) : v[j];
+            for (int k = 0; k < E; k += 4) load_four<E>(p.own + row * D + lane * E + k, v + k);
+            ref = end.x;
+            sum = end.y;
         }
-        ref = now;
+#pragma unroll 1
+        for (int i = second; i < count; i += 2 * BATCH) {
+            float x[BATCH][E];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k)
+#pragma unroll
+                for (int j = 0; j < E; j += 4) load_four<E>(from + size_t(min(i + 2 * k, count - 1)) * step + j, x[k] + j);
+            const bool mine = lane < BATCH && i + 2 * lane < count;
+            const float2 end = mine ? __ldcg(reinterpret_cast<const float2*>(ends + size_t(i + 2 * lane) * step)) : make_float2(kPreNoRef, 0.f);
+            // A denominator of zero: nothing seen.
+            const float own = end.y != 0.f ? end.x : kPreNoRef;
+            const uint32_t order = __float_as_uint(own) ^ (uint32_t(int32_t(__float_as_uint(own)) >> 31) | 0x80000000u);
+            const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, order);
+            const float now = fmaxf(ref, __uint_as_float(most & 0x80000000u ? most ^ 0x80000000u : ~most));
+            const float f = pre_ex2(ref - now), g = end.y != 0.f ? pre_ex2(end.x - now) : 0.f;
+            sum *= f;
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[j] *= f;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const float by = __shfl_sync(0xFFFFFFFFu, g, k), d = __shfl_sync(0xFFFFFFFFu, end.y, k);
+                sum = d != 0.f ? fmaf(d, by, sum) : sum;
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[j] = d != 0.f ? fmaf(x[k][j], by, v[j]) : v[j];
+            }
+            ref = now;
+        }
+        if (second) {
+#pragma unroll
+            for (int k = 0; k < E; ++k) halves[column][lane * E + k] = v[k];
+            if (lane == 0) halves[column][D] = ref, halves[column][D + 1] = sum;
+        }
+    }
+    __syncthreads();
+    if (!is || second) return;
+    const float r1 = halves[column][D], u1 = halves[column][D + 1];
+    if (u1 != 0.f) {
+        const float now = fmaxf(ref, r1), f0 = pre_ex2(ref - now), f1 = pre_ex2(r1 - now);
+        sum = fmaf(u1, f1, sum * f0);
+#pragma unroll
+        for (int k = 0; k < E; ++k) v[k] = fmaf(halves[column][lane * E + k], f1, v[k] * f0);
     }
     const float by = sum == 0.f ? 0.f : 1.f / sum;
     __half* out = p.out + row * D + lane * E;
@@ -768,18 +879,21 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(PreParams p) {
 }
 
 template <int D>
-cudaError_t launch_prefix_for(const PreParams& p, int sms, cudaStream_t s) {
+cudaError_t launch_prefix_for(PreParams& p, int sms, cudaStream_t s) {
     using C = PreCfg<D>;
-    const size_t most = C::SMEM + PrePlan::bytes(TETRA_KV_MAX_SEQS);
     static PerDeviceOnce once;  // per instantiation
-    const cudaError_t e = once.run([&] { return cudaFuncSetAttribute(k_kv_prefix<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)); });
+    const cudaError_t e = once.run([] { return cudaFuncSetAttribute(k_kv_prefix<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPreSmem); });
     if (e != cudaSuccess) return e;
-    return launch_pdl(k_kv_prefix<D>, sms < kPreMostCtas ? sms : kPreMostCtas, kPreThreads, C::SMEM + PrePlan::bytes(p.g.groups), s, p);
+    const size_t plan = PrePlan::bytes(p.g.groups);
+    static_assert(C::smem(2) + (TETRA_KV_MAX_SEQS * 6 + 1) * 4 <= kPreSmem, "two stages and the largest plan");
+    p.stages = 2;
+    while (p.stages < 6 && C::smem(p.stages + 1) + plan <= size_t(kPreSmem)) ++p.stages;
+    return launch_pdl(k_kv_prefix<D>, sms < kPreMostCtas ? sms : kPreMostCtas, kPreThreads, C::smem(p.stages) + plan, s, p);
 }
 template <int D>
 cudaError_t launch_join_for(const PreParams& p, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(p.c.rows), unsigned((p.c.kv_heads * p.group + kJoinWarps - 1) / kJoinWarps));
+    cfg.gridDim = dim3(unsigned(p.c.rows), unsigned((p.c.kv_heads * p.group + kJoinColumns - 1) / kJoinColumns));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -792,7 +906,7 @@ cudaError_t launch_join_for(const PreParams& p, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_prefix(const SharedCall& p, int head_dim, int sms, cudaStream_t s) {
+cudaError_t launch_prefix(SharedCall& p, int head_dim, int sms, cudaStream_t s) {
     return head_dim == 64 ? launch_prefix_for<64>(p, sms, s) : head_dim == 128 ? launch_prefix_for<128>(p, sms, s) : launch_prefix_for<256>(p, sms, s);
 }
 cudaError_t launch_join(const SharedCall& p, int head_dim, cudaStream_t s) {

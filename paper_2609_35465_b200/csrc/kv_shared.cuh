@@ -7,13 +7,49 @@ namespace tetra {
 namespace {
 
 constexpr int kPreColumns = 128;                                    // of a piece: rows of a tensor-core product
-__host__ __device__ constexpr int pre_slots(int D) { return D == 256 ? 1 : 2; }  // pieces of a part: what fits the SM's 512 columns of tensor memory
+__host__ __device__ constexpr int pre_slots(int D) { return D == 256 ? 1 : 2; }  // pieces of a part at most: what fits the SM's 512 columns of tensor memory
 __host__ __device__ constexpr int pre_tile(int D) { return kPreColumns * pre_slots(D); }  // columns of an item
 // Floats of a piece: [column][D] sums, then [column] reference and denominator.
 __host__ __device__ constexpr int pre_piece(int D) { return kPreColumns * (D + 2); }
+constexpr int kSharedLeast = 8;                                     // blocks: fewer are not worth their pieces
+
+// Blocks that sequence s, with rows [a, b) behind `before` tokens, shares with others of its group and does not read itself.  That goes
+// by the sequence and its group alone, so that all kernels know it without each other: where all of its rows see all of the shared blocks,
+// none of its own tokens is in them, and the group has other sequences.
+struct SharedGroups {
+    const int32_t* start;   // [groups + 1]: sequences
+    const int32_t* tokens;  // [groups]
+    int32_t groups;
+};
+// The group of sequence s and its sequences [first, last); -1: none.
+__device__ __forceinline__ int group_of(const SharedGroups& g, int seqs, int s, int& first, int& last) {
+    int lo = 0, hi = g.groups;  // the last one with start <= s
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldg(g.start + mid) <= s) lo = mid;
+        else hi = mid;
+    }
+    first = __ldg(g.start + lo);
+    last = __ldg(g.start + lo + 1);
+    return first >= 0 && last <= seqs && first <= s && s < last ? lo : -1;
+}
+__device__ __forceinline__ int shared_blocks(const KvCache& c, const SharedGroups& g, int group) {
+    const int64_t most = int64_t(c.width) * c.blocks_per_page, blocks = max(__ldg(g.tokens + group), 0) / kKvBlock;
+    return int(min(blocks, most));
+}
+__device__ __forceinline__ bool takes_part(int first, int last, int blocks, int a, int b, int before) {
+    return last - first >= 2 && blocks >= kSharedLeast && b > a && int64_t(before) >= int64_t(blocks) * kKvBlock;
+}
+__device__ __forceinline__ int shared_of(const KvCache& c, const SharedGroups& g, int s, int a, int b, int before) {
+    int first, last;
+    const int group = group_of(g, c.seqs, s, first, last);
+    if (group < 0) return 0;
+    const int blocks = shared_blocks(c, g, group);
+    return takes_part(first, last, blocks, a, b, before) ? blocks : 0;
+}
 
 // Where a sequence's share of the pieces is.  An item is (group, kv head, tile of columns), cut into `parts`; a part leaves a piece
-// for each 128 columns of its tile, or, where the tile has no more than that, two of the same columns and other tokens.
+// for each 128 columns of its tile.
 struct SharedSeq {
     int32_t first;   // blocks that the pieces stand for; 0: none, the sequence reads all of its tokens itself
     int32_t part0;   // of the group's first item
@@ -25,24 +61,6 @@ struct SharedSeq {
 };
 static_assert(sizeof(SharedSeq) == 32, "two 16-byte words");
 
-// A column's pieces.
-struct PieceRange {
-    int32_t first, count, step, column;
-};
-template <int D>
-__device__ __forceinline__ PieceRange pieces_of(const SharedSeq& s, int head, uint32_t column) {
-    constexpr uint32_t TILE = pre_tile(D);
-    const uint32_t tile = column / TILE, in = column % TILE;
-    const bool both = pre_slots(D) == 2 && uint32_t(s.cols) - tile * TILE <= kPreColumns;
-    const int32_t part = s.part0 + int32_t(uint32_t(head) * s.tiles + tile) * s.parts;
-    PieceRange r;
-    r.first = part * pre_slots(D) + (both ? 0 : int32_t(in / kPreColumns));
-    r.step = both ? 1 : pre_slots(D);
-    r.count = both ? 2 * s.parts : s.parts;
-    r.column = int32_t(in % kPreColumns);
-    return r;
-}
-
 constexpr int kPreMostCtas = 160, kPreWaves = 2;  // of a launch; parts a CTA where items are few
 
 // Where things are in the workspace of tetra_kv_attend_shared, behind tetra_kv_attend's: the sequences' shares, the sums of their own
@@ -50,7 +68,7 @@ constexpr int kPreMostCtas = 160, kPreWaves = 2;  // of a launch; parts a CTA wh
 struct SharedPlaces {
     size_t seqs, own, pieces, end, parts;
     SharedPlaces(int D, int64_t rows, int q_heads, int kv_heads, int groups) {
-        const int64_t sharing = groups < rows / 2 ? groups : rows / 2;  // two sequences with a row each, at least
+        const int64_t sharing = groups < rows ? groups : rows;  // a row each, at least
         const int64_t items = (rows * (q_heads / kv_heads) / pre_tile(D) + sharing) * kv_heads, few = kPreWaves * kPreMostCtas;
         parts = size_t(items > few ? items : few);
         seqs = (tetra_kv_workspace_bytes(D) + 255) / 256 * 256;
@@ -60,11 +78,18 @@ struct SharedPlaces {
     }
 };
 
+// k_kv_attend has nothing of k_kv_prefix's but starts behind what came before that (it is released when k_kv_prefix has waited); its
+// end has to imply that one's.
+__device__ __forceinline__ void end_behind_prefix() {
+    pdl_release();
+    pdl_wait();
+}
+
 }  // namespace
 
 struct SharedCall {
     KvCache c;
-    tetra_kv_groups g;
+    SharedGroups g;
     const __half* q;
     __half* out;
     int64_t q_stride;
@@ -75,8 +100,9 @@ struct SharedCall {
     int64_t own_ends;
     float* pieces;
     uint32_t most;      // parts
+    int32_t stages;     // of k_kv_prefix's ring
 };
-cudaError_t launch_prefix(const SharedCall& p, int head_dim, int sms, cudaStream_t s);
+cudaError_t launch_prefix(SharedCall& p, int head_dim, int sms, cudaStream_t s);
 cudaError_t launch_join(const SharedCall& p, int head_dim, cudaStream_t s);
 
 }  // namespace tetra
