@@ -4,19 +4,18 @@
 // answers of a model with four query heads to a kv head.  2 D bytes a token and kv head stand against 4 D multiply-adds a column, so
 // from about 100 columns on the tensor cores bound it, not HBM, and tcgen05 pays: a tile of 128 columns is one operand's 128 rows.
 //
-// Work.  An item is (group, kv head, tile of 256 columns; 128 with heads of 256), its tokens come in steps of 128 (64) and are cut into
+// Work.  An item is (group, kv head, tile of 256 columns; 128 with heads of 256), its tokens come in steps of 64 (four records) and are cut into
 // parts; what a CTA does is found by each CTA from the lengths, which are on the device.  A part leaves its sums in the workspace;
 // k_kv_attend does the sequences' own tokens meanwhile, and k_kv_join adds both.  No atomics on memory: bit-identical from run to run.
 //
 // A CTA.  One warp copies records by cp.async.bulk into a ring.  Four warps turn their bytes into float16 (exact: codes are small
 // integers) and lay them out for the tensor cores: keys as [token][dim], values as [dim][token], rows of 128 bytes, swizzled; the
-// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  Three tiles of keys or values are in use
-// or being made.  One thread issues the products: S = Q K^T and O += P V (P from tensor memory, over S).  Two groups of four warps
+// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  One thread issues the products: S = Q K^T and O += P V (P from tensor memory, over S).  Two groups of four warps
 // ("slots"), a thread a column, turn S into weights: no value of a column is in another thread, so there are no exchanges.  The
 // slots take the two halves of a tile's columns, or, where a tile has no more than 128, every other step, so that the products of
-// one run beside the exponentials of the other.  (Steps of 64 tokens: what a slot waits for between its steps, two barriers, two
-// products, loads and stores of tensor memory, takes longer than its 64 exponentials a thread: 3300 cycles a step where the products
-// take 1024.)
+// one run beside the exponentials of the other.  A slot has two places for scores, so that those of its next step are there when the
+// weights of this one are: with one place the slots' exponentials and the products took turns, 3300 to 3500 cycles for 64 tokens of 256
+// columns, where the exponentials alone are 1024 and the products 1280.
 //
 // Arithmetic is that of k_kv_attend: scores are exact products summed in float32, times s_K; weights enter as
 // float16(2^(score - m) s_V) with m a running reference, a whole number, that moves only when a block's weights together would pass
@@ -24,20 +23,20 @@
 #include <cfloat>
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "kv_shared.cuh"
 
 namespace tetra {
 namespace {
 
-constexpr int kPreHalf = 64;                              // tokens that are copied and converted at a time
-constexpr int kPreBlocks = kPreHalf / kKvBlock;
+constexpr int kPreStep = 64;                              // tokens
+constexpr int kPreBlocks = kPreStep / kKvBlock;
 constexpr int kPreSoft = 8, kPreConvert = 4;              // warps
 constexpr int kPreConvertAt = kPreSoft, kPreCopyWarp = kPreSoft + kPreConvert, kPreMmaWarp = kPreCopyWarp + 1;
 constexpr int kPreThreads = (kPreMmaWarp + 1) * 32;
-constexpr int kPreScales = 8;                             // halves of a step whose scales are kept
-constexpr int kPreTiles = 3;                              // of keys or values
-constexpr uint32_t kPrePartCost = 4;                      // steps that a part's beginning and end take
+constexpr int kPreScales = 8;                             // steps whose scales are kept
+constexpr uint32_t kPrePartCost = 8;                      // steps that a part's beginning and end take
 constexpr uint32_t kPreTries = 1u << 22;                  // of a wait: then the call's results are NaN
 constexpr int kPreSmem = 227 * 1024 - 2304;               // what a CTA may have, but for the barriers
 constexpr float kPreNoRef = -FLT_MAX, kPreLeastLog = -60.f, kPreHigh = 15.f, kPreBase = 7.f;  // as in k_kv_attend
@@ -46,15 +45,14 @@ constexpr float kPreMost = 32768.f;                       // 2^15
 template <int D>
 struct PreCfg {
     static constexpr int SLOTS = pre_slots(D);
-    static constexpr int HALVES = D == 256 ? 1 : 2, STEP = HALVES * kPreHalf;  // tokens of a step
     static constexpr bool QTENSOR = D == 256;             // queries in tensor memory, else in shared memory
     static constexpr int REC = kv_record_bytes(D), STAGE = kPreBlocks * REC;
-    static constexpr int TILE = STEP * D * 2;             // bytes of a step's keys, or values, in float16
+    static constexpr int TILE = kPreStep * D * 2, TILES = D == 256 ? 4 : 6;  // bytes of a step's keys, or values, in float16; tiles
     static constexpr int QTILE = QTENSOR ? 0 : kPreColumns * D * 2;
-    static constexpr int RING = kPreTiles * TILE + SLOTS * QTILE;  // the ring of records is behind the tiles and the queries
+    static constexpr int RING = TILES * TILE + SLOTS * QTILE;  // the ring of records is behind the tiles and the queries
     static constexpr int smem(int stages) { return RING + stages * STAGE + 1024; }  // 1024: alignment; and the plan
-    // Columns of tensor memory of a slot: queries, scores (weights over them), sums.
-    static constexpr int QCOLS = QTENSOR ? D / 2 : 0, SLOT = QCOLS + STEP + D;
+    // Columns of tensor memory of a slot: queries, scores (weights over them) twice, sums.
+    static constexpr int QCOLS = QTENSOR ? D / 2 : 0, SLOT = QCOLS + 2 * kPreStep + D;
     static_assert(SLOTS * SLOT <= 512, "tensor memory");
 };
 
@@ -131,8 +129,9 @@ __device__ __forceinline__ void copy_record(uint32_t to, const void* from, uint3
 
 // ---- tensor cores ------------------------------------------------------------------------------------------------------
 // Rows of 128 bytes in groups of eight (1024 bytes), 16-byte pieces of a row exchanged by the row's place in its group.
+// `at`: the address in shared memory, in units of 16 bytes.
 __device__ __forceinline__ uint64_t tile_descriptor(uint32_t at) {
-    return uint64_t((at & 0x3FFFFu) >> 4) | uint64_t(1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+    return uint64_t(at | 1u << 16) | uint64_t(1024 >> 4 | 1u << 14 | 2u << 29) << 32;
 }
 // float16 x float16 -> float32, 128 rows, n columns, both operands with k running fastest.
 __host__ __device__ constexpr uint32_t product_kind(int n) { return 1u << 4 | uint32_t(n / 8) << 17 | uint32_t(128 / 16) << 24; }
@@ -197,7 +196,7 @@ __device__ __forceinline__ PreGroup group_work(const PreParams& p, const PrePlan
     if (g < p.g.groups && plan.rows_end[g] > 0) {
         const uint32_t cols = uint32_t(plan.rows_end[g] - plan.row0[g]) * p.group;
         w.items = (cols + pre_tile(D) - 1) / pre_tile(D) * p.c.kv_heads;
-        w.steps = (uint32_t(plan.blocks[g]) * kKvBlock + PreCfg<D>::STEP - 1) / PreCfg<D>::STEP;
+        w.steps = (uint32_t(plan.blocks[g]) * kKvBlock + kPreStep - 1) / kPreStep;
     }
     return w;
 }
@@ -324,7 +323,7 @@ __device__ __forceinline__ bool part_of(const PreParams& p, const PrePlan& plan,
     if (parts == 0) return false;
     const uint32_t local = n - uint32_t(plan.part0[lo]), item = local / parts, part = local - item * parts;
     const uint32_t cols = uint32_t(plan.rows_end[lo] - plan.row0[lo]) * p.group, tiles = (cols + pre_tile(D) - 1) / pre_tile(D);
-    const uint32_t head = item / tiles, steps = (uint32_t(plan.blocks[lo]) * kKvBlock + PreCfg<D>::STEP - 1) / PreCfg<D>::STEP, each = (steps + parts - 1) / parts;
+    const uint32_t head = item / tiles, steps = (uint32_t(plan.blocks[lo]) * kKvBlock + kPreStep - 1) / kPreStep, each = (steps + parts - 1) / parts;
     q.leader = plan.leader[lo];
     q.head = int(head);
     q.col0 = int(item - head * tiles) * pre_tile(D);
@@ -374,9 +373,9 @@ __device__ __forceinline__ float block_weights(const uint32_t* scores, const flo
 template <int D>
 __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     using C = PreCfg<D>;
-    constexpr int SLOTS = C::SLOTS, HALVES = C::HALVES, STEP = C::STEP, CHUNKS = D / 32;
+    constexpr int SLOTS = C::SLOTS, TILES = C::TILES, CHUNKS = D / 32;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t raw_full[8], raw_empty[8], tile_full[kPreTiles], tile_empty[kPreTiles], q_ready[2], s_full[2], p_ready[2], o_done[2], scales_full[kPreScales],
+    __shared__ __align__(8) uint64_t raw_full[8], raw_empty[8], tile_full[TILES], tile_empty[TILES], q_ready[2], s_full[4], p_ready[4], o_done[2], scales_full[kPreScales],
         other_ready, other_free, drained;
     __shared__ __align__(16) float4 scales[kPreScales][kPreBlocks];  // s_K times the call's, s_V, log2 s_V, whether there is such a block
     __shared__ float2 other[kPreColumns];                            // of the slots that share columns: the second one's references and denominators
@@ -399,11 +398,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     if (threadIdx.x == 0) {
         failed = 0;
         for (uint32_t i = 0; i < stages; ++i) bar_init(smem_u32(raw_full + i), 1), bar_init(smem_u32(raw_empty + i), kPreConvert);
-        for (int i = 0; i < kPreTiles; ++i) bar_init(smem_u32(tile_full + i), kPreConvert * HALVES), bar_init(smem_u32(tile_empty + i), 1);
-        for (int i = 0; i < 2; ++i) {
-            bar_init(smem_u32(q_ready + i), 4), bar_init(smem_u32(p_ready + i), 4);
-            bar_init(smem_u32(s_full + i), 1), bar_init(smem_u32(o_done + i), 1);
-        }
+        for (int i = 0; i < TILES; ++i) bar_init(smem_u32(tile_full + i), kPreConvert), bar_init(smem_u32(tile_empty + i), 1);
+        for (int i = 0; i < 2; ++i) bar_init(smem_u32(q_ready + i), 4), bar_init(smem_u32(o_done + i), 1);
+        for (int i = 0; i < 4; ++i) bar_init(smem_u32(p_ready + i), 4), bar_init(smem_u32(s_full + i), 1);
         for (int i = 0; i < kPreScales; ++i) bar_init(smem_u32(scales_full + i), 1);
         bar_init(smem_u32(&other_ready), 4), bar_init(smem_u32(&other_free), 4);
         bar_init(smem_u32(&drained), 1);
@@ -418,7 +415,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     fence_after();
     const uint32_t tensor = tensor_base;
     volatile int* gave_up = &failed;
-    const uint32_t queries = base + kPreTiles * C::TILE, ring = base + C::RING;
+    const uint32_t queries = base + TILES * C::TILE, ring = base + C::RING;
     uint32_t n0 = 0;  // steps before the part
 
     if (warp == kPreCopyWarp) {
@@ -428,7 +425,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
             if (!part_of<D>(p, plan, at, q)) continue;
-            const uint32_t begin = q.begin * HALVES, last = q.end * HALVES, end = min(last * kPreBlocks, q.blocks);
+            const uint32_t begin = q.begin, last = q.end, end = min(last * kPreBlocks, q.blocks);
             auto look = [&](uint32_t first) { return first + lane < end ? p.c.template record<D>(q.leader, first + lane, q.head) : nullptr; };
             const unsigned char *now = look(begin * kPreBlocks), *next = look(begin * kPreBlocks + 32);
             for (uint32_t half = begin; half < last; ++half) {
@@ -473,126 +470,138 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
             if (!part_of<D>(p, plan, at, q)) continue;
             for (uint32_t step = q.begin; ok && step < q.end; ++step) {
                 const uint32_t key_tile = tile, key_turn = tile_turn;
-                if (++tile == kPreTiles) tile = 0, ++tile_turn;
+                if (++tile == TILES) tile = 0, ++tile_turn;
                 const uint32_t value_tile = tile, value_turn = tile_turn;
-                if (++tile == kPreTiles) tile = 0, ++tile_turn;
-#pragma unroll 1
-                for (int half = 0; half < HALVES; ++half, ++n) {
-                    const uint32_t from = ring + stage * C::STAGE;
-                    ok = bar_wait(smem_u32(raw_full + stage), turn & 1u, gave_up) && (half > 0 || bar_wait(smem_u32(tile_empty + key_tile), (key_turn & 1u) ^ 1u, gave_up));
-                    if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                    if (w == 0) {
-                        if (lane < kPreBlocks) {
-                            const bool is = placed[stage] >> lane & 1u;
-                            const uint4 raw4 = pre_lds(from + lane * C::REC + 32 * D);
-                            const float vs = __uint_as_float(raw4.y);
-                            float lv = pre_lg2(vs);
-                            lv = lv < kPreLeastLog ? kPreLeastLog : lv;  // NaN stays
-                            scales[n % kPreScales][lane] = is ? make_float4(__uint_as_float(raw4.x) * p.scale, vs, lv, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
-                        }
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(smem_u32(scales_full + n % kPreScales));
+                if (++tile == TILES) tile = 0, ++tile_turn;
+                const uint32_t from = ring + stage * C::STAGE;
+                ok = bar_wait(smem_u32(raw_full + stage), turn & 1u, gave_up) && bar_wait(smem_u32(tile_empty + key_tile), (key_turn & 1u) ^ 1u, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                if (w == 0) {
+                    if (lane < kPreBlocks) {
+                        const bool is = placed[stage] >> lane & 1u;
+                        const uint4 raw4 = pre_lds(from + lane * C::REC + 32 * D);
+                        const float vs = __uint_as_float(raw4.y);
+                        float lv = pre_lg2(vs);
+                        lv = lv < kPreLeastLog ? kPreLeastLog : lv;  // NaN stays
+                        scales[n % kPreScales][lane] = is ? make_float4(__uint_as_float(raw4.x) * p.scale, vs, lv, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
                     }
-                    {
-                        const uint32_t to = base + key_tile * C::TILE + half * (kPreHalf * 128);
-#pragma unroll
-                        for (int pair = 0; pair < CHUNKS / 2; ++pair) {
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const int g = (2 * (lane >> 3) + h) ^ odd, row = w * kKvBlock + (g >> 1) * 4 + (g & 1);
-                                const uint4 u = pre_lds(from + w * C::REC + (2 * pair + odd) * 512 + (g * 4 + tt) * 16);
-                                const uint32_t chunk = odd * 4 + tt, line = to + pair * (STEP * 128) + row * 128;
-                                pre_sts(line + ((chunk ^ (row & 7)) << 4), pre_codes<false>(u.x), pre_codes<true>(u.x), pre_codes<false>(u.y), pre_codes<true>(u.y));
-                                pre_sts(line + 256 + ((chunk ^ ((row + 2) & 7)) << 4), pre_codes<false>(u.z), pre_codes<true>(u.z), pre_codes<false>(u.w), pre_codes<true>(u.w));
-                            }
-                        }
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) bar_arrive(smem_u32(tile_full + key_tile));
-                    if (half == 0) {
-                        ok = bar_wait(smem_u32(tile_empty + value_tile), (value_turn & 1u) ^ 1u, gave_up);
-                        if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                    }
-                    {
-                        const uint32_t to = base + value_tile * C::TILE + half * (D * 128);
-#pragma unroll
-                        for (int it = 0; it < D / 32; ++it) {
-                            const int chunk = (w & 1) + 2 * (it >> 1), dq = ((it & 1) * 2 + (lane >> 4)) * 2 + e;
-                            const uint4 u = pre_lds(from + vblock * C::REC + 16 * D + chunk * 512 + (dq * 4 + tq) * 16);
-                            const uint32_t word[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int d = chunk * 32 + dq * 4 + i;
-                                pre_sts(to + d * 128 + (((2 * vblock + (tq >> 1)) ^ (d & 7)) << 4) + (tq & 1) * 8, pre_codes<false>(word[i]), pre_codes<true>(word[i]));
-                            }
-                        }
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        bar_arrive(smem_u32(tile_full + value_tile));
-                        bar_arrive(smem_u32(raw_empty + stage));
-                    }
-                    if (++stage == stages) stage = 0, ++turn;
+                    if (lane == 0) bar_arrive(smem_u32(scales_full + n % kPreScales));
                 }
+                {
+                    const uint32_t to = base + key_tile * C::TILE;
+#pragma unroll
+                    for (int pair = 0; pair < CHUNKS / 2; ++pair) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int g = (2 * (lane >> 3) + h) ^ odd, row = w * kKvBlock + (g >> 1) * 4 + (g & 1);
+                            const uint4 u = pre_lds(from + w * C::REC + (2 * pair + odd) * 512 + (g * 4 + tt) * 16);
+                            const uint32_t chunk = odd * 4 + tt, line = to + pair * (kPreStep * 128) + row * 128;
+                            pre_sts(line + ((chunk ^ (row & 7)) << 4), pre_codes<false>(u.x), pre_codes<true>(u.x), pre_codes<false>(u.y), pre_codes<true>(u.y));
+                            pre_sts(line + 256 + ((chunk ^ ((row + 2) & 7)) << 4), pre_codes<false>(u.z), pre_codes<true>(u.z), pre_codes<false>(u.w), pre_codes<true>(u.w));
+                        }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(tile_full + key_tile));
+                ok = bar_wait(smem_u32(tile_empty + value_tile), (value_turn & 1u) ^ 1u, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                {
+                    const uint32_t to = base + value_tile * C::TILE;
+#pragma unroll
+                    for (int it = 0; it < D / 32; ++it) {
+                        const int chunk = (w & 1) + 2 * (it >> 1), dq = ((it & 1) * 2 + (lane >> 4)) * 2 + e;
+                        const uint4 u = pre_lds(from + vblock * C::REC + 16 * D + chunk * 512 + (dq * 4 + tq) * 16);
+                        const uint32_t word[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int d = chunk * 32 + dq * 4 + i;
+                            pre_sts(to + d * 128 + (((2 * vblock + (tq >> 1)) ^ (d & 7)) << 4) + (tq & 1) * 8, pre_codes<false>(word[i]), pre_codes<true>(word[i]));
+                        }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    bar_arrive(smem_u32(tile_full + value_tile));
+                    bar_arrive(smem_u32(raw_empty + stage));
+                }
+                if (++stage == stages) stage = 0, ++turn;
+                ++n;
             }
         }
     } else if (warp == kPreMmaWarp) {
-        // ---- products, issued by one thread
+        // ---- products, issued by one thread.  A job is a slot's step: jobs 0, 1, 2, .. are slots 0, 1, 0, .. (of one slot: 0, 0, ..).
+        // A job's scores are issued one step of its slot ahead of its weights' products, into the place that the slot's last but one step had,
+        // whose products are waited for (products with different results are in no order).
         bool ok = true;
-        uint32_t jobs_of[2] = {0, 0}, q_of[2] = {0, 0};
-        const uint64_t tiles = tile_descriptor(base), q_tiles = tile_descriptor(queries);
+        uint32_t before[2] = {0, 0}, q_parts = 0;  // a slot's jobs of earlier parts
+        const uint32_t tiles = (base & 0x3FFFFu) >> 4, q_tiles = (queries & 0x3FFFFu) >> 4;
+        constexpr uint32_t PAIRS = TILES / 2;  // a step's keys are tile 2 (step % PAIRS), its values the next one
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
             if (!part_of<D>(p, plan, at, q)) continue;
             const uint32_t steps = q.end - q.begin;
             const bool halves = SLOTS == 2 && !q.both;  // each step is both slots' work
             const uint32_t jobs = halves ? 2 * steps : steps;
-            auto step_of = [&](uint32_t job) { return n0 + (halves ? job >> 1 : job); };
-            auto scores = [&](uint32_t job) {
-                const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, number = 2 * step_of(job), tile = number % kPreTiles;
-                if (job < (halves || SLOTS == 1 ? uint32_t(SLOTS) : 1u)) {  // (slots that share columns share the first one's queries)
-                    ok = ok && bar_wait(smem_u32(q_ready + slot), q_of[0] & 1u, gave_up);
-                }
-                if (!halves || slot == 0) ok = ok && bar_wait(smem_u32(tile_full + tile), number / kPreTiles & 1u, gave_up);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; return; }
+            auto scores = [&](auto which_slot, uint32_t job) {
+                constexpr uint32_t slot = decltype(which_slot)::value;
+                const uint32_t step = n0 + (halves ? job >> 1 : job), pair = step % PAIRS, own = before[slot] + (SLOTS == 2 ? job >> 1 : job), place = own & 1u;
+                if (job == slot && (halves || slot == 0)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_parts & 1u, gave_up);  // (slots that share columns: the first one's)
+                if (own >= 2) ok = ok && bar_wait(smem_u32(o_done + slot), own & 1u, gave_up);
+                if (!halves || slot == 0) ok = ok && bar_wait(smem_u32(tile_full + 2 * pair), step / PAIRS & 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) return;
                 fence_after();
+                const uint32_t to = tensor + slot * C::SLOT + C::QCOLS + place * kPreStep, keys = tiles + (2 * pair * C::TILE >> 4);
+                const uint32_t from = q_tiles + (halves ? slot * C::QTILE >> 4 : 0);
                 if (elected()) {
-                    const uint32_t to = tensor + slot * C::SLOT + C::QCOLS;
-                    const uint64_t b = tiles + (tile * C::TILE >> 4);
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
-                        const uint64_t keys = b + ((k / 4 * (STEP * 128) + k % 4 * 32) >> 4);
-                        if constexpr (C::QTENSOR) tensor_product(to, tensor + slot * C::SLOT + k * 8, keys, product_kind(STEP), k > 0);
-                        else tensor_product(to, q_tiles + (((halves ? slot : 0) * C::QTILE + k / 4 * (kPreColumns * 128) + k % 4 * 32) >> 4), keys, product_kind(STEP), k > 0);
+                        const uint64_t b = tile_descriptor(keys + ((k / 4 * (kPreStep * 128) + k % 4 * 32) >> 4));
+                        if constexpr (C::QTENSOR) tensor_product(to, tensor + slot * C::SLOT + k * 8, b, product_kind(kPreStep), k > 0);
+                        else tensor_product(to, tile_descriptor(from + ((k / 4 * (kPreColumns * 128) + k % 4 * 32) >> 4)), b, product_kind(kPreStep), k > 0);
                     }
-                    tensor_commit(smem_u32(s_full + slot));
-                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + tile));
+                    tensor_commit(smem_u32(s_full + slot * 2) + place * 8);
+                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty) + 16 * pair);
                 }
                 __syncwarp();
             };
-            for (uint32_t job = 0; ok && job < uint32_t(SLOTS) && job < jobs; ++job) scores(job);
-            for (uint32_t job = 0; ok && job < jobs; ++job) {
-                const uint32_t slot = SLOTS == 2 ? job & 1u : 0u, number = 2 * step_of(job) + 1, tile = number % kPreTiles;
-                if (!halves || slot == 0) ok = bar_wait(smem_u32(tile_full + tile), number / kPreTiles & 1u, gave_up);
-                ok = ok && bar_wait(smem_u32(p_ready + slot), jobs_of[slot]++ & 1u, gave_up);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+            auto sums = [&](auto which_slot, uint32_t job) {
+                constexpr uint32_t slot = decltype(which_slot)::value;
+                const uint32_t step = n0 + (halves ? job >> 1 : job), pair = step % PAIRS, own = before[slot] + (SLOTS == 2 ? job >> 1 : job), place = own & 1u;
+                if (!halves || slot == 0) ok = bar_wait(smem_u32(tile_full + 2 * pair + 1), step / PAIRS & 1u, gave_up);
+                ok = ok && bar_wait(smem_u32(p_ready + slot * 2) + place * 8, own >> 1 & 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) return;
                 fence_after();
+                const uint32_t to = tensor + slot * C::SLOT + C::QCOLS + 2 * kPreStep, a = tensor + slot * C::SLOT + C::QCOLS + place * kPreStep;
+                const uint32_t values = tiles + ((2 * pair + 1) * C::TILE >> 4);
                 if (elected()) {
-                    const uint32_t a = tensor + slot * C::SLOT + C::QCOLS, to = a + STEP;
-                    const uint64_t b = tiles + (tile * C::TILE >> 4);
 #pragma unroll
-                    for (int k = 0; k < STEP / 16; ++k)
-                        tensor_product(to, a + k * 8, b + ((k / 4 * (D * 128) + k % 4 * 32) >> 4), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
-                    if (job + SLOTS >= jobs) tensor_commit(smem_u32(o_done + slot));  // the slot's last of the part
-                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + tile));
+                    for (int k = 0; k < kPreStep / 16; ++k) tensor_product(to, a + k * 8, tile_descriptor(values + (k * 32 >> 4)), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
+                    tensor_commit(smem_u32(o_done + slot));
+                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + 1) + 16 * pair);
                 }
                 __syncwarp();
-                if (job + SLOTS < jobs) scores(job + SLOTS);
+            };
+            using First = std::integral_constant<uint32_t, 0>;
+            using Second = std::integral_constant<uint32_t, SLOTS - 1>;
+            scores(First(), 0);
+            if (SLOTS == 2 && ok && jobs > 1) scores(Second(), 1);
+            for (uint32_t job = 0; ok && job < jobs; job += SLOTS) {
+                if (job + SLOTS < jobs) scores(First(), job + SLOTS);
+                if (ok) sums(First(), job);
+                if (SLOTS == 2 && ok && job + 1 < jobs) {
+                    if (job + 3 < jobs) scores(Second(), job + 3);
+                    if (ok) sums(Second(), job + 1);
+                }
             }
             n0 += steps;
-            ++q_of[0];
+            ++q_parts;
+            before[0] += SLOTS == 2 ? (jobs + 1) / 2 : jobs;
+            before[1] += jobs / 2;
         }
         // What was issued has ended when the tensor memory is given back.
         if (elected()) tensor_commit(smem_u32(&drained));
@@ -602,8 +611,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     } else if (warp < 4 * SLOTS) {
         // ---- weights: a thread a column
         const uint32_t slot = warp >> 2, column = threadIdx.x & 127;
-        const uint32_t at_q = tensor + slot * C::SLOT + ((warp & 3u) << 21), at_s = at_q + C::QCOLS, at_o = at_s + STEP;  // lanes from bit 16 on
-        uint32_t jobs = 0, ends = 0, shared_parts = 0, freed = 0;
+        const uint32_t at_q = tensor + slot * C::SLOT + ((warp & 3u) << 21), at_scores = at_q + C::QCOLS, at_o = at_scores + 2 * kPreStep;  // lanes from bit 16 on
+        uint32_t jobs = 0, shared_parts = 0, freed = 0;
         bool ok = true;
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
@@ -648,18 +657,15 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 freed = shared_parts;
             }
             for (uint32_t i = first; ok && i < steps; i += by, ++jobs) {
-                ok = bar_wait(smem_u32(s_full + slot), jobs & 1u, gave_up);
+                const uint32_t which = jobs & 1u, at_s = at_scores + which * kPreStep, n = n0 + i;
+                ok = bar_wait(smem_u32(scales_full + n % kPreScales), n / kPreScales & 1u, gave_up) && bar_wait(smem_u32(s_full + slot * 2 + which), jobs >> 1 & 1u, gave_up);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                fence_after();
 #pragma unroll 1
-                for (int chunk = 0; chunk < STEP / 32; ++chunk) {  // 32 tokens at a time: what registers hold
-                    const uint32_t n = (n0 + i) * HALVES + (chunk >> 1);
-                    if ((chunk & 1) == 0) {
-                        ok = ok && bar_wait(smem_u32(scales_full + n % kPreScales), n / kPreScales & 1u, gave_up);
-                        if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                        fence_after();
-                    }
+                for (int chunk = 0; chunk < kPreStep / 32; ++chunk) {  // 32 tokens at a time: what registers hold
                     uint32_t r[32], w[16];
                     tensor_load(at_s + chunk * 32, r);
-                    const float4 c[2] = {scales[n % kPreScales][(chunk & 1) * 2], scales[n % kPreScales][(chunk & 1) * 2 + 1]};
+                    const float4 c[2] = {scales[n % kPreScales][chunk * 2], scales[n % kPreScales][chunk * 2 + 1]};
                     wait_loads();
                     // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
                     // column) call for a new one; as long as none does, no maximum is looked for.
@@ -687,7 +693,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                         sum *= f;
 #pragma unroll
                         for (int b = 0; b < 2; ++b) now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
-                        if (i > first) {  // the products before this step's scores have ended with them
+                        if (i > first) {
+                            ok = ok && bar_wait(smem_u32(o_done + slot), (jobs - 1) & 1u, gave_up);
+                            fence_after();
 #pragma unroll 1
                             for (int j = 0; j < D; j += 32) {
                                 tensor_load(at_o + j, r);
@@ -714,15 +722,16 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                     tensor_store16(at_s + chunk * 16, w);
                 }
                 wait_stores();
+                ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(smem_u32(p_ready + slot));
+                if (lane == 0) bar_arrive(smem_u32(p_ready + slot * 2 + which));
             }
             // The piece: sums, then references and denominators.
             float* piece = p.pieces + (size_t(at) * SLOTS + (mine ? slot : 0u)) * pre_piece(D);
             if (ok && first < steps) {
-                ok = bar_wait(smem_u32(o_done + slot), ends++ & 1u, gave_up);
+                ok = bar_wait(smem_u32(o_done + slot), (jobs - 1) & 1u, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (ok) fence_after();
             }
