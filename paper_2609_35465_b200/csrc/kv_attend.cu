@@ -23,7 +23,9 @@
 // m moves only when a weight would pass 2^15: a vote per block, a reduction when it does.
 //
 // SHARED: the second kernel of tetra_kv_attend_shared.  The first blocks of a sequence that shares them with others are k_kv_prefix's:
-// here they are not read, and the columns' sums are left for k_kv_join.
+// here they are not read, and the columns' sums are left for k_kv_join.  As that adds pieces anyway, items of eight columns are cut
+// into runs of blocks, a warp's each, and no warp waits for another (64 sequences of 100 to 1024 tokens of their own: 33 us where CTAs
+// have ranges of units and merge at the end of each item).
 #include <cfloat>
 #include <cmath>
 
@@ -83,6 +85,8 @@ struct AttParams {
     SharedGroups shared;      // SHARED
     float* own;               // SHARED: [row][head][D] sums and, behind them, [row][head][2] references and denominators
     int64_t own_ends;         // where these begin
+    OwnSeq* owns;             // SHARED, of eight columns: by sequence, which runs it has; then `own` is [run][8][D]
+    uint32_t runs_most;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -156,6 +160,13 @@ __device__ __forceinline__ Work sequence_work(const AttParams& p, int s) {
     w.units = max(1u, (w.blocks + (kAttWarps << p.unit_shift) - 1) / (kAttWarps << p.unit_shift));
     return w;
 }
+// Behind the blocks that an item's last row sees.
+template <int NT, bool SHARED>
+__device__ __forceinline__ uint32_t last_block(const AttParams& p, const Work& w, const Seg& q) {
+    const uint32_t rows = q.col0 + 8 * NT >= q.cols ? w.rows : (q.col0 + 8 * NT - 1) / uint32_t(p.group) + 1;  // up to the item's last
+    const int64_t seen = int64_t(w.before) + rows;
+    return seen <= 0 ? 0u : min(SHARED ? w.first + w.blocks : w.blocks, uint32_t((seen + kKvBlock - 1) / kKvBlock));
+}
 // The part of units [u0, u1) of an item.
 template <int NT, bool SHARED>
 __device__ __forceinline__ void set_seg(const AttParams& p, const Work& w, int s, uint32_t item, uint32_t u0, uint32_t u1, int first, int last, Seg& q) {
@@ -169,9 +180,7 @@ __device__ __forceinline__ void set_seg(const AttParams& p, const Work& w, int s
     q.joined = w.joined;
     q.first = first;
     q.last = last;
-    const uint32_t rows = q.col0 + 8 * NT >= q.cols ? w.rows : (q.col0 + 8 * NT - 1) / uint32_t(p.group) + 1;  // up to the item's last
-    const int64_t seen = int64_t(w.before) + rows;
-    const uint32_t n = seen <= 0 ? 0u : min(SHARED ? w.first + w.blocks : w.blocks, uint32_t((seen + kKvBlock - 1) / kKvBlock));
+    const uint32_t n = last_block<NT, SHARED>(p, w, q);
     q.r0 = (SHARED ? w.first : 0u) + u0 * (kAttWarps << p.unit_shift);
     q.r1 = min(n, (SHARED ? w.first : 0u) + u1 * (kAttWarps << p.unit_shift));
 }
@@ -228,6 +237,7 @@ template <int D, int NT, bool SHARED>
 __device__ __forceinline__ void attend(const AttParams& p) {
     using C = AttCfg<D, NT>;
     constexpr int CHUNKS = C::CHUNKS, STAGES = C::STAGES, REC = C::REC, FRAGS = C::FRAGS, ROUND = C::ROUND;
+    constexpr bool RUNS = SHARED && NT == 1;  // of an item, a warp's each
     extern __shared__ __align__(16) unsigned char smem[];
     unsigned char* ring = smem;
     float4* merge = reinterpret_cast<float4*>(smem + C::RING);                             // [warps][ROUND + NT][32]
@@ -251,9 +261,44 @@ __device__ __forceinline__ void attend(const AttParams& p) {
     // that would leave CTAs idle for long, a CTA takes a range of the sequence of all units; but of very short items each is a
     // warp's own.  Up to 32 sequences are one warp's work to cut, without a barrier.
     const uint32_t G = gridDim.x;
-    bool few, tiny = false;
-    uint32_t share;
-    if (p.c.seqs <= 32) {
+    bool few = false, tiny = RUNS;
+    uint32_t share = 0, run = 1;  // blocks of a run
+    if (RUNS) {
+        // Runs as long as leave every warp of the grid one, but of eight blocks at least (what a warp begins and ends with takes as long).
+        const int per = (p.c.seqs + kAttThreads - 1) / kAttThreads, s0 = threadIdx.x * per, s1 = min(s0 + per, p.c.seqs);
+        uint32_t total[1] = {0};
+#pragma unroll 1
+        for (int s = s0; s < s1; ++s) {
+            const Work w = sequence_work<NT, SHARED>(p, s);
+            total[0] += w.chunks * heads * w.blocks;
+        }
+        block_sums(total, warp_sums);
+        run = max(8u, (total[0] + G * kAttWarps - 1) / (G * kAttWarps));
+        auto wanted = [&](const Work& w) { return w.chunks * heads * max(1u, (w.blocks + run - 1) / run); };
+        uint32_t mine = 0;
+#pragma unroll 1
+        for (int s = s0; s < s1; ++s) mine += wanted(sequence_work<NT, SHARED>(p, s));
+        uint32_t sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        if (lane == 31) warp_sums[0][warp] = sum;
+        __syncthreads();
+        uint32_t at = sum - mine;
+        for (int w = 0; w < warp; ++w) at += warp_sums[0][w];
+        if (threadIdx.x == kAttThreads - 1) prefix[p.c.seqs] = min(at + mine, p.runs_most);
+#pragma unroll 1
+        for (int s = s0; s < s1; ++s) {
+            const Work w = sequence_work<NT, SHARED>(p, s);
+            prefix[s] = min(at, p.runs_most);
+            if (blockIdx.x == 0) p.owns[s] = OwnSeq{int32_t(at), int32_t(at + wanted(w) <= p.runs_most ? max(1u, (w.blocks + run - 1) / run) : 0u), int32_t(w.chunks), 0};
+            at += wanted(w);
+        }
+        if (threadIdx.x == 0) cursor_seq = 0;
+        __syncthreads();
+    } else if (p.c.seqs <= 32) {
         if (warp == 0) {
             const bool is = lane < p.c.seqs;
             Work w = is ? sequence_work<NT, SHARED>(p, lane) : Work{0, 0, 0, 0, 0, 1, 0, false};
@@ -407,7 +452,17 @@ __device__ __forceinline__ void attend(const AttParams& p) {
             }
             const Work w = sequence_work<NT, SHARED>(p, s);
             __syncwarp();
-            if (lane == 0) set_seg<NT, SHARED>(p, w, s, item - prefix[s], 0, w.units, 0, 0, segs[warp]);
+            if (RUNS) {
+                const uint32_t runs = max(1u, (w.blocks + run - 1) / run), local = item - prefix[s], it = quotient(local, runs), u = local - it * runs;
+                if (lane == 0) {
+                    set_seg<NT, SHARED>(p, w, s, it, 0, 0, 0, 0, segs[warp]);
+                    const uint32_t end = last_block<NT, SHARED>(p, w, segs[warp]);
+                    segs[warp].r0 = w.first + u * run;
+                    segs[warp].r1 = min(end, w.first + (u + 1) * run);
+                }
+            } else {
+                if (lane == 0) set_seg<NT, SHARED>(p, w, s, item - prefix[s], 0, w.units, 0, 0, segs[warp]);
+            }
             __syncwarp();
         } else if (!few) {  // the next parts of items of this CTA's range
             if (threadIdx.x == 0) {
@@ -673,11 +728,12 @@ __device__ __forceinline__ void attend(const AttParams& p) {
                     const float s = sum[0][k], by = s == 0.f ? 0.f : 1.f / s;  // nothing seen: zero
                     if (int(col) >= sg.cols) continue;
                     const int64_t at = int64_t(sg.row0 + row) * heads_all + sg.head * p.group + h;
-                    if (SHARED && sg.joined) {
+                    if (RUNS) {
+                        const int64_t piece = int64_t(item) * 8 + 2 * t + k;
 #pragma unroll
                         for (int j = 0; j < CHUNKS; ++j)
-                            __stcg(reinterpret_cast<float4*>(p.own + at * D + 4 * g + 32 * j), make_float4(o[2 * j][k], o[2 * j][k + 2], o[2 * j + 1][k], o[2 * j + 1][k + 2]));
-                        if (g == 0) __stcg(reinterpret_cast<float2*>(p.own + p.own_ends) + at, make_float2(ref[0][k], s));
+                            __stcg(reinterpret_cast<float4*>(p.own + piece * D + 4 * g + 32 * j), make_float4(o[2 * j][k], o[2 * j][k + 2], o[2 * j + 1][k], o[2 * j + 1][k + 2]));
+                        if (g == 0) __stcg(reinterpret_cast<float2*>(p.own + p.own_ends) + piece, make_float2(ref[0][k], s));
                         continue;
                     }
                     __half* out = p.out + at * D + 4 * g;
@@ -846,9 +902,10 @@ cudaError_t launch_attend(AttParams p, int sms, cudaStream_t s) {
 // 1000 and 8000 47 / 57 / 78, 2000 and 8000 64 / 76 / 101; one row in the piece's place 15, 20, 33 and 57 with 8.
 // (At the cap of 128 registers two CTAs to an SM leave 16 columns of 128 dims with 100 bytes spilt a thread, 32 of 64 with 12:
 // 64 sequences of 4 rows behind 4000 tokens, 16 columns of 128, take 106 us, 5.0 TB/s.)
+int64_t attend_columns(const AttParams& p) { return (int64_t(p.c.rows) * p.group + p.c.seqs - 1) / p.c.seqs; }
 template <int D, bool SHARED>
 cudaError_t launch_attend_for(const AttParams& p, int sms, cudaStream_t s) {
-    const int64_t columns = (int64_t(p.c.rows) * p.group + p.c.seqs - 1) / p.c.seqs;
+    const int64_t columns = attend_columns(p);
     if (columns <= 8) return launch_attend<D, 1, SHARED>(p, sms, s);
     if (D == 256 || columns <= 24) return launch_attend<D, 2, SHARED>(p, sms, s);
     return launch_attend<D, att_most_columns<D>(), SHARED>(p, sms, s);
@@ -880,6 +937,8 @@ int attend_params(const tetra_kv_cache* cache, const void* q, int64_t q_stride, 
     p.shared = SharedGroups{nullptr, nullptr, 0};
     p.own = nullptr;
     p.own_ends = 0;
+    p.owns = nullptr;
+    p.runs_most = 0;
     return TETRA_OK;
 }
 
@@ -937,12 +996,16 @@ int tetra_kv_attend_shared(const tetra_kv_cache* cache, const tetra_kv_groups* g
     call.group = p.group;
     call.seqs = reinterpret_cast<SharedSeq*>(ws + at.seqs);
     call.own = reinterpret_cast<float*>(ws + at.own);
-    call.own_ends = int64_t(rows) * q_heads * D;
+    call.runs = attend_columns(p) <= 8;
+    call.own_ends = (call.runs ? int64_t(at.runs) * 8 : int64_t(rows) * q_heads) * D;
+    call.owns = reinterpret_cast<OwnSeq*>(ws + at.owns);
     call.pieces = reinterpret_cast<float*>(ws + at.pieces);
     call.most = uint32_t(at.parts);
     p.shared = call.g;
     p.own = call.own;
     p.own_ends = call.own_ends;
+    p.owns = call.owns;
+    p.runs_most = uint32_t(at.runs);
     cudaError_t e = launch_prefix(call, D, sms, s);
     if (e == cudaSuccess) e = launch_attend_all<true>(p, D, sms, s);
     if (e == cudaSuccess) e = launch_join(call, D, s);

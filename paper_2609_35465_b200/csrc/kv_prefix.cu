@@ -814,43 +814,44 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(PreParams p) {
     pdl_wait();
     pdl_release();
     if (s < 0) return;
-    const uint4 s0 = __ldcg(reinterpret_cast<const uint4*>(p.seqs + s));
-    if (s0.x == 0) return;  // stored already
-    const int row0 = __ldcg(&p.seqs[s].row0);
+    const uint4 s0 = __ldcg(reinterpret_cast<const uint4*>(p.seqs + s)), s1 = __ldcg(reinterpret_cast<const uint4*>(p.seqs + s) + 1);
+    const uint4 o = p.runs ? __ldcg(reinterpret_cast<const uint4*>(p.owns + s)) : make_uint4(0, 1, 0, 0);
+    if (!p.runs && s0.x == 0) return;  // stored already
     const bool is = h < heads;
     float v[E], ref = kPreNoRef, sum = 0.f;
 #pragma unroll
     for (int k = 0; k < E; ++k) v[k] = 0.f;
     const int64_t row = int64_t(r) * heads + h;
     if (is) {
+        // Its own pieces, then those of the tokens that it shares.
         constexpr uint32_t TILE = pre_tile(D);
-        const uint32_t head = uint32_t(h) / uint32_t(p.group), at = uint32_t(r - row0) * p.group + (uint32_t(h) - head * p.group), tile = at / TILE, in = at % TILE;
-        const uint32_t cols = uint32_t(__ldcg(&p.seqs[s].cols));
-        const bool both = pre_slots(D) == 2 && cols - tile * TILE <= kPreColumns;
+        const uint32_t head = uint32_t(h) / uint32_t(p.group), in_group = uint32_t(h) - head * p.group;
+        const uint32_t mine_at = uint32_t(r - a) * p.group + in_group, own_count = o.y;
+        const int64_t first_own = p.runs ? (int64_t(o.x) + (int64_t(head) * o.z + mine_at / 8) * own_count) * 8 + mine_at % 8 : row;
+        const float *own = p.own + first_own * D + lane * E, *own_ends = p.own + p.own_ends + first_own * 2;
+        const uint32_t at = uint32_t(r - int(s1.x)) * p.group + in_group, tile = at / TILE, in = at % TILE;
+        const bool both = pre_slots(D) == 2 && s1.y - tile * TILE <= kPreColumns;
         const size_t piece = size_t(pre_piece(D)), step = piece * pre_slots(D);
         const float* from = p.pieces + (size_t(s0.y) + (size_t(head) * s0.w + tile) * s0.z) * step + (both ? 0 : in / kPreColumns) * piece;
         const float* ends = from + kPreColumns * D + in % kPreColumns * 2;
         from += in % kPreColumns * D + lane * E;
-        const int count = int(s0.z);
-        if (!second) {
-            const float2 end = __ldcg(reinterpret_cast<const float2*>(p.own + p.own_ends) + row);
-#pragma unroll
-            for (int k = 0; k < E; k += 4) load_four<E>(p.own + row * D + lane * E + k, v + k);
-            ref = end.x;
-            sum = end.y;
-        }
+        const int count = int(own_count + (s0.x ? s0.z : 0u));
+        auto sums_at = [&](int i) { return i < int(own_count) ? own + size_t(i) * 8 * D : from + size_t(i - int(own_count)) * step; };
+        auto ends_at = [&](int i) { return i < int(own_count) ? own_ends + size_t(i) * 16 : ends + size_t(i - int(own_count)) * step; };
 #pragma unroll 1
         for (int i = second; i < count; i += 2 * BATCH) {
             float x[BATCH][E];
 #pragma unroll
-            for (int k = 0; k < BATCH; ++k)
+            for (int k = 0; k < BATCH; ++k) {
+                const float* to = sums_at(min(i + 2 * k, count - 1));
 #pragma unroll
-                for (int j = 0; j < E; j += 4) load_four<E>(from + size_t(min(i + 2 * k, count - 1)) * step + j, x[k] + j);
+                for (int j = 0; j < E; j += 4) load_four<E>(to + j, x[k] + j);
+            }
             const bool mine = lane < BATCH && i + 2 * lane < count;
-            const float2 end = mine ? __ldcg(reinterpret_cast<const float2*>(ends + size_t(i + 2 * lane) * step)) : make_float2(kPreNoRef, 0.f);
+            const float2 end = mine ? __ldcg(reinterpret_cast<const float2*>(ends_at(i + 2 * lane))) : make_float2(kPreNoRef, 0.f);
             // A denominator of zero: nothing seen.
-            const float own = end.y != 0.f ? end.x : kPreNoRef;
-            const uint32_t order = __float_as_uint(own) ^ (uint32_t(int32_t(__float_as_uint(own)) >> 31) | 0x80000000u);
+            const float own_ref = end.y != 0.f ? end.x : kPreNoRef;
+            const uint32_t order = __float_as_uint(own_ref) ^ (uint32_t(int32_t(__float_as_uint(own_ref)) >> 31) | 0x80000000u);
             const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, order);
             const float now = fmaxf(ref, __uint_as_float(most & 0x80000000u ? most ^ 0x80000000u : ~most));
             const float f = pre_ex2(ref - now), g = end.y != 0.f ? pre_ex2(end.x - now) : 0.f;

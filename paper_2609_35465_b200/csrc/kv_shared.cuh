@@ -61,19 +61,30 @@ struct SharedSeq {
 };
 static_assert(sizeof(SharedSeq) == 32, "two 16-byte words");
 
+// A sequence's own tokens, of items of eight columns: its first run, runs of an item, items of a kv head.
+struct OwnSeq {
+    int32_t run0, runs, chunks, spare;
+};
+constexpr int kRunsMost = 8 * 384;  // warps of k_kv_attend's largest grid: runs beside one of each item
+
 constexpr int kPreMostCtas = 160, kPreWaves = 2;  // of a launch; parts a CTA where items are few
 
 // Where things are in the workspace of tetra_kv_attend_shared, behind tetra_kv_attend's: the sequences' shares, the sums of their own
 // tokens, the pieces; and how many parts may leave pieces.
 struct SharedPlaces {
-    size_t seqs, own, pieces, end, parts;
+    size_t seqs, owns, own, pieces, end, parts, runs;
     SharedPlaces(int D, int64_t rows, int q_heads, int kv_heads, int groups) {
         const int64_t sharing = groups < rows ? groups : rows;  // a row each, at least
         const int64_t items = (rows * (q_heads / kv_heads) / pre_tile(D) + sharing) * kv_heads, few = kPreWaves * kPreMostCtas;
         parts = size_t(items > few ? items : few);
         seqs = (tetra_kv_workspace_bytes(D) + 255) / 256 * 256;
-        own = seqs + size_t(TETRA_KV_MAX_SEQS) * sizeof(SharedSeq);
-        pieces = (own + size_t(rows) * q_heads * (D + 2) * sizeof(float) + 255) / 256 * 256;
+        owns = seqs + size_t(TETRA_KV_MAX_SEQS) * sizeof(SharedSeq);
+        own = owns + size_t(TETRA_KV_MAX_SEQS) * sizeof(OwnSeq);
+        // Items of eight columns are those of calls with no more than eight a sequence on average.
+        const int64_t group = q_heads / kv_heads, few_rows = rows * group < 8 * TETRA_KV_MAX_SEQS ? rows : 8 * TETRA_KV_MAX_SEQS / group;
+        runs = size_t(kv_heads * (few_rows * group / 8 + (few_rows < TETRA_KV_MAX_SEQS ? few_rows : TETRA_KV_MAX_SEQS)) + kRunsMost);
+        const size_t columns = runs * 8 > size_t(rows) * q_heads ? runs * 8 : size_t(rows) * q_heads;
+        pieces = (own + columns * (D + 2) * sizeof(float) + 255) / 256 * 256;
         end = pieces + parts * pre_slots(D) * pre_piece(D) * sizeof(float);
     }
 };
@@ -96,8 +107,10 @@ struct SharedCall {
     float scale;        // times log2 e
     int32_t group;      // query heads to a kv head
     SharedSeq* seqs;
-    float* own;         // [row][head][D] sums and, from own_ends on, [row][head][2] references and denominators
+    float* own;         // [row][head][D], or [run][8][D], sums and, from own_ends on, references and denominators of each
     int64_t own_ends;
+    OwnSeq* owns;
+    bool runs;          // own sums are those of runs, of all sequences; else of items, of sequences that share
     float* pieces;
     uint32_t most;      // parts
     int32_t stages;     // of k_kv_prefix's ring
