@@ -549,7 +549,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 constexpr uint32_t slot = decltype(which_slot)::value;
                 const uint32_t step = n0 + (halves ? job >> 1 : job), pair = step % PAIRS, own = before[slot] + (SLOTS == 2 ? job >> 1 : job), place = own & 1u;
                 if (job == slot && (halves || slot == 0)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_parts & 1u, gave_up);  // (slots that share columns: the first one's)
-                if (own >= 2) ok = ok && bar_wait(smem_u32(o_done + slot), own & 1u, gave_up);
+                // (Of a part's first job the slot's last one before has been issued too: a barrier tells of its last phase only.)
+                if (job < uint32_t(SLOTS) ? own >= 1 : own >= 2) ok = ok && bar_wait(smem_u32(o_done + slot), (job < uint32_t(SLOTS) ? own + 1 : own) & 1u, gave_up);
                 if (!halves || slot == 0) ok = ok && bar_wait(smem_u32(tile_full + 2 * pair), step / PAIRS & 1u, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) return;
@@ -674,7 +675,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
-                        over |= now[b] * c[b].y > kPreMost;
+                        over |= !(now[b] * c[b].y <= kPreMost);  // infinite times a scale of zero calls for one too
                     }
                     if (__any_sync(0xFFFFFFFFu, over)) {
                         float next = ref;
