@@ -266,14 +266,16 @@ __device__ __forceinline__ void attend(const AttParams& p) {
     if (RUNS) {
         // Runs as long as leave every warp of the grid one, but of eight blocks at least (what a warp begins and ends with takes as long).
         const int per = (p.c.seqs + kAttThreads - 1) / kAttThreads, s0 = threadIdx.x * per, s1 = min(s0 + per, p.c.seqs);
-        uint32_t total[1] = {0};
+        uint64_t read = 0;
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) {
             const Work w = sequence_work<NT, SHARED>(p, s);
-            total[0] += w.chunks * heads * w.blocks;
+            read += uint64_t(w.chunks * heads) * w.blocks;
         }
+        uint32_t total[2] = {uint32_t(read) & 0xFFFFFFu, uint32_t(read >> 24)};  // 256 threads' sums do not wrap
         block_sums(total, warp_sums);
-        run = max(8u, (total[0] + G * kAttWarps - 1) / (G * kAttWarps));
+        const uint32_t warps = G * kAttWarps;
+        run = max(8u, total[1] ? uint32_t(((uint64_t(total[1]) << 24) + total[0]) / warps) + 1u : (total[0] + warps - 1) / warps);
         auto wanted = [&](const Work& w) { return w.chunks * heads * max(1u, (w.blocks + run - 1) / run); };
         uint32_t mine = 0;
 #pragma unroll 1

@@ -60,8 +60,8 @@ using PreParams = SharedCall;
 
 // The plan, in shared memory, by group.
 struct PrePlan {
-    int32_t *part0, *leader, *row0, *rows_end, *blocks, *parts;
-    static __host__ __device__ size_t bytes(int groups) { return (size_t(groups) * 6 + 1) * 4; }
+    int32_t *part0, *leader, *row0, *rows_end, *blocks, *parts, *each;  // each: steps of a part
+    static __host__ __device__ size_t bytes(int groups) { return (size_t(groups) * 7 + 1) * 4; }
 };
 
 struct PrePart {
@@ -195,20 +195,22 @@ __device__ __forceinline__ PreGroup group_work(const PreParams& p, const PrePlan
     PreGroup w{0, 1};
     if (g < p.g.groups && plan.rows_end[g] > 0) {
         const uint32_t cols = uint32_t(plan.rows_end[g] - plan.row0[g]) * p.group;
-        w.items = (cols + pre_tile(D) - 1) / pre_tile(D) * p.c.kv_heads;
+        w.items = min((cols + pre_tile(D) - 1) / pre_tile(D) * p.c.kv_heads, 1u << 20);  // (that many have no place: no sum wraps)
         w.steps = (uint32_t(plan.blocks[g]) * kKvBlock + kPreStep - 1) / kPreStep;
     }
     return w;
 }
-// Parts of an item when none has more than `share` steps.
-__device__ __forceinline__ uint32_t pre_parts(uint32_t steps, uint32_t share) {
+// Parts of an item when none has more than `share` steps, all but the last of `each`.
+__device__ __forceinline__ uint32_t pre_parts(uint32_t steps, uint32_t share, uint32_t& each) {
+    each = steps;
     if (steps <= share) return 1;
-    const uint32_t parts = (steps + share - 1) / share, each = (steps + parts - 1) / parts;
+    const uint32_t parts = (steps + share - 1) / share;
+    each = (steps + parts - 1) / parts;
     return (steps + each - 1) / each;
 }
 
 // Every CTA finds out for itself how the work is cut.  The longest part decides, so the share of a part is the least with which
-// there are no more parts than CTAs, or twice as many, whichever takes less.  Returns the number of parts.
+// there are no more parts than CTAs, or twice as many, whichever takes less: 32 shares are looked at at a time.  Returns the number of parts.
 template <int D>
 __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan& plan, uint32_t* total) {
     const int groups = p.g.groups, seqs = p.c.seqs, tid = threadIdx.x, lane = tid & 31;
@@ -241,11 +243,13 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
     __syncthreads();
     if (tid < 32) {
         const uint32_t G = gridDim.x;
+        const PreGroup mine = group_work<D>(p, plan, lane);
+        auto work_of = [&](int g) { return g == lane ? mine : group_work<D>(p, plan, g); };
         uint32_t items = 0, work = 0, longest = 1;
         for (int g = lane; g < groups; g += 32) {
-            const PreGroup w = group_work<D>(p, plan, g);
+            const PreGroup w = work_of(g);
             items += w.items;
-            work += w.items * w.steps;
+            work += w.items * min(w.steps, 1u << 22);  // (looked at where items are few)
             longest = max(longest, w.steps);
         }
         items = __reduce_add_sync(0xFFFFFFFFu, items);
@@ -256,26 +260,30 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
         for (uint32_t k = 1; k <= kPreWaves && items; ++k) {
             const uint32_t may = min(k * G, p.most);
             if (items > may || (k > 1 && 2 * items <= G)) continue;
-            uint32_t tried = max(1u, (work + may - 1) / may);
-#pragma unroll 1
-            while (tried < longest) {
+            uint32_t from = max(1u, (work + may - 1) / may), tried, fits;
+            do {
+                const uint32_t by = max(1u, from >> 4);
+                tried = min(from + lane * by, longest);
                 uint32_t need = 0;
-                for (int g = lane; g < groups; g += 32) {
-                    const PreGroup w = group_work<D>(p, plan, g);
-                    need += w.items * ((w.steps + tried - 1) / tried);
+                for (int g0 = 0; g0 < groups; g0 += 32) {
+                    const PreGroup w = work_of(g0 + lane);
+#pragma unroll 1
+                    for (int g = 0; g < min(groups - g0, 32); ++g)
+                        need += __shfl_sync(0xFFFFFFFFu, w.items, g) * ((__shfl_sync(0xFFFFFFFFu, w.steps, g) + tried - 1) / tried);
                 }
-                if (__reduce_add_sync(0xFFFFFFFFu, need) <= may) break;
-                tried += max(1u, tried >> 4);
-            }
-            tried = min(tried, longest);
+                fits = __ballot_sync(0xFFFFFFFFu, need <= may);  // some does: an item in one part
+                from += 32 * by;
+            } while (fits == 0);
+            tried = __shfl_sync(0xFFFFFFFFu, tried, __ffs(fits) - 1);
             if (k * (tried + kPrePartCost) < cost) cost = k * (tried + kPrePartCost), share = tried;
         }
         // A group whose parts have no place (which takes sequences that have rows in common) has no parts.
         uint32_t at = 0;
         for (int g0 = 0; g0 < groups; g0 += 32) {
             const int g = g0 + lane;
-            const PreGroup w = group_work<D>(p, plan, g);
-            const uint32_t parts = w.items ? pre_parts(w.steps, share) : 0u;
+            const PreGroup w = work_of(g);
+            uint32_t each = 1;
+            const uint32_t parts = w.items ? pre_parts(w.steps, share, each) : 0u;
             uint32_t own = w.items * parts, sum = own;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -285,6 +293,7 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
             if (g < groups) {
                 plan.part0[g] = int(min(at + sum - own, p.most));
                 plan.parts[g] = at + sum <= p.most ? int(parts) : 0;
+                plan.each[g] = int(each);
             }
             at += __shfl_sync(0xFFFFFFFFu, sum, 31);
         }
@@ -321,9 +330,9 @@ __device__ __forceinline__ bool part_of(const PreParams& p, const PrePlan& plan,
     }
     const uint32_t parts = uint32_t(plan.parts[lo]);
     if (parts == 0) return false;
-    const uint32_t local = n - uint32_t(plan.part0[lo]), item = local / parts, part = local - item * parts;
+    const uint32_t local = n - uint32_t(plan.part0[lo]), item = parts == 1 ? local : local / parts, part = local - item * parts;
     const uint32_t cols = uint32_t(plan.rows_end[lo] - plan.row0[lo]) * p.group, tiles = (cols + pre_tile(D) - 1) / pre_tile(D);
-    const uint32_t head = item / tiles, steps = (uint32_t(plan.blocks[lo]) * kKvBlock + kPreStep - 1) / kPreStep, each = (steps + parts - 1) / parts;
+    const uint32_t head = tiles == 1 ? item : item / tiles, steps = (uint32_t(plan.blocks[lo]) * kKvBlock + kPreStep - 1) / kPreStep, each = uint32_t(plan.each[lo]);
     q.leader = plan.leader[lo];
     q.head = int(head);
     q.col0 = int(item - head * tiles) * pre_tile(D);
@@ -375,32 +384,20 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     using C = PreCfg<D>;
     constexpr int SLOTS = C::SLOTS, TILES = C::TILES, CHUNKS = D / 32;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t raw_full[8], raw_empty[8], tile_full[TILES], tile_empty[TILES], q_ready[2], s_full[4], p_ready[4], o_done[2], scales_full[kPreScales],
+    __shared__ __align__(8) uint64_t raw_full[8], raw_empty[8], tile_full[TILES], tile_empty[TILES], q_ready[2], s_full[4], p_ready[4], o_done[4], scales_full[kPreScales],
         other_ready, other_free, drained;
     __shared__ __align__(16) float4 scales[kPreScales][kPreBlocks];  // s_K times the call's, s_V, log2 s_V, whether there is such a block
     __shared__ float2 other[kPreColumns];                            // of the slots that share columns: the second one's references and denominators
     __shared__ uint32_t placed[8], total, tensor_base;
     __shared__ int failed;
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
-    pdl_wait();
-    pdl_release();
-
-    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u, stages = uint32_t(p.stages);
-    PrePlan plan;
-    {
-        int32_t* at = reinterpret_cast<int32_t*>(raw + (base - smem_u32(raw)) + C::RING + p.stages * C::STAGE);
-        const int n = p.g.groups;
-        plan = PrePlan{at, at + n + 1, at + 2 * n + 1, at + 3 * n + 1, at + 4 * n + 1, at + 5 * n + 1};
-    }
-    const uint32_t parts = make_plan<D>(p, plan, &total);
-    if (parts <= blockIdx.x) return;
-
+    const uint32_t stages = uint32_t(p.stages);
     if (threadIdx.x == 0) {
         failed = 0;
         for (uint32_t i = 0; i < stages; ++i) bar_init(smem_u32(raw_full + i), 1), bar_init(smem_u32(raw_empty + i), kPreConvert);
         for (int i = 0; i < TILES; ++i) bar_init(smem_u32(tile_full + i), kPreConvert), bar_init(smem_u32(tile_empty + i), 1);
-        for (int i = 0; i < 2; ++i) bar_init(smem_u32(q_ready + i), 4), bar_init(smem_u32(o_done + i), 1);
-        for (int i = 0; i < 4; ++i) bar_init(smem_u32(p_ready + i), 4), bar_init(smem_u32(s_full + i), 1);
+        for (int i = 0; i < 2; ++i) bar_init(smem_u32(q_ready + i), 4);
+        for (int i = 0; i < 4; ++i) bar_init(smem_u32(p_ready + i), 4), bar_init(smem_u32(s_full + i), 1), bar_init(smem_u32(o_done + i), 1);
         for (int i = 0; i < kPreScales; ++i) bar_init(smem_u32(scales_full + i), 1);
         bar_init(smem_u32(&other_ready), 4), bar_init(smem_u32(&other_free), 4);
         bar_init(smem_u32(&drained), 1);
@@ -411,8 +408,23 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     fence_before();
-    __syncthreads();
+    pdl_wait();
+    pdl_release();
+
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    PrePlan plan;
+    {
+        int32_t* at = reinterpret_cast<int32_t*>(raw + (base - smem_u32(raw)) + C::RING + p.stages * C::STAGE);
+        const int n = p.g.groups;
+        plan = PrePlan{at, at + n + 1, at + 2 * n + 1, at + 3 * n + 1, at + 4 * n + 1, at + 5 * n + 1, at + 6 * n + 1};
+    }
+    const uint32_t parts = make_plan<D>(p, plan, &total);  // (its barriers are also those behind what is above)
     fence_after();
+    if (parts <= blockIdx.x) {
+        if (warp == kPreMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor_base) : "memory");
+        return;
+    }
+
     const uint32_t tensor = tensor_base;
     volatile int* gave_up = &failed;
     const uint32_t queries = base + TILES * C::TILE, ring = base + C::RING;
@@ -534,7 +546,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     } else if (warp == kPreMmaWarp) {
         // ---- products, issued by one thread.  A job is a slot's step: jobs 0, 1, 2, .. are slots 0, 1, 0, .. (of one slot: 0, 0, ..).
         // A job's scores are issued one step of its slot ahead of its weights' products, into the place that the slot's last but one step had,
-        // whose products are waited for (products with different results are in no order).
+        // whose products are waited for (products with different results are in no order).  Each place has barriers of its own: a barrier tells
+        // of its last phase only, and the products of two jobs of a slot may both be on their way.
         bool ok = true;
         uint32_t before[2] = {0, 0}, q_parts = 0;  // a slot's jobs of earlier parts
         const uint32_t tiles = (base & 0x3FFFFu) >> 4, q_tiles = (queries & 0x3FFFFu) >> 4;
@@ -548,9 +561,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
             auto scores = [&](auto which_slot, uint32_t job) {
                 constexpr uint32_t slot = decltype(which_slot)::value;
                 const uint32_t step = n0 + (halves ? job >> 1 : job), pair = step % PAIRS, own = before[slot] + (SLOTS == 2 ? job >> 1 : job), place = own & 1u;
-                if (job == slot && (halves || slot == 0)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_parts & 1u, gave_up);  // (slots that share columns: the first one's)
-                // (Of a part's first job the slot's last one before has been issued too: a barrier tells of its last phase only.)
-                if (job < uint32_t(SLOTS) ? own >= 1 : own >= 2) ok = ok && bar_wait(smem_u32(o_done + slot), (job < uint32_t(SLOTS) ? own + 1 : own) & 1u, gave_up);
+                if (job == slot && (halves || slot == 0)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_parts & 1u, gave_up);
+                // (Slots that share columns have the first one's queries, but no phase of a barrier is left out.)
+                if (SLOTS == 2 && job == 0 && !halves) ok = ok && bar_wait(smem_u32(q_ready + 1), q_parts & 1u, gave_up);
+                if (own >= 2) ok = ok && bar_wait(smem_u32(o_done + slot * 2) + place * 8, (own >> 1) + 1 & 1u, gave_up);
                 if (!halves || slot == 0) ok = ok && bar_wait(smem_u32(tile_full + 2 * pair), step / PAIRS & 1u, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) return;
@@ -582,7 +596,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 if (elected()) {
 #pragma unroll
                     for (int k = 0; k < kPreStep / 16; ++k) tensor_product(to, a + k * 8, tile_descriptor(values + (k * 32 >> 4)), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
-                    tensor_commit(smem_u32(o_done + slot));
+                    tensor_commit(smem_u32(o_done + slot * 2) + place * 8);
                     if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + 1) + 16 * pair);
                 }
                 __syncwarp();
@@ -690,12 +704,13 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                             if (over && want > next) next = want;
                         }
                         const float f = pre_ex2(ref - next);  // a power of two
+                        wait_stores();                        // what is read back below
                         ref = next;
                         sum *= f;
 #pragma unroll
                         for (int b = 0; b < 2; ++b) now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
                         if (i > first) {
-                            ok = ok && bar_wait(smem_u32(o_done + slot), (jobs - 1) & 1u, gave_up);
+                            ok = ok && bar_wait(smem_u32(o_done + slot * 2 + (which ^ 1u)), (jobs - 1) >> 1 & 1u, gave_up);
                             fence_after();
 #pragma unroll 1
                             for (int j = 0; j < D; j += 32) {
@@ -732,7 +747,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
             // The piece: sums, then references and denominators.
             float* piece = p.pieces + (size_t(at) * SLOTS + (mine ? slot : 0u)) * pre_piece(D);
             if (ok && first < steps) {
-                ok = bar_wait(smem_u32(o_done + slot), (jobs - 1) & 1u, gave_up);
+                ok = bar_wait(smem_u32(o_done + slot * 2 + ((jobs - 1) & 1u)), (jobs - 1) >> 1 & 1u, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (ok) fence_after();
             }
@@ -896,7 +911,7 @@ cudaError_t launch_prefix_for(PreParams& p, int sms, cudaStream_t s) {
     const cudaError_t e = once.run([] { return cudaFuncSetAttribute(k_kv_prefix<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPreSmem); });
     if (e != cudaSuccess) return e;
     const size_t plan = PrePlan::bytes(p.g.groups);
-    static_assert(C::smem(2) + (TETRA_KV_MAX_SEQS * 6 + 1) * 4 <= kPreSmem, "two stages and the largest plan");
+    static_assert(C::smem(2) + (TETRA_KV_MAX_SEQS * 7 + 1) * 4 <= kPreSmem, "two stages and the largest plan");
     p.stages = 2;
     while (p.stages < 6 && C::smem(p.stages + 1) + plan <= size_t(kPreSmem)) ++p.stages;
     return launch_pdl(k_kv_prefix<D>, sms < kPreMostCtas ? sms : kPreMostCtas, kPreThreads, C::smem(p.stages) + plan, s, p);

@@ -90,7 +90,7 @@ struct SharedPlaces {
 };
 
 // k_kv_attend has nothing of k_kv_prefix's but starts behind what came before that (it is released when k_kv_prefix has waited); its
-// end has to imply that one's.
+// end has to imply that one's.  (Released at its beginning, k_kv_join waits beside both and takes nothing off: 67.8 and 69.5 us.)
 __device__ __forceinline__ void end_behind_prefix() {
     pdl_release();
     pdl_wait();
