@@ -135,15 +135,16 @@ typedef struct {
     int32_t groups;
 } tetra_kv_groups;
 
-/* Bytes of the workspace of tetra_kv_attend_shared for so many rows, heads and groups at most (more of any take no less);
- * 0 for what is rejected.  As with tetra_kv_attend, the caller zeroes it once, and calls that share it must not overlap. */
+/* Bytes of the workspace of tetra_kv_attend_shared for so many rows, heads and groups at most (more rows, groups or
+ * query heads take no less); 0 for what is rejected.  As with tetra_kv_attend, the caller zeroes it once, and calls that share it must not overlap. */
 size_t tetra_kv_shared_workspace_bytes(int head_dim, int rows, int q_heads, int kv_heads, int groups);
 
 /* What tetra_kv_attend gives, with the same arguments and limits, but for the rounding: tokens that a group shares are read once for
- * all of its rows, through the page table of the first of its sequences that take part.  Whole blocks are shared, the tokens
- * behind them are read by each sequence.  A sequence takes part where it has rows and lengths[s] is not below the shared
- * tokens of whole blocks; the others of the group, and a group with fewer than two that do, read all of their tokens
-themselves.  Three launches. */
+ * all of its rows, through the page table of the first of its sequences that take part.  Whole blocks are shared, where there are
+ * eight at least; the tokens behind them are read by each sequence.  A sequence takes part where its group has two sequences at least, it has
+ * rows, and lengths[s] is not below the shared tokens of whole blocks; others read all of their tokens themselves.  Three launches; where
+ * the table has no room for as many tokens as make up for that (width * page_tokens, for all sequences), tetra_kv_attend's
+ * one. */
 int tetra_kv_attend_shared(const tetra_kv_cache *cache, const tetra_kv_groups *groups, const void *q, int64_t q_stride,
                            void *out, int rows, int q_heads, float scale, void *workspace, size_t workspace_bytes,
                            void *stream);

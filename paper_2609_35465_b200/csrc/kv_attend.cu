@@ -917,6 +917,18 @@ cudaError_t launch_attend_all(const AttParams& p, int D, int sms, cudaStream_t s
     return D == 64 ? launch_attend_for<64, SHARED>(p, sms, s) : D == 128 ? launch_attend_for<128, SHARED>(p, sms, s) : launch_attend_for<256, SHARED>(p, sms, s);
 }
 
+// Whether one launch that reads all tokens for each sequence may take longer than three that read shared ones once.  What that saves is at
+// most what the table has room for, for all sequences but one; what it costs are two more launches and pieces of sums for each row.
+// Measured with 32/8 heads of 128, us apart and shared: 16 single tokens behind 1024 13.3 and 16.8 (34 MB apart), 2048 17.8 and 17.5 (65),
+// 4096 26.5 and 19.3 (128); 64 behind 512 23.2 and 25.3 (76), 1024 30.8 and 26.2 (142); 64 times 5 rows behind 512 39 and 50 (153), 1024
+// 55.5 and 53.2 (285); 64 times 16 behind 512 60 and 84 (153), 1024 98 and 100 (285).
+bool worth_sharing(const AttParams& p, int D) {
+    const int64_t columns = attend_columns(p), item = columns <= 8 ? 8 : D == 256 || columns <= 24 ? 16 : 32;
+    const int64_t items = int64_t(p.c.seqs - 1) * p.c.kv_heads * ((columns + item - 1) / item), tokens = int64_t(p.c.width) * p.c.blocks_per_page * kKvBlock;
+    const int64_t queries = int64_t(p.c.rows) * p.c.kv_heads * p.group * D * 2;
+    return double(items) * double(tokens) * (2 * D) >= 80e6 + 40. * double(queries);
+}
+
 // What both calls check, in the order in which they say so.
 int attend_params(const tetra_kv_cache* cache, const void* q, int64_t q_stride, void* out, int rows, int q_heads, float scale, void* workspace, size_t workspace_bytes,
                   size_t wanted_bytes, AttParams& p) {
@@ -985,7 +997,7 @@ int tetra_kv_attend_shared(const tetra_kv_cache* cache, const tetra_kv_groups* g
     if (device_sms(&sms) != cudaSuccess) return TETRA_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int D = cache->head_dim;
-    if (groups->groups == 0) return kv_status(launch_attend_all<false>(p, D, sms, s));
+    if (groups->groups == 0 || !worth_sharing(p, D)) return kv_status(launch_attend_all<false>(p, D, sms, s));
     const SharedPlaces at(D, rows, q_heads, cache->kv_heads, groups->groups);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     SharedCall call;

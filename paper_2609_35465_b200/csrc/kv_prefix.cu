@@ -220,11 +220,11 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
     }
     // A sequence's rows and its group, 0 blocks if it does not take part.
     auto look = [&](int s, int& group, int& a, int& b) {
-        p.c.rows_of(s, a, b);
         const int before = __ldg(p.c.lengths + s);
-        int first, last;
-        group = group_of(p.g, seqs, s, first, last);
-        const int blocks = group < 0 ? 0 : shared_blocks(p.c, p.g, group);
+        int first, last, which;
+        group = group_of(p.g, seqs, s, first, last, which);
+        const int blocks = shared_blocks(p.c, p.g, which);  // (loaded beside the others, whatever they say)
+        p.c.rows_of(s, a, b);
         return group >= 0 && takes_part(first, last, blocks, a, b, before) ? blocks : 0;
     };
     int group = -1, a = 0, b = 0, blocks = 0;
@@ -259,7 +259,7 @@ __device__ __forceinline__ uint32_t make_plan(const PreParams& p, const PrePlan&
 #pragma unroll 1
         for (uint32_t k = 1; k <= kPreWaves && items; ++k) {
             const uint32_t may = min(k * G, p.most);
-            if (items > may || (k > 1 && 2 * items <= G)) continue;
+            if (items > may || (k > 1 && (2 * items <= G || k * (1 + kPrePartCost) >= cost))) continue;
             uint32_t from = max(1u, (work + may - 1) / may), tried, fits;
             do {
                 const uint32_t by = max(1u, from >> 4);
@@ -685,11 +685,13 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                     // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
                     // column) call for a new one; as long as none does, no maximum is looked for.
                     float now[2];
-                    bool over = false;
+                    bool over = __all_sync(0xFFFFFFFFu, ref == kPreNoRef);
+                    if (!over) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
-                        over |= !(now[b] * c[b].y <= kPreMost);  // infinite times a scale of zero calls for one too
+                        for (int b = 0; b < 2; ++b) {
+                            now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
+                            over |= !(now[b] * c[b].y <= kPreMost);  // infinite times a scale of zero calls for one too
+                        }
                     }
                     if (__any_sync(0xFFFFFFFFu, over)) {
                         float next = ref;
@@ -768,23 +770,33 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 const bool two = q.both && steps > 1;  // else the other slot has nothing
                 sum = two ? fmaf(sum, f0, end.y * f1) : sum;
                 ref = two ? top : ref;
-#pragma unroll 1
-                for (int j = 0; ok && j < D; j += 32) {
-                    uint32_t o[32], u[32];
-                    tensor_load(at_o + j, o);
-                    if (two) tensor_load(at_o + C::SLOT + j, u);
-                    wait_loads();
+                uint32_t o[2][16], u[2][16];  // 16 dims are on their way while the 16 before are stored
+                auto load = [&](int which, int j) {
+                    tensor_load16(at_o + j, o[which]);
+                    if (two) tensor_load16(at_o + C::SLOT + j, u[which]);
+                };
+                auto store = [&](int which, int j) {
                     if (two) {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o[k]), f0, __uint_as_float(u[k]) * f1));
+                        for (int k = 0; k < 16; ++k) o[which][k] = __float_as_uint(fmaf(__uint_as_float(o[which][k]), f0, __uint_as_float(u[which][k]) * f1));
                     }
                     if (live) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            asm volatile("st.global.cg.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(piece + column * D + j + 8 * k), "r"(o[8 * k]), "r"(o[8 * k + 1]),
-                                         "r"(o[8 * k + 2]), "r"(o[8 * k + 3]), "r"(o[8 * k + 4]), "r"(o[8 * k + 5]), "r"(o[8 * k + 6]), "r"(o[8 * k + 7])
+                        for (int k = 0; k < 16; k += 8)
+                            asm volatile("st.global.cg.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(piece + column * D + j + k), "r"(o[which][k]), "r"(o[which][k + 1]),
+                                         "r"(o[which][k + 2]), "r"(o[which][k + 3]), "r"(o[which][k + 4]), "r"(o[which][k + 5]), "r"(o[which][k + 6]), "r"(o[which][k + 7])
                                          : "memory");
                     }
+                };
+                if (ok) load(0, 0);
+#pragma unroll 1
+                for (int j = 0; ok && j < D; j += 32) {
+                    wait_loads();
+                    load(1, j + 16);
+                    store(0, j);
+                    wait_loads();
+                    if (j + 32 < D) load(0, j + 32);
+                    store(1, j + 16);
                 }
                 fence_before();
                 if (q.both) {

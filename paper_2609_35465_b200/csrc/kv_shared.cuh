@@ -21,9 +21,10 @@ struct SharedGroups {
     const int32_t* tokens;  // [groups]
     int32_t groups;
 };
-// The group of sequence s and its sequences [first, last); -1: none.
-__device__ __forceinline__ int group_of(const SharedGroups& g, int seqs, int s, int& first, int& last) {
-    int lo = 0, hi = g.groups;  // the last one with start <= s
+// The group of sequence s and its sequences [first, last); -1: none, and `lo` is some group.
+__device__ __forceinline__ int group_of(const SharedGroups& g, int seqs, int s, int& first, int& last, int& lo) {
+    int hi = g.groups;
+    lo = 0;  // the last one with start <= s
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (__ldg(g.start + mid) <= s) lo = mid;
@@ -41,11 +42,10 @@ __device__ __forceinline__ bool takes_part(int first, int last, int blocks, int 
     return last - first >= 2 && blocks >= kSharedLeast && b > a && int64_t(before) >= int64_t(blocks) * kKvBlock;
 }
 __device__ __forceinline__ int shared_of(const KvCache& c, const SharedGroups& g, int s, int a, int b, int before) {
-    int first, last;
-    const int group = group_of(g, c.seqs, s, first, last);
-    if (group < 0) return 0;
-    const int blocks = shared_blocks(c, g, group);
-    return takes_part(first, last, blocks, a, b, before) ? blocks : 0;
+    int first, last, which;
+    const int group = group_of(g, c.seqs, s, first, last, which);
+    const int blocks = shared_blocks(c, g, which);
+    return group >= 0 && takes_part(first, last, blocks, a, b, before) ? blocks : 0;
 }
 
 // Where a sequence's share of the pieces is.  An item is (group, kv head, tile of columns), cut into `parts`; a part leaves a piece

@@ -21,20 +21,26 @@ def tt():
     return tetra
 
 
-def share(st, groups):
+def wide(st, table):
+    """A table with room for more tokens than there are: what a call could save is judged by that."""
+    room = int(120e6 + 200 * st.total * 64 * st.D) // (max(len(table) - 1, 1) * st.H * st.D * 2 * st.P) + 1
+    return i32(np.concatenate([table, np.full((len(table), max(st.gap, room)), -7)], 1))[:, :max(st.width, room)]
+
+
+def share(st, groups, narrow=False):
     """groups: (first sequence, the one behind the last, tokens): their table entries become the first one's."""
     for a, b, n in groups:
         pages = min(max(n, 0) // st.P, st.width)
         if b > a:
             st.table[a:b, :pages] = st.table[a, :pages]
-    st.d_table = i32(np.concatenate([st.table, np.full((len(st.table), st.gap), -7)], 1))[:, :st.width]
+    st.d_table = i32(np.concatenate([st.table, np.full((len(st.table), st.gap), -7)], 1))[:, :st.width] if narrow else wide(st, st.table)
     start = [g[0] for g in groups] + [groups[-1][1] if groups else 0]
     return i32(start), i32([g[2] for g in groups])
 
 
-def shared_check(tt, st, heads, groups, scale=None, q=None, workspace=None, plain=None):
+def shared_check(tt, st, heads, groups, scale=None, q=None, workspace=None, plain=None, narrow=False):
     n, D = st.total, st.D
-    start, shared = share(st, groups)
+    start, shared = share(st, groups, narrow)
     if q is None:
         q = st.rng.standard_normal((n, heads, D)).astype(np.float16)
     out = torch.full((n, heads, D), 7.5, dtype=torch.float16, device="cuda")
@@ -102,6 +108,16 @@ def test_many_groups(tt, D):
     shared_check(tt, Step(105, D, 4, 32, before, [1] * len(before)), 8, groups)
 
 
+@pytest.mark.parametrize("D,H,heads,P", [(128, 8, 32, 64), (64, 2, 16, 16), (256, 1, 7, 48)])
+@pytest.mark.parametrize("shared,before,rows", [(192, [192, 192, 200], [5, 1, 16]), (960, [960, 1000], [1, 1])])
+def test_tables_without_room_for_more(tt, D, H, heads, P, shared, before, rows):
+    """Too little to save: one launch, and the bits of tetra_kv_attend."""
+    st = Step(113, D, H, P, before, rows)
+    q = st.rng.standard_normal((st.total, heads, D)).astype(np.float16)
+    out = shared_check(tt, st, heads, [(0, len(before), shared)], q=q, narrow=True)
+    assert torch.equal(out, tt.tetra_kv_attend(dev(q), *st.args(), torch.empty_like(out), tt.tetra_kv_workspace(D)))
+
+
 def test_as_many_sequences_as_there_may_be(tt):
     n = 1024
     st = Step(106, 64, 1, 16, [160] * n, [1] * n)
@@ -131,7 +147,7 @@ def test_sequences_that_do_not_take_part(tt):
 def test_groups_that_make_no_sense_share_nothing(tt):
     st = Step(110, 64, 2, 16, [300, 300, 300], [1] * 3)
     st.table[:, :16] = st.table[0, :16]
-    st.d_table = i32(st.table)
+    st.d_table = wide(st, st.table)
     q = dev(st.rng.standard_normal((3, 4, 64)).astype(np.float16))
     want, bound = ref.attend(st.plain(), q.cpu().numpy(), st.table, st.starts, st.before, 1 / 8)
     for start in ([-2, 3], [0, 4], [2, 1], [3, 3], [0, 2 ** 31 - 1], [-2 ** 31, 2 ** 31 - 1], [1, 0, 3], [0, 5, 2]):
@@ -267,7 +283,7 @@ def test_offsets_that_pass_32_bits(tt):
     q = torch.randn((3, 32, D), device="cuda").half()
     ws = tt.tetra_kv_shared_workspace(D, 3, 32, H, 1)
     small = tt.tetra_kv_attend_shared(q, *st.args(), start, shared, torch.empty_like(q), ws)
-    big = tt.tetra_kv_attend_shared(q, cache, i32(moved), st.d_starts, st.d_lengths, start, shared, torch.empty_like(q), ws)
+    big = tt.tetra_kv_attend_shared(q, cache, wide(st, moved), st.d_starts, st.d_lengths, start, shared, torch.empty_like(q), ws)
     assert torch.equal(small, big)
 
 
@@ -276,7 +292,7 @@ def test_a_captured_call_follows_lengths_groups_and_pages(tt):
     """One graph, replayed with other groups, lengths, pages and queries; eager calls use its workspace in between."""
     D, H, heads, n = 128, 2, 8, 6
     st = Step(120, D, H, 16, [400] * n, [1] * n, width=40)
-    start, shared, table, lengths = i32([0, 3, 6]), i32([0, 0]), i32(st.table), i32([0] * n)
+    start, shared, table, lengths = i32([0, 3, 6]), i32([0, 0]), wide(st, st.table), i32([0] * n)
     q, out, ws = torch.zeros((n, heads, D), dtype=torch.float16, device="cuda"), torch.zeros((n, heads, D), dtype=torch.float16, device="cuda"), tt.tetra_kv_shared_workspace(D, n, heads, H, 2)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
@@ -286,7 +302,7 @@ def test_a_captured_call_follows_lengths_groups_and_pages(tt):
                                   ([0, 0, 0], [9, 9], [5] * 6), ([1, 3, 5], [512, 384], [7, 520, 513, 400, 385, -1])):
         st.table = rng.permutation(st.pages)[:n * st.width].reshape(n, st.width)
         new_start, new_shared = share(st, list(zip(split, split[1:], tokens)))
-        for to, x in ((start, new_start), (shared, new_shared), (table, i32(st.table)), (lengths, i32(before)), (q, torch.randn((n, heads, D), device="cuda").half())):
+        for to, x in ((start, new_start), (shared, new_shared), (table, wide(st, st.table)), (lengths, i32(before)), (q, torch.randn((n, heads, D), device="cuda").half())):
             to.copy_(x)
         graph.replay()
         replayed = out.clone()
