@@ -10,7 +10,7 @@
 //
 // A CTA.  One warp copies records by cp.async.bulk into a ring.  Four warps turn their bytes into float16 (exact: codes are small
 // integers) and lay them out for the tensor cores: keys as [token][dim], values as [dim][token], rows of 128 bytes, swizzled; the
-// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  One thread issues the products: S = Q K^T and O += P V (P from tensor memory, over S).  Two groups of four warps
+// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  One thread a slot issues the products: S = Q K^T and O += P V (P from tensor memory, over S).  Two groups of four warps
 // ("slots"), a thread a column, turn S into weights: no value of a column is in another thread, so there are no exchanges.  The
 // slots take the two halves of a tile's columns, or, where a tile has no more than 128, every other step, so that the products of
 // one run beside the exponentials of the other.  A slot has two places for scores, so that those of its next step are there when the
@@ -34,7 +34,7 @@ constexpr int kPreStep = 64;                              // tokens
 constexpr int kPreBlocks = kPreStep / kKvBlock;
 constexpr int kPreSoft = 8, kPreConvert = 4;              // warps
 constexpr int kPreConvertAt = kPreSoft, kPreCopyWarp = kPreSoft + kPreConvert, kPreMmaWarp = kPreCopyWarp + 1;
-constexpr int kPreThreads = (kPreMmaWarp + 1) * 32;
+constexpr int kPreThreads = (kPreMmaWarp + 2) * 32;       // a warp a slot issues products
 constexpr int kPreScales = 8;                             // steps whose scales are kept
 constexpr uint32_t kPrePartCost = 8;                      // steps that a part's beginning and end take
 constexpr uint32_t kPreTries = 1u << 22;                  // of a wait: then the call's results are NaN
@@ -179,9 +179,6 @@ __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t* r) {
 // 16 columns.
 __device__ __forceinline__ void tensor_load16(uint32_t at, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : TETRA_R8(r, 0), TETRA_R8(r, 8) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void tensor_store16(uint32_t at, const uint32_t* r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::TETRA_W8(r, 0), TETRA_W8(r, 8), "r"(at) : "memory");
 }
 #undef TETRA_R8
 #undef TETRA_W8
@@ -395,12 +392,12 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     if (threadIdx.x == 0) {
         failed = 0;
         for (uint32_t i = 0; i < stages; ++i) bar_init(smem_u32(raw_full + i), 1), bar_init(smem_u32(raw_empty + i), kPreConvert);
-        for (int i = 0; i < TILES; ++i) bar_init(smem_u32(tile_full + i), kPreConvert), bar_init(smem_u32(tile_empty + i), 1);
+        for (int i = 0; i < TILES; ++i) bar_init(smem_u32(tile_full + i), kPreConvert), bar_init(smem_u32(tile_empty + i), SLOTS);
         for (int i = 0; i < 2; ++i) bar_init(smem_u32(q_ready + i), 4);
         for (int i = 0; i < 4; ++i) bar_init(smem_u32(p_ready + i), 4), bar_init(smem_u32(s_full + i), 1), bar_init(smem_u32(o_done + i), 1);
         for (int i = 0; i < kPreScales; ++i) bar_init(smem_u32(scales_full + i), 1);
         bar_init(smem_u32(&other_ready), 4), bar_init(smem_u32(&other_free), 4);
-        bar_init(smem_u32(&drained), 1);
+        bar_init(smem_u32(&drained), SLOTS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kPreMmaWarp) {
@@ -543,80 +540,75 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 ++n;
             }
         }
-    } else if (warp == kPreMmaWarp) {
-        // ---- products, issued by one thread.  A job is a slot's step: jobs 0, 1, 2, .. are slots 0, 1, 0, .. (of one slot: 0, 0, ..).
-        // A job's scores are issued one step of its slot ahead of its weights' products, into the place that the slot's last but one step had,
-        // whose products are waited for (products with different results are in no order).  Each place has barriers of its own: a barrier tells
-        // of its last phase only, and the products of two jobs of a slot may both be on their way.
+    } else if (warp >= kPreMmaWarp && warp < kPreMmaWarp + SLOTS) {
+        // ---- products, issued by one thread a slot.  A job is a step of the slot's.  Its scores are issued one job ahead of its weights'
+        // products, into the place that the last job but one had, whose products are waited for (products with different results are in no
+        // order).  Each place has barriers of its own: a barrier tells of its last phase only, and the products of two jobs may both be
+        // on their way.  For the same reason each slot waits for every step's tiles, its own or not.
+        const uint32_t slot = warp - kPreMmaWarp;
         bool ok = true;
-        uint32_t before[2] = {0, 0}, q_parts = 0;  // a slot's jobs of earlier parts
-        const uint32_t tiles = (base & 0x3FFFFu) >> 4, q_tiles = (queries & 0x3FFFFu) >> 4;
+        uint32_t own = 0, q_parts = 0;  // jobs so far
+        const uint32_t tiles = (base & 0x3FFFFu) >> 4, to_slot = tensor + slot * C::SLOT;
         constexpr uint32_t PAIRS = TILES / 2;  // a step's keys are tile 2 (step % PAIRS), its values the next one
+        auto full = [&](uint32_t step, uint32_t value) { ok = ok && bar_wait(smem_u32(tile_full + 2 * (step % PAIRS) + value), step / PAIRS & 1u, gave_up); };
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
             if (!part_of<D>(p, plan, at, q)) continue;
-            const uint32_t steps = q.end - q.begin;
-            const bool halves = SLOTS == 2 && !q.both;  // each step is both slots' work
-            const uint32_t jobs = halves ? 2 * steps : steps;
-            auto scores = [&](auto which_slot, uint32_t job) {
-                constexpr uint32_t slot = decltype(which_slot)::value;
-                const uint32_t step = n0 + (halves ? job >> 1 : job), pair = step % PAIRS, own = before[slot] + (SLOTS == 2 ? job >> 1 : job), place = own & 1u;
-                if (job == slot && (halves || slot == 0)) ok = ok && bar_wait(smem_u32(q_ready + slot), q_parts & 1u, gave_up);
-                // (Slots that share columns have the first one's queries, but no phase of a barrier is left out.)
-                if (SLOTS == 2 && job == 0 && !halves) ok = ok && bar_wait(smem_u32(q_ready + 1), q_parts & 1u, gave_up);
-                if (own >= 2) ok = ok && bar_wait(smem_u32(o_done + slot * 2) + place * 8, (own >> 1) + 1 & 1u, gave_up);
-                if (!halves || slot == 0) ok = ok && bar_wait(smem_u32(tile_full + 2 * pair), step / PAIRS & 1u, gave_up);
+            const uint32_t steps = q.end - q.begin, by = q.both ? 2u : 1u, first = q.both ? slot : 0u;
+            const uint32_t queries_at = ((queries & 0x3FFFFu) + (q.both ? 0u : slot * C::QTILE)) >> 4;
+            for (int i = 0; i < SLOTS; ++i) ok = ok && bar_wait(smem_u32(q_ready + i), q_parts & 1u, gave_up);
+            auto scores = [&](uint32_t i, uint32_t job) {
+                const uint32_t step = n0 + i, pair = step % PAIRS, place = job & 1u;
+                if (job >= 2) ok = ok && bar_wait(smem_u32(o_done + slot * 2) + place * 8, (job >> 1) + 1 & 1u, gave_up);
+                full(step, 0);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) return;
                 fence_after();
-                const uint32_t to = tensor + slot * C::SLOT + C::QCOLS + place * kPreStep, keys = tiles + (2 * pair * C::TILE >> 4);
-                const uint32_t from = q_tiles + (halves ? slot * C::QTILE >> 4 : 0);
+                const uint32_t to = to_slot + C::QCOLS + place * kPreStep, keys = tiles + (2 * pair * C::TILE >> 4);
                 if (elected()) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint64_t b = tile_descriptor(keys + ((k / 4 * (kPreStep * 128) + k % 4 * 32) >> 4));
-                        if constexpr (C::QTENSOR) tensor_product(to, tensor + slot * C::SLOT + k * 8, b, product_kind(kPreStep), k > 0);
-                        else tensor_product(to, tile_descriptor(from + ((k / 4 * (kPreColumns * 128) + k % 4 * 32) >> 4)), b, product_kind(kPreStep), k > 0);
+                        if constexpr (C::QTENSOR) tensor_product(to, to_slot + k * 8, b, product_kind(kPreStep), k > 0);
+                        else tensor_product(to, tile_descriptor(queries_at + ((k / 4 * (kPreColumns * 128) + k % 4 * 32) >> 4)), b, product_kind(kPreStep), k > 0);
                     }
                     tensor_commit(smem_u32(s_full + slot * 2) + place * 8);
-                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty) + 16 * pair);
+                    tensor_commit(smem_u32(tile_empty) + 16 * pair);
                 }
                 __syncwarp();
             };
-            auto sums = [&](auto which_slot, uint32_t job) {
-                constexpr uint32_t slot = decltype(which_slot)::value;
-                const uint32_t step = n0 + (halves ? job >> 1 : job), pair = step % PAIRS, own = before[slot] + (SLOTS == 2 ? job >> 1 : job), place = own & 1u;
-                if (!halves || slot == 0) ok = bar_wait(smem_u32(tile_full + 2 * pair + 1), step / PAIRS & 1u, gave_up);
-                ok = ok && bar_wait(smem_u32(p_ready + slot * 2) + place * 8, own >> 1 & 1u, gave_up);
+            auto sums = [&](uint32_t i, uint32_t job) {
+                const uint32_t step = n0 + i, pair = step % PAIRS, place = job & 1u;
+                full(step, 1);
+                ok = ok && bar_wait(smem_u32(p_ready + slot * 2) + place * 8, job >> 1 & 1u, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) return;
                 fence_after();
-                const uint32_t to = tensor + slot * C::SLOT + C::QCOLS + 2 * kPreStep, a = tensor + slot * C::SLOT + C::QCOLS + place * kPreStep;
-                const uint32_t values = tiles + ((2 * pair + 1) * C::TILE >> 4);
+                const uint32_t to = to_slot + C::QCOLS + 2 * kPreStep, a = to_slot + C::QCOLS + place * kPreStep, values = tiles + ((2 * pair + 1) * C::TILE >> 4);
                 if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < kPreStep / 16; ++k) tensor_product(to, a + k * 8, tile_descriptor(values + (k * 32 >> 4)), product_kind(D), job >= uint32_t(SLOTS) || k > 0);
+                    for (int k = 0; k < kPreStep / 16; ++k) tensor_product(to, a + k * 8, tile_descriptor(values + (k * 32 >> 4)), product_kind(D), i > first || k > 0);
                     tensor_commit(smem_u32(o_done + slot * 2) + place * 8);
-                    if (!halves || slot == 1) tensor_commit(smem_u32(tile_empty + 1) + 16 * pair);
+                    tensor_commit(smem_u32(tile_empty + 1) + 16 * pair);
                 }
                 __syncwarp();
             };
-            using First = std::integral_constant<uint32_t, 0>;
-            using Second = std::integral_constant<uint32_t, SLOTS - 1>;
-            scores(First(), 0);
-            if (SLOTS == 2 && ok && jobs > 1) scores(Second(), 1);
-            for (uint32_t job = 0; ok && job < jobs; job += SLOTS) {
-                if (job + SLOTS < jobs) scores(First(), job + SLOTS);
-                if (ok) sums(First(), job);
-                if (SLOTS == 2 && ok && job + 1 < jobs) {
-                    if (job + 3 < jobs) scores(Second(), job + 3);
-                    if (ok) sums(Second(), job + 1);
+            auto others = [&](uint32_t i) {  // a step that is the other slot's
+                for (uint32_t value = 0; value < 2; ++value) {
+                    full(n0 + i, value);
+                    if (ok && lane == 0) bar_arrive(smem_u32(tile_empty + 2 * ((n0 + i) % PAIRS) + value));
                 }
+                ok = __all_sync(0xFFFFFFFFu, ok);
+            };
+            if (q.both && slot == 1) others(0);
+            if (ok && first < steps) scores(first, own);
+            for (uint32_t i = first; ok && i < steps; i += by, ++own) {
+                if (q.both && i + 1 < steps) others(i + 1);
+                if (ok && i + by < steps) scores(i + by, own + 1);
+                if (ok) sums(i, own);
             }
             n0 += steps;
             ++q_parts;
-            before[0] += SLOTS == 2 ? (jobs + 1) / 2 : jobs;
-            before[1] += jobs / 2;
         }
         // What was issued has ended when the tensor memory is given back.
         if (elected()) tensor_commit(smem_u32(&drained));
@@ -676,69 +668,58 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 ok = bar_wait(smem_u32(scales_full + n % kPreScales), n / kPreScales & 1u, gave_up) && bar_wait(smem_u32(s_full + slot * 2 + which), jobs >> 1 & 1u, gave_up);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 fence_after();
-#pragma unroll 1
-                for (int chunk = 0; chunk < kPreStep / 32; ++chunk) {  // 32 tokens at a time: what registers hold
-                    uint32_t r[32], w[16];
-                    tensor_load(at_s + chunk * 32, r);
-                    const float4 c[2] = {scales[n % kPreScales][chunk * 2], scales[n % kPreScales][chunk * 2 + 1]};
-                    wait_loads();
-                    // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
-                    // column) call for a new one; as long as none does, no maximum is looked for.
-                    float now[2];
-                    bool over = __all_sync(0xFFFFFFFFu, ref == kPreNoRef);
-                    if (!over) {
+                uint32_t r[kPreStep], w[kPreStep / 2];
+                tensor_load(at_s, r);
+                tensor_load(at_s + 32, r + 32);
+                const float4* c = scales[n % kPreScales];
+                wait_loads();
+                // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
+                // column) call for a new one; as long as none does, no maximum is looked for.
+                float now = 0.f;
+                bool over = __all_sync(0xFFFFFFFFu, ref == kPreNoRef);
+                if (!over) {
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
-                            over |= !(now[b] * c[b].y <= kPreMost);  // infinite times a scale of zero calls for one too
-                        }
+                    for (int b = 0; b < kPreBlocks; ++b) {
+                        const float4 by = c[b];
+                        const float one = block_weights(r + 16 * b, by, ref, w + 8 * b);
+                        over |= !(one * by.y <= kPreMost);  // infinite times a scale of zero calls for one too
+                        now += one;
                     }
-                    if (__any_sync(0xFFFFFFFFu, over)) {
-                        float next = ref;
+                }
+                if (__any_sync(0xFFFFFFFFu, over)) {
+                    float next = ref;
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            float top = -INFINITY;
+                    for (int b = 0; b < kPreBlocks; ++b) {
+                        const float4 by = c[b];
+                        float top = -INFINITY;
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) top = fmaxf(top, __uint_as_float(r[16 * b + k]) * c[b].x);
-                            if (c[b].w == 0.f) top = -INFINITY;
-                            float want = rintf(top + c[b].z - kPreBase);
-                            if (top - want > kPreHigh - c[b].z) want = top;  // a step of so large scores is more than the room there is
-                            if (over && want > next) next = want;
-                        }
-                        const float f = pre_ex2(ref - next);  // a power of two
-                        wait_stores();                        // what is read back below
-                        ref = next;
-                        sum *= f;
+                        for (int k = 0; k < 16; ++k) top = fmaxf(top, __uint_as_float(r[16 * b + k]) * by.x);
+                        if (by.w == 0.f) top = -INFINITY;
+                        float want = rintf(top + by.z - kPreBase);
+                        if (top - want > kPreHigh - by.z) want = top;  // a step of so large scores is more than the room there is
+                        if (over && want > next) next = want;
+                    }
+                    const float f = pre_ex2(ref - next);  // a power of two
+                    ref = next;
+                    sum *= f;
+                    now = 0.f;
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) now[b] = block_weights(r + 16 * b, c[b], ref, w + 8 * b);
-                        if (i > first) {
-                            ok = ok && bar_wait(smem_u32(o_done + slot * 2 + (which ^ 1u)), (jobs - 1) >> 1 & 1u, gave_up);
-                            fence_after();
+                    for (int b = 0; b < kPreBlocks; ++b) now += block_weights(r + 16 * b, c[b], ref, w + 8 * b);
+                    if (i > first) {
+                        ok = ok && bar_wait(smem_u32(o_done + slot * 2 + (which ^ 1u)), (jobs - 1) >> 1 & 1u, gave_up);
+                        fence_after();
 #pragma unroll 1
-                            for (int j = 0; j < D; j += 32) {
-                                tensor_load(at_o + j, r);
-                                wait_loads();
-#pragma unroll
-                                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
-                                tensor_store(at_o + j, r);
-                            }
-                        }
-#pragma unroll 1
-                        for (int j = 0; j < chunk; ++j) {  // the step's weights so far
-                            tensor_load16(at_s + j * 16, r);
+                        for (int j = 0; j < D; j += 32) {
+                            tensor_load(at_o + j, r);
                             wait_loads();
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&r[k]));
-                                const __half2 h = __floats2half2_rn(v.x * f, v.y * f);
-                                r[k] = *reinterpret_cast<const uint32_t*>(&h);
-                            }
-                            tensor_store16(at_s + j * 16, r);
+                            for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
+                            tensor_store(at_o + j, r);
                         }
                     }
-                    sum += now[0] + now[1];
-                    tensor_store16(at_s + chunk * 16, w);
                 }
+                sum += now;
+                tensor_store(at_s, w);
                 wait_stores();
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
