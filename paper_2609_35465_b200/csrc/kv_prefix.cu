@@ -180,6 +180,10 @@ __device__ __forceinline__ void tensor_store(uint32_t at, const uint32_t* r) {
 __device__ __forceinline__ void tensor_load16(uint32_t at, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : TETRA_R8(r, 0), TETRA_R8(r, 8) : "r"(at) : "memory");
 }
+// 8 columns.
+__device__ __forceinline__ void tensor_store8(uint32_t at, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::TETRA_W8(r, 0), "r"(at) : "memory");
+}
 #undef TETRA_R8
 #undef TETRA_W8
 
@@ -631,20 +635,32 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
             if (mine) {
                 const uint32_t row = live ? uint32_t(col) / uint32_t(p.group) : 0u, h = live ? uint32_t(col) - row * p.group : 0u;
                 const uint4* src = reinterpret_cast<const uint4*>(p.q + int64_t(q.row0 + row) * p.q_stride + (int64_t(q.head) * p.group + h) * D);
+                if constexpr (C::QTENSOR) {
 #pragma unroll
-                for (int j = 0; j < D / 64; ++j) {
-                    uint32_t r[32];
+                    for (int j = 0; j < D / 64; ++j) {
+                        uint32_t r[32];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint4 v = live ? __ldg(src + j * 8 + i) : make_uint4(0, 0, 0, 0);
-                        r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
-                    }
-                    if constexpr (C::QTENSOR) {
+                        for (int i = 0; i < 8; ++i) {
+                            const uint4 v = live ? __ldg(src + j * 8 + i) : make_uint4(0, 0, 0, 0);
+                            r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
+                        }
                         tensor_store(at_q + j * 32, r);
-                    } else {
-                        const uint32_t line = queries + slot * C::QTILE + j * (kPreColumns * 128) + column * 128;
+                    }
+                } else {
+                    // Lanes read a column's 16 bytes side by side, several columns at a time.
+                    constexpr int LANES = D / 8, COLS = 32 / LANES, LOADS = 32 / COLS;
+                    const uint32_t chunk = lane % LANES;
+                    const uint64_t mine_at = live ? reinterpret_cast<uint64_t>(src) : 0;
+                    uint4 v[LOADS];
 #pragma unroll
-                        for (uint32_t i = 0; i < 8; ++i) pre_sts(line + ((i ^ (column & 7u)) << 4), r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                    for (int i = 0; i < LOADS; ++i) {
+                        const uint64_t from = __shfl_sync(0xFFFFFFFFu, mine_at, i * COLS + lane / LANES);
+                        v[i] = from ? __ldg(reinterpret_cast<const uint4*>(from) + chunk) : make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < LOADS; ++i) {
+                        const uint32_t to = (warp & 3) * 32 + i * COLS + lane / LANES;
+                        pre_sts(queries + slot * C::QTILE + chunk / 8 * (kPreColumns * 128) + to * 128 + ((chunk % 8 ^ to % 8) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
                     }
                 }
                 if constexpr (C::QTENSOR) {
@@ -686,14 +702,17 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                         now += one;
                     }
                 }
-                if (__any_sync(0xFFFFFFFFu, over)) {
+                if (__any_sync(0xFFFFFFFFu, over)) {  // from tensor memory again, a block at a time: little code, which is cold the first time
                     float next = ref;
-#pragma unroll
+#pragma unroll 1
                     for (int b = 0; b < kPreBlocks; ++b) {
+                        uint32_t x[16];
+                        tensor_load16(at_s + 16 * b, x);
+                        wait_loads();
                         const float4 by = c[b];
                         float top = -INFINITY;
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) top = fmaxf(top, __uint_as_float(r[16 * b + k]) * by.x);
+                        for (int k = 0; k < 16; ++k) top = fmaxf(top, __uint_as_float(x[k]) * by.x);
                         if (by.w == 0.f) top = -INFINITY;
                         float want = rintf(top + by.z - kPreBase);
                         if (top - want > kPreHigh - by.z) want = top;  // a step of so large scores is more than the room there is
@@ -703,8 +722,14 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                     ref = next;
                     sum *= f;
                     now = 0.f;
-#pragma unroll
-                    for (int b = 0; b < kPreBlocks; ++b) now += block_weights(r + 16 * b, c[b], ref, w + 8 * b);
+#pragma unroll 1
+                    for (int b = 0; b < kPreBlocks; ++b) {  // (weights are behind or over the scores of their block)
+                        uint32_t x[16];
+                        tensor_load16(at_s + 16 * b, x);
+                        wait_loads();
+                        now += block_weights(x, c[b], ref, w);
+                        tensor_store8(at_s + 8 * b, w);
+                    }
                     if (i > first) {
                         ok = ok && bar_wait(smem_u32(o_done + slot * 2 + (which ^ 1u)), (jobs - 1) >> 1 & 1u, gave_up);
                         fence_after();
@@ -717,9 +742,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                             tensor_store(at_o + j, r);
                         }
                     }
+                } else {
+                    tensor_store(at_s, w);
                 }
                 sum += now;
-                tensor_store(at_s, w);
                 wait_stores();
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
