@@ -103,9 +103,25 @@ __device__ __forceinline__ void lp_rank(const uint64_t* from, int n, int k, uint
     }
 }
 
-struct LpTile {
-    float part, product;
-};
+// The `top` first of LISTS lists of so many entries each, which are in order (0: none).  An entry's place is how many of each list are ahead of it.
+template <int THREADS, int LISTS>
+__device__ __forceinline__ void lp_merge(const uint64_t* from, int top, uint64_t* to) {
+    for (int e = threadIdx.x; e < LISTS * top; e += THREADS) {
+        const uint64_t mine = from[e];
+        int ahead[LISTS] = {}, above = 0;
+#pragma unroll
+        for (int step = kLpTop; step >= 1; step >>= 1) {
+#pragma unroll
+            for (int l = 0; l < LISTS; ++l) {
+                const int at = ahead[l] + step;
+                if (at <= top && from[l * top + at - 1] > mine) ahead[l] = at;
+            }
+        }
+#pragma unroll
+        for (int l = 0; l < LISTS; ++l) above += ahead[l];
+        if (mine != 0 && above < top) to[above] = mine;
+    }
+}
 
 // A row, and the part of it that is a CTA's.
 struct LpRow {
@@ -484,7 +500,7 @@ __device__ __forceinline__ void lp_run(const tetra_logprobs_rows& p, LpShared<TH
         if (rank > 0) return;
         if (threadIdx.x < kLpTop) sm.best[threadIdx.x] = 0;
         __syncthreads();
-        lp_rank<THREADS>(sm.gathered, CTAS * top, top, sm.best);
+        lp_merge<THREADS, CTAS>(sm.gathered, top, sm.best);
         __syncthreads();
     }
     if (warp > 0) return;
@@ -505,7 +521,7 @@ __device__ __forceinline__ void lp_run(const tetra_logprobs_rows& p, LpShared<TH
         p.logprob[int64_t(r) * p.given + g] = t >= 0 ? logprob(sm.given[g], head != 0 && uint32_t(t) == lp_index(head)) : -INFINITY;
         if (p.rank) p.rank[int64_t(r) * p.given + g] = t >= 0 ? sm.count[g] : -1;
     }
-    if (lane == 0 && p.entropy) p.entropy[r] = greedy || head == 0 ? 0.f : float(norm - 0.693147180559945309417 * (s.product / s.sum));
+    if (lane == 0 && p.entropy) p.entropy[r] = greedy || head == 0 ? 0.f : fmaxf(float(norm - 0.693147180559945309417 * (s.product / s.sum)), 0.f);
 }
 
 template <bool HALF, int THREADS, int E, int CTAS>
