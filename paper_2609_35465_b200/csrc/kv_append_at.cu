@@ -134,7 +134,7 @@ __device__ __forceinline__ void load_side(const T* from, float (&x)[N]) {
 // sines on (made in 64 bits, rounded to 32) they are in 32 bits, which moves a result by 2^-21 at most where float16 rounds by 2^-12; keys,
 // whose codes a last bit may decide, stay in 64.  SIDE: rows of q are aligned for loads of a lane's D / 64 neighbours at once.
 template <int D, typename T, bool SIDE>
-__global__ void __launch_bounds__(kAppendThreads) k_kv_append_blocks(KvCache c, KvRows p, KvAxes t) {
+__global__ void __launch_bounds__(kAppendThreads, D == 256 ? 3 : 4) k_kv_append_blocks(KvCache c, KvRows p, KvAxes t) {
     constexpr int E = D / 32, N = D / 64, PAIRS = D / 2;
     extern __shared__ __align__(16) unsigned char smem[];
     double2* turns = reinterpret_cast<double2*>(smem);                                                             // [16][D / 2]
