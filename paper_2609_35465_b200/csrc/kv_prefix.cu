@@ -404,13 +404,14 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         bar_init(smem_u32(&drained), SLOTS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    pdl_wait();
+    pdl_release();
+    // (Not ahead of the wait: what is waited for may want tensor memory itself.)
     if (warp == kPreMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tensor_base)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     fence_before();
-    pdl_wait();
-    pdl_release();
 
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     PrePlan plan;
