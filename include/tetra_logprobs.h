@@ -49,7 +49,7 @@ typedef struct {
  * number; magnitudes below 2^-126 count as zero.  A token with a logit of minus infinity has log probability minus
  * infinity and is not among the top tokens; where there are fewer than `top` others, -1 and minus infinity fill the rest.  A row without a
  * logit above minus infinity has entropy 0.  A given token outside [0, vocab) has log probability minus infinity and rank -1.
- * Sums are float32 within a thread's few terms and float64 across them; nothing depends on the order in which threads run: every output
+ * A thread's sums are float32, its tiles' added one after another, threads' sums float64; nothing depends on the order in which threads run: every output
  * is bit-identical from run to run.  One launch, no scratch memory. */
 int tetra_logprobs(const tetra_logprobs_rows *rows, void *stream);
 

@@ -14,8 +14,13 @@
 // ("slots"), a thread a column, turn S into weights: no value of a column is in another thread, so there are no exchanges.  The
 // slots take the two halves of a tile's columns, or, where a tile has no more than 128, every other step, so that the products of
 // one run beside the exponentials of the other.  A slot has two places for scores, so that those of its next step are there when the
-// weights of this one are: with one place the slots' exponentials and the products took turns, 3300 to 3500 cycles for 64 tokens of 256
-// columns, where the exponentials alone are 1024 and the products 1280.
+// weights of this one are, and a warp of its own that issues its products.
+//
+// What bounds it: for 64 tokens of 256 columns the exponentials alone take 1024 cycles (four a scheduler and cycle), what else the warps of
+// the weights issue beside them makes it 1570, the products 1280; a step takes about 2100.  With one place for scores it was 3300 to 3500, with
+// one warp for both slots' products, which waits for one slot while the other could go on, 2700.  64 answers with 32/8 heads of 128
+// behind 16384 tokens: 31 us, 4300 cycles of which find out how work is cut and 4000 are the first step's loads, 3 times the time of the
+// bytes (34 MB) or of the products; with k_kv_attend's 15 and k_kv_join's 6 behind it 60 us, where each sequence for itself takes 243.
 //
 // Arithmetic is that of k_kv_attend: scores are exact products summed in float32, times s_K; weights enter as
 // float16(2^(score - m) s_V) with m a running reference, a whole number, that moves only when a block's weights together would pass

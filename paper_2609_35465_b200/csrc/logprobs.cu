@@ -11,9 +11,10 @@
 //     on the list, cut it to its k best and have a new bound.  What was noted of a run may be too much (logits that rise along
 //     the row): its tiles are then gone through again, each as the first.
 // Entries are 64-bit numbers in the order that ranks them, so all of that is exact.
-// The loop over a run's tiles keeps nothing but a tile and the sums in registers, calls nothing, and no warp waits for another in it: 6
-// operations a logit, which the memory outlasts.  (With the list kept there, the next tile in registers and a barrier a tile it
-// were 13 to 27, and 1024 rows of 151936 took 146 to 226 us.)
+// The loop over a run's tiles keeps nothing but a tile and the sums in registers, calls nothing, and no warp waits for another in it: 12
+// instructions of a thread for a logit, all phases together, which the memory outlasts.  (With the list kept there, the next tile in registers and a barrier a tile it
+// were up to 27, and 1024 rows of 151936 took 146 to 226 us.)  1024 rows of 151936 float32 logits take 110 us, 5.7 TB/s, 87 % of a copy's rate; 64
+// rows 19.6 us, of which the memory needs 6: a CTA has 2.3 tiles, and behind them 4 barriers of the choice, the cut and the cluster; one row 9.8 us.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
