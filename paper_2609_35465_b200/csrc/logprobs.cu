@@ -14,7 +14,7 @@
 // The loop over a run's tiles keeps nothing but a tile and the sums in registers, calls nothing, and no warp waits for another in it: 12
 // instructions of a thread for a logit, all phases together, which the memory outlasts.  (With the list kept there, the next tile in registers and a barrier a tile it
 // were up to 27, and 1024 rows of 151936 took 146 to 226 us.)  1024 rows of 151936 float32 logits take 110 us, 5.7 TB/s, 87 % of a copy's rate; 64
-// rows 19.6 us, of which the memory needs 6: a CTA has 2.3 tiles, and behind them 4 barriers of the choice, the cut and the cluster; one row 9.8 us.
+// rows 17.2 us, of which the memory needs 6: a CTA of 1024 threads has 3.7 tiles, and the choice, the cut and the cluster's barriers; one row 9.8 us.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
@@ -33,7 +33,7 @@ namespace cg = cooperative_groups;
 constexpr int kLpTop = TETRA_LOGPROBS_MAX_TOP, kLpGiven = TETRA_LOGPROBS_MAX_GIVEN;
 constexpr int kLpNear = 128;                       // entries of which each is compared with each at once
 constexpr int kLpMostCtas = 8;
-constexpr int kLpShortRow = 8192, kLpWideRow = 65536;  // logits
+constexpr int kLpShortRow = 8192, kLpMiddleRow = 16384, kLpWideRow = 131072;  // logits
 constexpr float kLpNoRef = -FLT_MAX, kLpLeast = -200.f;  // a weight of 2^-200 is zero
 
 struct LpSums {
@@ -42,12 +42,13 @@ struct LpSums {
 };
 template <int THREADS, int E>
 struct LpShared {
-    // Groups whose maxima bound a tile's candidates: of two threads, or of eight where few entries are looked for (so much less there is
-    // to compare; no more than kLpTop * 2 E entries reach the bound either way).
-    static constexpr int kGroups = THREADS / 2, kFewTop = kLpTop / 4;
-    static_assert(kGroups >= kLpTop && THREADS / 8 >= kFewTop && THREADS <= 1024, "as many groups as candidates");
-    static constexpr int kList = kLpTop * 2 * E + kLpTop, kNotes = 1024;
-    static constexpr int kNear = kLpTop * 2 * ((kList + THREADS - 1) / THREADS);  // entries of kLpTop groups
+    // Groups whose maxima bound a tile's candidates: of two threads, four of a large CTA, or eight where few entries are looked for (so
+    // much less there is to compare: 4.1 us of 17.4 for 20 of 8 rows' entries by groups of two of 1024 threads; no more than kLpTop * kShare E entries
+    // reach the bound either way).
+    static constexpr int kShare = THREADS >= 1024 ? 4 : 2, kGroups = THREADS / 2, kFewTop = kLpTop * kShare / 8;
+    static_assert(THREADS / kShare >= kLpTop && THREADS / 8 >= kFewTop && THREADS <= 1024, "as many groups as candidates");
+    static constexpr int kList = kLpTop * kShare * E + kLpTop, kNotes = 1024;
+    static constexpr int kNear = kLpTop * kShare * ((kList + THREADS - 1) / THREADS);  // entries of kLpTop groups
     uint64_t list[kList];
     uint64_t best[kLpTop];
     uint64_t near[kNear];
@@ -251,7 +252,7 @@ struct Reader {
         if (n > kLpNear) {
             uint64_t mine = 0;
             for (int i = threadIdx.x; i < n; i += THREADS) mine = sm->list[i] > mine ? sm->list[i] : mine;
-            const uint64_t least = reached(mine, 2, top, sm);
+            const uint64_t least = reached(mine, Shared::kShare, top, sm);
             for (int i = threadIdx.x; i < n; i += THREADS) {
                 const uint64_t entry = sm->list[i];
                 if (entry != 0 && entry >= least) sm->near[atomicAdd(&sm->nearby, 1u)] = entry;
@@ -284,7 +285,7 @@ struct Reader {
     // A tile's candidates by its groups' maxima, of which `which` is the thread's (all of the CTA's threads come here); returns the bound for later tiles.
     static __device__ __forceinline__ float choose(LpRow r, int tile, float most, int which, float bound, int top, Shared* sm) {
         uint64_t mine = most > bound ? lp_entry(fminf(most, FLT_MAX), uint32_t(place((tile + int(threadIdx.x)) * V - r.skip, which))) : 0;
-        const uint64_t least = reached(mine, top <= Shared::kFewTop ? 8 : 2, top, sm);
+        const uint64_t least = reached(mine, top <= Shared::kFewTop ? 8 : Shared::kShare, top, sm);
         if (most > bound && (least == 0 || most >= lp_value(least))) note(r, tile, sm);
         __syncthreads();
         look(r, bound, least, sm);
@@ -531,12 +532,44 @@ __cluster_dims__(CTAS, 1, 1) __global__ void __launch_bounds__(THREADS, 1024 / T
     lp_run<HALF, THREADS, E, CTAS>(p, sm);
 }
 
+// A row's CTAs where each has 1024 threads and an SM of its own.
+template <bool HALF, int CTAS>
+struct Wide {
+    static constexpr int E = HALF ? 24 : 20;
+    static cudaError_t launch(const tetra_logprobs_rows& p, cudaStream_t s) { return launch_pdl(k_logprobs<HALF, 1024, E, CTAS>, p.rows * CTAS, 1024, 0, s, p); }
+    // Rows whose clusters run at once (a cluster is within a GPC, which leaves some SMs over).
+    static cudaError_t rows_at_once(int& rows) {
+        static PerDeviceOnce once;
+        static int fit[PerDeviceOnce::kMaxDevices];
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
+        if (e != cudaSuccess) return e;
+        e = once.run([device] {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(CTAS);
+            cfg.blockDim = dim3(1024);
+            return cudaOccupancyMaxActiveClusters(&fit[device], k_logprobs<HALF, 1024, E, CTAS>, &cfg);
+        });
+        if (e == cudaSuccess) rows = fit[device];
+        return e;
+    }
+};
+
+// CTAs of 1024 threads: clusters of eight for as many long rows as run at once, then two or one a row that fill the SMs; else of 256, as
+// many as fill them four times.  Measured, us with 1024 and 256 threads (1 and 20 likeliest tokens): 151936 logits, 8 rows 10.3 and 11.3 (12.2,
+// 12.8), 15 10.9 and 11.5, 16 (in two waves) 18.2 and 12.2, 24 by fours 13.5 and 12.8, 64 17.9 and 19.4 (21.1, 22.8), 74 18.2 and 25.6, 100 25.8 and 23.7 (30.0,
+// 30.5), 148 27.3 and 36.3; 100003 logits, 8 rows 10.1 and 9.8 (12.0, 10.9), 64 16.0 and 16.5; 20011 logits, 36 rows 9.7 and 10.6 (11.5, 13.3), 148 10.2 and 15.4.
 template <bool HALF>
 cudaError_t launch_logprobs(const tetra_logprobs_rows& p, int sms, cudaStream_t s) {
     if (p.vocab <= kLpShortRow) return launch_pdl(k_logprobs<HALF, 128, 16, 1>, p.rows, 128, 0, s, p);
-    constexpr int wide = HALF ? 24 : 20;
+    if (p.vocab > kLpWideRow && p.rows * 8 <= sms) {
+        int rows = 0;
+        const cudaError_t e = Wide<HALF, 8>::rows_at_once(rows);
+        if (e != cudaSuccess) return e;
+        if (p.rows <= rows) return Wide<HALF, 8>::launch(p, s);
+    }
+    if (p.vocab > kLpMiddleRow && p.rows * 4 >= sms && p.rows <= sms) return p.rows * 2 <= sms ? Wide<HALF, 2>::launch(p, s) : Wide<HALF, 1>::launch(p, s);
     const int at_once = 4 * sms + sms / 2;  // CTAs of 256 threads, and some that come behind them
-    if (p.rows * 8 <= sms && p.vocab > kLpWideRow) return launch_pdl(k_logprobs<HALF, 1024, wide, 8>, p.rows * 8, 1024, 0, s, p);
     return p.rows * 8 <= at_once ? launch_pdl(k_logprobs<HALF, 256, 32, 8>, p.rows * 8, 256, 0, s, p)
          : p.rows * 4 <= at_once ? launch_pdl(k_logprobs<HALF, 256, 32, 4>, p.rows * 4, 256, 0, s, p)
          : p.rows * 2 <= at_once ? launch_pdl(k_logprobs<HALF, 256, 32, 2>, p.rows * 2, 256, 0, s, p)

@@ -12,6 +12,8 @@ namespace tetra {
 // make their first call at once.
 class PerDeviceOnce {
 public:
+    static constexpr int kMaxDevices = 64;
+
     template <typename F>
     cudaError_t run(F&& setup) {
         int dev = 0;
@@ -28,7 +30,6 @@ public:
     }
 
 private:
-    static constexpr int kMaxDevices = 64;
     std::mutex mu_;
     bool done_[kMaxDevices] = {};
 };

@@ -107,6 +107,12 @@ def test_numbers_of_rows(tt, R, V):
     check(tt, logits(R, R, V), some(R, R, V, 2), top=3, rows_of=sorted({0, 1, R // 2, R - 1} & set(range(R))))
 
 
+@pytest.mark.parametrize("R", [15, 16, 36, 37, 74, 75, 148, 149])
+@pytest.mark.parametrize("V,dtype,top", [(16385, torch.float16, 20), (40003, torch.float32, 32), (140001, torch.float32, 16)])
+def test_numbers_of_long_rows(tt, R, V, dtype, top):
+    check(tt, logits(R + V, R, V, dtype), some(R, R, V, 1), top=top, rows_of=[0, R // 2, R - 1])
+
+
 @pytest.mark.parametrize("given,top", [(0, 0), (0, 32), (64, 0), (64, 32), (5, 8), (2, 9), (1, 31)])
 @pytest.mark.parametrize("R,V", [(2, 5003), (2, 100003), (40, 20011), (200, 9001)])
 def test_numbers_of_tokens(tt, R, V, given, top):
