@@ -232,3 +232,30 @@ def test_the_binding_refuses(tt):
     refused("v: Half", q, f, f.half(), *st.args(), pos, axis, h, inv)
     none = torch.zeros((0, 4, 128), dtype=torch.float16, device="cuda")
     assert tt.tetra_kv_append_at(q[:0], f[:0], f[:0], *st.args(), pos[:0], axis, none, inv) is none
+
+
+def test_as_many_rows_as_there_may_be(tt):
+    """65536 rows of one sequence at once, read back: what tetra_kv_append makes of the same positions."""
+    n, D = 65536, 64
+    cache = tt.tetra_kv_cache(n // 64 + 1, 64, 1, D)
+    table, starts, zero = torch.arange(n // 64 + 1, device="cuda", dtype=torch.int32).flip(0)[None], i32([0, n]), i32([7])
+    x = torch.randn((n, 3, D), device="cuda")
+    at = torch.arange(7, n + 7, device="cuda", dtype=torch.int32)[:, None].repeat(1, 2)
+    axis = torch.arange(D // 2, device="cuda").remainder(2).byte()
+    made = []
+    for positions in (False, True):
+        cache.fill_(0x81)
+        q = torch.empty((n, 1, D), dtype=torch.float16, device="cuda")
+        where = (cache, table, starts, zero)
+        if positions:
+            tt.tetra_kv_append_at(x[:, :1], x[:, 1:2], x[:, 2:], *where, at, axis, q, dev(INV[D]))
+        else:
+            tt.tetra_kv_append(x[:, :1], x[:, 1:2], x[:, 2:], *where, q, inv_freq=dev(INV[D]))
+        k, v = (torch.empty((n, 1, D), dtype=torch.float16, device="cuda") for _ in range(2))
+        tt.tetra_kv_read(*where, k, v)
+        made.append((cache[..., :32 * D + 8].clone(), k, v, q))
+    for a, b in list(zip(*made))[:3]:
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert (made[0][3].float() - made[1][3].float()).abs().max() <= 2.0 ** -10 * made[0][3].float().abs().max()
+    step = made[0][0].view(-1, 32 * D + 8)[:, 32 * D:].contiguous().view(torch.float32).max()
+    assert (made[1][2].float() - x[:, 2:]).abs().max() <= step * 0.5 + 2.0 ** -10 * x.abs().max()  # half a code, and float16's rounding

@@ -287,6 +287,21 @@ def test_offsets_that_pass_32_bits(tt):
     assert torch.equal(small, big)
 
 
+@pytest.mark.parametrize("D,heads,H,rows,shared", [(128, 32, 8, [3000, 2500], 4096), (64, 16, 8, [3000, 1, 1500], 1024), (256, 16, 4, [900, 1100], 1024)])
+def test_prompts_behind_prompts(tt, D, heads, H, rows, shared):
+    """More items than parts, several of a CTA: against tetra_kv_attend, of which the sums and the weights' roundings are another's of the same bounds
+    (two of 2^-11 of the mean of |v| a weight, one of 2^-11 of the result each)."""
+    st = Step(125, D, H, 64, [shared + 5] * len(rows), rows)
+    start, tokens = share(st, [(0, len(rows), shared)])
+    q = torch.randn((st.total, heads, D), device="cuda").half()
+    out = tt.tetra_kv_attend_shared(q, *st.args(), start, tokens, torch.empty_like(q), tt.tetra_kv_shared_workspace(D, st.total, heads, H, 1))
+    want = tt.tetra_kv_attend(q, *st.args(), torch.empty_like(q), tt.tetra_kv_workspace(D))
+    k, v = (torch.empty((shared, H, D), dtype=torch.float16, device="cuda") for _ in range(2))
+    tt.tetra_kv_read(st.cache, st.d_table[:1], i32([0, shared]), i32([0]), k, v)
+    most = v.float().abs().max()
+    assert (out.float() - want.float()).abs().max() <= 2 * 2.0 ** -11 * most + 2 * 2.0 ** -11 * want.float().abs().max()
+
+
 # ---- streams, graphs, refusals -----------------------------------------------------------------------------------------
 def test_a_captured_call_follows_lengths_groups_and_pages(tt):
     """One graph, replayed with other groups, lengths, pages and queries; eager calls use its workspace in between."""

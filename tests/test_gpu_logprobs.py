@@ -253,3 +253,19 @@ def test_the_binding_refuses(tt):
     none = torch.zeros((0, 3), device="cuda")
     assert tt.tetra_logprobs(x[:0], t[:0], none) is none
     assert tt.tetra_logprobs(x, None, None, entropy=torch.zeros(2, device="cuda")) is None
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_the_longest_rows(tt, dtype):
+    """2^24 logits: the sums' terms are 42 times those of 400000, added by 8192 threads; (50 + 3700 of a thread's tiles) 2^-24 is below 2^-12."""
+    V = 1 << 24
+    x = logits(31, 2, V, dtype)
+    lp, top, top_lp, rank, entropy = (torch.empty(s, device="cuda", dtype=t) for s, t in (((2, 1), torch.float32), ((2, 8), torch.int32), ((2, 8), torch.float32), ((2, 1), torch.int32), ((2,), torch.float32)))
+    t = torch.tensor([[V - 1], [5]], dtype=torch.int32, device="cuda")
+    tt.tetra_logprobs(x, t, lp, rank=rank, entropy=entropy, top_tokens=top, top_logprob=top_lp)
+    want = torch.log_softmax(x.double(), -1)
+    assert (lp.double() - want.gather(1, t.long())).abs().max() <= 2.0 ** -12
+    assert (entropy.double() + (want.exp() * want).sum(-1)).abs().max() <= 2.0 ** -8
+    order = torch.sort(x.float(), dim=-1, descending=True, stable=True).indices
+    assert torch.equal(top.long(), order[:, :8])
+    assert torch.equal(rank.long()[:, 0], (order == t.long()).nonzero()[:, 1])
