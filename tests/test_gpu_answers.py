@@ -46,7 +46,7 @@ def test_a_picture_its_answers_and_their_worth(tt):
     logits = torch.from_numpy(rng.standard_normal((answers, V)).astype(np.float32) * 3).cuda()
     tokens = rng.integers(0, V, (answers, 1)).astype(np.int32)
 
-    d_x, d_y, d_pos, d_next, d_tokens, d_lengths = dev(x), dev(y), i32(positions), i32(next_positions), dev(tokens), i32(lengths)
+    d_x, d_y, d_pos, d_next, d_tokens, d_lengths = dev(x), dev(y), i32(positions), i32(next_positions), dev(tokens), i32(list(lengths) + [0] * (len(st.d_lengths) - answers))
     half = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda")  # noqa: E731
     q0, q1, out = half(prompt, heads, D), half(answers, heads, D), half(answers, heads, D)
     lp, rank = torch.zeros((answers, 1), device="cuda"), torch.zeros((answers, 1), dtype=torch.int32, device="cuda")

@@ -22,9 +22,13 @@ def tt():
 
 
 def wide(st, table):
-    """A table with room for more tokens than there are: what a call could save is judged by that."""
-    room = int(120e6 + 200 * st.total * 64 * st.D) // (max(len(table) - 1, 1) * st.H * st.D * 2 * st.P) + 1
-    return i32(np.concatenate([table, np.full((len(table), max(st.gap, room)), -7)], 1))[:, :max(st.width, room)]
+    """A table with room for more tokens and sequences than there are, the others without rows: what a call could save is judged by that."""
+    n = len(table)
+    idle = max(0, 24 - n) if st.total <= 2 * n else 0
+    room = int(126e6 + 160 * st.total * 64 * st.D) // (st.H * max(900, (n + idle) * st.D) * st.P) + 1
+    st.d_starts, st.d_lengths = i32(list(st.starts) + [st.starts[-1]] * idle), i32(list(st.before) + [0] * idle)
+    t = np.concatenate([table, np.full((n, max(st.gap, room)), -7)], 1)
+    return i32(np.concatenate([t, np.full((idle, t.shape[1]), -7)]))[:, :max(st.width, room)]
 
 
 def share(st, groups, narrow=False):
@@ -163,7 +167,7 @@ def test_ranges_of_rows_that_make_no_sense_have_no_rows(tt):
     ws = tt.tetra_kv_shared_workspace(64, 4, 4, 2, 1)
     for starts, live in (([0, 1, 1, 2, 9], [0, 1]), ([-1, 1, 2, 3, 4], [1, 2, 3]), ([4, 4, 4, 4, 4], []), ([9, 9, 9, 9, 9], [])):
         out = torch.full_like(q, 7.5)
-        tt.tetra_kv_attend_shared(q, st.cache, st.d_table, i32(starts), st.d_lengths, start, shared, out, ws)
+        tt.tetra_kv_attend_shared(q, st.cache, st.d_table, i32(starts + starts[-1:] * (len(st.d_lengths) - 4)), st.d_lengths, start, shared, out, ws)
         rows = torch.zeros(4, dtype=torch.bool, device="cuda")
         rows[live] = True
         assert (out[~rows] == 7.5).all() and (out[rows] != 7.5).any(-1).all(), starts
@@ -307,21 +311,22 @@ def test_a_captured_call_follows_lengths_groups_and_pages(tt):
     """One graph, replayed with other groups, lengths, pages and queries; eager calls use its workspace in between."""
     D, H, heads, n = 128, 2, 8, 6
     st = Step(120, D, H, 16, [400] * n, [1] * n, width=40)
-    start, shared, table, lengths = i32([0, 3, 6]), i32([0, 0]), wide(st, st.table), i32([0] * n)
+    start, shared, table = i32([0, 3, 6]), i32([0, 0]), wide(st, st.table)
+    rows, lengths = st.d_starts, torch.zeros_like(st.d_lengths)
     q, out, ws = torch.zeros((n, heads, D), dtype=torch.float16, device="cuda"), torch.zeros((n, heads, D), dtype=torch.float16, device="cuda"), tt.tetra_kv_shared_workspace(D, n, heads, H, 2)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
-        tt.tetra_kv_attend_shared(q, st.cache, table, st.d_starts, lengths, start, shared, out, ws)
+        tt.tetra_kv_attend_shared(q, st.cache, table, rows, lengths, start, shared, out, ws)
     rng = np.random.default_rng(121)
     for split, tokens, before in (([0, 3, 6], [320, 160], [330, 340, 320, 200, 161, 160]), ([0, 6, 6], [128, 0], [128, 600, 130, 129, 400, 500]),
                                   ([0, 0, 0], [9, 9], [5] * 6), ([1, 3, 5], [512, 384], [7, 520, 513, 400, 385, -1])):
         st.table = rng.permutation(st.pages)[:n * st.width].reshape(n, st.width)
         new_start, new_shared = share(st, list(zip(split, split[1:], tokens)))
-        for to, x in ((start, new_start), (shared, new_shared), (table, wide(st, st.table)), (lengths, i32(before)), (q, torch.randn((n, heads, D), device="cuda").half())):
+        for to, x in ((start, new_start), (shared, new_shared), (table, wide(st, st.table)), (lengths, i32(before + [0] * (len(lengths) - n))), (q, torch.randn((n, heads, D), device="cuda").half())):
             to.copy_(x)
         graph.replay()
         replayed = out.clone()
-        eager = tt.tetra_kv_attend_shared(q, st.cache, table, st.d_starts, lengths, start, shared, torch.zeros_like(q), ws)
+        eager = tt.tetra_kv_attend_shared(q, st.cache, table, rows, lengths, start, shared, torch.zeros_like(q), ws)
         assert torch.equal(replayed.view(torch.int16), eager.view(torch.int16))
         plain, bound = ref.attend(st.plain(), q.cpu().numpy(), st.table, st.starts, before, 1 / np.sqrt(D))
         assert (np.abs(replayed.cpu().numpy() - plain) <= 3 * bound).all()
