@@ -918,15 +918,15 @@ cudaError_t launch_attend_all(const AttParams& p, int D, int sms, cudaStream_t s
 }
 
 // Whether one launch in which each sequence reads all of its tokens may take longer than three that read shared ones once, if the table is full
-// and shared by all: in bytes at 7.9 TB/s, a token and kv head are 2 D of them for an item of 8 columns, twice that of 16 and 2.7 times of 32 (whose
+// and shared by all: in bytes at 7.9 TB/s, a token and kv head are 2 D of them for an item of 8 columns, 1.75 times that of 16 and 2.7 of 32 (whose
 // products bound it), and for a tile of k_kv_prefix what its steps take; two more launches are 63 MB, a row's pieces 40 times its queries.
 // Measured with 32/8 heads, us apart and shared: heads of 128, 16 single tokens behind 1024 13.3 and 16.8, 2048 17.8 and 17.5, 4096 26.5 and 19.3; 64
 // behind 512 23.2 and 25.3, 1024 30.8 and 26.2; 64 times 5 rows behind 512 39 and 50, 1024 55.5 and 53.2; 2 tokens behind 65536 41 and 62, 4 behind
 // 16384 26.2 and 26.7; heads of 64, 4 behind 32768 27 and 34; heads of 256, 2 behind 32768 44 and 50.  Of 312 calls the better one is missed by
-// 1.2 % on average, 20 % at worst.
+// 1.2 % on average, 23 % at worst.
 bool worth_sharing(const AttParams& p, int D) {
     const int64_t columns = attend_columns(p), item = columns <= 8 ? 8 : D == 256 || columns <= 24 ? 16 : 32, all = int64_t(p.c.rows) * p.group;
-    const double apart = double(p.c.seqs * ((columns + item - 1) / item)) * (item == 8 ? 1. : item == 16 ? 2. : 2.7) * (2 * D);
+    const double apart = double(p.c.seqs * ((columns + item - 1) / item)) * (item == 8 ? 1. : item == 16 ? 1.75 : 2.7) * (2 * D);
     const double shared = D < 256 && all <= kPreColumns ? (D == 64 ? 576. : 712.) : (D == 64 ? 800. : 1040.) * double((all + pre_tile(D) - 1) / pre_tile(D));
     const double tokens = double(p.c.kv_heads) * p.c.width * p.c.blocks_per_page * kKvBlock, queries = double(all) * p.c.kv_heads * D * 2;
     return (apart - shared) * tokens >= 63e6 + 40. * queries;
