@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     using C = PreCfg<D>;
     constexpr int SLOTS = C::SLOTS, TILES = C::TILES, CHUNKS = D / 32;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t raw_full[8], raw_empty[8], tile_full[TILES], tile_empty[TILES], q_ready[2], s_full[4], p_ready[4], o_done[4], scales_full[kPreScales],
+    __shared__ __align__(8) uint64_t raw_full[8], raw_empty[8], tile_full[TILES], tile_empty[TILES], q_ready, q_seen, s_full[4], p_ready[4], o_done[4], scales_full[kPreScales],
         other_ready, other_free, drained;
     __shared__ __align__(16) float4 scales[kPreScales][kPreBlocks];  // s_K times the call's, s_V, log2 s_V, whether there is such a block
     __shared__ float2 other[kPreColumns];                            // of the slots that share columns: the second one's references and denominators
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         failed = 0;
         for (uint32_t i = 0; i < stages; ++i) bar_init(smem_u32(raw_full + i), 1), bar_init(smem_u32(raw_empty + i), kPreConvert);
         for (int i = 0; i < TILES; ++i) bar_init(smem_u32(tile_full + i), kPreConvert), bar_init(smem_u32(tile_empty + i), SLOTS);
-        for (int i = 0; i < 2; ++i) bar_init(smem_u32(q_ready + i), 4);
+        bar_init(smem_u32(&q_ready), 4 * SLOTS), bar_init(smem_u32(&q_seen), SLOTS);
         for (int i = 0; i < 4; ++i) bar_init(smem_u32(p_ready + i), 4), bar_init(smem_u32(s_full + i), 1), bar_init(smem_u32(o_done + i), 1);
         for (int i = 0; i < kPreScales; ++i) bar_init(smem_u32(scales_full + i), 1);
         bar_init(smem_u32(&other_ready), 4), bar_init(smem_u32(&other_free), 4);
@@ -554,7 +554,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         // ---- products, issued by one thread a slot.  A job is a step of the slot's.  Its scores are issued one job ahead of its weights'
         // products, into the place that the last job but one had, whose products are waited for (products with different results are in no
         // order).  Each place has barriers of its own: a barrier tells of its last phase only, and the products of two jobs may both be
-        // on their way.  For the same reason each slot waits for every step's tiles, its own or not.
+        // on their way.  For the same reason each slot waits for every step's tiles, its own or not, and for every part's queries, which are
+        // announced by all warps of the weights, whoever brings them, and not again before both slots have said that they have seen them: a
+        // part of one step that the slots share is no work for the second one's weights, which would be two parts ahead otherwise.
         const uint32_t slot = warp - kPreMmaWarp;
         bool ok = true;
         uint32_t own = 0, q_parts = 0;  // jobs so far
@@ -566,7 +568,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
             if (!part_of<D>(p, plan, at, q)) continue;
             const uint32_t steps = q.end - q.begin, by = q.both ? 2u : 1u, first = q.both ? slot : 0u;
             const uint32_t queries_at = ((queries & 0x3FFFFu) + (q.both ? 0u : slot * C::QTILE)) >> 4;
-            for (int i = 0; i < SLOTS; ++i) ok = ok && bar_wait(smem_u32(q_ready + i), q_parts & 1u, gave_up);
+            ok = bar_wait(smem_u32(&q_ready), q_parts & 1u, gave_up);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            if (lane == 0) bar_arrive(smem_u32(&q_seen));
             auto scores = [&](uint32_t i, uint32_t job) {
                 const uint32_t step = n0 + i, pair = step % PAIRS, place = job & 1u;
                 if (job >= 2) ok = ok && bar_wait(smem_u32(o_done + slot * 2) + place * 8, (job >> 1) + 1 & 1u, gave_up);
@@ -629,7 +634,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         // ---- weights: a thread a column
         const uint32_t slot = warp >> 2, column = threadIdx.x & 127;
         const uint32_t at_q = tensor + slot * C::SLOT + ((warp & 3u) << 21), at_scores = at_q + C::QCOLS, at_o = at_scores + 2 * kPreStep;  // lanes from bit 16 on
-        uint32_t jobs = 0, shared_parts = 0, freed = 0;
+        uint32_t jobs = 0, shared_parts = 0, freed = 0, q_parts = 0;
         bool ok = true;
         for (uint32_t at = blockIdx.x; ok && at < parts; at += gridDim.x) {
             PrePart q;
@@ -676,10 +681,15 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 __syncwarp();
-                if (lane == 0) bar_arrive(smem_u32(q_ready + slot));
-            } else if (lane == 0) {
-                bar_arrive(smem_u32(q_ready + slot));
             }
+            if (q_parts > 0) {  // the last part's have been seen
+                ok = bar_wait(smem_u32(&q_seen), (q_parts - 1) & 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+            }
+            ++q_parts;
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_u32(&q_ready));
             if (slot == 1 && freed < shared_parts) {  // the first slot has yet to read the sums of the last part that they shared
                 ok = bar_wait(smem_u32(&other_free), (shared_parts - 1) & 1u, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
