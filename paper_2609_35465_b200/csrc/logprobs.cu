@@ -318,7 +318,9 @@ __device__ __forceinline__ void lp_run(const tetra_logprobs_rows& p, LpShared<TH
     constexpr int V = R::V, WARPS = THREADS / 32;
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
     const int r = blockIdx.x / CTAS, rank = CTAS == 1 ? 0 : int(cg::this_cluster().block_rank()), top = max(p.top, 1);
-    if (CTAS > 1) cg::this_cluster().barrier_arrive();  // the first CTA is written to when all have begun
+    static_assert(THREADS >= kLpGiven, "a thread a counter");
+    if (threadIdx.x < kLpGiven) sm.count[threadIdx.x] = 0;
+    if (CTAS > 1) cg::this_cluster().barrier_arrive();  // the first CTA is written to when all have begun: what others add to is zero by then
     pdl_wait();
     pdl_release();
     const int size = HALF ? 2 : 4;
@@ -340,7 +342,6 @@ __device__ __forceinline__ void lp_run(const tetra_logprobs_rows& p, LpShared<TH
         sm.given[g] = x;
         sm.below[g] = x == 0.f ? -1.17549435e-38f : x > 0.f ? __uint_as_float(bits - 1) : __uint_as_float(bits + 1);  // (not used of minus infinity)
         sm.token[g] = is ? t : -1;
-        sm.count[g] = 0;
     }
     if (threadIdx.x == 0) sm.listed = sm.noted = 0;
 
