@@ -332,7 +332,10 @@ __device__ __forceinline__ void lp_run(const tetra_logprobs_rows& p, LpShared<TH
 
     const float T = p.temperature ? __ldg(p.temperature + r) : 1.f;
     const bool greedy = !(T > 0.f);
-    const float c = greedy ? 1.f : fminf(__fdiv_rn(1.4426950408889634f, T), FLT_MAX);
+    // Distances between logits are taken of sixteenths where T is above 1: exact, and float32 holds the largest of them (two logits
+    // may lie 2 FLT_MAX apart) and the factor that goes with the largest T.  Where T is not above 1 an infinite distance is no weight.
+    const float part = T > 1.f ? 0.0625f : 1.f, c = greedy ? 1.f : fminf(__fdiv_rn(1.4426950408889634f / part, T), FLT_MAX);
+    auto distance = [&](float x, float to) { return fmaxf(fmaf(x, part, -to * part) * c, kLpLeast); };  // log2 of a weight
     const double by_temperature = 1. / double(T);
     for (int g = THREADS - 1 - int(threadIdx.x); g < p.given; g += THREADS) {
         const int t = __ldg(p.tokens + int64_t(r) * p.given + g);
@@ -362,19 +365,19 @@ __device__ __forceinline__ void lp_run(const tetra_logprobs_rows& p, LpShared<TH
             most = FLT_MAX;
         }
         if (most > ref) {
-            const float d = fmaxf((ref - most) * c, kLpLeast), f = lp_ex2(d);
+            const float d = distance(ref, most), f = lp_ex2(d);
             product = f * fmaf(sum, d, product);
             sum *= f;
             ref = most;
         }
         {
-            const uint64_t from = lp_two(-ref, -ref), by = lp_two(c, c);
+            const uint64_t from = lp_two(-ref * part, -ref * part), by = lp_two(c, c), parts = lp_two(part, part);
             uint64_t s2 = 0, w2 = 0;
 #pragma unroll
             for (int j = 0; j < E; j += 2) {
                 uint64_t z, e;
                 float a, b;
-                asm("add.rn.f32x2 %0, %1, %2;" : "=l"(z) : "l"(lp_two(x[j], x[j + 1])), "l"(from));
+                asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(z) : "l"(lp_two(x[j], x[j + 1])), "l"(parts), "l"(from));
                 asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(z) : "l"(z), "l"(by));
                 lp_two(z, a, b);
                 a = fmaxf(a, kLpLeast), b = fmaxf(b, kLpLeast);  // infinite distances and NaN: the least
@@ -472,7 +475,7 @@ __device__ __forceinline__ void lp_run(const tetra_logprobs_rows& p, LpShared<TH
     LpSums s;
     s.top = largest(ref);
     {
-        const float d = fmaxf((ref - s.top) * c, kLpLeast), f = lp_ex2(d);
+        const float d = distance(ref, s.top), f = lp_ex2(d);
         s.sum = double(sum * f);
         s.product = double(f * fmaf(sum, d, product));
         add_lanes(s.sum, s.product);
@@ -483,7 +486,7 @@ __device__ __forceinline__ void lp_run(const tetra_logprobs_rows& p, LpShared<TH
     // Sums of n warps, or CTAs, lane by lane.
     auto join = [&](const LpSums* of, int n) {
         s = lane < n ? of[lane] : LpSums{0., 0., kLpNoRef};
-        const float all = largest(s.top), d = fmaxf((s.top - all) * c, kLpLeast), f = lp_ex2(d);
+        const float all = largest(s.top), d = distance(s.top, all), f = lp_ex2(d);
         s.product = f * (s.product + s.sum * d);
         s.sum *= f;
         s.top = all;
