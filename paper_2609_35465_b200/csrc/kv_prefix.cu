@@ -46,6 +46,10 @@ constexpr uint32_t kPreTries = 1u << 22;                  // of a wait: then the
 constexpr int kPreSmem = 227 * 1024 - 2304;               // what a CTA may have, but for the barriers
 constexpr float kPreNoRef = -FLT_MAX, kPreLeastLog = -60.f, kPreHigh = 15.f, kPreBase = 7.f;  // as in k_kv_attend
 constexpr float kPreMost = 32768.f;                       // 2^15
+// Next to a reference up to this a score is not rounded before the reference is taken off (one fma for two scores).  From 2^27 on a score that is
+// not rounded is powers of two beside the one that is, which is what the reference was found from: next to larger references a score is
+// rounded first, as in k_kv_attend, and what a column's weights are made from does not depend on the other columns.
+constexpr float kPreLargeRef = 65536.f;
 
 template <int D>
 struct PreCfg {
@@ -708,8 +712,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
                 // column) call for a new one; as long as none does, no maximum is looked for.
                 float now = 0.f;
-                bool over = __all_sync(0xFFFFFFFFu, ref == kPreNoRef);
-                if (!over) {
+                bool over = !(fabsf(ref) <= kPreLargeRef);  // a column that has seen nothing, too
+                if (!__all_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
                     for (int b = 0; b < kPreBlocks; ++b) {
                         const float4 by = c[b];
@@ -743,7 +747,13 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                         uint32_t x[16];
                         tensor_load16(at_s + 16 * b, x);
                         wait_loads();
-                        now += block_weights(x, c[b], ref, w);
+                        float4 by = c[b];
+                        const bool large = !(fabsf(ref) <= kPreLargeRef);
+                        const float first_by = large ? by.x : 1.f;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__fmul_rn(__uint_as_float(x[k]), first_by));
+                        by.x = large ? 1.f : by.x;
+                        now += block_weights(x, by, ref, w);
                         tensor_store8(at_s + 8 * b, w);
                     }
                     if (i > first) {
