@@ -45,7 +45,6 @@ constexpr uint32_t kPrePartCost = 8;                      // steps that a part's
 constexpr uint32_t kPreTries = 1u << 22;                  // of a wait: then the call's results are NaN
 constexpr int kPreSmem = 227 * 1024 - 2304;               // what a CTA may have, but for the barriers
 constexpr float kPreNoRef = -FLT_MAX, kPreLeastLog = -60.f, kPreHigh = 15.f, kPreBase = 7.f;  // as in k_kv_attend
-constexpr float kPreMost = 32768.f;                       // 2^15
 // Next to a reference up to this a score is not rounded before the reference is taken off (one fma for two scores).  From 2^27 on a score that is
 // not rounded is powers of two beside the one that is, which is what the reference was found from: next to larger references a score is
 // rounded first, as in k_kv_attend, and what a column's weights are made from does not depend on the other columns.
@@ -361,8 +360,8 @@ __device__ __forceinline__ uint64_t two_floats(float a, float b) {
     return v;
 }
 __device__ __forceinline__ void two_floats(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-// Weights of a block of 16 tokens, two and two as float16; returns the sum of 2^(score - ref).  scale: s_K times the call's, s_V, log2 s_V,
-// whether there is such a block.
+// Weights of a block of 16 tokens, two and two as float16; returns the sum of 2^(score - ref).  scale: s_K times the call's, s_V, log2 s_V, the
+// most that the sum may come to; 0: no such block.
 __device__ __forceinline__ float block_weights(const uint32_t* scores, const float4& scale, float ref, uint32_t* weights) {
     if (scale.w == 0.f) {
 #pragma unroll
@@ -396,7 +395,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
     extern __shared__ unsigned char raw[];
     __shared__ __align__(8) uint64_t raw_full[8], raw_empty[8], tile_full[TILES], tile_empty[TILES], q_ready, q_seen, s_full[4], p_ready[4], o_done[4], scales_full[kPreScales],
         other_ready, other_free, drained;
-    __shared__ __align__(16) float4 scales[kPreScales][kPreBlocks];  // s_K times the call's, s_V, log2 s_V, whether there is such a block
+    __shared__ __align__(16) float4 scales[kPreScales][kPreBlocks];  // s_K times the call's, s_V, log2 s_V (-60 at least), the most that weights may come to; 0: no such block
     __shared__ float2 other[kPreColumns];                            // of the slots that share columns: the second one's references and denominators
     __shared__ uint32_t placed[8], total, tensor_base;
     __shared__ int failed;
@@ -506,7 +505,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                         const float vs = __uint_as_float(raw4.y);
                         float lv = pre_lg2(vs);
                         lv = lv < kPreLeastLog ? kPreLeastLog : lv;  // NaN stays
-                        scales[n % kPreScales][lane] = is ? make_float4(__uint_as_float(raw4.x) * p.scale, vs, lv, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        // The most that a block's 2^(score - reference) may come to, by the same logarithm as the reference; never zero.
+                        const float most = fmaxf(pre_ex2(kPreHigh - lv), FLT_MIN);
+                        scales[n % kPreScales][lane] = is ? make_float4(__uint_as_float(raw4.x) * p.scale, vs, lv, most) : make_float4(0.f, 0.f, 0.f, 0.f);
                     }
                     __syncwarp();
                     if (lane == 0) bar_arrive(smem_u32(scales_full + n % kPreScales));
@@ -709,8 +710,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 tensor_load(at_s + 32, r + 32);
                 const float4* c = scales[n % kPreScales];
                 wait_loads();
-                // Weights next to the reference so far.  A block's weights of more than 2^15 together (or infinite ones: the first of a
-                // column) call for a new one; as long as none does, no maximum is looked for.
+                // Weights next to the reference so far.  A block's weights that with s_V are more than 2^15 together (or infinite ones: the first
+                // of a column) call for a new one; as long as none does, no maximum is looked for.  An s_V below 2^-60 counts as that:
+                // the weights of values that are zero, or next to it, stay within what the denominator holds, 2^75 a block.
                 float now = 0.f;
                 bool over = !(fabsf(ref) <= kPreLargeRef);  // a column that has seen nothing, too
                 if (!__all_sync(0xFFFFFFFFu, over)) {
@@ -718,7 +720,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                     for (int b = 0; b < kPreBlocks; ++b) {
                         const float4 by = c[b];
                         const float one = block_weights(r + 16 * b, by, ref, w + 8 * b);
-                        over |= !(one * by.y <= kPreMost);  // infinite times a scale of zero calls for one too
+                        over |= !(one <= by.w);
                         now += one;
                     }
                 }

@@ -1,4 +1,4 @@
-"""Attention of groups: scores that float32 has no fractions of and scores far below zero.
+"""Attention of groups: scores that float32 has no fractions of, scores far below zero, and values that are zero where the scores are largest.
 
 A key block's scale is no power of two here: score times scale is rounded, and what is rounded is what the weights go by."""
 import numpy as np
@@ -6,9 +6,10 @@ import pytest
 import torch
 
 import step_reference as ref
+from shared_cut import cut
 from test_gpu_kv import Step, dev
 from test_gpu_kv_large_scores import SCALE
-from test_gpu_kv_shared import share, tt  # noqa: F401
+from test_gpu_kv_shared import share, shared_check, tt  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +95,32 @@ def test_scores_far_below_zero(tt, D, heads, seqs, log_scale, times):  # noqa: F
                 # equal weights are powers of two, exact in float16; sums as above
                 want, size = v.mean(0), np.abs(v).mean(0)
                 assert (np.abs(out[s] - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -16 * size + 2.0 ** -25).all(), s
+
+
+@pytest.mark.parametrize("D,seqs,group,cases", [(128, 3, 2, 12), (128, 9, 16, 2), (64, 2, 2, 12), (256, 2, 2, 5)])
+def test_values_of_zero_under_the_largest_scores(tt, D, seqs, group, cases):  # noqa: F811
+    """Blocks of ordinary values set a reference; blocks of zeros, or of next to nothing, have a token each so many powers of two above it;
+    then come blocks of ordinary values, as much above or below that.  The prompt is 512 such tokens again and again, so that each of the
+    parts that it is cut into has all of them."""
+    heads, times = 8, 18
+    ctas = torch.cuda.get_device_properties(0).multi_processor_count
+    parts = cut(D, heads, group, [(seqs, 512 * times)], ctas)
+    assert any(steps >= 6 for mine in parts for steps, _ in mine)
+    st = Step(503, D, heads, 16, [512] * seqs, [1] * seqs)
+    own = st.table[:, 32:]
+    st.table = np.concatenate([np.tile(st.table[:1, :32], (seqs, times)), own], 1)
+    st.width, st.before = st.table.shape[1], [512 * times + i % 3 for i in range(seqs)]
+    block = st.table[0, :32]
+    q = np.zeros((seqs, group * heads, D), np.float16)
+    q[..., :2] = 1
+    codes, scales = ref.unpack(st.raw, D)
+    for above, last, log_value in [(a, b, v) for a in (127, 120) for b in (60, 10, -30) for v in (None, -100)][:cases]:
+        codes[0] = 0
+        codes[0, ..., 0] = -60                              # the reference is -67
+        scales[..., 0], scales[..., 1] = 1.0, 1.0
+        codes[0, block[8:24], :, 0, 5, 0] = above - 67      # both slots' steps
+        scales[block[8:24], :, 0, 1] = 0.0 if log_value is None else 2.0 ** log_value
+        codes[0, block[[24, 28]], :, 0, 3, 0], codes[0, block[[24, 28]], :, 0, 3, 1] = above - 67, last
+        st.raw = ref.pack(codes, scales, D)
+        st.cache = dev(st.raw)
+        shared_check(tt, st, group * heads, [(0, seqs, 512 * times)], scale=SCALE, q=q)
