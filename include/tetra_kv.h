@@ -100,7 +100,10 @@ typedef struct {
 
 /* tetra_kv_append, but for the angle: row r turns pair i by positions[r][axis[i]] * inv_freq[i], in 64 bits.  Positions may be
  * negative; an axis that is not below axes does not turn its pairs.  Where a row's key and value go is, as there, the next
- * slot of its sequence (row_start, lengths).  inv_freq is required.  One launch. */
+ * slot of its sequence (row_start, lengths).  inv_freq is required.  One launch.
+ * Queries of calls with more than two rows a sequence or so (rows - rows / 16 > 2 seqs) are turned in 32 bits, with sines that were made in 64 and
+ * rounded: beside the rounding to float16, 2^-11 of a result, that moves each of a pair by 2^-20 of the two's sizes together at most.  Norms
+ * hold for rows of any size, as there. */
 int tetra_kv_append_at(const tetra_kv_cache *cache, const tetra_kv_rows *rows, const tetra_kv_axes *axes, void *stream);
 
 /* What the cache holds for the rows' positions, as values: k_out, v_out float16 [rows][kv_heads][head_dim] (16-byte

@@ -135,8 +135,12 @@ __device__ __forceinline__ void load_side(const T* from, float (&x)[N]) {
 }
 
 // Many rows a sequence: a CTA for each block.  Queries are most of the work; they are rounded to float16 at the end, so from their
-// sines on (made in 64 bits, rounded to 32) they are in 32 bits, which moves a result by 2^-21 at most where float16 rounds by 2^-12; keys,
-// whose codes a last bit may decide, stay in 64.  SIDE: rows of q are aligned for loads of a lane's D / 64 neighbours at once.
+// sines on (made in 64 bits, rounded to 32) they are in 32 bits.  That moves a result by 2^-20 of its pair's two sizes together at most (the sum of
+// squares 7 2^-24, its root's reciprocal 4, products, sines and rotation 5), where float16 rounds by 2^-11 of the result.  Keys,
+// whose codes a last bit may decide, stay in 64, and so does a row whose norm could leave what 32 bits hold: squares of less than 2^-126 are
+// nothing beside a mean of 2^-80, and sums up to 2^108 or products up to 2^100 are far from the end.
+// SIDE: rows of q are aligned for loads of a lane's D / 64 neighbours at once.
+constexpr float kLeastMean = 8.2718061e-25f, kMostMean = 1.2676506e30f, kMostWeight = 1.1529215e18f;  // 2^-80, 2^100, 2^60
 template <int D, typename T, bool SIDE>
 __global__ void __launch_bounds__(kAppendThreads, D == 256 ? 3 : 4) k_kv_append_blocks(KvCache c, KvRows p, KvAxes t) {
     constexpr int E = D / 32, N = D / 64, PAIRS = D / 2;
@@ -221,10 +225,16 @@ __global__ void __launch_bounds__(kAppendThreads, D == 256 ? 3 : 4) k_kv_append_
 
     if (p.group == 0) return;
     float weight[2][N];
+    bool plain = true;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int i = 0; i < N; ++i) weight[k][i] = p.q_weight ? __ldg(p.q_weight + k * PAIRS + lane * N + i) : 1.f;
+        for (int i = 0; i < N; ++i) {
+            weight[k][i] = p.q_weight ? __ldg(p.q_weight + k * PAIRS + lane * N + i) : 1.f;
+            plain = plain && fabsf(weight[k][i]) <= kMostWeight;
+        }
+    plain = __all_sync(0xFFFFFFFFu, plain);
+    bool all_fine = true;
     while (next_row < rows) {
       float batch[AT_ONCE][2][N];
       int row = next_row, j = next_head;
@@ -241,6 +251,7 @@ __global__ void __launch_bounds__(kAppendThreads, D == 256 ? 3 : 4) k_kv_append_
       for (int o = 0; o < AT_ONCE; ++o, advance(row, j)) {
         if (row >= rows) break;
         float (&now)[2][N] = batch[o];
+        bool fine = true;
         if (p.q_weight) {
             float sum = 0.f;
 #pragma unroll
@@ -248,8 +259,11 @@ __global__ void __launch_bounds__(kAppendThreads, D == 256 ? 3 : 4) k_kv_append_
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum = fmaf(now[k][i], now[k][i], sum);
 #pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            const float by = rsqrtf(sum * (1.f / D) + float(p.eps));
+            for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
+            const float mean = fmaf(sum, 1.f / D, float(p.eps));
+            fine = plain && mean >= kLeastMean && mean <= kMostMean;
+            all_fine = all_fine && fine;
+            const float by = rsqrtf(mean);
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -263,6 +277,7 @@ __global__ void __launch_bounds__(kAppendThreads, D == 256 ? 3 : 4) k_kv_append_
             lo[i] = now[0][i] * u.x - now[1][i] * u.y;
             hi[i] = now[1][i] * u.x + now[0][i] * u.y;
         }
+        if (!fine) continue;
         if constexpr (N == 1) {
             out[0] = __float2half_rn(lo[0]);
             out[PAIRS] = __float2half_rn(hi[0]);
@@ -278,7 +293,26 @@ __global__ void __launch_bounds__(kAppendThreads, D == 256 ? 3 : 4) k_kv_append_
                 }
             }
         }
+      }
     }
+    if (all_fine) return;
+    // The others as k_kv_append_at makes them; those next to the border are made twice.
+#pragma unroll 1
+    for (int row = warp / p.group, j = warp % p.group; row < rows; advance(row, j)) {
+        float xq[E], sum = 0.f;
+        double z[E];
+        const int h = head * p.group + j;
+        load_row<T>(p.q, (int64_t(r) + row) * p.q_stride + int64_t(h) * D, lane, xq);
+#pragma unroll
+        for (int i = 0; i < E; ++i) sum = fmaf(xq[i], xq[i], sum);
+#pragma unroll
+        for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
+        const float mean = fmaf(sum, 1.f / D, float(p.eps));
+        if (plain && mean >= 2.f * kLeastMean && mean <= 0.5f * kMostMean) continue;
+        turn<E>(xq, p.q_weight, p.eps, turns + row * PAIRS, lane, z);
+        __half* out = p.q_out + ((int64_t(r) + row) * heads + h) * D;
+#pragma unroll
+        for (int i = 0; i < E; ++i) out[lane + 32 * i] = __double2half(z[i]);
     }
 }
 
