@@ -80,9 +80,9 @@ struct SharedPlaces {
         seqs = (tetra_kv_workspace_bytes(D) + 255) / 256 * 256;
         owns = seqs + size_t(TETRA_KV_MAX_SEQS) * sizeof(SharedSeq);
         own = owns + size_t(TETRA_KV_MAX_SEQS) * sizeof(OwnSeq);
-        // Items of eight columns are those of calls with no more than eight a sequence on average.
-        const int64_t group = q_heads / kv_heads, few_rows = rows * group < 8 * TETRA_KV_MAX_SEQS ? rows : 8 * TETRA_KV_MAX_SEQS / group;
-        runs = size_t(kv_heads * (few_rows * group / 8 + (few_rows < TETRA_KV_MAX_SEQS ? few_rows : TETRA_KV_MAX_SEQS)) + kRunsMost);
+        // Items of eight columns are those of calls with no more than eight a sequence on average; no bound gets less with more rows or heads.
+        const int64_t most = 8 * TETRA_KV_MAX_SEQS, cols = rows * (q_heads / kv_heads);
+        runs = size_t(kv_heads * ((cols < most ? cols : most) / 8 + (rows < TETRA_KV_MAX_SEQS ? rows : TETRA_KV_MAX_SEQS)) + kRunsMost);
         const size_t columns = runs * 8 > size_t(rows) * q_heads ? runs * 8 : size_t(rows) * q_heads;
         pieces = (own + columns * (D + 2) * sizeof(float) + 255) / 256 * 256;
         end = pieces + parts * pre_slots(D) * pre_piece(D) * sizeof(float);
