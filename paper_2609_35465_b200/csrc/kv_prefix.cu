@@ -469,13 +469,11 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 if (++stage == stages) stage = 0, ++turn;
             }
         }
-        // Nothing is in flight when the CTA ends: what was copied has been waited for by who converts it, unless that gave up.
-        if (!ok) {
-            int none = 0;
-            for (uint32_t back = 0; back < stages && back < issued; ++back) {
-                if (stage == 0) stage = stages, --turn;
-                bar_wait(smem_u32(raw_full + --stage), turn & 1u, &none);
-            }
+        // Nothing is in flight when the CTA ends, whoever gave up: the last copies into each stage have arrived.
+        int none = 0;
+        for (uint32_t back = 0; back < stages && back < issued; ++back) {
+            if (stage == 0) stage = stages, --turn;
+            bar_wait(smem_u32(raw_full + --stage), turn & 1u, &none);
         }
     } else if (warp >= kPreConvertAt && warp < kPreCopyWarp) {
         // ---- bytes to operands
