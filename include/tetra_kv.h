@@ -6,9 +6,11 @@
  * the step's rows over everything before them gives float16 activations for the next product.
  *
  * Conventions are those of tetra.h (status codes, device/host pointers, stream, validation before launch; a rejected
- * call launches nothing).  All of these kernels wait for the end of the kernels before them on the stream before
- * they read or write anything, so their operands may come from any call; what they write may be used as activations
- * as it is.  No result depends on the order in which threads run: every output is bit-identical from run to run.
+ * call launches nothing).  Every call waits for the end of the kernels before it on the stream before it reads or writes
+ * anything, so its operands may come from any call; what it writes may be used as activations as it is.  (Of the three
+ * kernels of tetra_kv_attend_shared the first one waits; the others start behind that wait, and the second one
+ * reads, the third one looks up its rows, without one of their own.)  No result depends on the order in which threads run:
+ * every output is bit-identical from run to run.
  *
  * Cache.  Tokens are kept in blocks of 16; a page is page_tokens / 16 blocks; cache[pages][kv_heads][page_tokens/16]
  * holds one record of 32 D + 16 bytes for each page, head and block:

@@ -69,6 +69,10 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) {
 //     ahead of the wait behind the stores of a predecessor that has released, so a
 //     kernel that writes weights (k_pack, k_q4_pack) never calls pdl_release,
 //     wherever its stores are: its dependents start when it has completed.
+//   * Kernels of one call whose first one waits before it releases start when what came
+//     before the call has completed.  The list behind k_prepare_x, and k_kv_attend and
+//     k_kv_join behind k_kv_prefix, read the call's operands on that ground ahead of a wait
+//     of their own; what the call's own kernels have written they read behind one.
 //   * A kernel that releases also waits, all of its CTAs, so that the completion of
 //     a kernel implies that of all kernels before it.
 // ---------------------------------------------------------------------------
