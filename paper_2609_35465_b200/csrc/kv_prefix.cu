@@ -4,27 +4,31 @@
 // answers of a model with four query heads to a kv head.  2 D bytes a token and kv head stand against 4 D multiply-adds a column, so
 // from about 100 columns on the tensor cores bound it, not HBM, and tcgen05 pays: a tile of 128 columns is one operand's 128 rows.
 //
-// Work.  An item is (group, kv head, tile of 256 columns; 128 with heads of 256), its tokens come in steps of 64 (four records) and are cut into
-// parts; what a CTA does is found by each CTA from the lengths, which are on the device.  A part leaves its sums in the workspace;
-// k_kv_attend does the sequences' own tokens meanwhile, and k_kv_join adds both.  No atomics on memory: bit-identical from run to run.
+// Work.  An item is (group, kv head, tile of 256 columns; 128 with heads of 256), its tokens come in steps of 64 (four records)
+// and are cut into parts; what a CTA does is found by each CTA from the lengths, which are on the device.  A part leaves its sums
+// in the workspace; k_kv_attend does the sequences' own tokens meanwhile, and k_kv_join adds both.  No atomics on memory:
+// bit-identical from run to run.
 //
 // A CTA.  One warp copies records by cp.async.bulk into a ring.  Four warps turn their bytes into float16 (exact: codes are small
 // integers) and lay them out for the tensor cores: keys as [token][dim], values as [dim][token], rows of 128 bytes, swizzled; the
-// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  One thread a slot issues the products: S = Q K^T and O += P V (P from tensor memory, over S).  Two groups of four warps
-// ("slots"), a thread a column, turn S into weights: no value of a column is in another thread, so there are no exchanges.  The
-// slots take the two halves of a tile's columns, or, where a tile has no more than 128, every other step, so that the products of
-// one run beside the exponentials of the other.  A slot has two places for scores, so that those of its next step are there when the
-// weights of this one are, and a warp of its own that issues its products.
+// order of the tokens inside a block is that in which a lane's bytes lie, the same for both.  One thread a slot issues the
+// products: S = Q K^T and O += P V (P from tensor memory, over S).  Two groups of four warps ("slots"), a thread a column, turn S
+// into weights: no value of a column is in another thread, so there are no exchanges.  The slots take the two halves of a tile's
+// columns, or, where a tile has no more than 128, every other step, so that the products of one run beside the exponentials of the
+// other.  A slot has two places for scores, so that those of its next step are there when the weights of this one are, and a warp
+// of its own that issues its products.
 //
-// What bounds it: for 64 tokens of 256 columns the exponentials alone take 1024 cycles (four a scheduler and cycle), what else the warps of
-// the weights issue beside them makes it 1570, the products 1280; a step takes about 2100.  With one place for scores it was 3300 to 3500, with
-// one warp for both slots' products, which waits for one slot while the other could go on, 2700.  64 answers with 32/8 heads of 128
-// behind 16384 tokens: 31 us, 4300 cycles of which find out how work is cut and 4000 are the first step's loads, 3 times the time of the
-// bytes (34 MB) or of the products; with k_kv_attend's 15 and k_kv_join's 6 behind it 60 us, where each sequence for itself takes 243.
+// What bounds it: for 64 tokens of 256 columns the exponentials alone take 1024 cycles (four a scheduler and cycle), what else the
+// warps of the weights issue beside them makes it 1570, the products 1280; a step takes about 2100.  With one place for scores it
+// was 3300 to 3500, with one warp for both slots' products, which waits for one slot while the other could go on, 2700.  64 answers
+// with 32/8 heads of 128 behind 16384 tokens: 31 us, 4300 cycles of which find out how work is cut and 4000 are the first step's
+// loads, 3 times the time of the bytes (34 MB) or of the products; with k_kv_attend's 15 and k_kv_join's 6 behind it 60 us, where
+// each sequence for itself takes 243.
 //
-// Arithmetic is that of k_kv_attend: scores are exact products summed in float32, times s_K; weights enter as
-// float16(2^(score - m) s_V) with m a running reference, a whole number, that moves only when a block's weights together would pass
-// 2^15; the denominator sums 2^(score - m) in float32.
+// Arithmetic is that of k_kv_attend: scores are exact products summed in float32, times s_K (not rounded before the reference is
+// taken off, where that is small: kPreLargeRef); weights enter as float16(2^(score - m) s_V) with m a running reference, a whole
+// number, that moves only when a block's weights together would pass 2^15, an s_V below 2^-60 counting as that; the denominator
+// sums 2^(score - m) in float32.
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -45,9 +49,10 @@ constexpr uint32_t kPrePartCost = 8;                      // steps that a part's
 constexpr uint32_t kPreTries = 1u << 22;                  // of a wait: then the call's results are NaN
 constexpr int kPreSmem = 227 * 1024 - 2304;               // what a CTA may have, but for the barriers
 constexpr float kPreNoRef = -FLT_MAX, kPreLeastLog = -60.f, kPreHigh = 15.f, kPreBase = 7.f;  // as in k_kv_attend
-// Next to a reference up to this a score is not rounded before the reference is taken off (one fma for two scores).  From 2^27 on a score that is
-// not rounded is powers of two beside the one that is, which is what the reference was found from: next to larger references a score is
-// rounded first, as in k_kv_attend, and what a column's weights are made from does not depend on the other columns.
+// Next to a reference up to this a score is not rounded before the reference is taken off (one fma for two scores).  From 2^27 on
+// a score that is not rounded is powers of two beside the one that is, which is what the reference was found from: next to larger
+// references a score is rounded first, as in k_kv_attend.  That goes by the column's own reference: what its weights are made from
+// does not depend on the other columns.  (A packed product and a packed sum with .rn become one fma all the same: measured.)
 constexpr float kPreLargeRef = 65536.f;
 
 template <int D>
@@ -557,9 +562,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
         // ---- products, issued by one thread a slot.  A job is a step of the slot's.  Its scores are issued one job ahead of its weights'
         // products, into the place that the last job but one had, whose products are waited for (products with different results are in no
         // order).  Each place has barriers of its own: a barrier tells of its last phase only, and the products of two jobs may both be
-        // on their way.  For the same reason each slot waits for every step's tiles, its own or not, and for every part's queries, which are
-        // announced by all warps of the weights, whoever brings them, and not again before both slots have said that they have seen them: a
-        // part of one step that the slots share is no work for the second one's weights, which would be two parts ahead otherwise.
+        // on their way.  For the same reason each slot waits for every step's tiles, its own or not, and for every part's queries,
+        // which are announced by all warps of the weights, whoever brings them, and not again before both slots have said that they
+        // have seen them: a part of one step that the slots share is no work for the second one's weights, which would be two parts
+        // ahead otherwise.
         const uint32_t slot = warp - kPreMmaWarp;
         bool ok = true;
         uint32_t own = 0, q_parts = 0;  // jobs so far
@@ -708,9 +714,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) k_kv_prefix(PreParams p) {
                 tensor_load(at_s + 32, r + 32);
                 const float4* c = scales[n % kPreScales];
                 wait_loads();
-                // Weights next to the reference so far.  A block's weights that with s_V are more than 2^15 together (or infinite ones: the first
-                // of a column) call for a new one; as long as none does, no maximum is looked for.  An s_V below 2^-60 counts as that:
-                // the weights of values that are zero, or next to it, stay within what the denominator holds, 2^75 a block.
+                // Weights next to the reference so far.  A block's weights that with s_V are more than 2^15 together (or infinite ones:
+                // the first of a column) call for a new one; as long as none does, no maximum is looked for.  An s_V below 2^-60
+                // counts as that: the weights of values that are zero, or next to it, stay within what the denominator holds, 2^75 a
+                // block.
                 float now = 0.f;
                 bool over = !(fabsf(ref) <= kPreLargeRef);  // a column that has seen nothing, too
                 if (!__all_sync(0xFFFFFFFFu, over)) {

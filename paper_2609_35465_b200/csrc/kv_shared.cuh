@@ -89,10 +89,11 @@ struct SharedPlaces {
     }
 };
 
-// k_kv_attend has nothing of k_kv_prefix's but starts behind what came before that (it is released when k_kv_prefix has waited, so the
-// call's operands are complete and it reads them without a wait); its end has to imply that one's.  What it writes, k_kv_join reads behind a
-// wait.  (Released at its beginning, k_kv_join waits beside both and takes nothing off: 67.8 and 69.5 us.  With a fence at its beginning k_kv_attend
-// takes 1 us longer, and a lookup of its row behind k_kv_join's wait 3, of 56 for 64 answers on 16384.)
+// k_kv_attend has nothing of k_kv_prefix's but starts behind what came before that (it is released when k_kv_prefix has waited, so
+// the call's operands are complete and it reads them without a wait); its end has to imply that one's.  What it writes, k_kv_join
+// reads behind a wait.  (Released at its beginning, k_kv_join waits beside both and takes nothing off: 67.8 and 69.5 us.  With a
+// fence at its beginning k_kv_attend takes 1 us longer, and a lookup of its row behind k_kv_join's wait 3, of 56 for 64 answers on
+// 16384.)
 __device__ __forceinline__ void end_behind_prefix() {
     pdl_release();
     pdl_wait();

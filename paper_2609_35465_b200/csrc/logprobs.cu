@@ -13,8 +13,9 @@
 // Entries are 64-bit numbers in the order that ranks them, so all of that is exact.
 // The loop over a run's tiles keeps nothing but a tile and the sums in registers, calls nothing, and no warp waits for another in it: 12
 // instructions of a thread for a logit, all phases together, which the memory outlasts.  (With the list kept there, the next tile in registers and a barrier a tile it
-// were up to 27, and 1024 rows of 151936 took 146 to 226 us.)  1024 rows of 151936 float32 logits take 110 us, 5.7 TB/s, 87 % of a copy's rate; 64
-// rows 17.2 us, of which the memory needs 6: a CTA of 1024 threads has 3.7 tiles, and the choice, the cut and the cluster's barriers; one row 9.8 us.
+// were up to 27, and 1024 rows of 151936 took 146 to 226 us.)  1024 rows of 151936 float32 logits take 111 us, 5.6 TB/s, 86 % of a copy's rate; 64
+// rows that L2 holds 17.8 us, of which the memory would need 6: a CTA of 1024 threads has 3.7 tiles, and the choice, the cut and the cluster's
+// barriers; one row 10 us.  (1 to 4 % of that are for distances beyond float32, taken of parts.)
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
